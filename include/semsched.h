@@ -38,7 +38,8 @@
  *                decreasing, or not ending at the total, workspace too small.
  *   SEM_ERANGE   some length < 0, or some priority >= num_classes (256 for
  *                the single-queue calls). Detected on the device.
- *   SEM_ENOMEM   the library could not allocate its internal workspace.
+ *   SEM_ENOMEM   the library could not allocate its internal workspace, or a
+ *                page pool has too few free pages.
  *   SEM_EDEVICE  a HIP runtime call failed, or (asynchronous calls only) the
  *                grid barrier of the middle passes, needed only by very wide
  *                key ranges, gave up waiting because its workgroups were not
@@ -424,6 +425,180 @@ int sem_evict_async(const uint8_t *priority, const int32_t *length, int64_t n_id
 int sem_schedule_static(const uint8_t *priority, const int32_t *length, int64_t n,
                         int32_t *order_out, int64_t *wait_out, sem_i128 *totals_out,
                         int32_t *status_out, void *stream);
+
+/*
+ * Paged 8-bit KV cache of the scheduled requests: the memory that sem_evict
+ * decides about, and the attention that reads it.
+ *
+ * A cache is a pool of num_pages pages. A page holds page_tokens consecutive
+ * tokens of one sequence, for every layer their keys, then their values, for
+ * every KV head, as 8-bit codes:
+ *   data  [num_pages][layers][2 (K, V)][kv_heads] blocks of page_tokens *
+ *         head_dim bytes. A block is a row of tiles of 16 tokens; a K tile is
+ *         [head_dim / 16][16 tokens][16 channels], a V tile
+ *         [head_dim][16 tokens] (the operand order of the matrix cores).
+ *   scale [num_pages][layers][2][kv_heads] float: a code c of a block stands
+ *         for c * scale.
+ *   format SEM_KV_INT8: two's complement in [-127, 127]; SEM_KV_FP8: e4m3
+ *         (largest value 448, no infinities). No code that the library writes
+ *         is a NaN.
+ * Sequences are slots 0 .. slots-1; the bookkeeping is in four arrays, which
+ * the caller may copy and put back to undo steps:
+ *   live   [ceil(num_pages / 32)] bit p % 32 of word p / 32: page p is in use;
+ *   refs   [num_pages] number of table entries that name the page;
+ *   lens   [slots] tokens of each sequence;
+ *   tables [slots][max_blocks] the pages of each sequence, -1 beyond them.
+ * All arrays are DEVICE memory of the caller, all zero (tables: -1) for an
+ * empty cache; data need not be cleared. The structure itself is a HOST
+ * pointer. page_tokens is a power of two from 16 to 1024, head_dim 64, 128 or
+ * 256 (SEM_ENOTIMPL for others), data 16-byte aligned, max_blocks *
+ * page_tokens at most INT32_MAX.
+ *
+ * Every call has a blocking form and an asynchronous one that allocates
+ * nothing, does not synchronise, and takes a caller-owned DEVICE workspace
+ * (256-byte aligned) and the stream; its calls may be captured into a HIP
+ * graph. The asynchronous calls add their errors to the workspace's first word
+ * and never clear it, so that one sem_check covers a whole step; the caller
+ * zeroes that word before the first call and after an error. A cache and a
+ * workspace must not be used by calls in flight on different streams.
+ *
+ * Lists of sequences name each at most once. Errors: SEM_EINVAL for null
+ * pointers, sizes or strides out of range, a workspace too small, and,
+ * detected on the device, sequences, lengths, offsets or page numbers outside
+ * the cache (no memory outside the arguments is accessed); SEM_ERANGE for a
+ * negative token count.
+ */
+#define SEM_KV_INT8 0
+#define SEM_KV_FP8 1
+#define SEM_KV_BF16 0
+#define SEM_KV_F16 1
+typedef struct {
+  void *data;
+  float *scale;
+  uint32_t *live;
+  int32_t *refs;
+  int32_t *lens;
+  int32_t *tables;
+  int64_t num_pages;
+  int32_t slots, max_blocks;
+  int32_t layers, kv_heads, head_dim, page_tokens;
+  int32_t format;
+} sem_kv_cache;
+
+/* Bytes of one page (0 for sizes that the library does not take). */
+size_t sem_kv_page_bytes(const sem_kv_cache *cache);
+
+/* Workspace of the asynchronous calls other than attend (fork, free and
+ * append need only the first 256 bytes of it). */
+size_t sem_kv_workspace_bytes(const sem_kv_cache *cache);
+
+/*
+ * Fork: the empty sequences dst[i] become copies of the first tokens[i]
+ * tokens of src[i] (all of them where tokens is NULL or larger), sharing their
+ * pages. A sequence that is a dst is not a src of the same call; a src may be
+ * listed for several dst. [n] int32 DEVICE arrays. Device-detected SEM_EINVAL:
+ * a dst that is not empty.
+ */
+int sem_kv_fork(const sem_kv_cache *cache, const int32_t *src, const int32_t *dst,
+                const int32_t *tokens, int64_t n);
+int sem_kv_fork_async(const sem_kv_cache *cache, const int32_t *src, const int32_t *dst,
+                      const int32_t *tokens, int64_t n, void *workspace, size_t ws_bytes,
+                      void *stream);
+
+/*
+ * Reserve: sequence seqs[i] grows by tokens[i] tokens and gets the pages that
+ * it needs for them. A partly filled last page that it shares is copied first
+ * (codes and scales of all layers), so that append never writes into a shared
+ * page. Pages are taken lowest free number first, in the order of the list, a
+ * sequence's copy before its new blocks. All or nothing: with too few free
+ * pages nothing changes and the status is SEM_ENOMEM; with any invalid entry
+ * nothing changes either (a full table is SEM_EINVAL).
+ */
+int sem_kv_reserve(const sem_kv_cache *cache, const int32_t *seqs, const int32_t *tokens,
+                   int64_t n);
+int sem_kv_reserve_async(const sem_kv_cache *cache, const int32_t *seqs, const int32_t *tokens,
+                         int64_t n, void *workspace, size_t ws_bytes, void *stream);
+
+/*
+ * Free: sequence seqs[i] keeps its first min(keep[i], length) tokens (none
+ * where keep is NULL) and gives back the pages beyond them; a page is free
+ * once no table names it. With sem_evict's victims and what sem_evict_plan
+ * saves, this carries out an eviction.
+ */
+int sem_kv_free(const sem_kv_cache *cache, const int32_t *seqs, const int32_t *keep, int64_t n);
+int sem_kv_free_async(const sem_kv_cache *cache, const int32_t *seqs, const int32_t *keep,
+                      int64_t n, void *workspace, size_t ws_bytes, void *stream);
+
+/*
+ * Compact: with L pages in use, the used pages numbered L and above move, in
+ * ascending order, into the free ones below L, ascending too; tables, refs
+ * and live follow. Afterwards pages 0 .. L-1 are in use.
+ */
+int sem_kv_compact(const sem_kv_cache *cache);
+int sem_kv_compact_async(const sem_kv_cache *cache, void *workspace, size_t ws_bytes,
+                         void *stream);
+
+/*
+ * Append: writes the keys and values of new tokens of one layer. Sequence
+ * seqs[i] has cu[i+1] - cu[i] new tokens, rows cu[i] .. of k and v; they are
+ * the last ones of its (already grown) length. cu is [n + 1] int32 DEVICE from
+ * 0 to `tokens`, or NULL: one token each. k, v: elements of `dtype`, element
+ * (token, head, channel) at token * token_stride + head * head_stride +
+ * channel.
+ * The scale of a block becomes s' = max(s if it holds older tokens else 0,
+ * a * (1 / top)), a the largest finite magnitude of its new elements, top 127
+ * or 448; if s' > s its older codes become round(c * s / s'); new codes are
+ * round(x / s'), ties to even, in 32-bit arithmetic. Infinities are stored as
+ * the largest code, NaN as 0, and either is reported as SEM_ERANGE.
+ */
+int sem_kv_append(const sem_kv_cache *cache, int32_t layer, const void *k, const void *v,
+                  int32_t dtype, int64_t k_token_stride, int64_t k_head_stride,
+                  int64_t v_token_stride, int64_t v_head_stride, const int32_t *seqs,
+                  const int32_t *cu, int64_t n, int64_t tokens);
+int sem_kv_append_async(const sem_kv_cache *cache, int32_t layer, const void *k, const void *v,
+                        int32_t dtype, int64_t k_token_stride, int64_t k_head_stride,
+                        int64_t v_token_stride, int64_t v_head_stride, const int32_t *seqs,
+                        const int32_t *cu, int64_t n, int64_t tokens, void *workspace,
+                        size_t ws_bytes, void *stream);
+
+/*
+ * Attend: softmax attention of query tokens over the cache of one layer. The
+ * queries of sequence seqs[i] are rows cu[i] .. cu[i+1]-1 (cu NULL: row i),
+ * at the last positions of its length. `heads` query heads share the KV heads
+ * in groups of heads / kv_heads consecutive ones. With causal set a query sees
+ * the keys up to its own position, else all of the sequence's; with window
+ * w > 0 only those less than w before it, too. A row that sees no key (an
+ * empty sequence) gives zeros and lse -infinity.
+ *   out [tokens][heads][head_dim] of the queries' type; lse [tokens][heads]
+ *   float: the logarithm of the sum of exp(score), NULL if not wanted.
+ *   max_new, max_len: bounds that the caller knows on the queries and the
+ *   length of a sequence, 0 if none. They only decide how the work is split;
+ *   results stay right if they do not hold.
+ */
+typedef struct {
+  const void *q;
+  void *out;
+  float *lse;
+  int64_t q_token_stride, q_head_stride;     /* in elements */
+  int64_t out_token_stride, out_head_stride; /* in elements */
+  int64_t tokens;
+  int64_t max_new, max_len;
+  int32_t heads;
+  int32_t dtype; /* SEM_KV_BF16 or SEM_KV_F16 */
+  int32_t causal;
+  int32_t window;
+  float scale; /* of the scores, e.g. 1 / sqrt(head_dim) */
+} sem_kv_query;
+
+/* Workspace of sem_kv_attend_async for n sequences, `tokens` queries and those
+ * bounds (0 for invalid sizes). */
+size_t sem_kv_attend_workspace_bytes(const sem_kv_cache *cache, int32_t heads, int64_t n,
+                                     int64_t tokens, int64_t max_new, int64_t max_len);
+int sem_kv_attend(const sem_kv_cache *cache, int32_t layer, const sem_kv_query *query,
+                  const int32_t *seqs, const int32_t *cu, int64_t n);
+int sem_kv_attend_async(const sem_kv_cache *cache, int32_t layer, const sem_kv_query *query,
+                        const int32_t *seqs, const int32_t *cu, int64_t n, void *workspace,
+                        size_t ws_bytes, void *stream);
 
 /* Stream used by the blocking calls (NULL = null stream). */
 int sem_set_stream(void *stream);

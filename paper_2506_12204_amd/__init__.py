@@ -61,6 +61,21 @@ SYMBOLS = (
     "sem_evict_workspace_bytes",
     "sem_evict_async",
     "sem_schedule_static",
+    "sem_kv_page_bytes",
+    "sem_kv_workspace_bytes",
+    "sem_kv_fork",
+    "sem_kv_fork_async",
+    "sem_kv_reserve",
+    "sem_kv_reserve_async",
+    "sem_kv_free",
+    "sem_kv_free_async",
+    "sem_kv_compact",
+    "sem_kv_compact_async",
+    "sem_kv_append",
+    "sem_kv_append_async",
+    "sem_kv_attend_workspace_bytes",
+    "sem_kv_attend",
+    "sem_kv_attend_async",
 )
 STATIC_MAX_N = 1048576
 STATIC_SCRATCH_BYTES = 33554432
@@ -71,6 +86,7 @@ PREFILL, DECODE = 0, 1
 STAGE_HIST, STAGE_FIRST, STAGE_FINAL, STAGE_MERGE, STAGE_POLICY, STAGE_COST, STAGE_MID = range(7)
 # comparison policies (Section 4): the key fields before the id
 POLICY_SEMANTIC, POLICY_FCFS, POLICY_SJF, POLICY_HPJF = 0, 1, 2, 3
+KV_INT8, KV_FP8 = 0, 1  # the codes of a KV cache
 
 
 class CostModelC(ctypes.Structure):
@@ -78,6 +94,25 @@ class CostModelC(ctypes.Structure):
     for alpha1)."""
     _fields_ = [(name, ctypes.c_uint64)
                 for name in ("alpha1", "alpha2", "beta", "gamma1", "gamma2")]
+
+
+class KVCacheC(ctypes.Structure):
+    """sem_kv_cache."""
+    _fields_ = ([(name, ctypes.c_void_p) for name in ("data", "scale", "live", "refs", "lens",
+                                                      "tables")]
+                + [("num_pages", ctypes.c_int64)]
+                + [(name, ctypes.c_int32) for name in ("slots", "max_blocks", "layers", "kv_heads",
+                                                       "head_dim", "page_tokens", "format")])
+
+
+class KVQueryC(ctypes.Structure):
+    """sem_kv_query."""
+    _fields_ = ([(name, ctypes.c_void_p) for name in ("q", "out", "lse")]
+                + [(name, ctypes.c_int64) for name in ("q_token_stride", "q_head_stride",
+                                                       "out_token_stride", "out_head_stride",
+                                                       "tokens", "max_new", "max_len")]
+                + [(name, ctypes.c_int32) for name in ("heads", "dtype", "causal", "window")]
+                + [("scale", ctypes.c_float)])
 
 
 def cost_model(model) -> CostModelC:
@@ -140,6 +175,20 @@ def _load() -> ctypes.CDLL:
     lib.sem_evict_async.argtypes = [vp, vp, i64, vp, vp, i64, i64, i64, vp, i64, vp, vp, vp, sz,
                                     vp]
     lib.sem_schedule_static.argtypes = [vp, vp, i64, vp, vp, vp, vp, vp]
+    kv, kq = ctypes.POINTER(KVCacheC), ctypes.POINTER(KVQueryC)
+    rows = [vp, vp, i64]  # sequences, offsets, their number
+    tail = [vp, sz, vp]   # workspace, its size, stream
+    append = [kv, i32, vp, vp, i32, i64, i64, i64, i64] + rows + [i64]
+    for name, args in (("fork", [kv, vp, vp, vp, i64]), ("reserve", [kv, vp, vp, i64]),
+                       ("free", [kv, vp, vp, i64]), ("compact", [kv]), ("append", append),
+                       ("attend", [kv, i32, kq] + rows)):
+        for form, more in (("", []), ("_async", tail)):
+            fn = getattr(lib, f"sem_kv_{name}{form}")
+            fn.argtypes, fn.restype = args + more, ctypes.c_int
+    for name, args in (("page_bytes", [kv]), ("workspace_bytes", [kv]),
+                       ("attend_workspace_bytes", [kv, i32, i64, i64, i64, i64])):
+        fn = getattr(lib, f"sem_kv_{name}")
+        fn.argtypes, fn.restype = args, sz
     lib.sem_strerror.argtypes = [ctypes.c_int]
     lib.sem_strerror.restype = ctypes.c_char_p
     for name in ("sem_schedule", "sem_schedule_batched", "sem_schedule_async",
@@ -535,3 +584,198 @@ def evict(priority: torch.Tensor, length: torch.Tensor, cached: torch.Tensor, kv
     upto = upto[:demands.numel()]
     k = int(upto[-1]) if demands.numel() else 0
     return victims[:k], upto
+
+
+def _round64(n: int) -> int:
+    return -(-n // 64) * 64
+
+
+_KV_DTYPES = {torch.bfloat16: 0, torch.float16: 1}
+
+
+class KVCache:
+    """Paged 8-bit KV cache of the scheduled requests (layout and operations:
+    semsched.h). A request's cache is a sequence, one of ``slots``.
+
+    ``data`` (uint8 [num_pages, page bytes]) holds the codes, ``scale``
+    (float32 [num_pages, layers, 2, kv_heads]) what they are multiplied by.
+    ``book`` is one int32 buffer with the views ``live``, ``refs``, ``lens`` and
+    ``tables``, each padded to 64 entries: copying it and putting it back
+    undoes reserve, fork and free (and append's growth) of the steps between,
+    though not compact. The three may be passed in; otherwise they are
+    allocated, empty.
+
+    Every operation enqueues on the current stream without synchronising;
+    ``check`` waits and raises on a device-detected error of any of them since
+    the last check. A step is: ``reserve`` room for the new tokens, then for
+    every layer ``append`` their keys and values and ``attend``. Lists of
+    sequences are int32 GPU tensors that name each at most once.
+    """
+
+    def __init__(self, num_pages: int, slots: int, max_blocks: int, *, layers: int, kv_heads: int,
+                 head_dim: int, page_tokens: int = 64, format: int = KV_INT8, device="cuda",
+                 data: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+                 book: Optional[torch.Tensor] = None):
+        self.num_pages, self.slots, self.max_blocks = int(num_pages), int(slots), int(max_blocks)
+        self.layers, self.kv_heads, self.head_dim = int(layers), int(kv_heads), int(head_dim)
+        self.page_tokens, self.format = int(page_tokens), int(format)
+        self.device = torch.device(device)
+        c = KVCacheC(None, None, None, None, None, None, self.num_pages, self.slots,
+                     self.max_blocks, self.layers, self.kv_heads, self.head_dim,
+                     self.page_tokens, self.format)
+        self.page_bytes = int(lib.sem_kv_page_bytes(ctypes.byref(c)))
+        if self.page_bytes == 0:
+            raise ValueError("a size that the KV cache does not take")
+        words = -(-self.num_pages // 32)
+        ends = [_round64(words)]
+        ends.append(ends[0] + _round64(self.num_pages))
+        ends.append(ends[1] + _round64(self.slots))
+        size = ends[2] + self.slots * self.max_blocks
+        fresh = book is None
+        if data is None:
+            data = torch.empty((self.num_pages, self.page_bytes), dtype=torch.uint8,
+                               device=self.device)
+        if scale is None:
+            scale = torch.zeros((self.num_pages, self.layers, 2, self.kv_heads),
+                                dtype=torch.float32, device=self.device)
+        if book is None:
+            book = torch.zeros(size, dtype=torch.int32, device=self.device)
+        for t, dtype, numel in ((data, torch.uint8, self.num_pages * self.page_bytes),
+                                (scale, torch.float32,
+                                 self.num_pages * self.layers * 2 * self.kv_heads),
+                                (book, torch.int32, size)):
+            if t.dtype != dtype or t.device.type != "cuda" or t.device != data.device:
+                raise TypeError("data (uint8), scale (float32) and book (int32) must live on "
+                                "one GPU")
+            if t.numel() != numel or not t.is_contiguous():
+                raise ValueError("data, scale and book must be contiguous and of the cache's sizes")
+        self.device = data.device
+        self.data, self.scale, self.book = data, scale, book
+        self.live = book[:words]
+        self.refs = book[ends[0]:ends[0] + self.num_pages]
+        self.lens = book[ends[1]:ends[1] + self.slots]
+        self.tables = book[ends[2]:].view(self.slots, self.max_blocks)
+        if fresh:
+            self.tables.fill_(-1)
+        for name in ("data", "scale", "live", "refs", "lens", "tables"):
+            setattr(c, name, getattr(self, name).data_ptr())
+        self._c, self._ref = c, ctypes.byref(c)
+        self.ws_bytes = int(lib.sem_kv_workspace_bytes(self._ref))
+        self.workspace = torch.zeros(self.ws_bytes, dtype=torch.uint8, device=self.device)
+
+    def _list(self, t: Optional[torch.Tensor], n: Optional[int], what: str) -> None:
+        if t is None:
+            return
+        if t.dtype != torch.int32 or t.device != self.device or t.dim() != 1 \
+                or not t.is_contiguous():
+            raise TypeError(f"{what} must be a contiguous 1-D int32 tensor on the cache's GPU")
+        if n is not None and t.numel() != n:
+            raise ValueError(f"{what} must hold {n} entries")
+
+    def _rows(self, x: torch.Tensor, heads: Optional[int], what: str) -> None:
+        if x.dtype not in _KV_DTYPES or x.device != self.device:
+            raise TypeError(f"{what} must be bfloat16 or float16 on the cache's GPU")
+        if x.dim() != 3 or x.shape[2] != self.head_dim or x.stride(2) != 1 \
+                or (heads is not None and x.shape[1] != heads):
+            raise ValueError(f"{what} must be [tokens, heads, head_dim] with adjacent channels")
+
+    def _room(self, need: int) -> None:
+        """A larger workspace, the status word carried over."""
+        if need > self.ws_bytes:
+            ws = torch.zeros(need, dtype=torch.uint8, device=self.device)
+            ws[:4].copy_(self.workspace[:4])
+            self.workspace, self.ws_bytes = ws, need
+
+    def _tail(self):
+        return self.workspace.data_ptr(), self.ws_bytes, torch.cuda.current_stream(
+            self.device).cuda_stream
+
+    def reserve(self, seqs: torch.Tensor, tokens: torch.Tensor) -> None:
+        """Room for tokens[i] more tokens of seqs[i] (their lengths grow)."""
+        self._list(seqs, None, "seqs")
+        self._list(tokens, seqs.numel(), "tokens")
+        _raise(lib.sem_kv_reserve_async(self._ref, _ptr(seqs), _ptr(tokens), seqs.numel(),
+                                        *self._tail()), "sem_kv_reserve_async")
+
+    def fork(self, src: torch.Tensor, dst: torch.Tensor,
+             tokens: Optional[torch.Tensor] = None) -> None:
+        """The empty dst[i] share the first tokens[i] tokens of src[i] (default: all)."""
+        self._list(src, None, "src")
+        self._list(dst, src.numel(), "dst")
+        self._list(tokens, src.numel(), "tokens")
+        _raise(lib.sem_kv_fork_async(self._ref, _ptr(src), _ptr(dst), _ptr(tokens), src.numel(),
+                                     *self._tail()), "sem_kv_fork_async")
+
+    def free(self, seqs: torch.Tensor, keep: Optional[torch.Tensor] = None) -> None:
+        """seqs[i] keeps its first keep[i] tokens (default: none)."""
+        self._list(seqs, None, "seqs")
+        self._list(keep, seqs.numel(), "keep")
+        _raise(lib.sem_kv_free_async(self._ref, _ptr(seqs), _ptr(keep), seqs.numel(),
+                                     *self._tail()), "sem_kv_free_async")
+
+    def compact(self) -> None:
+        """Moves the pages in use to the lowest numbers."""
+        _raise(lib.sem_kv_compact_async(self._ref, *self._tail()), "sem_kv_compact_async")
+
+    def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, seqs: torch.Tensor,
+               cu: Optional[torch.Tensor] = None) -> None:
+        """Writes k, v [tokens, kv_heads, head_dim] (bfloat16 or float16; strides of
+        tokens and heads are free) of one layer. Sequence seqs[i]'s new tokens are
+        rows cu[i]..cu[i+1] (None: row i), the last ones of its length."""
+        self._rows(k, self.kv_heads, "k")
+        self._rows(v, self.kv_heads, "v")
+        if v.dtype != k.dtype or v.shape != k.shape:
+            raise ValueError("k and v must have one type and shape")
+        self._list(seqs, None, "seqs")
+        n = seqs.numel()
+        self._list(cu, n + 1, "cu")
+        _raise(lib.sem_kv_append_async(self._ref, layer, _ptr(k), _ptr(v), _KV_DTYPES[k.dtype],
+                                       k.stride(0), k.stride(1), v.stride(0), v.stride(1),
+                                       _ptr(seqs), _ptr(cu), n, k.shape[0], *self._tail()),
+               "sem_kv_append_async")
+
+    def attend(self, layer: int, q: torch.Tensor, seqs: torch.Tensor,
+               cu: Optional[torch.Tensor] = None, *, causal: bool = True, window: int = 0,
+               scale: Optional[float] = None, max_new: int = 0, max_len: int = 0,
+               out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None
+               ) -> torch.Tensor:
+        """Attention of q [tokens, heads, head_dim] over the cache of one layer.
+
+        Rows belong to sequences as in ``append``. ``scale`` of the scores
+        defaults to head_dim ** -0.5; ``window`` > 0 limits a causal or full row
+        to that many positions up to its own; ``max_new`` and ``max_len`` bound
+        a sequence's queries and length (0: unknown) and only guide how the
+        work is split. ``lse`` (float32 [tokens, heads]) receives the log of
+        the softmax sums. Returns ``out``."""
+        self._rows(q, None, "q")
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        else:
+            self._rows(out, q.shape[1], "out")
+            if out.dtype != q.dtype or out.shape != q.shape:
+                raise ValueError("out must have q's type and shape")
+        tokens, heads = q.shape[0], q.shape[1]
+        if lse is not None and (lse.dtype != torch.float32 or lse.device != self.device
+                                or lse.shape != (tokens, heads) or not lse.is_contiguous()):
+            raise ValueError("lse must be contiguous float32 [tokens, heads] on the cache's GPU")
+        self._list(seqs, None, "seqs")
+        n = seqs.numel()
+        self._list(cu, n + 1, "cu")
+        query = KVQueryC(q.data_ptr(), out.data_ptr(), lse.data_ptr() if lse is not None else None,
+                         q.stride(0), q.stride(1), out.stride(0), out.stride(1), tokens,
+                         max_new, max_len, heads, _KV_DTYPES[q.dtype], bool(causal), window,
+                         self.head_dim ** -0.5 if scale is None else scale)
+        self._room(int(lib.sem_kv_attend_workspace_bytes(self._ref, heads, n, tokens, max_new,
+                                                         max_len)))
+        _raise(lib.sem_kv_attend_async(self._ref, layer, ctypes.byref(query), _ptr(seqs),
+                                       _ptr(cu), n, *self._tail()), "sem_kv_attend_async")
+        return out
+
+    def check(self) -> None:
+        """Waits for the current stream; raises on an error of any operation
+        since the last check."""
+        ws, _, stream = self._tail()
+        code = lib.sem_check(ws, stream)
+        if code != SEM_OK:
+            self.workspace[:4].zero_()
+        _raise(code, "KVCache")

@@ -22,7 +22,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libsemsched.so")
 SOURCES = ["abi.hip", "batched.hip", "global_sort.hip", "tile_sort.hip", "long_sort.hip",
            "insert.hip", "policy.hip",
-           "cost.hip", "batch.hip"]
+           "cost.hip", "batch.hip",
+           "kv_abi.hip", "kv_pages.hip", "kv_append.hip", "kv_attend.hip"]
 ARCH = os.environ.get("SEMSCHED_ARCH", "gfx950")
 NOISE = "is not a recognized feature for this target"
 

@@ -10,17 +10,13 @@
 #include <mutex>
 #include <vector>
 
+#include "abi_common.h"
 #include "kernels.h"
 #include "semsched.h"
 
 using namespace semsched;
 
 namespace {
-
-constexpr size_t kAlign = 256;
-constexpr size_t kHeaderBytes = 256;  // flags, counters, ranges, plan
-
-size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
 struct Layout {
   size_t flags = 0, sink = 16, plan = 64;
@@ -142,6 +138,7 @@ int num_cus() {
 int map_flags(uint32_t f) {
   if (f & kFlagDevice) return SEM_EDEVICE;
   if (f & kFlagInval) return SEM_EINVAL;
+  if (f & kFlagNoMem) return SEM_ENOMEM;
   if (f & kFlagRange) return SEM_ERANGE;
   return SEM_OK;
 }
@@ -780,6 +777,15 @@ int scratch_address(void** out) {
 
 }  // namespace
 
+namespace semsched {
+
+std::mutex& blocking_mutex() { return state().mu; }
+hipStream_t blocking_stream() { return state().stream; }
+int blocking_workspace(size_t bytes, void** out) { return cached_workspace(bytes, out); }
+int blocking_finish(void* ws, hipStream_t st) { return finish(ws, st); }
+
+}  // namespace semsched
+
 extern "C" {
 
 int sem_schedule_static(const uint8_t* priority, const int32_t* length, int64_t n,
@@ -806,7 +812,7 @@ const char* sem_strerror(int code) {
   switch (code) {
     case SEM_OK: return "success";
     case SEM_EINVAL: return "invalid argument";
-    case SEM_ERANGE: return "length < 0 or priority >= num_classes";
+    case SEM_ERANGE: return "value out of range (length < 0, priority >= num_classes, ...)";
     case SEM_ENOMEM: return "out of device memory";
     case SEM_EDEVICE: return "HIP runtime error";
     case SEM_ENOTIMPL: return "size beyond what this entry point implements";

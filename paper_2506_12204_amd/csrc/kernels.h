@@ -10,6 +10,7 @@ namespace semsched {
 constexpr uint32_t kFlagInval = 1u;  // bad offsets / queue longer than promised
 constexpr uint32_t kFlagRange = 2u;  // length < 0 or priority >= num_classes
 constexpr uint32_t kFlagDevice = 4u; // an internal consistency check failed on the device
+constexpr uint32_t kFlagNoMem = 8u;  // a page pool has too few free pages
 
 // ---------------------------------------------------------------------------
 // Queues scheduled inside one workgroup's LDS (batched.hip).

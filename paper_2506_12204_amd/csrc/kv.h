@@ -1,0 +1,98 @@
+// Host/device interface of the paged 8-bit KV cache (internal to the library;
+// the operations are defined in semsched.h).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "kernels.h"
+
+namespace semsched {
+
+constexpr int kKvTile = 16;          // tokens per tile of a page's block
+
+// The cache as the kernels see it: the caller's arrays and the derived sizes.
+struct KvView {
+  uint8_t* data;    // [num_pages][layers][2][kv_heads][page_tokens * head_dim]
+  float* scale;     // [num_pages][layers][2][kv_heads]
+  uint32_t* live;   // one bit per page
+  int32_t* refs;    // [num_pages]
+  int32_t* lens;    // [slots]
+  int32_t* tables;  // [slots][max_blocks], -1 beyond a sequence's blocks
+  int64_t num_pages, page_bytes;
+  int32_t slots, max_blocks, layers, kv_heads, head_dim, page_tokens, page_shift, format;
+  int32_t page_scales;  // layers * 2 * kv_heads
+  uint32_t* flags;
+};
+
+struct KvForkArgs {
+  KvView c;
+  const int32_t *src, *dst, *tokens;  // tokens may be null: the whole source
+  int64_t n;
+};
+
+struct KvFreeArgs {
+  KvView c;
+  const int32_t *seqs, *keep;  // keep may be null: all 0
+  int64_t n;
+};
+
+struct KvReserveArgs {
+  KvView c;
+  const int32_t *seqs, *grow;
+  int64_t n;
+  uint32_t* begin;    // [n] first entry of each sequence in `fresh`
+  uint32_t* fresh;    // [room] the free pages taken, ascending
+  uint64_t* copies;   // [n] pages to copy: from | to << 32
+  uint32_t* ncopies;  // [1]
+  int64_t room;       // entries of `fresh`
+};
+
+struct KvCompactArgs {
+  KvView c;
+  uint64_t* moves;   // [num_pages / 2] from | to << 32
+  uint32_t* remap;   // [num_pages] where a moved page goes
+  uint32_t* counts;  // [2] moves, live pages
+};
+
+struct KvAppendArgs {
+  KvView c;
+  const uint16_t *k, *v;  // 16-bit elements
+  int64_t k_token, k_head, v_token, v_head;  // strides in elements
+  const int32_t *seqs, *cu;                  // cu may be null: one token each
+  int64_t n, tokens;
+  int32_t layer;
+  int32_t bf16;  // else IEEE half
+  int32_t wide;  // 16-byte loads are aligned
+};
+
+struct KvAttendArgs {
+  KvView c;
+  const uint16_t* q;
+  uint16_t* out;
+  float* lse;  // [tokens][heads], may be null
+  int64_t q_token, q_head, out_token, out_head;  // strides in elements
+  const int32_t *seqs, *cu;
+  int64_t n, tokens;
+  int32_t layer, heads, group;
+  int32_t bf16, wide;
+  int32_t causal, window;
+  float scale_log2;  // softmax scale * log2(e)
+  int32_t splits;    // parts of the key axis
+  float* part_o;     // [splits][tokens * heads][head_dim]
+  float* part_ml;    // [splits][tokens * heads][2]: maximum (log2), sum
+};
+
+hipError_t launch_kv_fork(const KvForkArgs& a, hipStream_t st);
+hipError_t launch_kv_free(const KvFreeArgs& a, hipStream_t st);
+hipError_t launch_kv_reserve(const KvReserveArgs& a, hipStream_t st);
+hipError_t launch_kv_compact(const KvCompactArgs& a, hipStream_t st);
+hipError_t launch_kv_append(const KvAppendArgs& a, hipStream_t st);
+hipError_t launch_kv_attend(const KvAttendArgs& a, hipStream_t st);
+
+// Parts of the key axis that an attention call of these sizes is split into
+// (its workspace holds the parts' partial outputs).
+int kv_attend_splits(int64_t n, int64_t tokens, int heads, int kv_heads, int64_t max_new,
+                     int64_t max_len);
+
+}  // namespace semsched

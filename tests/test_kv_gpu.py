@@ -1,0 +1,692 @@
+"""The paged 8-bit KV cache against its 64-bit reference.
+
+Page numbers, counts and copies are exact. Tolerances:
+  * attention: a weight p_j vs_j is rounded to 11 bits (relative 2^-12, to the
+    nearest), scores and sums carry 32-bit errors (a score of magnitude below
+    2^7 is off by at most 2^-15, and so is its weight, relatively), and the output
+    is rounded to its type. Hence |error| <= u |o| + (2^-12 + 2^-14) sum_j p_j |v_j|
+    + tiny, with u the type's half unit, 2^-9 (bf16) or 2^-12 (half), both doubled
+    for slack.
+  * a scale is one 32-bit product, a code the nearest to a 32-bit quotient: it
+    is off by at most half a step, plus 2^-20 of the largest code.
+"""
+
+import numpy as np
+import pytest
+
+from oracle import kv_oracle as ko
+from tests._lib import ensure_built, gpu_available
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ss():
+    ensure_built()
+    if not gpu_available():
+        pytest.skip("no GPU")
+    import paper_2506_12204_amd as mod
+    return mod
+
+
+def i32(x):
+    import torch
+    return torch.tensor(np.asarray(x, dtype=np.int32), device="cuda")
+
+
+def random_codes(rng, shape, fmt):
+    if fmt == ko.INT8:
+        return rng.integers(-127, 128, shape).astype(np.int8).view(np.uint8)
+    b = rng.integers(0, 256, shape).astype(np.uint8)
+    return np.where((b & 127) == 127, b - 1, b).astype(np.uint8)
+
+
+class Case:
+    """A cache with sequences of given lengths on scattered pages."""
+
+    def __init__(self, ss, lens, *, fmt, dim, pt, kv_heads, layers=2, layer=1, seed=0, spare=3,
+                 dirty=False):
+        import torch
+        rng = self.rng = np.random.default_rng(seed)
+        self.lens, self.layer = lens, layer
+        blocks = [-(-n // pt) for n in lens]
+        pages, mb = sum(blocks) + spare, max(blocks + [1]) + 1
+        self.geom = (layers, kv_heads, pt, dim, fmt)
+        self.c = ss.KVCache(pages, len(lens), mb, layers=layers, kv_heads=kv_heads, head_dim=dim,
+                            page_tokens=pt, format=fmt)
+        self.data = random_codes(rng, (pages, self.c.page_bytes), fmt)
+        if dirty:  # bytes that no sequence holds may be anything, NaN codes too
+            self.data[:] = 0x7f if fmt == ko.FP8 else 0x80
+            good = random_codes(rng, self.data.shape, fmt)
+        self.scale = np.exp(rng.normal(size=(pages, layers, 2, kv_heads))).astype(np.float32)
+        self.scale *= 1 / 64 if fmt == ko.INT8 else 1 / 200
+        perm = rng.permutation(pages)
+        self.tables = np.full((len(lens), mb), -1, np.int32)
+        at = 0
+        for s, nb in enumerate(blocks):
+            self.tables[s, :nb] = perm[at:at + nb]
+            at += nb
+            if dirty:
+                for b in range(nb):
+                    rows = min(pt, lens[s] - b * pt)
+                    p = perm[at - nb + b]
+                    view = self.data[p].reshape(layers, 2, kv_heads, pt * dim)
+                    new = good[p].reshape(layers, 2, kv_heads, pt * dim)
+                    for w in (0, 1):
+                        idx = ko.block_index(w, pt, dim)[:rows].reshape(-1)
+                        view[:, w][..., idx] = new[:, w][..., idx]
+        refs = np.zeros(pages, np.int32)
+        refs[perm[:at]] = 1
+        self.c.data.copy_(torch.from_numpy(self.data))
+        self.c.scale.copy_(torch.from_numpy(self.scale))
+        self.c.tables.copy_(torch.from_numpy(self.tables))
+        self.c.lens.copy_(i32(lens))
+        self.c.refs.copy_(i32(refs))
+        words = np.zeros(-(-pages // 32), np.uint32)
+        for p in perm[:at]:
+            words[p // 32] |= np.uint32(1 << (p % 32))
+        self.c.live.copy_(torch.from_numpy(words.view(np.int32)))
+
+    def queries(self, new, heads, dtype, big=False, pad=0):
+        import torch
+        dim = self.geom[3]
+        x = self.rng.normal(size=(sum(new), heads * dim + pad))
+        if big:  # magnitudes that half precision does not hold
+            x = x * 2.0 ** self.rng.integers(-40, 40, (sum(new), 1))
+        t = torch.from_numpy(x).to(dtype).cuda()
+        return t[:, :heads * dim].view(sum(new), heads, dim)
+
+    def check(self, q, new, out, lse, scale, causal, window, seqs=None):
+        import torch
+        layers, kvh, pt, dim, fmt = self.geom
+        group = q.shape[1] // kvh
+        qh, o = q.double().cpu().numpy(), out.double().cpu().numpy()
+        u = 2.0 ** -9 if out.dtype == torch.bfloat16 else 2.0 ** -12
+        at = 0
+        for i, m in enumerate(new):
+            s = i if seqs is None else seqs[i]
+            for kh in range(kvh):
+                k, v = (ko.read(self.data, self.scale, self.geom, self.tables[s], self.lens[s],
+                                self.layer, w, kh) for w in (0, 1))
+                for h in range(kh * group, (kh + 1) * group):
+                    want, wl, mag = ko.attend(qh[at:at + m, h], k, v, scale, causal, window)
+                    got = o[at:at + m, h]
+                    tol = 2 * (u * np.abs(want) + (2.0 ** -12 + 2.0 ** -14) * mag) + 2.0 ** -24
+                    worst = np.max((np.abs(got - want) / tol)) if m else 0
+                    assert worst <= 1, (i, h, worst)
+                    if lse is not None:
+                        gl = lse[at:at + m, h].double().cpu().numpy()
+                        none = np.isinf(wl)
+                        assert (gl[none] == wl[none]).all()
+                        err = np.abs(gl[~none] - wl[~none])
+                        assert (err <= 2.0 ** -15 * (1 + np.abs(wl[~none]))).all(), err.max()
+            at += m
+
+
+def dtype_of(name):
+    import torch
+    return {"bf16": torch.bfloat16, "f16": torch.float16}[name]
+
+
+def run_attend(ss, lens, new, *, heads, kv_heads, dim=128, pt=64, fmt=ko.INT8, dtype="bf16",
+               causal=True, window=0, scale=None, seed=0, big=False, pad=8, max_len=0, max_new=0,
+               with_cu=True, dirty=False, lse=True, strided_out=False):
+    import torch
+    case = Case(ss, lens, fmt=fmt, dim=dim, pt=pt, kv_heads=kv_heads, seed=seed, dirty=dirty)
+    scale = dim ** -0.5 if scale is None else scale
+    q = case.queries(new, heads, dtype_of(dtype), big, pad)
+    if big:
+        scale *= 2.0 ** -40
+    t = sum(new)
+    out = None
+    if strided_out:
+        out = torch.full((t, heads + 1, dim), 7.0, dtype=q.dtype, device="cuda")[:, :heads]
+    sums = torch.empty(t, heads, device="cuda") if lse else None
+    cu = i32(np.concatenate([[0], np.cumsum(new)])) if with_cu else None
+    out = case.c.attend(case.layer, q, i32(range(len(lens))), cu, causal=causal, window=window,
+                        scale=scale, max_len=max_len, max_new=max_new, out=out, lse=sums)
+    case.c.check()
+    case.check(q, new, out, sums, scale, causal, window)
+    if strided_out:
+        assert (out.as_strided((t, dim), (out.stride(0), 1),
+                               out.storage_offset() + heads * dim) == 7.0).all()
+    return case, q, out
+
+
+DIMS = [(64, 16), (64, 64), (128, 16), (128, 32), (128, 64), (128, 256), (256, 64), (256, 1024)]
+
+
+@pytest.mark.parametrize("dim,pt", DIMS)
+@pytest.mark.parametrize("fmt", [ko.INT8, ko.FP8])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_single_tokens(ss, dim, pt, fmt, dtype):
+    # one key, tile and chunk borders, a page that ends inside a chunk, an idle slot
+    lens = [1, 15, 16, 17, 63, 64, 65, 0, 200, 129]
+    print("decode", dim, pt, fmt, dtype, flush=True)
+    run_attend(ss, lens, [1] * len(lens), heads=4, kv_heads=2, dim=dim, pt=pt, fmt=fmt,
+               dtype=dtype, with_cu=False, seed=dim + pt + fmt)
+
+
+@pytest.mark.parametrize("heads,kv_heads", [(1, 1), (3, 1), (16, 1), (17, 1), (40, 1), (6, 3),
+                                            (5, 5)])
+def test_head_groups(ss, heads, kv_heads):
+    print("groups", heads, kv_heads, flush=True)
+    run_attend(ss, [70, 5, 130], [1, 1, 1], heads=heads, kv_heads=kv_heads, fmt=ko.FP8)
+    run_attend(ss, [70, 5, 130], [9, 5, 33], heads=heads, kv_heads=kv_heads, dtype="f16")
+
+
+@pytest.mark.parametrize("split", [0, 1, 4000])
+@pytest.mark.parametrize("fmt", [ko.INT8, ko.FP8])
+def test_long_contexts(ss, split, fmt):
+    # few rows: the key axis is split, by a bound that may be wrong either way
+    print("long", split, fmt, flush=True)
+    run_attend(ss, [3001, 17, 4000, 0], [1] * 4, heads=2, kv_heads=1, fmt=fmt, max_len=split,
+               with_cu=False, seed=5)
+
+
+@pytest.mark.parametrize("dim,pt", [(64, 32), (128, 16), (128, 64), (256, 128)])
+@pytest.mark.parametrize("causal,window", [(True, 0), (True, 1), (True, 50), (False, 0),
+                                           (False, 40)])
+@pytest.mark.parametrize("fmt,dtype", [(ko.INT8, "bf16"), (ko.FP8, "f16")])
+def test_several_tokens(ss, dim, pt, causal, window, fmt, dtype):
+    # whole prompts, chunks on a context, drafts, a sequence without queries
+    lens, new = [100, 300, 65, 40, 1, 333], [100, 70, 3, 0, 1, 129]
+    print("several", dim, pt, causal, window, fmt, flush=True)
+    run_attend(ss, lens, new, heads=4, kv_heads=2, dim=dim, pt=pt, fmt=fmt, dtype=dtype,
+               causal=causal, window=window, seed=window + dim)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_more_queries_than_keys(ss, causal):
+    # rows before the first key see nothing: zeros, and a sum of minus infinity
+    print("empty rows", causal, flush=True)
+    run_attend(ss, [3, 0, 70], [20, 4, 200], heads=3, kv_heads=1, causal=causal, fmt=ko.FP8)
+
+
+@pytest.mark.parametrize("fmt", [ko.INT8, ko.FP8])
+@pytest.mark.parametrize("new", [1, 40])
+def test_bytes_beyond_the_length_do_not_count(ss, fmt, new):
+    print("dirty", fmt, new, flush=True)
+    lens = [41, 100, 64, 77]
+    run_attend(ss, lens, [new] * 4, heads=4, kv_heads=2, fmt=fmt, dirty=True, pt=32)
+
+
+def test_magnitudes_and_strides(ss):
+    print("magnitudes", flush=True)
+    run_attend(ss, [90, 33], [2, 30], heads=4, kv_heads=2, big=True)
+    # rows that are not 16-byte aligned, an output with a stride
+    run_attend(ss, [90, 33], [2, 30], heads=4, kv_heads=2, pad=1, strided_out=True)
+    run_attend(ss, [90, 33], [1, 1], heads=4, kv_heads=2, pad=3, dtype="f16", strided_out=True)
+    run_attend(ss, [90, 33], [1, 1], heads=4, kv_heads=2, scale=0.0)
+    run_attend(ss, [90, 33], [1, 9], heads=4, kv_heads=2, scale=-0.3)
+
+
+def test_scales_of_very_different_pages(ss):
+    """Weights are rounded relative to the largest V scale, zero scales included."""
+    import torch
+    print("page scales", flush=True)
+    for new in (1, 50):
+        case = Case(ss, [300, 200], fmt=ko.INT8, dim=64, pt=16, kv_heads=1, seed=3)
+        mult = 10.0 ** case.rng.integers(-6, 4, case.scale.shape[0])
+        mult[case.tables[0, 0]] = 0.0
+        case.scale[:, :, 1] *= mult[:, None, None].astype(np.float32)
+        case.c.scale.copy_(torch.from_numpy(case.scale))
+        q = case.queries([new, new], 2, torch.bfloat16)
+        out = case.c.attend(1, q, i32([0, 1]), i32([0, new, 2 * new]))
+        case.c.check()
+        case.check(q, [new, new], out, None, 64 ** -0.5, True, 0)
+    # all of V zero
+    case.scale[:, :, 1] = 0
+    case.c.scale.copy_(torch.from_numpy(case.scale))
+    assert (case.c.attend(1, q, i32([0, 1]), i32([0, new, 2 * new])) == 0).all()
+
+
+def test_nan_and_infinity_of_a_query_stay_in_its_row(ss):
+    import torch
+    print("nan rows", flush=True)
+    case = Case(ss, [130], fmt=ko.FP8, dim=64, pt=32, kv_heads=1)
+    q = case.queries([40], 1, torch.float16).clone()
+    ref = case.c.attend(1, q, i32([0]), i32([0, 40]))
+    q[7, 0, 3], q[20, 0, 0] = float("nan"), float("inf")
+    out = case.c.attend(1, q, i32([0]), i32([0, 40]))
+    case.c.check()
+    rows = [i for i in range(40) if i not in (7, 20)]
+    assert torch.equal(out[rows], ref[rows])
+    assert out[7].isnan().all()
+
+
+def test_page_offsets_beyond_32_bits(ss):
+    """A pool of more than 4 GiB, read and written beyond that."""
+    import torch
+    print("large pool", flush=True)
+    c = ss.KVCache(1100, 2, 8, layers=8, kv_heads=16, head_dim=256, page_tokens=64,
+                   format=ss.KV_INT8)
+    assert c.data.numel() > 1 << 32
+    c.tables[0, :2] = i32([1098, 1099])
+    c.refs[1098:1100] = 1
+    c.live[1098 // 32] = (1 << (1098 % 32)) | (1 << (1099 % 32))
+    c.lens[0] = 70
+    gen = torch.Generator("cuda").manual_seed(1)
+    kv = torch.randn(2, 70, 16, 256, generator=gen, device="cuda").bfloat16()
+    c.append(7, kv[0], kv[1], i32([0]), i32([0, 70]))
+    q = torch.randn(1, 16, 256, generator=gen, device="cuda").bfloat16()
+    out = c.attend(7, q, i32([0])).clone()
+    c.compact()
+    again = c.attend(7, q, i32([0]))
+    c.check()
+    assert c.tables[0, :2].tolist() == [0, 1] and c.refs[:3].tolist() == [1, 1, 0]
+    assert torch.equal(out, again)
+    k, v = kv.double().cpu().numpy()
+    for h in range(16):
+        want, _, mag = ko.attend(q[:, h].double().cpu().numpy(), k[:, h], v[:, h], 1 / 16, True, 0)
+        # int8 keys and values: half a step of 1/127 of the largest each
+        assert np.abs(again[0, h].double().cpu().numpy() - want).max() < 0.1
+
+
+@pytest.mark.parametrize("dim,pt,kv_heads", [(64, 16, 1), (128, 64, 2), (256, 32, 3),
+                                             (128, 256, 1)])
+@pytest.mark.parametrize("fmt", [ko.INT8, ko.FP8])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("pad", [8, 1])
+def test_append(ss, dim, pt, kv_heads, fmt, dtype, pad):
+    """New tokens beside older ones, over page borders, on reused pages."""
+    import torch
+    print("append", dim, pt, kv_heads, fmt, dtype, pad, flush=True)
+    lens = [1, 40, 300, 17, 64, 65, 130, 16]
+    new = [1, 1, 300, 16, 1, 64, 33, 0]
+    case = Case(ss, lens, fmt=fmt, dim=dim, pt=pt, kv_heads=kv_heads, seed=dim + pt)
+    rng, c, t = case.rng, case.c, sum(new)
+    x = rng.normal(size=(t, 2 * kv_heads * dim + pad)) * np.exp(rng.normal(size=(t, 1)))
+    x[5, :dim] = 0
+    x = torch.from_numpy(x).to(dtype_of(dtype)).cuda()
+    k = x[:, :kv_heads * dim].view(t, kv_heads, dim)
+    v = x[:, kv_heads * dim:2 * kv_heads * dim].view(t, kv_heads, dim)
+    c.append(1, k, v, i32(range(len(lens))), i32(np.concatenate([[0], np.cumsum(new)])))
+    c.check()
+    data, scale = c.data.cpu().numpy(), c.scale.cpu().numpy()
+    val, top = ko.code_values(fmt), ko.TOP[fmt]
+    steps = np.sort(val[~np.isnan(val)])
+    touched = np.zeros(case.data.shape, bool)
+    marked = np.zeros(scale.shape, bool)
+    L = (2, kv_heads, pt * dim)
+
+    def nearest(codes, quotient):
+        """Each code is as near to its quotient as any other one."""
+        got = np.abs(val[codes] - quotient)
+        j = np.clip(np.searchsorted(steps, quotient), 1, len(steps) - 1)
+        best = np.minimum(np.abs(steps[j] - quotient), np.abs(steps[j - 1] - quotient))
+        assert (got <= best + top * 2.0 ** -20).all()
+
+    at = 0
+    for s, (n, m) in enumerate(zip(lens, new)):
+        for b in range((n - m) // pt, -(-n // pt) if m else 0):
+            page, lo, hi = case.tables[s, b], max(0, n - m - b * pt), min(pt, n - b * pt)
+            r0 = at + b * pt + lo - (n - m)
+            for w, src in ((0, k), (1, v)):
+                idx = ko.block_index(w, pt, dim)
+                for h in range(kv_heads):
+                    xs = src[r0:r0 + hi - lo, h].double().cpu().numpy()
+                    was = float(case.scale[page, 1, w, h]) if lo else 0.0
+                    want = max(was, np.abs(xs).max() / top)
+                    now = float(scale[page, 1, w, h])
+                    marked[page, 1, w, h] = True
+                    assert abs(now - want) <= want * 2.0 ** -22
+                    block = data[page].reshape(2, *L)[1, w, h]
+                    old = case.data[page].reshape(2, *L)[1, w, h]
+                    by = now if now > 0 else 1.0
+                    nearest(block[idx[lo:hi]], xs / by)
+                    if now > was:
+                        nearest(block[idx[:lo]], val[old[idx[:lo]]] * was / by)
+                    else:
+                        assert (block[idx[:lo]] == old[idx[:lo]]).all()
+                    touched[page].reshape(2, *L)[1, w, h][idx[:hi]] = True
+        at += m
+    assert (data[~touched] == case.data[~touched]).all()
+    assert (scale[~marked] == case.scale[~marked]).all()
+
+
+def test_append_step_by_step_equals_a_prompt_where_scales_do_not_grow(ss):
+    """One token at a time with the largest first gives the codes of one call."""
+    import torch
+    print("append steps", flush=True)
+    gen = torch.Generator("cuda").manual_seed(2)
+    x = torch.randn(2, 50, 2, 64, generator=gen, device="cuda").clamp(-2, 2).bfloat16()
+    x[:, ::16, :, 0] = 3.0
+    out = []
+    for chunk in (50, 1):
+        c = ss.KVCache(8, 1, 8, layers=1, kv_heads=2, head_dim=64, page_tokens=16)
+        c.data.zero_()
+        for a in range(0, 50, chunk):
+            c.reserve(i32([0]), i32([chunk]))
+            c.append(0, x[0, a:a + chunk], x[1, a:a + chunk], i32([0]), i32([0, chunk]))
+        c.check()
+        out.append((c.data.clone(), c.scale.clone(), c.book.clone()))
+    for a, b in zip(*out):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("fmt", [ko.INT8, ko.FP8])
+def test_append_of_values_that_are_not_finite(ss, fmt):
+    import torch
+    print("append inf", fmt, flush=True)
+    c = ss.KVCache(2, 1, 2, layers=1, kv_heads=1, head_dim=64, page_tokens=16, format=fmt)
+    c.reserve(i32([0]), i32([3]))
+    x = torch.ones(3, 1, 64, dtype=torch.bfloat16, device="cuda")
+    x[0, 0, 0], x[0, 0, 1], x[1, 0, 2] = float("inf"), float("-inf"), float("nan")
+    c.append(0, x, torch.zeros_like(x), i32([0]), i32([0, 3]))
+    with pytest.raises(ss.SemschedRangeError):
+        c.check()
+    c.check()  # reported once
+    val = ko.code_values(fmt)
+    got = val[c.data.cpu().numpy()[0][ko.block_index(0, 16, 64)[:3]]]
+    top = ko.TOP[fmt]
+    assert got[0, 0] == top and got[0, 1] == -top and got[1, 2] == 0 and got[2, 5] == top
+    out = c.attend(0, x[2:], i32([0]))
+    assert (out == 0).all()  # V of zeros: scale 0
+    c.check()
+
+
+def assert_pages(c, ref, label):
+    assert c.refs.tolist() == ref.refs, label
+    assert c.lens.tolist() == ref.lens, label
+    assert c.tables.tolist() == ref.table_rows(), label
+    assert [w & 0xffffffff for w in c.live.tolist()] == ref.live_words(), label
+    data = c.data.cpu().numpy()
+    scale = c.scale.cpu().numpy().reshape(data.shape[0], -1)
+    for p, r in enumerate(ref.refs):
+        if r:
+            b, s = ref.content[p]
+            assert (data[p] == b).all() and (scale[p] == s).all(), (label, p)
+
+
+@pytest.mark.parametrize("pt,pages,slots,seed", [(16, 40, 9, 0), (64, 33, 12, 1), (16, 300, 40, 2),
+                                                 (32, 1000, 70, 3), (16, 5, 3, 4)])
+def test_pages_against_the_reference(ss, pt, pages, slots, seed):
+    """A random program of all page operations, compared after every step."""
+    import torch
+    print("pages", pt, pages, slots, seed, flush=True)
+    rng = np.random.default_rng(seed)
+    mb = max(2, 2 * pages // slots)
+    c = ss.KVCache(pages, slots, mb, layers=2, kv_heads=3, head_dim=64, page_tokens=pt,
+                   format=ss.KV_FP8)
+    data = rng.integers(0, 256, c.data.shape).astype(np.uint8)
+    scale = rng.normal(size=tuple(c.scale.shape)).astype(np.float32)
+    c.data.copy_(torch.from_numpy(data))
+    c.scale.copy_(torch.from_numpy(scale))
+    ref = ko.Pages(pages, slots, mb, pt)
+    ref.content = [(data[p], scale[p].reshape(-1)) for p in range(pages)]
+    refused = 0
+    for step in range(60):
+        op = rng.choice(["reserve", "reserve", "fork", "free", "compact"])
+        some = rng.permutation(slots)[:rng.integers(1, slots + 1)].tolist()
+        if op == "reserve":
+            grow = [int(min(rng.integers(0, 3 * pt), mb * pt - ref.lens[s])) for s in some]
+            ok = ref.reserve(some, grow)
+            c.reserve(i32(some), i32(grow))
+            if not ok:
+                refused += 1
+                with pytest.raises(ss.SemschedError) as e:
+                    c.check()
+                assert e.value.code == ss.SEM_ENOMEM
+        elif op == "fork":
+            empty = [s for s in some if ref.lens[s] == 0]
+            full = [s for s in range(slots) if ref.lens[s] > 0]
+            if not full or not empty:
+                continue
+            src = rng.choice(full, len(empty)).tolist()
+            tokens = rng.integers(0, mb * pt, len(empty)).tolist() if rng.random() < 0.5 else None
+            ref.fork(src, empty, tokens)
+            c.fork(i32(src), i32(empty), None if tokens is None else i32(tokens))
+        elif op == "free":
+            keep = rng.integers(0, mb * pt, len(some)).tolist() if rng.random() < 0.6 else None
+            ref.free(some, keep)
+            c.free(i32(some), None if keep is None else i32(keep))
+        else:
+            ref.compact()
+            c.compact()
+        c.check()
+        assert_pages(c, ref, f"step {step}: {op}")
+    assert refused > 0 or pages > 40
+
+
+def test_many_pages(ss):
+    """More live words than the planner has threads, and more sequences."""
+    import torch
+    print("many pages", flush=True)
+    pages, slots, pt = 50_000, 3000, 16
+    c = ss.KVCache(pages, slots, 32, layers=1, kv_heads=1, head_dim=64, page_tokens=pt)
+    ref = ko.Pages(pages, slots, 32, pt)
+    rng = np.random.default_rng(9)
+    mark = np.arange(pages, dtype=np.float32)
+    c.scale.copy_(torch.from_numpy(mark).view(-1, 1, 1, 1).expand(-1, 1, 2, 1))
+    ref.content = [(None, p) for p in range(pages)]
+    ids = rng.permutation(slots).tolist()
+    grow = rng.integers(1, 32 * pt, slots).tolist()
+    assert ref.reserve(ids, grow)
+    c.reserve(i32(ids), i32(grow))
+    out = rng.permutation(slots)[:2000].tolist()
+    keep = rng.integers(0, 100, 2000).tolist()
+    ref.free(out, keep)
+    c.free(i32(out), i32(keep))
+    ref.compact()
+    c.compact()
+    c.check()
+    assert c.refs.tolist() == ref.refs and c.tables.tolist() == ref.table_rows()
+    assert [w & 0xffffffff for w in c.live.tolist()] == ref.live_words()
+    got = c.scale.cpu().numpy()[:, 0, 0, 0]
+    assert all(got[p] == ref.content[p][1] for p in range(pages) if ref.refs[p])
+
+
+def test_undo_by_the_book(ss):
+    import torch
+    print("undo", flush=True)
+    c = ss.KVCache(16, 4, 4, layers=1, kv_heads=1, head_dim=64, page_tokens=16)
+    c.reserve(i32([0]), i32([20]))
+    saved = c.book.clone()
+    c.fork(i32([0, 0]), i32([1, 2]))
+    c.reserve(i32([1, 2]), i32([4, 30]))
+    c.book.copy_(saved)
+    c.reserve(i32([3]), i32([1]))
+    c.check()
+    assert c.tables[3, 0].item() == 2 and c.lens.tolist() == [20, 0, 0, 1]
+
+
+def test_device_detected_errors(ss):
+    """Each leaves the rest of the cache as it was, and memory alone."""
+    import torch
+    print("errors", flush=True)
+
+    def fresh():
+        c = ss.KVCache(8, 4, 3, layers=1, kv_heads=1, head_dim=64, page_tokens=16)
+        c.data.zero_()
+        c.reserve(i32([0, 1]), i32([20, 5]))
+        c.check()
+        return c
+
+    x = torch.ones(1, 1, 64, dtype=torch.bfloat16, device="cuda")
+    bad = [
+        ("slot beyond", ss.SEM_EINVAL, lambda c: c.reserve(i32([4]), i32([1]))),
+        ("negative slot", ss.SEM_EINVAL, lambda c: c.free(i32([-1]))),
+        ("negative growth", ss.SEM_ERANGE, lambda c: c.reserve(i32([2]), i32([-1]))),
+        ("full table", ss.SEM_EINVAL, lambda c: c.reserve(i32([2, 0]), i32([5, 40]))),
+        ("too few pages", ss.SEM_ENOMEM, lambda c: c.reserve(i32([2, 3, 1]), i32([48, 48, 1]))),
+        ("fork to a full one", ss.SEM_EINVAL, lambda c: c.fork(i32([0]), i32([1]))),
+        ("fork to itself", ss.SEM_EINVAL, lambda c: c.fork(i32([2]), i32([2]))),
+        ("fork of a negative count", ss.SEM_ERANGE, lambda c: c.fork(i32([0]), i32([2]), i32([-3]))),
+        ("negative keep", ss.SEM_ERANGE, lambda c: c.free(i32([0]), i32([-2]))),
+        ("append to a bad slot", ss.SEM_EINVAL, lambda c: c.append(0, x, x, i32([9]))),
+        ("append without room", ss.SEM_EINVAL, lambda c: c.append(0, x, x, i32([2]))),
+        ("append with bad offsets", ss.SEM_EINVAL, lambda c: c.append(0, x, x, i32([0]), i32([0, 2]))),
+        ("attend of a bad slot", ss.SEM_EINVAL, lambda c: c.attend(0, x, i32([7]))),
+        ("attend with bad offsets", ss.SEM_EINVAL, lambda c: c.attend(0, x, i32([0]), i32([0, 5]))),
+    ]
+    for name, code, call in bad:
+        print(" ", name, flush=True)
+        c = fresh()
+        book, scale = c.book.clone(), c.scale.clone()
+        call(c)
+        with pytest.raises(ss.SemschedError) as e:
+            c.check()
+        assert e.value.code == code, name
+        if name != "fork of a negative count":
+            assert torch.equal(c.book, book) and torch.equal(c.scale, scale), name
+        c.check()
+    # page numbers and lengths that the cache cannot hold
+    for what in ("page", "length"):
+        print(" ", what, flush=True)
+        c = fresh()
+        if what == "page":
+            c.tables[0, 1] = 1 << 30
+        else:
+            c.lens[0] = 100
+        for call in (lambda: c.attend(0, x, i32([0])), lambda: c.append(0, x, x, i32([0])),
+                     lambda: c.reserve(i32([0]), i32([1])), lambda: c.fork(i32([0]), i32([2])),
+                     lambda: c.free(i32([0]))):
+            call()
+            with pytest.raises(ss.SemschedError):
+                c.check()
+
+
+def test_empty_calls(ss):
+    import torch
+    print("empty", flush=True)
+    c = ss.KVCache(4, 2, 2, layers=1, kv_heads=2, head_dim=64, page_tokens=16)
+    none = i32([])
+    c.reserve(none, none)
+    c.fork(none, none)
+    c.free(none)
+    c.compact()
+    q = torch.empty(0, 4, 64, dtype=torch.float16, device="cuda")
+    c.append(0, q[:, :2], q[:, :2], none)
+    assert c.attend(0, q, none).shape == (0, 4, 64)
+    c.check()
+    empty = ss.KVCache(0, 0, 0, layers=1, kv_heads=1, head_dim=64, page_tokens=16)
+    empty.compact()
+    empty.check()
+
+
+def test_on_another_stream_and_in_a_graph(ss):
+    """A decode step enqueued on a side stream, then captured and replayed."""
+    import torch
+    print("graph", flush=True)
+    c = ss.KVCache(64, 3, 16, layers=2, kv_heads=2, head_dim=64, page_tokens=16)
+    gen = torch.Generator("cuda").manual_seed(4)
+    seqs, one = i32([0, 1, 2]), i32([1, 1, 1])
+    x = torch.randn(3, 8, 64, generator=gen, device="cuda").bfloat16()
+    out = torch.empty(2, 3, 4, 64, dtype=torch.bfloat16, device="cuda")
+    c.reserve(seqs, i32([30, 1, 100]))
+    for layer in (0, 1):
+        kv = torch.randn(2, 131, 2, 64, generator=gen, device="cuda").bfloat16()
+        c.append(layer, kv[0], kv[1], seqs, i32([0, 30, 31, 131]))
+
+    def step():
+        c.reserve(seqs, one)
+        for layer in (0, 1):
+            c.append(layer, x[:, 4:6], x[:, 6:], seqs)
+            c.attend(layer, x[:, :4], seqs, out=out[layer], max_len=256)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    saved = [t.clone() for t in (c.book, c.data, c.scale)]
+    eager = []
+    with torch.cuda.stream(side):
+        for _ in range(3):
+            step()
+            eager.append((out.clone(), c.book.clone(), c.data.clone(), c.scale.clone()))
+        c.check()
+        for t, s in zip((c.book, c.data, c.scale), saved):
+            t.copy_(s)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    torch.cuda.synchronize()
+    for want in eager:
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip((out, c.book, c.data, c.scale), want):
+            assert torch.equal(a, b)
+        torch.ones(1000, device="cuda").sum()  # the program's own work between replays
+    c.check()
+
+
+def test_blocking_forms(ss):
+    """The blocking C calls give the asynchronous ones' results and statuses."""
+    import ctypes
+
+    import torch
+    print("blocking", flush=True)
+    L = ss.lib
+    torch.cuda.synchronize()
+    L.sem_set_stream(ctypes.c_void_p(torch.cuda.current_stream().cuda_stream))
+    gen = torch.Generator("cuda").manual_seed(6)
+    x = torch.randn(20, 8, 64, generator=gen, device="cuda").half()
+    a, b = (ss.KVCache(16, 3, 4, layers=1, kv_heads=2, head_dim=64, page_tokens=16) for _ in "ab")
+    a.data.zero_(), b.data.zero_()
+    s0, s01, cu = i32([0]), i32([0, 1]), i32([0, 20])
+    a.reserve(s0, i32([20]))
+    a.append(0, x[:, 4:6], x[:, 6:], s0, cu)
+    a.fork(s0, i32([1]), i32([18]))
+    a.reserve(s01, i32([3, 3]))
+    a.free(s0, i32([17]))
+    a.compact()
+    want = a.attend(0, x[:, :4], s0, cu)
+    a.check()
+    p, ref = (lambda t: ctypes.c_void_p(t.data_ptr())), b._ref
+    grow, three, keep, eighteen, dst = i32([20]), i32([3, 3]), i32([17]), i32([18]), i32([1])
+    out = torch.empty_like(want)
+    assert L.sem_kv_reserve(ref, p(s0), p(grow), 1) == 0
+    assert L.sem_kv_append(ref, 0, p(x[:, 4:6]), p(x[:, 6:]), 1, 512, 64, 512, 64, p(s0), p(cu), 1,
+                           20) == 0
+    assert L.sem_kv_fork(ref, p(s0), p(dst), p(eighteen), 1) == 0
+    assert L.sem_kv_reserve(ref, p(s01), p(three), 2) == 0
+    assert L.sem_kv_free(ref, p(s0), p(keep), 1) == 0
+    assert L.sem_kv_compact(ref) == 0
+    q = ss.KVQueryC(x.data_ptr(), out.data_ptr(), None, 512, 64, 256, 64, 20, 0, 0, 4, 1, 1, 0,
+                    0.125)
+    assert L.sem_kv_attend(ref, 0, ctypes.byref(q), p(s0), p(cu), 1) == 0
+    assert torch.equal(out, want) and torch.equal(a.book, b.book) and torch.equal(a.scale, b.scale)
+    assert L.sem_kv_reserve(ref, p(i32([2])), p(i32([1 << 20])), 1) == ss.SEM_EINVAL
+    assert L.sem_kv_free(ref, p(s0), p(i32([-1])), 1) == ss.SEM_ERANGE
+    assert L.sem_kv_compact(ref) == 0  # the status does not outlive its call
+
+
+def test_results_do_not_depend_on_the_run(ss):
+    import torch
+    print("repeat", flush=True)
+    case = Case(ss, [700, 300, 5], fmt=ko.FP8, dim=128, pt=64, kv_heads=2)
+    q = case.queries([1, 1, 1], 8, torch.bfloat16)
+    first = case.c.attend(1, q, i32([0, 1, 2])).clone()
+    for _ in range(5):
+        assert torch.equal(case.c.attend(1, q, i32([0, 1, 2])), first)
+
+
+def test_eviction_carried_out(ss):
+    """sem_evict's victims leave with the prefixes sem_evict_plan saves, and the
+    next requests get their pages."""
+    import torch
+    print("eviction", flush=True)
+
+    class Model:  # reloading pays from 5 tokens of prompt on
+        alpha1, alpha2, beta, gamma1, gamma2 = 1 << 32, 0, 5 << 32, 1 << 31, 1 << 31
+
+    c = ss.KVCache(24, 6, 12, layers=1, kv_heads=1, head_dim=64, page_tokens=16)
+    prompt, decoded = np.array([40, 3, 70, 20, 0, 0]), np.array([8, 30, 0, 25, 0, 0])
+    lens = prompt + decoded
+    c.reserve(i32(range(6)), i32(lens))
+    p = torch.tensor([0, 2, 1, 2, 0, 0], dtype=torch.uint8, device="cuda")
+    left = i32([5, 9, 3, 50, 1, 1])
+    blocks = torch.from_numpy(-(-lens // 16)).cuda()
+    victims, upto = ss.evict(p, left, i32([0, 1, 2, 3]), blocks[:4].contiguous(),
+                             int(blocks.sum()), 12, torch.tensor([4], device="cuda"))
+    assert victims.tolist() == [3, 1]  # 14 + 4 - 12 = 6 pages over: the two hold 3 each
+    keep_prompt, save = ss.evict_plan(i32(prompt), i32(decoded), Model())
+    kept = torch.where(keep_prompt.bool(), i32(prompt) + save, torch.zeros_like(save))
+    c.free(victims, kept[victims.long()].contiguous())
+    c.compact()
+    c.check()
+    kept = kept.tolist()
+    want = [int(lens[0]), kept[1], int(lens[2]), kept[3], 0, 0]
+    assert c.lens.tolist() == want
+    used = sum(-(-n // 16) for n in want)
+    assert c.refs.tolist() == [1] * used + [0] * (24 - used)
