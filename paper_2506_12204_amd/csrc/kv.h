@@ -78,9 +78,11 @@ struct KvAttendArgs {
   int32_t bf16, wide;
   int32_t causal, window;
   float scale_log2;  // softmax scale * log2(e)
-  int32_t splits;    // parts of the key axis
-  float* part_o;     // [splits][tokens * heads][head_dim]
-  float* part_ml;    // [splits][tokens * heads][2]: maximum (log2), sum
+  int32_t tiled;       // the kernel for many rows per sequence
+  int32_t parts;       // most parts that the keys of a row tile are split into,
+  int32_t part_chunks; // of so many chunks of 64 keys each
+  float* part_o;       // [parts][tokens * heads][head_dim]
+  float* part_ml;      // [parts][tokens * heads][2]: maximum (log2), sum
 };
 
 hipError_t launch_kv_fork(const KvForkArgs& a, hipStream_t st);
@@ -90,9 +92,12 @@ hipError_t launch_kv_compact(const KvCompactArgs& a, hipStream_t st);
 hipError_t launch_kv_append(const KvAppendArgs& a, hipStream_t st);
 hipError_t launch_kv_attend(const KvAttendArgs& a, hipStream_t st);
 
-// Parts of the key axis that an attention call of these sizes is split into
-// (its workspace holds the parts' partial outputs).
-int kv_attend_splits(int64_t n, int64_t tokens, int heads, int kv_heads, int64_t max_new,
-                     int64_t max_len);
+// How an attention call of these sizes is split (its workspace holds the
+// parts' partial outputs).
+struct KvSplit {
+  int tiled, parts, part_chunks;
+};
+KvSplit kv_attend_split(int dim, int64_t n, int64_t tokens, int heads, int kv_heads,
+                        int64_t max_new, int64_t max_len);
 
 }  // namespace semsched

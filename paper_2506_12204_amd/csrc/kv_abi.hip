@@ -155,7 +155,7 @@ int check_append(const sem_kv_cache* c, int32_t layer, const void* k, const void
 }
 
 struct AttendPlan {
-  int splits = 1;
+  KvSplit split = {};
   size_t part_o = 0, part_ml = 0, total = kHeaderBytes;
 };
 
@@ -165,9 +165,9 @@ AttendPlan attend_plan(const sem_kv_cache* c, int32_t heads, int64_t n, int64_t 
   max_len = std::min<int64_t>(max_len > 0 ? max_len : INT32_MAX,
                               (int64_t)c->max_blocks * c->page_tokens);
   max_new = std::min<int64_t>(max_new > 0 ? max_new : tokens, std::max<int64_t>(tokens, 1));
-  p.splits = kv_attend_splits(n, tokens, heads, c->kv_heads, max_new, max_len);
-  if (p.splits > 1) {
-    const size_t rows = (size_t)p.splits * (size_t)tokens * (size_t)heads;
+  p.split = kv_attend_split(c->head_dim, n, tokens, heads, c->kv_heads, max_new, max_len);
+  if (p.split.parts > 1) {
+    const size_t rows = (size_t)p.split.parts * (size_t)tokens * (size_t)heads;
     p.part_o = kHeaderBytes;
     p.part_ml = align_up(p.part_o + 4 * rows * (size_t)c->head_dim);
     p.total = align_up(p.part_ml + 8 * rows);
@@ -374,7 +374,9 @@ int sem_kv_attend_async(const sem_kv_cache* cache, int32_t layer, const sem_kv_q
   a.causal = query->causal != 0;
   a.window = query->window;
   a.scale_log2 = query->scale * 1.4426950408889634f;
-  a.splits = p.splits;
+  a.tiled = p.split.tiled;
+  a.parts = p.split.parts;
+  a.part_chunks = p.split.part_chunks;
   a.part_o = reinterpret_cast<float*>(base + p.part_o);
   a.part_ml = reinterpret_cast<float*>(base + p.part_ml);
   return status_of(launch_kv_attend(a, static_cast<hipStream_t>(stream)));

@@ -14,6 +14,7 @@
 // largest vs seen, 2^14 above, so that weights down to 2^-28 of the largest
 // keep 11 bits.
 #include <algorithm>
+#include <type_traits>
 
 #include "device_common.h"
 #include "kv.h"
@@ -88,6 +89,12 @@ __device__ __forceinline__ void visible(const KvAttendArgs& a, const Sequence& q
   low = a.window > 0 ? max(pos + 1 - a.window, 0) : 0;
 }
 
+// Parts that chunks [c0, c1) of the keys are split into (the last one takes
+// what is beyond the parts that the caller's bound on the length allows for).
+__device__ __forceinline__ int parts_of(const KvAttendArgs& a, int c0, int c1) {
+  return max(1, min((c1 - c0 + a.part_chunks - 1) / a.part_chunks, a.parts));
+}
+
 __device__ __forceinline__ uint16_t to16(float x, int bf16) {
   if (bf16) {
     const uint32_t u = __float_as_uint(x);
@@ -97,44 +104,48 @@ __device__ __forceinline__ uint16_t to16(float x, int bf16) {
   return __builtin_bit_cast(uint16_t, (_Float16)x);
 }
 
-// A row's query in halves: lane group g holds channels (4 j + g) * 16 .. + 15
-// for j < D / 64. Returns what the scores have to be multiplied by.
-template <int D>
-__device__ __forceinline__ float load_query(const KvAttendArgs& a, const uint16_t* row, bool live,
-                                            int g, half8_t (&q)[D / 32]) {
-  uint16_t e[D / 4];
+// A row's query in halves, as the lane's D / (8 G) operands of eight: of G = 4
+// lane groups, group g holds channels (4 j + g) * 16 .. + 15 in operands 2 j and
+// 2 j + 1; of G = 2, channels 16 j + 8 g .. + 7 in operand j. Returns what the
+// scores have to be multiplied by, which is not negative (a negative scale
+// changes the query's sign).
+template <int D, int G>
+__device__ __forceinline__ float load_query(const KvAttendArgs& a, const uint16_t* row, int g,
+                                            half8_t (&q)[D / (8 * G)]) {
+  constexpr int N = D / (8 * G);
+  uint16_t e[N][8];
 #pragma unroll
-  for (int j = 0; j < D / 64; ++j) {
-    const uint16_t* p = row + (4 * j + g) * 16;
-    if (!live) {
-#pragma unroll
-      for (int k = 0; k < 16; ++k) e[16 * j + k] = 0;
-    } else if (a.wide) {
-      *reinterpret_cast<uint4*>(e + 16 * j) = reinterpret_cast<const uint4*>(p)[0];
-      *reinterpret_cast<uint4*>(e + 16 * j + 8) = reinterpret_cast<const uint4*>(p)[1];
+  for (int j = 0; j < N; ++j) {
+    const uint16_t* p = row + (G == 4 ? (4 * (j / 2) + g) * 16 + j % 2 * 8 : 16 * j + 8 * g);
+    if (a.wide) {
+      *reinterpret_cast<uint4*>(e[j]) = *reinterpret_cast<const uint4*>(p);
     } else {
 #pragma unroll
-      for (int k = 0; k < 16; ++k) e[16 * j + k] = p[k];
+      for (int k = 0; k < 8; ++k) e[j][k] = p[k];
     }
   }
-  if (!a.bf16) {
+  const float sign = a.scale_log2 < 0.0f ? -1.0f : 1.0f;
+  float up = 1.0f, undo = 1.0f;
+  if (a.bf16) {
+    float top = 0.0f;
 #pragma unroll
-    for (int k = 0; k < D / 4; ++k) q[k / 8][k % 8] = __builtin_bit_cast(_Float16, e[k]);
-    return 1.0f;
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) top = fmaxf(top, fabsf(load16(e[j][k], 1)));
+    if (G == 4) top = fmaxf(top, __shfl_xor(top, 16, kWave));
+    top = fmaxf(top, __shfl_xor(top, 32, kWave));
+    // 2^(14 - exponent), between 2^-126 and 2^126; rows of zeros or with an
+    // infinity stay as they are
+    const int e2 = (int)(__float_as_uint(top) >> 23);
+    const int shift = top > 0.0f && e2 < 255 ? min(max(14 - (e2 - 127), -126), 126) : 0;
+    up = __uint_as_float((uint32_t)(127 + shift) << 23);
+    undo = __uint_as_float((uint32_t)(127 - shift) << 23);
   }
-  float top = 0.0f;
 #pragma unroll
-  for (int k = 0; k < D / 4; ++k) top = fmaxf(top, fabsf(load16(e[k], 1)));
-  top = fmaxf(top, __shfl_xor(top, 16, kWave));
-  top = fmaxf(top, __shfl_xor(top, 32, kWave));
-  // 2^(14 - exponent), between 2^-126 and 2^126; rows of zeros or with an
-  // infinity stay as they are
-  const int e2 = (int)(__float_as_uint(top) >> 23);
-  const int shift = top > 0.0f && e2 < 255 ? min(max(14 - (e2 - 127), -126), 126) : 0;
-  const float up = __uint_as_float((uint32_t)(127 + shift) << 23);
+  for (int j = 0; j < N; ++j)
 #pragma unroll
-  for (int k = 0; k < D / 4; ++k) q[k / 8][k % 8] = (_Float16)(load16(e[k], 1) * up);
-  return __uint_as_float((uint32_t)(127 - shift) << 23);
+    for (int k = 0; k < 8; ++k) q[j][k] = (_Float16)(load16(e[j][k], a.bf16) * (up * sign));
+  return undo * fabsf(a.scale_log2);
 }
 
 // Sixteen codes as two operands of eight halves.
@@ -186,9 +197,8 @@ __global__ __launch_bounds__(kWaves* kWave) void kv_attend_rows(KvAttendArgs a) 
   const int token = (int)((live ? row : rows - 1) / a.group);
   const int head = kh * a.group + (int)((live ? row : rows - 1) % a.group);
   half8_t query[D / 32];
-  const float undo = load_query<D>(
-      a, a.q + (q.row0 + token) * a.q_token + head * a.q_head, live, g, query);
-  const float factor = undo * a.scale_log2;
+  const float factor = load_query<D, 4>(
+      a, a.q + (q.row0 + token) * a.q_token + head * a.q_head, g, query);
   int low, high;
   visible(a, q, token, low, high);
   // the keys that any row of the tile sees
@@ -196,8 +206,10 @@ __global__ __launch_bounds__(kWaves* kWave) void kv_attend_rows(KvAttendArgs a) 
   visible(a, q, (int)(tile * kRows / a.group), from, unused);
   visible(a, q, (int)((min(tile * kRows + kRows, rows) - 1) / a.group), unused, to);
   const int c0 = from / kChunk, c1 = (to + kChunk - 1) / kChunk;
-  const int per = (max(c1 - c0, 0) + a.splits - 1) / a.splits;
-  const int begin = c0 + (int)blockIdx.z * per, stop = min(begin + per, c1);
+  const int parts = parts_of(a, c0, c1), part = blockIdx.z;
+  if (part >= parts) return;
+  const int begin = c0 + part * a.part_chunks;
+  const int stop = part == parts - 1 ? c1 : begin + a.part_chunks;
 
   float m = kNone, l = 0.0f, vref = 0.0f;
   float4_t acc[D / 16];
@@ -342,15 +354,15 @@ __global__ __launch_bounds__(kWaves* kWave) void kv_attend_rows(KvAttendArgs a) 
   }
   if (wave != 0 || !live) return;
   const int64_t at = (q.row0 + token) * a.heads + head;
-  if (a.splits > 1) {
-    const int64_t part = (int64_t)blockIdx.z * a.tokens * a.heads + at;
-    float* o = a.part_o + part * D;
+  if (parts > 1) {
+    const int64_t slot = (int64_t)part * a.tokens * a.heads + at;
+    float* o = a.part_o + slot * D;
 #pragma unroll
     for (int y = 0; y < D / 16; ++y)
       *reinterpret_cast<float4_t*>(o + y * 16 + g * 4) = acc[y];
     if (g == 0) {
-      a.part_ml[2 * part] = most;
-      a.part_ml[2 * part + 1] = total;
+      a.part_ml[2 * slot] = most;
+      a.part_ml[2 * slot + 1] = total;
     }
     return;
   }
@@ -366,46 +378,464 @@ __global__ __launch_bounds__(kWaves* kWave) void kv_attend_rows(KvAttendArgs a) 
                     : kNone;
 }
 
-// Joins the parts of the key axis: one wave per row.
-template <int D>
-__global__ __launch_bounds__(256) void kv_attend_join(KvAttendArgs a) {
-  const int64_t all = a.tokens * a.heads;
-  const int64_t at = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
-  if (at >= all) return;
-  const int lane = lane_id();
-  float most = kNone;
-  for (int k = 0; k < a.splits; ++k) most = fmaxf(most, a.part_ml[2 * (k * all + at)]);
-  const float base = most == kNone ? 0.0f : most;
-  float total = 0.0f, o[D / 64];
-#pragma unroll
-  for (int j = 0; j < D / 64; ++j) o[j] = 0.0f;
-  for (int k = 0; k < a.splits; ++k) {
-    const int64_t part = k * all + at;
-    const float w = __builtin_amdgcn_exp2f(a.part_ml[2 * part] - base);
-    total += a.part_ml[2 * part + 1] * w;
-#pragma unroll
-    for (int j = 0; j < D / 64; ++j) o[j] += a.part_o[part * D + j * 64 + lane] * w;
-  }
-  const float inv = total > 0.0f || total != total ? 1.0f / total : 0.0f;
-  uint16_t* out = a.out + at / a.heads * a.out_token + at % a.heads * a.out_head;
-#pragma unroll
-  for (int j = 0; j < D / 64; ++j) out[j * 64 + lane] = to16(o[j] * inv, a.bf16);
-  if (a.lse && lane == 0)
-    a.lse[at] = total > 0.0f || total != total
-                    ? (most + __builtin_amdgcn_logf(total)) * 0.6931471805599453f
-                    : kNone;
+// ---------------------------------------------------------------------------
+// Many rows: tiles of NW * RT * 32 rows of one KV head.
+//
+// A wave holds RT * 32 rows (their queries and outputs in registers) and goes
+// through the keys 32 at a time; the workgroup turns their codes into halves
+// once and keeps them in LDS in operand order, so that every operand is one
+// 16-byte LDS read without bank conflicts. As above, scores are taken as K q^T:
+// a lane has the scores of one row (lane % 32) and, by the order in which keys
+// are fed, of 16 consecutive keys, which the second product takes from
+// registers.
+//
+// Three steps overlap, so that the matrix cores are fed while the vector units
+// turn scores into weights: step j takes the scores of keys j + 1, the weights
+// of keys j and the outputs of keys j - 1, which do not depend on each other.
+// Codes are loaded four steps ahead and put into LDS two steps ahead.
+constexpr int kWide = 32;  // rows of a matrix tile, and keys of a step
+// The running maximum is raised only when a score passes it by this much (in
+// powers of two), which is seldom: most steps then need no rescaling of the
+// outputs. Weights stay below 2^(kSlack + 6), which half precision holds.
+constexpr float kSlack = 8.0f;
+constexpr float kTileLift = 64.0f;  // 2^6
+typedef float float16_t __attribute__((ext_vector_type(16)));
+
+// The value of the lane 32 away.
+__device__ __forceinline__ float other_half(float x) {
+  const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                  false);
+  return __uint_as_float(lane_id() < 32 ? p[1] : p[0]);
 }
+
+// The order of a step's instructions: every matrix instruction is followed by
+// vector ones that run beside it, an operand read and an exponential.
+template <int MATRIX, int VECTOR>
+__device__ __forceinline__ void interleave() {
+#pragma unroll
+  for (int i = 0; i < MATRIX; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);       // matrix
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);       // LDS reads
+    __builtin_amdgcn_sched_group_barrier(0x002, VECTOR, 0);  // vector
+    __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);       // exponentials
+  }
+}
+
+template <int D, int FMT, int NW, int RT>
+__global__ __launch_bounds__(NW* kWave, 1) void kv_attend_tile(KvAttendArgs a) {
+  constexpr int NT = NW * kWave;
+  constexpr int KS = D / 16;       // matrix steps of the score product
+  constexpr int DY = D / 32;       // output tiles
+  constexpr int PER = 4 * D / NT;  // 16-byte units of a step's K and V per thread
+  constexpr int ROWS = NW * RT * kWide;
+  static_assert(PER >= 1 && NT * PER == 4 * D, "whole rounds of units");
+  __shared__ half8_t keys[2 * KS * kWave];      // [buffer][step][lane]
+  __shared__ half8_t vals[4 * 2 * DY * kWave];  // [buffer][8 keys of either half][tile][lane]
+  __shared__ float scales[4 * 4];               // [buffer][K tile 0, 1, V tile 0, 1]
+  const KvView& c = a.c;
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int r = lane % kWide, h = lane / kWide;
+  const int kh = blockIdx.x % c.kv_heads;
+  Sequence q;
+  int64_t tile;
+  if (!find_sequence(a, (int64_t)(gridDim.x / c.kv_heads) - 1 - blockIdx.x / c.kv_heads, ROWS, q,
+                     tile))
+    return;
+  const int64_t rows = (int64_t)q.fresh * a.group;
+  // the keys that the workgroup's rows see
+  int from, to, unused;
+  visible(a, q, (int)(tile * ROWS / a.group), from, unused);
+  visible(a, q, (int)((min(tile * ROWS + ROWS, rows) - 1) / a.group), unused, to);
+  const int c0 = from / kChunk, c1 = (to + kChunk - 1) / kChunk;
+  const int parts = parts_of(a, c0, c1), part = blockIdx.y;
+  if (part >= parts) return;
+  const int begin = 2 * (c0 + part * a.part_chunks);
+  const int stop = part == parts - 1 ? 2 * c1 : begin + 2 * a.part_chunks;
+
+  const int64_t row0 = tile * ROWS + wave * (RT * kWide);
+  half8_t query[RT][KS];
+  float factor[RT];
+  int low[RT], high[RT], token[RT], head[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const int64_t row = row0 + t * kWide + r;
+    const bool live = row < rows;
+    const int64_t at = live ? row : rows - 1;
+    token[t] = (int)(at / a.group);
+    head[t] = kh * a.group + (int)(at % a.group);
+    factor[t] = load_query<D, 2>(
+        a, a.q + (q.row0 + token[t]) * a.q_token + head[t] * a.q_head, h, query[t]);
+    visible(a, q, token[t], low[t], high[t]);
+    if (!live) {
+      low[t] = 0;
+      high[t] = 0;
+      token[t] = -1;
+    }
+  }
+  // Through LDS and back: loads may put the queries into the accumulation
+  // registers, from where the matrix cores take them; values that vector
+  // instructions computed would be copied for every use.
+  half8_t* spare = vals + wave * (KS * kWave);
+  static_assert(NW * KS <= 4 * 2 * DY, "a row tile of each wave fits the V buffers");
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+#pragma unroll
+    for (int k = 0; k < KS; ++k) spare[k * kWave + lane] = query[t][k];
+    block_sync();
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      query[t][k] = spare[k * kWave + lane];
+      asm volatile("" : "+a"(query[t][k]));
+    }
+    block_sync();
+  }
+  // the keys that all of this wave's rows see
+  int all_from = 0, all_to = 0;
+  if (row0 + RT * kWide <= rows) {
+    visible(a, q, (int)(row0 / a.group), unused, all_to);
+    visible(a, q, (int)((row0 + RT * kWide - 1) / a.group), all_from, unused);
+    if (all_from >= all_to) all_to = 0;
+  }
+
+  const int64_t block_bytes = (int64_t)c.page_tokens * D;
+  const int64_t k_off = ((int64_t)a.layer * 2 * c.kv_heads + kh) * block_bytes;
+  const int64_t v_off = k_off + c.kv_heads * block_bytes;
+  const int in_page = c.page_tokens - 1;
+  const int last_block = (q.len - 1) >> c.page_shift;
+  bool wrong = false;
+  auto page_of = [&](int t) __attribute__((always_inline)) -> int64_t {
+    const int64_t page = q.table[min(t >> c.page_shift, last_block)];
+    if (page >= 0 && page < c.num_pages) return page;
+    wrong = true;
+    return 0;
+  };
+  // A thread's 16-byte units of a step: the first half of them K, the rest V; a
+  // wave's lie in one tile of 16 keys. Pages are looked up a step before their
+  // codes are loaded, and those two steps before they are put into LDS.
+  auto is_key = [&](int k) __attribute__((always_inline)) {
+    return PER > 1 ? k < PER / 2 : wave < NW / 2;
+  };
+  auto unit_tile = [&](int k) __attribute__((always_inline)) {
+    return (int)((threadIdx.x + k * NT) / D) & 1;
+  };
+  int64_t unit_off[PER];  // where a unit is in a tile's page
+  int unit_to[PER];       // and where its operands go
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const int in = (threadIdx.x + k * NT) % D, tl = unit_tile(k), tok = in % 16;
+    unit_off[k] = (is_key(k) ? k_off : v_off) + in * 16;
+    // K: 16 channels (step in / 16) of key in % 16; V: 16 keys of channel `in`
+    unit_to[k] = is_key(k) ? in / 16 * kWave + tok / 4 * 8 + tl * 4 + tok % 4
+                           : in / 32 * kWave + tl * kWide + in % 32;
+  }
+  uint4 raw[2][PER];
+  float sraw[2] = {0.0f, 0.0f};
+  int64_t page[PER], scale_page = 0;
+  auto look_up = [&](int j) __attribute__((always_inline)) {
+    const int t = min(j, stop - 1) * kWide;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) page[k] = page_of(t + unit_tile(k) * kKvTile);
+    scale_page = page_of(t + threadIdx.x % 2 * kKvTile);
+  };
+  // (all threads load and store one of the four scales: no branch)
+  auto fetch = [&](int j, uint4 (&to)[PER], float& sc) __attribute__((always_inline)) {
+    const int t0 = min(j, stop - 1) * kWide;
+    int64_t at[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) at[k] = page[k];
+    const int64_t at_scale = scale_page;
+    // the next look-up goes first: loads return in order, and the next step
+    // needs it before these
+    look_up(j + 1);
+    sc = c.scale[((at_scale * c.layers + a.layer) * 2 + threadIdx.x / 2 % 2) * c.kv_heads + kh];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      const int t = t0 + unit_tile(k) * kKvTile;
+      to[k] = *reinterpret_cast<const uint4*>(c.data + at[k] * c.page_bytes + (t & in_page) * D +
+                                              unit_off[k]);
+    }
+  };
+  auto stage = [&](auto mask, int j, const uint4 (&from)[PER], float sc)
+      __attribute__((always_inline)) {
+    scales[(j & 3) * 4 + threadIdx.x % 4] = sc;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      uint4 w = from[k];
+      // V codes beyond the length may be anything; K ones are hidden later
+      if (decltype(mask)::value && !is_key(k)) {
+        const int n = q.len - j * kWide - unit_tile(k) * kKvTile;
+        w.x = keep_bytes(w.x, n);
+        w.y = keep_bytes(w.y, n - 4);
+        w.z = keep_bytes(w.z, n - 8);
+        w.w = keep_bytes(w.w, n - 12);
+      }
+      half8_t lo, hi;
+      codes_to_operands<FMT>(w, lo, hi);
+      half8_t* to = is_key(k) ? keys + (j & 1) * (KS * kWave) : vals + (j & 3) * (2 * DY * kWave);
+      to[unit_to[k]] = lo;
+      to[unit_to[k] + (is_key(k) ? kWide : DY * kWave)] = hi;
+    }
+  };
+
+  float m[RT], l[RT], vref = 0.0f;
+  float16_t acc[RT][DY], s0[RT], s1[RT];
+  half8_t w0[RT][2], w1[RT][2];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    m[t] = kNone;
+    l[t] = 0.0f;
+#pragma unroll
+    for (int y = 0; y < DY; ++y)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[t][y][i] = 0.0f;
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w1[t][x][i] = (_Float16)0.0f;
+  }
+  auto score = [&](int j, float16_t (&s)[RT]) __attribute__((always_inline)) {
+    const half8_t* from = keys + (j & 1) * (KS * kWave) + lane;
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      const half8_t kf = from[k * kWave];
+#pragma unroll
+      for (int t = 0; t < RT; ++t)
+        s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, query[t][k], s[t], 0, 0, 0);
+    }
+  };
+  auto output = [&](const half8_t (&vf)[2][DY], const half8_t (&w)[RT][2])
+      __attribute__((always_inline)) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int y = 0; y < DY; ++y)
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+          acc[t][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[x][y], w[t][x], acc[t][y], 0, 0, 0);
+  };
+  auto read_vals = [&](int j, half8_t (&vf)[2][DY]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int y = 0; y < DY; ++y)
+        vf[x][y] = vals[(j & 3) * (2 * DY * kWave) + (x * DY + y) * kWave + lane];
+  };
+  // Scores of a row tile become weights; its outputs so far are to be multiplied
+  // by `fade`.
+  struct Scales {
+    float ks, bias, unrel, older;
+  };
+  auto scales_of = [&](int j) __attribute__((always_inline)) {
+    const float ks = scales[(j & 3) * 4 + h];
+    const float vs0 = scales[(j & 3) * 4 + 2], vs1 = scales[(j & 3) * 4 + 3];
+    // weights are relative to the largest V scale so far (the same in all lanes)
+    const float vmax = fmaxf(fmaxf(vs0, vs1), vref);
+    const float inv = vmax > 0.0f ? __builtin_amdgcn_rcpf(vmax) : 0.0f;
+    const float older = vmax > vref ? vref * inv : 1.0f;
+    vref = vmax;
+    const float rel = fmaxf((h ? vs1 : vs0) * inv, 9.3e-10f) * kTileLift;  // (2^-30)
+    return Scales{ks, __builtin_amdgcn_logf(rel), __builtin_amdgcn_rcpf(rel), older};
+  };
+  auto weigh = [&](int t, const Scales& z, const float16_t& s, half8_t (&w)[2], float& fade)
+      __attribute__((always_inline)) {
+    // (not zero, so that a hidden key's minus infinity stays one)
+    const float f = fmaxf(z.ks * factor[t], 1e-30f);
+    float top = s[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+    top *= f;
+    top = fmaxf(top, other_half(top));
+    const bool raise = top > m[t] + kSlack;
+    const float next = raise ? top : m[t];
+    const float shrink = raise ? __builtin_amdgcn_exp2f(m[t] - next) : 1.0f;
+    m[t] = next;
+    const float b = z.bias - (next == kNone ? 0.0f : next);
+    float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], f, b));
+      sum[i % 2] += p;
+      w[i / 8][i % 8] = (_Float16)p;
+    }
+    l[t] = l[t] * shrink + (sum[0] + sum[1]) * z.unrel;
+    fade = z.older * shrink;
+    asm volatile("" : "+v"(w[0]), "+v"(w[1]));  // here, not where they are used
+  };
+  auto step = [&](auto mask, int j, float16_t (&cur)[RT], float16_t (&nxt)[RT],
+                  const half8_t (&wp)[RT][2], half8_t (&wc)[RT][2], uint4 (&rw)[PER], float& sc)
+      __attribute__((always_inline)) {
+    if (decltype(mask)::value) {
+      const int t0 = j * kWide + h * kKvTile;
+#pragma unroll
+      for (int t = 0; t < RT; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          cur[t][i] = t0 + i >= low[t] && t0 + i < high[t] ? cur[t][i] : kNone;
+    }
+    float fade[RT];
+    half8_t vf[2][DY];
+    __builtin_amdgcn_sched_barrier(0);
+    const Scales z = scales_of(j);
+    score(j + 1, nxt);
+    weigh(0, z, cur[0], wc[0], fade[0]);
+    read_vals(max(j - 1, begin), vf);
+    __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+    interleave<RT * KS, 6>();
+    __builtin_amdgcn_sched_barrier(0);
+    output(vf, wp);
+    if (RT > 1) weigh(RT - 1, z, cur[RT - 1], wc[RT - 1], fade[RT - 1]);
+    stage(mask, j + 2, rw, sc);
+    fetch(j + 4, rw, sc);
+    interleave<RT * 2 * DY, 8>();
+    __builtin_amdgcn_sched_barrier(0);
+    bool any = false;
+#pragma unroll
+    for (int t = 0; t < RT; ++t) any |= fade[t] != 1.0f;
+    if (__ballot(any)) {
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+#pragma unroll
+        for (int y = 0; y < DY; ++y) {
+          // one after the other: all of them at once in the vector registers
+          // would push out other values
+          asm volatile("" : "+a"(acc[t][y]));
+          acc[t][y] *= fade[t];
+          asm volatile("" : "+a"(acc[t][y]));
+        }
+      }
+    }
+    block_sync();
+  };
+  if (begin < stop) {
+    constexpr std::false_type plain{};
+    constexpr std::true_type masked{};
+    look_up(begin);
+    fetch(begin, raw[0], sraw[0]);
+    fetch(begin + 1, raw[1], sraw[1]);
+    stage(masked, begin, raw[0], sraw[0]);
+    stage(masked, begin + 1, raw[1], sraw[1]);
+    fetch(begin + 2, raw[0], sraw[0]);
+    fetch(begin + 3, raw[1], sraw[1]);
+    block_sync();
+    score(begin, s0);
+    block_sync();  // step `begin` puts keys begin + 2 where these were
+    for (int j = begin; j < stop; j += 2) {
+      // keys that all rows see, and codes that all are there
+      if (j * kWide >= all_from && (j + 2) * kWide <= all_to && (j + 4) * kWide <= q.len) {
+        step(plain, j, s0, s1, w1, w0, raw[0], sraw[0]);
+        step(plain, j + 1, s1, s0, w0, w1, raw[1], sraw[1]);
+      } else {
+        step(masked, j, s0, s1, w1, w0, raw[0], sraw[0]);
+        step(masked, j + 1, s1, s0, w0, w1, raw[1], sraw[1]);
+      }
+    }
+    half8_t vf[2][DY];
+    read_vals(stop - 1, vf);
+    output(vf, w1);
+  }
+  if (__ballot(wrong) && lane == 0) atomicOr(c.flags, kFlagInval);
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    l[t] += __shfl_xor(l[t], 32, kWave);
+    if (token[t] < 0) continue;
+    const int64_t at = (q.row0 + token[t]) * a.heads + head[t];
+    if (parts > 1) {
+      const int64_t slot = (int64_t)part * a.tokens * a.heads + at;
+      const float by = vref * (1.0f / kTileLift);
+      float* o = a.part_o + slot * D;
+#pragma unroll
+      for (int y = 0; y < DY; ++y)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float4_t x = {acc[t][y][4 * k] * by, acc[t][y][4 * k + 1] * by,
+                              acc[t][y][4 * k + 2] * by, acc[t][y][4 * k + 3] * by};
+          *reinterpret_cast<float4_t*>(o + y * 32 + k * 8 + h * 4) = x;
+        }
+      if (h == 0) {
+        a.part_ml[2 * slot] = m[t];
+        a.part_ml[2 * slot + 1] = l[t];
+      }
+      continue;
+    }
+    const bool some = l[t] > 0.0f || l[t] != l[t];
+    const float inv = some ? vref * (1.0f / kTileLift) / l[t] : 0.0f;
+    uint16_t* o = a.out + (q.row0 + token[t]) * a.out_token + head[t] * a.out_head;
+#pragma unroll
+    for (int y = 0; y < DY; ++y)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        o[y * 32 + i / 4 * 8 + h * 4 + i % 4] = to16(acc[t][y][i] * inv, a.bf16);
+    if (a.lse && h == 0)
+      a.lse[at] = some ? (m[t] + __builtin_amdgcn_logf(l[t])) * 0.6931471805599453f : kNone;
+  }
+}
+
+// Joins the parts of the key axis: one workgroup per row tile that has several,
+// a wave per row.
+template <int D>
+__global__ __launch_bounds__(256) void kv_attend_join(KvAttendArgs a, int tile_rows) {
+  Sequence q;
+  int64_t tile;
+  if (!find_sequence(a, blockIdx.x, tile_rows, q, tile)) return;
+  const int64_t rows = (int64_t)q.fresh * a.group;
+  const int kh = blockIdx.y, lane = lane_id();
+  int from, to, unused;
+  visible(a, q, (int)(tile * tile_rows / a.group), from, unused);
+  visible(a, q, (int)((min(tile * tile_rows + tile_rows, rows) - 1) / a.group), unused, to);
+  const int parts = parts_of(a, from / kChunk, (to + kChunk - 1) / kChunk);
+  if (parts == 1) return;
+  const int64_t all = a.tokens * a.heads;
+  const int64_t row0 = tile * tile_rows + (int64_t)blockIdx.z * 16;
+  for (int64_t row = row0 + threadIdx.x / kWave; row < min(row0 + 16, rows); row += 4) {
+    const int64_t token = q.row0 + row / a.group, head = kh * a.group + row % a.group;
+    const int64_t at = token * a.heads + head;
+    float most = kNone;
+    for (int k = 0; k < parts; ++k) most = fmaxf(most, a.part_ml[2 * (k * all + at)]);
+    const float base = most == kNone ? 0.0f : most;
+    float total = 0.0f, o[D / 64];
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) o[j] = 0.0f;
+    for (int k = 0; k < parts; ++k) {
+      const int64_t slot = k * all + at;
+      const float w = __builtin_amdgcn_exp2f(a.part_ml[2 * slot] - base);
+      total += a.part_ml[2 * slot + 1] * w;
+#pragma unroll
+      for (int j = 0; j < D / 64; ++j) o[j] += a.part_o[slot * D + j * 64 + lane] * w;
+    }
+    const bool some = total > 0.0f || total != total;
+    const float inv = some ? 1.0f / total : 0.0f;
+    uint16_t* out = a.out + token * a.out_token + head * a.out_head;
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) out[j * 64 + lane] = to16(o[j] * inv, a.bf16);
+    if (a.lse && lane == 0)
+      a.lse[at] = some ? (most + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : kNone;
+  }
+}
+
+constexpr int kTileWaves = 4;
+template <int D>
+constexpr int tile_rows() { return kTileWaves * (D > 128 ? 1 : 2) * kWide; }
 
 template <int D, int FMT>
 hipError_t launch(const KvAttendArgs& a, hipStream_t st) {
-  const int64_t tiles = a.tokens * a.group / kRows + a.n;
-  hipLaunchKernelGGL((kv_attend_rows<D, FMT>),
-                     dim3((unsigned)tiles, (unsigned)a.c.kv_heads, (unsigned)a.splits),
-                     dim3(kWaves * kWave), 0, st, a);
-  if (a.splits > 1) {
-    const int64_t all = a.tokens * a.heads;
-    hipLaunchKernelGGL(kv_attend_join<D>, dim3((unsigned)((all + 3) / 4)), dim3(256), 0, st, a);
-  }
+  const int rows = a.tiled ? tile_rows<D>() : kRows;
+  const int64_t tiles = a.tokens * a.group / rows + a.n;
+  if (a.tiled)
+    hipLaunchKernelGGL((kv_attend_tile<D, FMT, kTileWaves, D <= 128 ? 2 : 1>),
+                       dim3((unsigned)(tiles * a.c.kv_heads), (unsigned)a.parts),
+                       dim3(kTileWaves * kWave), 0, st, a);
+  else
+    hipLaunchKernelGGL((kv_attend_rows<D, FMT>),
+                       dim3((unsigned)tiles, (unsigned)a.c.kv_heads, (unsigned)a.parts),
+                       dim3(kWaves * kWave), 0, st, a);
+  if (a.parts > 1)
+    hipLaunchKernelGGL(kv_attend_join<D>,
+                       dim3((unsigned)tiles, (unsigned)a.c.kv_heads, (unsigned)(rows / 16)),
+                       dim3(256), 0, st, a, rows);
   return hipGetLastError();
 }
 
@@ -416,13 +846,20 @@ hipError_t launch_dim(const KvAttendArgs& a, hipStream_t st) {
 
 }  // namespace
 
-int kv_attend_splits(int64_t n, int64_t tokens, int heads, int kv_heads, int64_t max_new,
-                     int64_t max_len) {
-  (void)max_new;
-  const int64_t groups = (tokens * (heads / kv_heads) / kRows + n) * kv_heads;
-  const int64_t most = (max_len + 4 * kChunk - 1) / (4 * kChunk);  // a chunk per wave at least
-  return (int)std::max<int64_t>(1, std::min<int64_t>({most, 2048 / std::max<int64_t>(groups, 1),
-                                                      128}));
+KvSplit kv_attend_split(int dim, int64_t n, int64_t tokens, int heads, int kv_heads,
+                        int64_t max_new, int64_t max_len) {
+  KvSplit s = {};
+  const int group = heads / kv_heads;
+  s.tiled = max_new * group > 2 * kRows;
+  const int rows = s.tiled ? (dim == 256 ? tile_rows<256>() : tile_rows<128>()) : kRows;
+  const int64_t groups = std::max<int64_t>((tokens * group / rows + n) * kv_heads, 1);
+  const int64_t chunks = std::max<int64_t>((max_len + kChunk - 1) / kChunk, 1);
+  const int64_t want = s.tiled ? 512 : 2048;
+  const int64_t least = s.tiled ? 32 : 2 * kWaves;  // chunks of a part
+  const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(want / groups, 128));
+  s.part_chunks = (int)std::max<int64_t>(least, (chunks + parts - 1) / parts);
+  s.parts = (int)((chunks + s.part_chunks - 1) / s.part_chunks);
+  return s;
 }
 
 hipError_t launch_kv_attend(const KvAttendArgs& a, hipStream_t st) {
