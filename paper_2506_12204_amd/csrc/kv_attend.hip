@@ -31,6 +31,7 @@ constexpr int kChunk = 64;           // keys a wave takes at a time
 constexpr int kWaves = 4;
 constexpr float kLift = 16384.0f;    // 2^14
 constexpr float kNone = -__builtin_inff();
+constexpr int kMostParts = 128;      // of the key axis
 
 // Row tiles are numbered without reading the lengths: those of sequence i start
 // at cu[i] * group / rows + i, which leaves room for a partly filled one.
@@ -503,11 +504,13 @@ __global__ __launch_bounds__(NW* kWave, 1) void kv_attend_tile(KvAttendArgs a) {
   const int in_page = c.page_tokens - 1;
   const int last_block = (q.len - 1) >> c.page_shift;
   bool wrong = false;
-  auto page_of = [&](int t) __attribute__((always_inline)) -> int64_t {
-    const int64_t page = q.table[min(t >> c.page_shift, last_block)];
-    if (page >= 0 && page < c.num_pages) return page;
-    wrong = true;
-    return 0;
+  auto entry_of = [&](int t) __attribute__((always_inline)) {
+    return q.table[min(t >> c.page_shift, last_block)];
+  };
+  auto checked = [&](int32_t entry) __attribute__((always_inline)) -> uint32_t {
+    const bool bad = (uint32_t)entry >= (uint32_t)c.num_pages;
+    wrong |= bad;
+    return bad ? 0u : (uint32_t)entry;
   };
   // A thread's 16-byte units of a step: the first half of them K, the rest V; a
   // wave's lie in one tile of 16 keys. Pages are looked up a step before their
@@ -530,20 +533,20 @@ __global__ __launch_bounds__(NW* kWave, 1) void kv_attend_tile(KvAttendArgs a) {
   }
   uint4 raw[2][PER];
   float sraw[2] = {0.0f, 0.0f};
-  int64_t page[PER], scale_page = 0;
+  int32_t page[PER], scale_page = 0;
   auto look_up = [&](int j) __attribute__((always_inline)) {
     const int t = min(j, stop - 1) * kWide;
 #pragma unroll
-    for (int k = 0; k < PER; ++k) page[k] = page_of(t + unit_tile(k) * kKvTile);
-    scale_page = page_of(t + threadIdx.x % 2 * kKvTile);
+    for (int k = 0; k < PER; ++k) page[k] = entry_of(t + unit_tile(k) * kKvTile);
+    scale_page = entry_of(t + threadIdx.x % 2 * kKvTile);
   };
   // (all threads load and store one of the four scales: no branch)
   auto fetch = [&](int j, uint4 (&to)[PER], float& sc) __attribute__((always_inline)) {
     const int t0 = min(j, stop - 1) * kWide;
     int64_t at[PER];
 #pragma unroll
-    for (int k = 0; k < PER; ++k) at[k] = page[k];
-    const int64_t at_scale = scale_page;
+    for (int k = 0; k < PER; ++k) at[k] = checked(page[k]);
+    const int64_t at_scale = checked(scale_page);
     // the next look-up goes first: loads return in order, and the next step
     // needs it before these
     look_up(j + 1);
@@ -789,31 +792,48 @@ __global__ __launch_bounds__(256) void kv_attend_join(KvAttendArgs a, int tile_r
   const int parts = parts_of(a, from / kChunk, (to + kChunk - 1) / kChunk);
   if (parts == 1) return;
   const int64_t all = a.tokens * a.heads;
-  const int64_t row0 = tile * tile_rows + (int64_t)blockIdx.z * 16;
-  for (int64_t row = row0 + threadIdx.x / kWave; row < min(row0 + 16, rows); row += 4) {
-    const int64_t token = q.row0 + row / a.group, head = kh * a.group + row % a.group;
-    const int64_t at = token * a.heads + head;
-    float most = kNone;
-    for (int k = 0; k < parts; ++k) most = fmaxf(most, a.part_ml[2 * (k * all + at)]);
-    const float base = most == kNone ? 0.0f : most;
-    float total = 0.0f, o[D / 64];
+  const int64_t row = tile * tile_rows + (int64_t)blockIdx.z * 4 + threadIdx.x / kWave;
+  if (row >= rows) return;
+  const int64_t token = q.row0 + row / a.group, head = kh * a.group + row % a.group;
+  const int64_t at = token * a.heads + head;
+  // lane k has parts k and k + 64
+  static_assert(kMostParts == 2 * kWave, "two parts per lane");
+  const int far = kWave + lane;
+  const float2_t* ml = reinterpret_cast<const float2_t*>(a.part_ml) + at;
+  const float2_t p0 = lane < parts ? ml[lane * all] : float2_t{kNone, 0.0f};
+  const float2_t p1 = far < parts ? ml[far * all] : float2_t{kNone, 0.0f};
+  float most = fmaxf(p0[0], p1[0]);
 #pragma unroll
-    for (int j = 0; j < D / 64; ++j) o[j] = 0.0f;
-    for (int k = 0; k < parts; ++k) {
-      const int64_t slot = k * all + at;
-      const float w = __builtin_amdgcn_exp2f(a.part_ml[2 * slot] - base);
-      total += a.part_ml[2 * slot + 1] * w;
+  for (int off = 32; off > 0; off /= 2) most = fmaxf(most, __shfl_xor(most, off, kWave));
+  const float base = most == kNone ? 0.0f : most;
+  const float w0 = __builtin_amdgcn_exp2f(p0[0] - base), w1 = __builtin_amdgcn_exp2f(p1[0] - base);
+  float total = p0[1] * w0 + p1[1] * w1;
 #pragma unroll
-      for (int j = 0; j < D / 64; ++j) o[j] += a.part_o[slot * D + j * 64 + lane] * w;
+  for (int off = 32; off > 0; off /= 2) total += __shfl_xor(total, off, kWave);
+  constexpr int W = D / 64;  // channels of a lane
+  typedef float row_t __attribute__((ext_vector_type(W > 1 ? W : 2)));
+  float o[W];
+#pragma unroll
+  for (int j = 0; j < W; ++j) o[j] = 0.0f;
+  const float* part = a.part_o + at * D + lane * W;
+#pragma unroll 4
+  for (int k = 0; k < parts; ++k) {
+    const float w = __shfl(k < kWave ? w0 : w1, k % kWave, kWave);
+    if (W == 1) {
+      o[0] += part[k * all * D] * w;
+    } else {
+      const row_t x = *reinterpret_cast<const row_t*>(part + k * all * D);
+#pragma unroll
+      for (int j = 0; j < W; ++j) o[j] += x[j] * w;
     }
-    const bool some = total > 0.0f || total != total;
-    const float inv = some ? 1.0f / total : 0.0f;
-    uint16_t* out = a.out + token * a.out_token + head * a.out_head;
-#pragma unroll
-    for (int j = 0; j < D / 64; ++j) out[j * 64 + lane] = to16(o[j] * inv, a.bf16);
-    if (a.lse && lane == 0)
-      a.lse[at] = some ? (most + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : kNone;
   }
+  const bool some = total > 0.0f || total != total;
+  const float inv = some ? 1.0f / total : 0.0f;
+  uint16_t* out = a.out + token * a.out_token + head * a.out_head + lane * W;
+#pragma unroll
+  for (int j = 0; j < W; ++j) out[j] = to16(o[j] * inv, a.bf16);
+  if (a.lse && lane == 0)
+    a.lse[at] = some ? (most + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : kNone;
 }
 
 constexpr int kTileWaves = 4;
@@ -834,7 +854,7 @@ hipError_t launch(const KvAttendArgs& a, hipStream_t st) {
                        dim3(kWaves * kWave), 0, st, a);
   if (a.parts > 1)
     hipLaunchKernelGGL(kv_attend_join<D>,
-                       dim3((unsigned)tiles, (unsigned)a.c.kv_heads, (unsigned)(rows / 16)),
+                       dim3((unsigned)tiles, (unsigned)a.c.kv_heads, (unsigned)(rows / 4)),
                        dim3(256), 0, st, a, rows);
   return hipGetLastError();
 }
@@ -856,7 +876,7 @@ KvSplit kv_attend_split(int dim, int64_t n, int64_t tokens, int heads, int kv_he
   const int64_t chunks = std::max<int64_t>((max_len + kChunk - 1) / kChunk, 1);
   const int64_t want = s.tiled ? 512 : 2048;
   const int64_t least = s.tiled ? 32 : 2 * kWaves;  // chunks of a part
-  const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(want / groups, 128));
+  const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(want / groups, kMostParts));
   s.part_chunks = (int)std::max<int64_t>(least, (chunks + parts - 1) / parts);
   s.parts = (int)((chunks + s.part_chunks - 1) / s.part_chunks);
   return s;
