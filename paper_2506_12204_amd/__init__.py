@@ -17,6 +17,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import List, Optional, Tuple
 
 import torch
@@ -175,13 +176,13 @@ def _load() -> ctypes.CDLL:
     lib.sem_evict_async.argtypes = [vp, vp, i64, vp, vp, i64, i64, i64, vp, i64, vp, vp, vp, sz,
                                     vp]
     lib.sem_schedule_static.argtypes = [vp, vp, i64, vp, vp, vp, vp, vp]
-    kv, kq = ctypes.POINTER(KVCacheC), ctypes.POINTER(KVQueryC)
+    kv = ctypes.POINTER(KVCacheC)
     rows = [vp, vp, i64]  # sequences, offsets, their number
     tail = [vp, sz, vp]   # workspace, its size, stream
     append = [kv, i32, vp, vp, i32, i64, i64, i64, i64] + rows + [i64]
     for name, args in (("fork", [kv, vp, vp, vp, i64]), ("reserve", [kv, vp, vp, i64]),
                        ("free", [kv, vp, vp, i64]), ("compact", [kv]), ("append", append),
-                       ("attend", [kv, i32, kq] + rows)):
+                       ("attend", [kv, i32, vp] + rows)):  # (a sem_kv_query)
         for form, more in (("", []), ("_async", tail)):
             fn = getattr(lib, f"sem_kv_{name}{form}")
             fn.argtypes, fn.restype = args + more, ctypes.c_int
@@ -586,11 +587,18 @@ def evict(priority: torch.Tensor, length: torch.Tensor, cached: torch.Tensor, kv
     return victims[:k], upto
 
 
+# The handle of a device's current stream (torch.cuda.current_stream makes an
+# object of it, which takes longer than the rest of a call).
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
+
 def _round64(n: int) -> int:
     return -(-n // 64) * 64
 
 
 _KV_DTYPES = {torch.bfloat16: 0, torch.float16: 1}
+_KV_QUERY = struct.Struct("PPPqqqqqqqiiiif4x")  # sem_kv_query
+assert _KV_QUERY.size == ctypes.sizeof(KVQueryC)
 
 
 class KVCache:
@@ -662,22 +670,35 @@ class KVCache:
         self._c, self._ref = c, ctypes.byref(c)
         self.ws_bytes = int(lib.sem_kv_workspace_bytes(self._ref))
         self.workspace = torch.zeros(self.ws_bytes, dtype=torch.uint8, device=self.device)
+        self._ws, self._index = self.workspace.data_ptr(), data.get_device()
+        self._needs = {}  # workspace bytes of attention by its sizes
 
-    def _list(self, t: Optional[torch.Tensor], n: Optional[int], what: str) -> None:
-        if t is None:
-            return
-        if t.dtype != torch.int32 or t.device != self.device or t.dim() != 1 \
+    # The operations are called for every layer of every step, so their checks
+    # avoid what is slow in Python: device objects, stream objects, ctypes values.
+
+    def _list(self, t: torch.Tensor, what: str) -> int:
+        """The address of a list of int32."""
+        if t.dtype != torch.int32 or t.get_device() != self._index or t.dim() != 1 \
                 or not t.is_contiguous():
             raise TypeError(f"{what} must be a contiguous 1-D int32 tensor on the cache's GPU")
-        if n is not None and t.numel() != n:
-            raise ValueError(f"{what} must hold {n} entries")
+        return t.data_ptr()
 
-    def _rows(self, x: torch.Tensor, heads: Optional[int], what: str) -> None:
-        if x.dtype not in _KV_DTYPES or x.device != self.device:
+    def _same(self, t: Optional[torch.Tensor], n: int, what: str) -> Optional[int]:
+        if t is None:
+            return None
+        at = self._list(t, what)
+        if t.shape[0] != n:
+            raise ValueError(f"{what} must hold {n} entries")
+        return at
+
+    def _rows(self, x: torch.Tensor, what: str) -> int:
+        """The type of rows [tokens, heads, head_dim]."""
+        dtype = _KV_DTYPES.get(x.dtype)
+        if dtype is None or x.get_device() != self._index:
             raise TypeError(f"{what} must be bfloat16 or float16 on the cache's GPU")
-        if x.dim() != 3 or x.shape[2] != self.head_dim or x.stride(2) != 1 \
-                or (heads is not None and x.shape[1] != heads):
+        if x.dim() != 3 or x.shape[2] != self.head_dim or x.stride(2) != 1:
             raise ValueError(f"{what} must be [tokens, heads, head_dim] with adjacent channels")
+        return dtype
 
     def _room(self, need: int) -> None:
         """A larger workspace, the status word carried over."""
@@ -685,54 +706,59 @@ class KVCache:
             ws = torch.zeros(need, dtype=torch.uint8, device=self.device)
             ws[:4].copy_(self.workspace[:4])
             self.workspace, self.ws_bytes = ws, need
-
-    def _tail(self):
-        return self.workspace.data_ptr(), self.ws_bytes, torch.cuda.current_stream(
-            self.device).cuda_stream
+            self._ws = ws.data_ptr()
 
     def reserve(self, seqs: torch.Tensor, tokens: torch.Tensor) -> None:
         """Room for tokens[i] more tokens of seqs[i] (their lengths grow)."""
-        self._list(seqs, None, "seqs")
-        self._list(tokens, seqs.numel(), "tokens")
-        _raise(lib.sem_kv_reserve_async(self._ref, _ptr(seqs), _ptr(tokens), seqs.numel(),
-                                        *self._tail()), "sem_kv_reserve_async")
+        n = seqs.numel()
+        rc = lib.sem_kv_reserve_async(self._ref, self._list(seqs, "seqs"),
+                                      self._same(tokens, n, "tokens"), n, self._ws, self.ws_bytes,
+                                      _raw_stream(self._index))
+        if rc:
+            _raise(rc, "sem_kv_reserve_async")
 
     def fork(self, src: torch.Tensor, dst: torch.Tensor,
              tokens: Optional[torch.Tensor] = None) -> None:
         """The empty dst[i] share the first tokens[i] tokens of src[i] (default: all)."""
-        self._list(src, None, "src")
-        self._list(dst, src.numel(), "dst")
-        self._list(tokens, src.numel(), "tokens")
-        _raise(lib.sem_kv_fork_async(self._ref, _ptr(src), _ptr(dst), _ptr(tokens), src.numel(),
-                                     *self._tail()), "sem_kv_fork_async")
+        n = src.numel()
+        rc = lib.sem_kv_fork_async(self._ref, self._list(src, "src"), self._same(dst, n, "dst"),
+                                   self._same(tokens, n, "tokens"), n, self._ws, self.ws_bytes,
+                                   _raw_stream(self._index))
+        if rc:
+            _raise(rc, "sem_kv_fork_async")
 
     def free(self, seqs: torch.Tensor, keep: Optional[torch.Tensor] = None) -> None:
         """seqs[i] keeps its first keep[i] tokens (default: none)."""
-        self._list(seqs, None, "seqs")
-        self._list(keep, seqs.numel(), "keep")
-        _raise(lib.sem_kv_free_async(self._ref, _ptr(seqs), _ptr(keep), seqs.numel(),
-                                     *self._tail()), "sem_kv_free_async")
+        n = seqs.numel()
+        rc = lib.sem_kv_free_async(self._ref, self._list(seqs, "seqs"),
+                                   self._same(keep, n, "keep"), n, self._ws, self.ws_bytes,
+                                   _raw_stream(self._index))
+        if rc:
+            _raise(rc, "sem_kv_free_async")
 
     def compact(self) -> None:
         """Moves the pages in use to the lowest numbers."""
-        _raise(lib.sem_kv_compact_async(self._ref, *self._tail()), "sem_kv_compact_async")
+        _raise(lib.sem_kv_compact_async(self._ref, self._ws, self.ws_bytes,
+                                        _raw_stream(self._index)), "sem_kv_compact_async")
 
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, seqs: torch.Tensor,
                cu: Optional[torch.Tensor] = None) -> None:
         """Writes k, v [tokens, kv_heads, head_dim] (bfloat16 or float16; strides of
         tokens and heads are free) of one layer. Sequence seqs[i]'s new tokens are
         rows cu[i]..cu[i+1] (None: row i), the last ones of its length."""
-        self._rows(k, self.kv_heads, "k")
-        self._rows(v, self.kv_heads, "v")
-        if v.dtype != k.dtype or v.shape != k.shape:
-            raise ValueError("k and v must have one type and shape")
-        self._list(seqs, None, "seqs")
+        dtype = self._rows(k, "k")
+        self._rows(v, "v")
+        if v.dtype != k.dtype or v.shape != k.shape or k.shape[1] != self.kv_heads:
+            raise ValueError("k and v must have one type and shape, with a row per KV head")
         n = seqs.numel()
-        self._list(cu, n + 1, "cu")
-        _raise(lib.sem_kv_append_async(self._ref, layer, _ptr(k), _ptr(v), _KV_DTYPES[k.dtype],
-                                       k.stride(0), k.stride(1), v.stride(0), v.stride(1),
-                                       _ptr(seqs), _ptr(cu), n, k.shape[0], *self._tail()),
-               "sem_kv_append_async")
+        k0, k1, _ = k.stride()
+        v0, v1, _ = v.stride()
+        rc = lib.sem_kv_append_async(self._ref, layer, k.data_ptr(), v.data_ptr(), dtype, k0, k1,
+                                     v0, v1, self._list(seqs, "seqs"),
+                                     self._same(cu, n + 1, "cu"), n, k.shape[0], self._ws,
+                                     self.ws_bytes, _raw_stream(self._index))
+        if rc:
+            _raise(rc, "sem_kv_append_async")
 
     def attend(self, layer: int, q: torch.Tensor, seqs: torch.Tensor,
                cu: Optional[torch.Tensor] = None, *, causal: bool = True, window: int = 0,
@@ -747,35 +773,43 @@ class KVCache:
         a sequence's queries and length (0: unknown) and only guide how the
         work is split. ``lse`` (float32 [tokens, heads]) receives the log of
         the softmax sums. Returns ``out``."""
-        self._rows(q, None, "q")
+        dtype = self._rows(q, "q")
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         else:
-            self._rows(out, q.shape[1], "out")
+            self._rows(out, "out")
             if out.dtype != q.dtype or out.shape != q.shape:
                 raise ValueError("out must have q's type and shape")
-        tokens, heads = q.shape[0], q.shape[1]
-        if lse is not None and (lse.dtype != torch.float32 or lse.device != self.device
+        tokens, heads, _ = q.shape
+        if lse is not None and (lse.dtype != torch.float32 or lse.get_device() != self._index
                                 or lse.shape != (tokens, heads) or not lse.is_contiguous()):
             raise ValueError("lse must be contiguous float32 [tokens, heads] on the cache's GPU")
-        self._list(seqs, None, "seqs")
         n = seqs.numel()
-        self._list(cu, n + 1, "cu")
-        query = KVQueryC(q.data_ptr(), out.data_ptr(), lse.data_ptr() if lse is not None else None,
-                         q.stride(0), q.stride(1), out.stride(0), out.stride(1), tokens,
-                         max_new, max_len, heads, _KV_DTYPES[q.dtype], bool(causal), window,
-                         self.head_dim ** -0.5 if scale is None else scale)
-        self._room(int(lib.sem_kv_attend_workspace_bytes(self._ref, heads, n, tokens, max_new,
-                                                         max_len)))
-        _raise(lib.sem_kv_attend_async(self._ref, layer, ctypes.byref(query), _ptr(seqs),
-                                       _ptr(cu), n, *self._tail()), "sem_kv_attend_async")
+        sizes = (heads, n, tokens, max_new, max_len)
+        need = self._needs.get(sizes)
+        if need is None:
+            if len(self._needs) > 4096:
+                self._needs.clear()
+            need = int(lib.sem_kv_attend_workspace_bytes(self._ref, *sizes))
+            self._needs[sizes] = need
+        if need > self.ws_bytes:
+            self._room(need)
+        q0, q1, _ = q.stride()
+        o0, o1, _ = out.stride()
+        query = _KV_QUERY.pack(q.data_ptr(), out.data_ptr(), 0 if lse is None else lse.data_ptr(),
+                               q0, q1, o0, o1, tokens, max_new, max_len, heads, dtype, causal,
+                               window, self.head_dim ** -0.5 if scale is None else scale)
+        rc = lib.sem_kv_attend_async(self._ref, layer, query, self._list(seqs, "seqs"),
+                                     self._same(cu, n + 1, "cu"), n, self._ws, self.ws_bytes,
+                                     _raw_stream(self._index))
+        if rc:
+            _raise(rc, "sem_kv_attend_async")
         return out
 
     def check(self) -> None:
         """Waits for the current stream; raises on an error of any operation
         since the last check."""
-        ws, _, stream = self._tail()
-        code = lib.sem_check(ws, stream)
+        code = lib.sem_check(self._ws, _raw_stream(self._index))
         if code != SEM_OK:
             self.workspace[:4].zero_()
         _raise(code, "KVCache")

@@ -34,9 +34,10 @@ constexpr float kNone = -__builtin_inff();
 constexpr int kMostParts = 128;      // of the key axis
 
 // Row tiles are numbered without reading the lengths: those of sequence i start
-// at cu[i] * group / rows + i, which leaves room for a partly filled one.
+// at cu[i] * group / rows + i, which leaves room for a partly filled one. Without
+// offsets, one token each, every sequence has the same number of them.
 __device__ __forceinline__ int64_t tile_start(const KvAttendArgs& a, int64_t i, int rows) {
-  return ((int64_t)(a.cu ? a.cu[i] : (int32_t)i) * a.group) / rows + i;
+  return (int64_t)a.cu[i] * a.group / rows + i;
 }
 
 struct Sequence {
@@ -49,21 +50,29 @@ struct Sequence {
 __device__ __forceinline__ bool find_sequence(const KvAttendArgs& a, int64_t u, int rows,
                                               Sequence& q, int64_t& tile) {
   const KvView& c = a.c;
-  int64_t i = 0, end = a.n;
-  while (end - i > 1) {
-    const int64_t mid = (i + end) / 2;
-    if (tile_start(a, mid, rows) <= u) i = mid;
-    else end = mid;
+  int64_t i;
+  if (a.cu) {
+    int64_t end = a.n;
+    i = 0;
+    while (end - i > 1) {
+      const int64_t mid = (i + end) / 2;
+      if (tile_start(a, mid, rows) <= u) i = mid;
+      else end = mid;
+    }
+    tile = u - tile_start(a, i, rows);
+    if (u == 0 && (a.cu[0] != 0 || a.cu[a.n] != a.tokens) && threadIdx.x == 0)
+      atomicOr(c.flags, kFlagInval);
+  } else {
+    const uint32_t each = (uint32_t)(a.group + rows - 1) / (uint32_t)rows;
+    i = (uint32_t)u / each;
+    tile = (uint32_t)u % each;
   }
-  if (a.cu && u == 0 && (a.cu[0] != 0 || a.cu[a.n] != a.tokens) && threadIdx.x == 0)
-    atomicOr(c.flags, kFlagInval);
   q.row0 = a.cu ? a.cu[i] : i;
   const int64_t fresh = a.cu ? (int64_t)a.cu[i + 1] - q.row0 : 1;
   if (fresh < 0 || q.row0 < 0 || q.row0 + fresh > a.tokens) {
     if (threadIdx.x == 0) atomicOr(c.flags, kFlagInval);
     return false;
   }
-  tile = u - tile_start(a, i, rows);
   if (tile < 0 || tile * rows >= fresh * a.group) return false;
   q.fresh = (int)fresh;
   const int32_t s = a.seqs[i];
@@ -217,38 +226,60 @@ __global__ __launch_bounds__(kWaves* kWave) void kv_attend_rows(KvAttendArgs a) 
 #pragma unroll
   for (int y = 0; y < D / 16; ++y) acc[y] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
   const int64_t block_bytes = (int64_t)c.page_tokens * D;
-  const int64_t k_off = (((int64_t)a.layer * 2) * c.kv_heads + kh) * block_bytes;
-  const int64_t v_off = (((int64_t)a.layer * 2 + 1) * c.kv_heads + kh) * block_bytes;
+  const int64_t k_off =
+      ((int64_t)a.layer * 2 * c.kv_heads + kh) * block_bytes + (r % 4) * 16 + g * 256;
+  const int64_t v_off =
+      (((int64_t)a.layer * 2 + 1) * c.kv_heads + kh) * block_bytes + r * 16;
   const int in_page = c.page_tokens - 1;
   const int last_block = (q.len - 1) >> c.page_shift;
   bool wrong = false;
-  for (int ch = begin + wave; ch < stop; ch += kWaves) {
-    const int t0 = ch * kChunk;
-    // the pages of this lane's key rows and of its 16 keys
-    const int kt = t0 + r / 4 * kKvTile, vt = t0 + g * kKvTile;
-    int64_t kpage = q.table[min(kt >> c.page_shift, last_block)];
-    int64_t vpage = q.table[min(vt >> c.page_shift, last_block)];
-    if (kpage < 0 || kpage >= c.num_pages) {
-      wrong = true;
-      kpage = 0;
-    }
-    if (vpage < 0 || vpage >= c.num_pages) {
-      wrong = true;
-      vpage = 0;
-    }
-    const uint8_t* kp = c.data + kpage * c.page_bytes + k_off + (int64_t)(kt & in_page) * D +
-                        (r % 4) * 16 + g * 256;
-    const uint8_t* vp = c.data + vpage * c.page_bytes + v_off + (int64_t)(vt & in_page) * D + r * 16;
+  auto checked = [&](int32_t entry) __attribute__((always_inline)) -> int64_t {
+    const bool bad = (uint32_t)entry >= (uint32_t)c.num_pages;
+    wrong |= bad;
+    return bad ? 0 : entry;
+  };
+  // Loads run ahead: table entries two of this wave's chunks, then K (and the
+  // scales) and V one, each as soon as the registers of the last are free. They
+  // return in order, so the entries that the next loads wait for go first.
+  int32_t kentry = 0, ventry = 0;  // of the pages of this lane's K rows and of its 16 keys
+  uint4 kc[4][D / 64], vc[D / 16];
+  float kscale = 0.0f, vscale = 0.0f;
+  auto look_up = [&](int ch) __attribute__((always_inline)) {
+    const int t0 = min(ch, stop - 1) * kChunk;
+    kentry = q.table[min((t0 + r / 4 * kKvTile) >> c.page_shift, last_block)];
+    ventry = q.table[min((t0 + g * kKvTile) >> c.page_shift, last_block)];
+  };
+  auto load_k = [&](int ch, int64_t kpage, int64_t vpage) __attribute__((always_inline)) {
     const float* sp = c.scale + (vpage * c.layers + a.layer) * 2 * c.kv_heads + kh;
-    const float ks = sp[0] * factor, vs = sp[c.kv_heads];
-    uint4 kc[4][D / 64], vc[D / 16];
+    kscale = sp[0];
+    vscale = sp[c.kv_heads];
+    const uint8_t* kp = c.data + kpage * c.page_bytes + k_off +
+                        ((ch * kChunk + r / 4 * kKvTile) & in_page) * D;
 #pragma unroll
     for (int x = 0; x < 4; ++x)
 #pragma unroll
       for (int j = 0; j < D / 64; ++j)
         kc[x][j] = *reinterpret_cast<const uint4*>(kp + x * 64 + j * 1024);
+  };
+  auto load_v = [&](int ch, int64_t vpage) __attribute__((always_inline)) {
+    const uint8_t* vp = c.data + vpage * c.page_bytes + v_off +
+                        ((ch * kChunk + g * kKvTile) & in_page) * D;
 #pragma unroll
     for (int y = 0; y < D / 16; ++y) vc[y] = *reinterpret_cast<const uint4*>(vp + y * 256);
+  };
+  if (begin + wave < stop) {
+    look_up(begin + wave);
+    const int64_t kpage = checked(kentry), vpage = checked(ventry);
+    look_up(begin + wave + kWaves);
+    load_k(begin + wave, kpage, vpage);
+    load_v(begin + wave, vpage);
+  }
+  for (int ch = begin + wave; ch < stop; ch += kWaves) {
+    const int t0 = ch * kChunk, vt = t0 + g * kKvTile;
+    const bool more = ch + kWaves < stop;
+    const float ks = kscale * factor, vs = vscale;
+    const int64_t kpage = checked(kentry), vpage = checked(ventry);
+    look_up(ch + 2 * kWaves);
     float s[16];
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
@@ -263,6 +294,7 @@ __global__ __launch_bounds__(kWaves* kWave) void kv_attend_rows(KvAttendArgs a) 
 #pragma unroll
       for (int i = 0; i < 4; ++i) s[4 * x + i] = t[i] * ks;
     }
+    if (more) load_k(ch + kWaves, kpage, vpage);
     // keys that this row does not see (whatever is held there)
 #pragma unroll
     for (int k = 0; k < 16; ++k) s[k] = vt + k >= low && vt + k < high && live ? s[k] : kNone;
@@ -315,6 +347,7 @@ __global__ __launch_bounds__(kWaves* kWave) void kv_attend_rows(KvAttendArgs a) 
       acc[y] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, w0, acc[y], 0, 0, 0);
       acc[y] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, w1, acc[y], 0, 0, 0);
     }
+    if (more) load_v(ch + kWaves, vpage);
   }
   if (__ballot(wrong) && lane == 0) atomicOr(c.flags, kFlagInval);
   // the four lane groups of a row each hold a quarter of its sum
@@ -843,7 +876,8 @@ constexpr int tile_rows() { return kTileWaves * (D > 128 ? 1 : 2) * kWide; }
 template <int D, int FMT>
 hipError_t launch(const KvAttendArgs& a, hipStream_t st) {
   const int rows = a.tiled ? tile_rows<D>() : kRows;
-  const int64_t tiles = a.tokens * a.group / rows + a.n;
+  const int64_t tiles = a.cu ? a.tokens * a.group / rows + a.n
+                             : a.n * ((a.group + rows - 1) / rows);
   if (a.tiled)
     hipLaunchKernelGGL((kv_attend_tile<D, FMT, kTileWaves, D <= 128 ? 2 : 1>),
                        dim3((unsigned)(tiles * a.c.kv_heads), (unsigned)a.parts),
