@@ -457,9 +457,10 @@ int sem_schedule_static(const uint8_t *priority, const int32_t *length, int64_t 
  * Every call has a blocking form and an asynchronous one that allocates
  * nothing, does not synchronise, and takes a caller-owned DEVICE workspace
  * (256-byte aligned) and the stream; its calls may be captured into a HIP
- * graph. The asynchronous calls add their errors to the workspace's first word
- * and never clear it, so that one sem_check covers a whole step; the caller
- * zeroes that word before the first call and after an error. A cache and a
+ * graph. The caller zeroes the workspace's first SEM_KV_ZEROED_BYTES bytes
+ * before the first call. The asynchronous calls add their errors to its first
+ * word and never clear it, so that one sem_check covers a whole step; the
+ * caller zeroes that word again after an error. A cache and a
  * workspace must not be used by calls in flight on different streams.
  *
  * Lists of sequences name each at most once. Errors: SEM_EINVAL for null
@@ -468,6 +469,7 @@ int sem_schedule_static(const uint8_t *priority, const int32_t *length, int64_t 
  * the cache (no memory outside the arguments is accessed); SEM_ERANGE for a
  * negative token count.
  */
+#define SEM_KV_ZEROED_BYTES 4352
 #define SEM_KV_INT8 0
 #define SEM_KV_FP8 1
 #define SEM_KV_BF16 0
@@ -489,7 +491,7 @@ typedef struct {
 size_t sem_kv_page_bytes(const sem_kv_cache *cache);
 
 /* Workspace of the asynchronous calls other than attend (fork, free and
- * append need only the first 256 bytes of it). */
+ * append need only its first SEM_KV_ZEROED_BYTES). */
 size_t sem_kv_workspace_bytes(const sem_kv_cache *cache);
 
 /*

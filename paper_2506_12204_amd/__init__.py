@@ -704,7 +704,7 @@ class KVCache:
         """A larger workspace, the status word carried over."""
         if need > self.ws_bytes:
             ws = torch.zeros(need, dtype=torch.uint8, device=self.device)
-            ws[:4].copy_(self.workspace[:4])
+            ws[:4].copy_(self.workspace[:4])  # (the rest of its first bytes is zero between calls)
             self.workspace, self.ws_bytes = ws, need
             self._ws = ws.data_ptr()
 

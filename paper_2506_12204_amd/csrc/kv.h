@@ -9,6 +9,7 @@
 
 namespace semsched {
 
+constexpr int kKvCounts = 1024;      // counters of attention's tiles with several parts
 constexpr int kKvTile = 16;          // tokens per tile of a page's block
 
 // The cache as the kernels see it: the caller's arrays and the derived sizes.
@@ -79,8 +80,10 @@ struct KvAttendArgs {
   int32_t causal, window;
   float scale_log2;  // softmax scale * log2(e)
   int32_t tiled;       // the kernel for many rows per sequence
+  int32_t waves;       // of the other kernel's workgroups, 4 or 8
   int32_t parts;       // most parts that the keys of a row tile are split into,
   int32_t part_chunks; // of so many chunks of 64 keys each
+  uint32_t* counts;    // [kKvCounts] parts finished, zero between calls
   float* part_o;       // [parts][tokens * heads][head_dim]
   float* part_ml;      // [parts][tokens * heads][2]: maximum (log2), sum
 };
@@ -95,7 +98,7 @@ hipError_t launch_kv_attend(const KvAttendArgs& a, hipStream_t st);
 // How an attention call of these sizes is split (its workspace holds the
 // parts' partial outputs).
 struct KvSplit {
-  int tiled, parts, part_chunks;
+  int tiled, waves, parts, part_chunks;
 };
 KvSplit kv_attend_split(int dim, int64_t n, int64_t tokens, int heads, int kv_heads,
                         int64_t max_new, int64_t max_len);

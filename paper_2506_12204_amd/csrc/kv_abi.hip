@@ -14,6 +14,10 @@ using namespace semsched;
 
 namespace {
 
+// What callers zero: the status word's 256 bytes and the counters.
+constexpr size_t kZeroed = kHeaderBytes + 4 * (size_t)kKvCounts;
+static_assert(kZeroed == SEM_KV_ZEROED_BYTES, "the header's size is the layouts'");
+
 constexpr int32_t kMaxLayers = 4096, kMaxHeads = 1024, kMaxPageTokens = 1024;
 
 // The sizes alone (no pointer is looked at).
@@ -69,12 +73,12 @@ KvView view_of(const sem_kv_cache* c, void* ws) {
 // Reserve's lists and compact's lists share the space after the header.
 struct PagesLayout {
   size_t ncopies = 64, counts = 64;  // in the header, after the status word
-  size_t begin = 0, copies = 0, fresh = 0, moves = 0, remap = 0, total = kHeaderBytes;
+  size_t begin = 0, copies = 0, fresh = 0, moves = 0, remap = 0, total = kZeroed;
 };
 
 PagesLayout pages_layout(const sem_kv_cache* c) {
   PagesLayout L;
-  size_t off = kHeaderBytes;
+  size_t off = kZeroed;
   auto take = [&](size_t bytes) {
     const size_t at = off;
     off = align_up(off + bytes);
@@ -85,7 +89,7 @@ PagesLayout pages_layout(const sem_kv_cache* c) {
   L.copies = take(8 * slots);
   L.fresh = take(4 * pages);
   const size_t reserve = off;
-  off = kHeaderBytes;
+  off = kZeroed;
   L.moves = take(8 * (pages / 2 + 1));
   L.remap = take(4 * pages);
   L.total = std::max(off, reserve);
@@ -98,7 +102,7 @@ bool workspace_ok(const void* ws, size_t have, size_t need) {
 
 int status_of(hipError_t e) { return e == hipSuccess ? SEM_OK : SEM_EDEVICE; }
 
-// A blocking call: the library's workspace with a clear status word, the
+// A blocking call: the library's workspace with its first bytes zeroed, the
 // asynchronous form on the blocking calls' stream, the status.
 template <typename F>
 int blocking(size_t bytes, F enqueue) {
@@ -107,7 +111,8 @@ int blocking(size_t bytes, F enqueue) {
   int rc = blocking_workspace(bytes, &ws);
   if (rc != SEM_OK) return rc;
   const hipStream_t st = blocking_stream();
-  if (launch_fill_zero(static_cast<uint32_t*>(ws), 1, st) != hipSuccess) return SEM_EDEVICE;
+  if (launch_fill_zero(static_cast<uint32_t*>(ws), kZeroed / 4, st) != hipSuccess)
+    return SEM_EDEVICE;
   rc = enqueue(ws, bytes, st);
   return rc != SEM_OK ? rc : blocking_finish(ws, st);
 }
@@ -156,7 +161,7 @@ int check_append(const sem_kv_cache* c, int32_t layer, const void* k, const void
 
 struct AttendPlan {
   KvSplit split = {};
-  size_t part_o = 0, part_ml = 0, total = kHeaderBytes;
+  size_t part_o = 0, part_ml = 0, total = kZeroed;
 };
 
 AttendPlan attend_plan(const sem_kv_cache* c, int32_t heads, int64_t n, int64_t tokens,
@@ -168,7 +173,7 @@ AttendPlan attend_plan(const sem_kv_cache* c, int32_t heads, int64_t n, int64_t 
   p.split = kv_attend_split(c->head_dim, n, tokens, heads, c->kv_heads, max_new, max_len);
   if (p.split.parts > 1) {
     const size_t rows = (size_t)p.split.parts * (size_t)tokens * (size_t)heads;
-    p.part_o = kHeaderBytes;
+    p.part_o = kZeroed;
     p.part_ml = align_up(p.part_o + 4 * rows * (size_t)c->head_dim);
     p.total = align_up(p.part_ml + 8 * rows);
   }
@@ -221,7 +226,7 @@ int sem_kv_fork_async(const sem_kv_cache* cache, const int32_t* src, const int32
                       void* stream) {
   const int rc = check_lists(cache, src, dst, n);
   if (rc != SEM_OK) return rc;
-  if (!workspace_ok(workspace, ws_bytes, kHeaderBytes)) return SEM_EINVAL;
+  if (!workspace_ok(workspace, ws_bytes, kZeroed)) return SEM_EINVAL;
   const KvForkArgs a = {view_of(cache, workspace), src, dst, tokens, n};
   return status_of(launch_kv_fork(a, static_cast<hipStream_t>(stream)));
 }
@@ -230,7 +235,7 @@ int sem_kv_fork(const sem_kv_cache* cache, const int32_t* src, const int32_t* ds
                 const int32_t* tokens, int64_t n) {
   const int rc = check_lists(cache, src, dst, n);
   if (rc != SEM_OK) return rc;
-  return blocking(kHeaderBytes, [&](void* ws, size_t bytes, hipStream_t st) {
+  return blocking(kZeroed, [&](void* ws, size_t bytes, hipStream_t st) {
     return sem_kv_fork_async(cache, src, dst, tokens, n, ws, bytes, st);
   });
 }
@@ -239,7 +244,7 @@ int sem_kv_free_async(const sem_kv_cache* cache, const int32_t* seqs, const int3
                       int64_t n, void* workspace, size_t ws_bytes, void* stream) {
   const int rc = check_free(cache, seqs, n);
   if (rc != SEM_OK) return rc;
-  if (!workspace_ok(workspace, ws_bytes, kHeaderBytes)) return SEM_EINVAL;
+  if (!workspace_ok(workspace, ws_bytes, kZeroed)) return SEM_EINVAL;
   const KvFreeArgs a = {view_of(cache, workspace), seqs, keep, n};
   return status_of(launch_kv_free(a, static_cast<hipStream_t>(stream)));
 }
@@ -247,7 +252,7 @@ int sem_kv_free_async(const sem_kv_cache* cache, const int32_t* seqs, const int3
 int sem_kv_free(const sem_kv_cache* cache, const int32_t* seqs, const int32_t* keep, int64_t n) {
   const int rc = check_free(cache, seqs, n);
   if (rc != SEM_OK) return rc;
-  return blocking(kHeaderBytes, [&](void* ws, size_t bytes, hipStream_t st) {
+  return blocking(kZeroed, [&](void* ws, size_t bytes, hipStream_t st) {
     return sem_kv_free_async(cache, seqs, keep, n, ws, bytes, st);
   });
 }
@@ -312,7 +317,7 @@ int sem_kv_append_async(const sem_kv_cache* cache, int32_t layer, const void* k,
   const int rc = check_append(cache, layer, k, v, dtype, k_token_stride, k_head_stride,
                               v_token_stride, v_head_stride, seqs, cu, n, tokens);
   if (rc != SEM_OK) return rc;
-  if (!workspace_ok(workspace, ws_bytes, kHeaderBytes)) return SEM_EINVAL;
+  if (!workspace_ok(workspace, ws_bytes, kZeroed)) return SEM_EINVAL;
   KvAppendArgs a = {};
   a.c = view_of(cache, workspace);
   a.k = static_cast<const uint16_t*>(k);
@@ -338,7 +343,7 @@ int sem_kv_append(const sem_kv_cache* cache, int32_t layer, const void* k, const
   const int rc = check_append(cache, layer, k, v, dtype, k_token_stride, k_head_stride,
                               v_token_stride, v_head_stride, seqs, cu, n, tokens);
   if (rc != SEM_OK) return rc;
-  return blocking(kHeaderBytes, [&](void* ws, size_t bytes, hipStream_t st) {
+  return blocking(kZeroed, [&](void* ws, size_t bytes, hipStream_t st) {
     return sem_kv_append_async(cache, layer, k, v, dtype, k_token_stride, k_head_stride,
                                v_token_stride, v_head_stride, seqs, cu, n, tokens, ws, bytes, st);
   });
@@ -375,8 +380,10 @@ int sem_kv_attend_async(const sem_kv_cache* cache, int32_t layer, const sem_kv_q
   a.window = query->window;
   a.scale_log2 = query->scale * 1.4426950408889634f;
   a.tiled = p.split.tiled;
+  a.waves = p.split.waves;
   a.parts = p.split.parts;
   a.part_chunks = p.split.part_chunks;
+  a.counts = reinterpret_cast<uint32_t*>(base + kHeaderBytes);
   a.part_o = reinterpret_cast<float*>(base + p.part_o);
   a.part_ml = reinterpret_cast<float*>(base + p.part_ml);
   return status_of(launch_kv_attend(a, static_cast<hipStream_t>(stream)));

@@ -28,10 +28,13 @@ typedef float float4_t __attribute__((ext_vector_type(4)));
 
 constexpr int kRows = 16;            // rows of a tile: a token and a head each
 constexpr int kChunk = 64;           // keys a wave takes at a time
-constexpr int kWaves = 4;
-constexpr float kLift = 16384.0f;    // 2^14
+constexpr float kLift = 64.0f;       // 2^6
 constexpr float kNone = -__builtin_inff();
 constexpr int kMostParts = 128;      // of the key axis
+// The running maximum is raised only when a score passes it by this much (in
+// powers of two), which is seldom: most steps then need no rescaling of the
+// outputs. Weights stay below kLift * 2^kSlack, which half precision holds.
+constexpr float kSlack = 8.0f;
 
 // Row tiles are numbered without reading the lengths: those of sequence i start
 // at cu[i] * group / rows + i, which leaves room for a partly filled one. Without
@@ -180,8 +183,68 @@ __device__ __forceinline__ uint32_t keep_bytes(uint32_t w, int n) {
   return n >= 4 ? w : n <= 0 ? 0u : w & ((1u << (8 * n)) - 1u);
 }
 
-// One workgroup: a tile of 16 rows of one KV head over one part of the key
-// axis; its four waves take chunks of 64 keys in turn and join at the end.
+// The value of the lane 32 away.
+__device__ __forceinline__ float other_half(float x) {
+  const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                  false);
+  return __uint_as_float(lane_id() < 32 ? p[1] : p[0]);
+}
+
+// Writes a row that is joined: a lane holds D / 64 channels, not divided by the
+// sum yet.
+template <int D>
+__device__ __forceinline__ void finish_row(const KvAttendArgs& a, int64_t token, int64_t head,
+                                           float most, float total, const float (&o)[D / 64]) {
+  constexpr int W = D / 64;
+  const bool some = total > 0.0f || total != total;
+  const float inv = some ? 1.0f / total : 0.0f;
+  uint16_t* out = a.out + token * a.out_token + head * a.out_head + lane_id() * W;
+#pragma unroll
+  for (int j = 0; j < W; ++j) out[j] = to16(o[j] * inv, a.bf16);
+  if (a.lse && lane_id() == 0)
+    a.lse[token * a.heads + head] =
+        some ? (most + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : kNone;
+}
+
+// Joins a row's parts with one wave.
+template <int D>
+__device__ __forceinline__ void join_row(const KvAttendArgs& a, int64_t token, int64_t head,
+                                         int parts) {
+  constexpr int W = D / 64;
+  const int64_t all = a.tokens * a.heads, at = token * a.heads + head;
+  const int lane = lane_id();
+  // lane k has parts k and k + 64
+  static_assert(kMostParts == 2 * kWave, "two parts per lane");
+  const int far = kWave + lane;
+  const float* ml = a.part_ml + 2 * at;
+  const float m0 = lane < parts ? load_agent(ml + 2 * lane * all) : kNone;
+  const float l0 = lane < parts ? load_agent(ml + 2 * lane * all + 1) : 0.0f;
+  const float m1 = far < parts ? load_agent(ml + 2 * far * all) : kNone;
+  const float l1 = far < parts ? load_agent(ml + 2 * far * all + 1) : 0.0f;
+  float most = fmaxf(m0, m1);
+#pragma unroll
+  for (int off = 32; off > 0; off /= 2) most = fmaxf(most, __shfl_xor(most, off, kWave));
+  const float base = most == kNone ? 0.0f : most;
+  const float w0 = __builtin_amdgcn_exp2f(m0 - base), w1 = __builtin_amdgcn_exp2f(m1 - base);
+  float total = l0 * w0 + l1 * w1;
+#pragma unroll
+  for (int off = 32; off > 0; off /= 2) total += __shfl_xor(total, off, kWave);
+  float o[W];
+#pragma unroll
+  for (int j = 0; j < W; ++j) o[j] = 0.0f;
+  const float* from = a.part_o + at * D + lane * W;
+#pragma unroll 8
+  for (int k = 0; k < parts; ++k) {
+    const float w = __shfl(k < kWave ? w0 : w1, k % kWave, kWave);
+#pragma unroll
+    for (int j = 0; j < W; ++j) o[j] += load_agent(from + k * all * D + j) * w;
+  }
+  finish_row<D>(a, token, head, most, total, o);
+}
+
+// Few rows. One workgroup: a tile of 16 rows of one KV head over one part of the
+// key axis; its waves take chunks of 64 keys in turn and join at the end. The
+// last part of a tile to finish joins the parts, in their order.
 //
 // The score product is taken as K q^T, so that a lane ends up with scores of
 // one row (lane % 16) and of 16 consecutive keys (tile lane / 16 of the chunk),
@@ -190,12 +253,15 @@ __device__ __forceinline__ uint32_t keep_bytes(uint32_t w, int n) {
 // lane's 16-byte load is 16 channels of a key or 16 keys of a channel, and no
 // LDS is used before the join. A lane's 16 keys lie in one page, so the scales
 // are one number each per lane and chunk.
-template <int D, int FMT>
-__global__ __launch_bounds__(kWaves* kWave) void kv_attend_rows(KvAttendArgs a) {
-  __shared__ float join_o[2][D][kRows];
-  __shared__ float join_m[kWaves][kRows], join_l[kWaves][kRows];
+template <int D, int FMT, int NW>
+__global__ __launch_bounds__(NW* kWave) void kv_attend_rows(KvAttendArgs a) {
+  constexpr int PITCH = D + 4;
+  constexpr int W = D / 64;  // channels of a lane in the joins
+  __shared__ float join_o[NW][kRows][PITCH];
+  __shared__ float join_m[NW][kRows], join_l[NW][kRows];
+  __shared__ int last;
   const KvView& c = a.c;
-  const int lane = lane_id(), wave = threadIdx.x / kWave;
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int r = lane % 16, g = lane / 16;
   const int kh = blockIdx.y;
   Sequence q;
@@ -211,10 +277,10 @@ __global__ __launch_bounds__(kWaves* kWave) void kv_attend_rows(KvAttendArgs a) 
       a, a.q + (q.row0 + token) * a.q_token + head * a.q_head, g, query);
   int low, high;
   visible(a, q, token, low, high);
-  // the keys that any row of the tile sees
-  int from, to, unused;
-  visible(a, q, (int)(tile * kRows / a.group), from, unused);
-  visible(a, q, (int)((min(tile * kRows + kRows, rows) - 1) / a.group), unused, to);
+  // the keys that any row of the tile sees, and those that all see
+  int from, to, all_from, all_to;
+  visible(a, q, (int)(tile * kRows / a.group), from, all_to);
+  visible(a, q, (int)((min(tile * kRows + kRows, rows) - 1) / a.group), all_from, to);
   const int c0 = from / kChunk, c1 = (to + kChunk - 1) / kChunk;
   const int parts = parts_of(a, c0, c1), part = blockIdx.z;
   if (part >= parts) return;
@@ -270,16 +336,17 @@ __global__ __launch_bounds__(kWaves* kWave) void kv_attend_rows(KvAttendArgs a) 
   if (begin + wave < stop) {
     look_up(begin + wave);
     const int64_t kpage = checked(kentry), vpage = checked(ventry);
-    look_up(begin + wave + kWaves);
+    look_up(begin + wave + NW);
     load_k(begin + wave, kpage, vpage);
     load_v(begin + wave, vpage);
   }
-  for (int ch = begin + wave; ch < stop; ch += kWaves) {
+  for (int ch = begin + wave; ch < stop; ch += NW) {
     const int t0 = ch * kChunk, vt = t0 + g * kKvTile;
-    const bool more = ch + kWaves < stop;
-    const float ks = kscale * factor, vs = vscale;
+    const bool more = ch + NW < stop;
+    // (not zero, so that a hidden key's minus infinity stays one)
+    const float f = fmaxf(kscale * factor, 1e-30f), vs = vscale;
     const int64_t kpage = checked(kentry), vpage = checked(ventry);
-    look_up(ch + 2 * kWaves);
+    look_up(ch + 2 * NW);
     float s[16];
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
@@ -292,16 +359,16 @@ __global__ __launch_bounds__(kWaves* kWave) void kv_attend_rows(KvAttendArgs a) 
         t = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, query[2 * j + 1], t, 0, 0, 0);
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[4 * x + i] = t[i] * ks;
+      for (int i = 0; i < 4; ++i) s[4 * x + i] = t[i];
     }
-    if (more) load_k(ch + kWaves, kpage, vpage);
-    // keys that this row does not see (whatever is held there)
+    if (more) load_k(ch + NW, kpage, vpage);
+    if (t0 < all_from || t0 + kChunk > all_to) {
+      // keys that some rows do not see (whatever is held there)
 #pragma unroll
-    for (int k = 0; k < 16; ++k) s[k] = vt + k >= low && vt + k < high && live ? s[k] : kNone;
-    if (t0 + kChunk > q.len) {
+      for (int k = 0; k < 16; ++k) s[k] = vt + k >= low && vt + k < high ? s[k] : kNone;
+      const int n = q.len - vt;
 #pragma unroll
       for (int y = 0; y < D / 16; ++y) {
-        const int n = q.len - vt;
         vc[y].x = keep_bytes(vc[y].x, n);
         vc[y].y = keep_bytes(vc[y].y, n - 4);
         vc[y].z = keep_bytes(vc[y].z, n - 8);
@@ -311,105 +378,106 @@ __global__ __launch_bounds__(kWaves* kWave) void kv_attend_rows(KvAttendArgs a) 
     float top = s[0];
 #pragma unroll
     for (int k = 1; k < 16; ++k) top = fmaxf(top, s[k]);
+    top *= f;
     top = fmaxf(top, __shfl_xor(top, 16, kWave));
-    top = fmaxf(top, __shfl_xor(top, 32, kWave));
-    const float next = fmaxf(m, top);
-    const float base = next == kNone ? 0.0f : next;  // no key so far: exp2(-inf) = 0
-    float shrink = __builtin_amdgcn_exp2f(m - base);
+    top = fmaxf(top, other_half(top));
+    // weights are relative to the largest V scale so far
+    float vmax = fmaxf(vs, __shfl_xor(vs, 16, kWave));
+    vmax = fmaxf(fmaxf(vmax, other_half(vmax)), vref);
+    const float inv = vmax > 0.0f ? __builtin_amdgcn_rcpf(vmax) : 0.0f;
+    const bool raise = top > m + kSlack;
+    const float next = raise ? top : m;
+    const float shrink = raise ? __builtin_amdgcn_exp2f(m - next) : 1.0f;
+    const float fade = vmax > vref ? shrink * (vref * inv) : shrink;
     m = next;
-    float sum = 0.0f;
-    float p[16];
+    vref = vmax;
+    l *= shrink;
+    if (__ballot(fade != 1.0f)) {
+#pragma unroll
+      for (int y = 0; y < D / 16; ++y) acc[y] *= fade;
+    }
+    const float base = next == kNone ? 0.0f : next;  // no key so far: exp2(-inf) = 0
+    const float rel = vs * inv * kLift;
+    half8_t w[2];
 #pragma unroll
     for (int k = 0; k < 16; ++k) {
-      p[k] = __builtin_amdgcn_exp2f(s[k] - base);
-      sum += p[k];
-    }
-    l = l * shrink + sum;
-    // weights relative to the largest V scale so far
-    float vmax = fmaxf(vs, __shfl_xor(vs, 16, kWave));
-    vmax = fmaxf(vmax, __shfl_xor(vmax, 32, kWave));
-    if (vmax > vref) {
-      shrink *= vref / vmax;
-      vref = vmax;
-    }
-    const float rel = vref > 0.0f ? vs / vref * kLift : 0.0f;
-    half8_t w0, w1;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      w0[k] = (_Float16)(p[k] * rel);
-      w1[k] = (_Float16)(p[8 + k] * rel);
+      const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k], f, -base));
+      l += p;
+      w[k / 8][k % 8] = (_Float16)(p * rel);
     }
 #pragma unroll
     for (int y = 0; y < D / 16; ++y) {
       half8_t lo, hi;
       codes_to_operands<FMT>(vc[y], lo, hi);
-      acc[y] *= shrink;
-      acc[y] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, w0, acc[y], 0, 0, 0);
-      acc[y] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, w1, acc[y], 0, 0, 0);
+      acc[y] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, w[0], acc[y], 0, 0, 0);
+      acc[y] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, w[1], acc[y], 0, 0, 0);
     }
-    if (more) load_v(ch + kWaves, vpage);
+    if (more) load_v(ch + NW, vpage);
   }
   if (__ballot(wrong) && lane == 0) atomicOr(c.flags, kFlagInval);
   // the four lane groups of a row each hold a quarter of its sum
   l += __shfl_xor(l, 16, kWave);
-  l += __shfl_xor(l, 32, kWave);
-  if (g == 0) {
-    join_m[wave][r] = m;
-    join_l[wave][r] = l;
+  l += other_half(l);
+  const int busy = max(min(stop - begin, NW), 0);  // waves that had keys
+  if (wave < busy) {
+    if (g == 0) {
+      join_m[wave][r] = m;
+      join_l[wave][r] = l;
+    }
+    const float by = vref * (1.0f / kLift);
+#pragma unroll
+    for (int y = 0; y < D / 16; ++y) {
+      const float4_t o = acc[y] * by;
+      *reinterpret_cast<float4_t*>(&join_o[wave][r][y * 16 + g * 4]) = o;
+    }
   }
   block_sync();
-  float most = kNone;
+  // a wave joins every NW-th row, a lane its W channels of it
+  const int64_t all = a.tokens * a.heads;
+  for (int i = wave; i < kRows; i += NW) {
+    const int64_t rr = tile * kRows + i;
+    if (rr >= rows) break;
+    float most = kNone;
+    for (int w = 0; w < busy; ++w) most = fmaxf(most, join_m[w][i]);
+    const float base = most == kNone ? 0.0f : most;
+    float total = 0.0f, o[W];
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) most = fmaxf(most, join_m[w][r]);
-  const float base = most == kNone ? 0.0f : most;
-  float total = 0.0f;
+    for (int j = 0; j < W; ++j) o[j] = 0.0f;
+    for (int w = 0; w < busy; ++w) {
+      const float e = __builtin_amdgcn_exp2f(join_m[w][i] - base);
+      total += join_l[w][i] * e;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w)
-    total += join_l[w][r] * __builtin_amdgcn_exp2f(join_m[w][r] - base);
-  const float mine = __builtin_amdgcn_exp2f(m - base) * (vref * (1.0f / kLift));
-#pragma unroll
-  for (int y = 0; y < D / 16; ++y) acc[y] *= mine;
-#pragma unroll
-  for (int half = kWaves / 2; half > 0; half /= 2) {
-    if (wave >= half && wave < 2 * half) {
-#pragma unroll
-      for (int y = 0; y < D / 16; ++y)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) join_o[wave - half][y * 16 + g * 4 + i][r] = acc[y][i];
+      for (int j = 0; j < W; ++j) o[j] += join_o[w][i][lane * W + j] * e;
     }
-    block_sync();
-    if (wave < half) {
+    const int64_t tok = q.row0 + rr / a.group, hd = kh * a.group + rr % a.group;
+    if (parts == 1) {
+      finish_row<D>(a, tok, hd, most, total, o);
+    } else {
+      // past the L2 caches, for the part that joins: it may run on another die
+      const int64_t at = (int64_t)part * all + tok * a.heads + hd;
 #pragma unroll
-      for (int y = 0; y < D / 16; ++y)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[y][i] += join_o[wave][y * 16 + g * 4 + i][r];
+      for (int j = 0; j < W; ++j) store_agent(a.part_o + at * D + lane * W + j, o[j]);
+      if (lane == 0) {
+        store_agent(a.part_ml + 2 * at, most);
+        store_agent(a.part_ml + 2 * at + 1, total);
+      }
     }
-    block_sync();
   }
-  if (wave != 0 || !live) return;
-  const int64_t at = (q.row0 + token) * a.heads + head;
-  if (parts > 1) {
-    const int64_t slot = (int64_t)part * a.tokens * a.heads + at;
-    float* o = a.part_o + slot * D;
-#pragma unroll
-    for (int y = 0; y < D / 16; ++y)
-      *reinterpret_cast<float4_t*>(o + y * 16 + g * 4) = acc[y];
-    if (g == 0) {
-      a.part_ml[2 * slot] = most;
-      a.part_ml[2 * slot + 1] = total;
-    }
-    return;
+  if (parts == 1) return;
+  wait_stores();
+  block_sync();
+  if (threadIdx.x == 0) {
+    uint32_t* count = a.counts + (int64_t)blockIdx.x * c.kv_heads + kh;
+    last = atomicAdd(count, 1u) == (uint32_t)parts - 1;
+    if (last) store_agent(count, 0u);  // for the next call
   }
-  const float inv = total > 0.0f || total != total ? 1.0f / total : 0.0f;
-  uint16_t* o = a.out + (q.row0 + token) * a.out_token + head * a.out_head;
-#pragma unroll
-  for (int y = 0; y < D / 16; ++y)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) o[y * 16 + g * 4 + i] = to16(acc[y][i] * inv, a.bf16);
-  if (a.lse && g == 0)
-    a.lse[at] = total > 0.0f || total != total
-                    ? (most + __builtin_amdgcn_logf(total)) * 0.6931471805599453f
-                    : kNone;
+  block_sync();
+  if (!last) return;
+  for (int i = wave; i < kRows; i += NW) {
+    const int64_t rr = tile * kRows + i;
+    if (rr >= rows) break;
+    join_row<D>(a, q.row0 + rr / a.group, kh * a.group + rr % a.group, parts);
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -428,19 +496,7 @@ __global__ __launch_bounds__(kWaves* kWave) void kv_attend_rows(KvAttendArgs a) 
 // of keys j and the outputs of keys j - 1, which do not depend on each other.
 // Codes are loaded four steps ahead and put into LDS two steps ahead.
 constexpr int kWide = 32;  // rows of a matrix tile, and keys of a step
-// The running maximum is raised only when a score passes it by this much (in
-// powers of two), which is seldom: most steps then need no rescaling of the
-// outputs. Weights stay below 2^(kSlack + 6), which half precision holds.
-constexpr float kSlack = 8.0f;
-constexpr float kTileLift = 64.0f;  // 2^6
 typedef float float16_t __attribute__((ext_vector_type(16)));
-
-// The value of the lane 32 away.
-__device__ __forceinline__ float other_half(float x) {
-  const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
-                                                  false);
-  return __uint_as_float(lane_id() < 32 ? p[1] : p[0]);
-}
 
 // The order of a step's instructions: every matrix instruction is followed by
 // vector ones that run beside it, an operand read and an exponential.
@@ -673,7 +729,7 @@ __global__ __launch_bounds__(NW* kWave, 1) void kv_attend_tile(KvAttendArgs a) {
     const float inv = vmax > 0.0f ? __builtin_amdgcn_rcpf(vmax) : 0.0f;
     const float older = vmax > vref ? vref * inv : 1.0f;
     vref = vmax;
-    const float rel = fmaxf((h ? vs1 : vs0) * inv, 9.3e-10f) * kTileLift;  // (2^-30)
+    const float rel = fmaxf((h ? vs1 : vs0) * inv, 9.3e-10f) * kLift;  // (2^-30)
     return Scales{ks, __builtin_amdgcn_logf(rel), __builtin_amdgcn_rcpf(rel), older};
   };
   auto weigh = [&](int t, const Scales& z, const float16_t& s, half8_t (&w)[2], float& fade)
@@ -781,7 +837,7 @@ __global__ __launch_bounds__(NW* kWave, 1) void kv_attend_tile(KvAttendArgs a) {
     const int64_t at = (q.row0 + token[t]) * a.heads + head[t];
     if (parts > 1) {
       const int64_t slot = (int64_t)part * a.tokens * a.heads + at;
-      const float by = vref * (1.0f / kTileLift);
+      const float by = vref * (1.0f / kLift);
       float* o = a.part_o + slot * D;
 #pragma unroll
       for (int y = 0; y < DY; ++y)
@@ -798,7 +854,7 @@ __global__ __launch_bounds__(NW* kWave, 1) void kv_attend_tile(KvAttendArgs a) {
       continue;
     }
     const bool some = l[t] > 0.0f || l[t] != l[t];
-    const float inv = some ? vref * (1.0f / kTileLift) / l[t] : 0.0f;
+    const float inv = some ? vref * (1.0f / kLift) / l[t] : 0.0f;
     uint16_t* o = a.out + (q.row0 + token[t]) * a.out_token + head[t] * a.out_head;
 #pragma unroll
     for (int y = 0; y < DY; ++y)
@@ -818,60 +874,27 @@ __global__ __launch_bounds__(256) void kv_attend_join(KvAttendArgs a, int tile_r
   int64_t tile;
   if (!find_sequence(a, blockIdx.x, tile_rows, q, tile)) return;
   const int64_t rows = (int64_t)q.fresh * a.group;
-  const int kh = blockIdx.y, lane = lane_id();
+  const int kh = blockIdx.y;
   int from, to, unused;
   visible(a, q, (int)(tile * tile_rows / a.group), from, unused);
   visible(a, q, (int)((min(tile * tile_rows + tile_rows, rows) - 1) / a.group), unused, to);
   const int parts = parts_of(a, from / kChunk, (to + kChunk - 1) / kChunk);
   if (parts == 1) return;
-  const int64_t all = a.tokens * a.heads;
   const int64_t row = tile * tile_rows + (int64_t)blockIdx.z * 4 + threadIdx.x / kWave;
-  if (row >= rows) return;
-  const int64_t token = q.row0 + row / a.group, head = kh * a.group + row % a.group;
-  const int64_t at = token * a.heads + head;
-  // lane k has parts k and k + 64
-  static_assert(kMostParts == 2 * kWave, "two parts per lane");
-  const int far = kWave + lane;
-  const float2_t* ml = reinterpret_cast<const float2_t*>(a.part_ml) + at;
-  const float2_t p0 = lane < parts ? ml[lane * all] : float2_t{kNone, 0.0f};
-  const float2_t p1 = far < parts ? ml[far * all] : float2_t{kNone, 0.0f};
-  float most = fmaxf(p0[0], p1[0]);
-#pragma unroll
-  for (int off = 32; off > 0; off /= 2) most = fmaxf(most, __shfl_xor(most, off, kWave));
-  const float base = most == kNone ? 0.0f : most;
-  const float w0 = __builtin_amdgcn_exp2f(p0[0] - base), w1 = __builtin_amdgcn_exp2f(p1[0] - base);
-  float total = p0[1] * w0 + p1[1] * w1;
-#pragma unroll
-  for (int off = 32; off > 0; off /= 2) total += __shfl_xor(total, off, kWave);
-  constexpr int W = D / 64;  // channels of a lane
-  typedef float row_t __attribute__((ext_vector_type(W > 1 ? W : 2)));
-  float o[W];
-#pragma unroll
-  for (int j = 0; j < W; ++j) o[j] = 0.0f;
-  const float* part = a.part_o + at * D + lane * W;
-#pragma unroll 4
-  for (int k = 0; k < parts; ++k) {
-    const float w = __shfl(k < kWave ? w0 : w1, k % kWave, kWave);
-    if (W == 1) {
-      o[0] += part[k * all * D] * w;
-    } else {
-      const row_t x = *reinterpret_cast<const row_t*>(part + k * all * D);
-#pragma unroll
-      for (int j = 0; j < W; ++j) o[j] += x[j] * w;
-    }
-  }
-  const bool some = total > 0.0f || total != total;
-  const float inv = some ? 1.0f / total : 0.0f;
-  uint16_t* out = a.out + token * a.out_token + head * a.out_head + lane * W;
-#pragma unroll
-  for (int j = 0; j < W; ++j) out[j] = to16(o[j] * inv, a.bf16);
-  if (a.lse && lane == 0)
-    a.lse[at] = some ? (most + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : kNone;
+  if (row < rows) join_row<D>(a, q.row0 + row / a.group, kh * a.group + row % a.group, parts);
 }
 
 constexpr int kTileWaves = 4;
 template <int D>
 constexpr int tile_rows() { return kTileWaves * (D > 128 ? 1 : 2) * kWide; }
+
+template <int D, int FMT>
+void launch_rows(const KvAttendArgs& a, dim3 grid, hipStream_t st) {
+  if (D <= 128 && a.waves == 8)
+    hipLaunchKernelGGL((kv_attend_rows<D, FMT, D <= 128 ? 8 : 4>), grid, dim3(8 * kWave), 0, st, a);
+  else
+    hipLaunchKernelGGL((kv_attend_rows<D, FMT, 4>), grid, dim3(4 * kWave), 0, st, a);
+}
 
 template <int D, int FMT>
 hipError_t launch(const KvAttendArgs& a, hipStream_t st) {
@@ -883,10 +906,8 @@ hipError_t launch(const KvAttendArgs& a, hipStream_t st) {
                        dim3((unsigned)(tiles * a.c.kv_heads), (unsigned)a.parts),
                        dim3(kTileWaves * kWave), 0, st, a);
   else
-    hipLaunchKernelGGL((kv_attend_rows<D, FMT>),
-                       dim3((unsigned)tiles, (unsigned)a.c.kv_heads, (unsigned)a.parts),
-                       dim3(kWaves * kWave), 0, st, a);
-  if (a.parts > 1)
+    launch_rows<D, FMT>(a, dim3((unsigned)tiles, (unsigned)a.c.kv_heads, (unsigned)a.parts), st);
+  if (a.tiled && a.parts > 1)
     hipLaunchKernelGGL(kv_attend_join<D>,
                        dim3((unsigned)tiles, (unsigned)a.c.kv_heads, (unsigned)(rows / 4)),
                        dim3(256), 0, st, a, rows);
@@ -908,8 +929,15 @@ KvSplit kv_attend_split(int dim, int64_t n, int64_t tokens, int heads, int kv_he
   const int rows = s.tiled ? (dim == 256 ? tile_rows<256>() : tile_rows<128>()) : kRows;
   const int64_t groups = std::max<int64_t>((tokens * group / rows + n) * kv_heads, 1);
   const int64_t chunks = std::max<int64_t>((max_len + kChunk - 1) / kChunk, 1);
-  const int64_t want = s.tiled ? 512 : 2048;
-  const int64_t least = s.tiled ? 32 : 2 * kWaves;  // chunks of a part
+  int64_t want = s.tiled ? 512 : 2048;
+  int64_t least = 32;  // chunks of a part
+  if (!s.tiled) {
+    s.waves = groups < 256 && dim <= 128 ? 8 : 4;
+    least = 2 * s.waves;
+    if (chunks <= 3 * s.waves) want = 1;
+    // (their counters lie in the workspace's first bytes)
+    static_assert(2048 / 2 <= kKvCounts, "a counter for every tile with parts");
+  }
   const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(want / groups, kMostParts));
   s.part_chunks = (int)std::max<int64_t>(least, (chunks + parts - 1) / parts);
   s.parts = (int)((chunks + s.part_chunks - 1) / s.part_chunks);
