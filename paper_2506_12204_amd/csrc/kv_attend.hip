@@ -512,13 +512,17 @@ __device__ __forceinline__ void interleave() {
 }
 
 template <int D, int FMT, int NW, int RT>
-__global__ __launch_bounds__(NW* kWave, 1) void kv_attend_tile(KvAttendArgs a) {
+__global__ __launch_bounds__(NW* kWave, NW / 4) void kv_attend_tile(KvAttendArgs a) {
   constexpr int NT = NW * kWave;
   constexpr int KS = D / 16;       // matrix steps of the score product
   constexpr int DY = D / 32;       // output tiles
-  constexpr int PER = 4 * D / NT;  // 16-byte units of a step's K and V per thread
+  constexpr int UNITS = 4 * D;     // 16-byte units of a step's K and V
+  constexpr int PER = UNITS > NT ? UNITS / NT : 1;  // of them per thread
+  // Two waves per SIMD hold everything in vector registers; one has to keep
+  // outputs and queries in the accumulation registers.
+  constexpr bool PINNED = NW == 4;
   constexpr int ROWS = NW * RT * kWide;
-  static_assert(PER >= 1 && NT * PER == 4 * D, "whole rounds of units");
+  static_assert(NT * PER % UNITS == 0, "whole rounds of units");
   __shared__ half8_t keys[2 * KS * kWave];      // [buffer][step][lane]
   __shared__ half8_t vals[4 * 2 * DY * kWave];  // [buffer][8 keys of either half][tile][lane]
   __shared__ float scales[4 * 4];               // [buffer][K tile 0, 1, V tile 0, 1]
@@ -562,22 +566,11 @@ __global__ __launch_bounds__(NW* kWave, 1) void kv_attend_tile(KvAttendArgs a) {
       token[t] = -1;
     }
   }
-  // Through LDS and back: loads may put the queries into the accumulation
-  // registers, from where the matrix cores take them; values that vector
-  // instructions computed would be copied for every use.
-  half8_t* spare = vals + wave * (KS * kWave);
-  static_assert(NW * KS <= 4 * 2 * DY, "a row tile of each wave fits the V buffers");
+  if (PINNED) {
 #pragma unroll
-  for (int t = 0; t < RT; ++t) {
+    for (int t = 0; t < RT; ++t)
 #pragma unroll
-    for (int k = 0; k < KS; ++k) spare[k * kWave + lane] = query[t][k];
-    block_sync();
-#pragma unroll
-    for (int k = 0; k < KS; ++k) {
-      query[t][k] = spare[k * kWave + lane];
-      asm volatile("" : "+a"(query[t][k]));
-    }
-    block_sync();
+      for (int k = 0; k < KS; ++k) asm volatile("" : "+a"(query[t][k]));
   }
   // the keys that all of this wave's rows see
   int all_from = 0, all_to = 0;
@@ -601,55 +594,55 @@ __global__ __launch_bounds__(NW* kWave, 1) void kv_attend_tile(KvAttendArgs a) {
     wrong |= bad;
     return bad ? 0u : (uint32_t)entry;
   };
-  // A thread's 16-byte units of a step: the first half of them K, the rest V; a
-  // wave's lie in one tile of 16 keys. Pages are looked up a step before their
-  // codes are loaded, and those two steps before they are put into LDS.
-  auto is_key = [&](int k) __attribute__((always_inline)) {
-    return PER > 1 ? k < PER / 2 : wave < NW / 2;
+  // A thread's 16-byte units of a step: the first half of all are K, the rest V;
+  // a wave's lie side by side in one tile of 16 keys, so all of their address
+  // but the lane is scalar. Pages are looked up a step before their codes are
+  // loaded (even lanes the first tile's, odd lanes the second's), and those two
+  // steps before they are put into LDS.
+  auto unit_of = [&](int k) __attribute__((always_inline)) {
+    return (wave * kWave + k * NT) % UNITS;  // of lane 0
   };
-  auto unit_tile = [&](int k) __attribute__((always_inline)) {
-    return (int)((threadIdx.x + k * NT) / D) & 1;
-  };
+  auto is_key = [&](int k) __attribute__((always_inline)) { return unit_of(k) < UNITS / 2; };
+  auto unit_tile = [&](int k) __attribute__((always_inline)) { return unit_of(k) / D & 1; };
   int64_t unit_off[PER];  // where a unit is in a tile's page
   int unit_to[PER];       // and where its operands go
 #pragma unroll
   for (int k = 0; k < PER; ++k) {
-    const int in = (threadIdx.x + k * NT) % D, tl = unit_tile(k), tok = in % 16;
-    unit_off[k] = (is_key(k) ? k_off : v_off) + in * 16;
+    const int in = unit_of(k) % D + lane, tl = unit_tile(k), tok = in % 16;
+    unit_off[k] = (is_key(k) ? k_off : v_off) + unit_of(k) % D * 16;
     // K: 16 channels (step in / 16) of key in % 16; V: 16 keys of channel `in`
     unit_to[k] = is_key(k) ? in / 16 * kWave + tok / 4 * 8 + tl * 4 + tok % 4
                            : in / 32 * kWave + tl * kWide + in % 32;
   }
   uint4 raw[2][PER];
   float sraw[2] = {0.0f, 0.0f};
-  int32_t page[PER], scale_page = 0;
+  int32_t page = 0;
+  const float* const scale_at =
+      c.scale + ((int64_t)a.layer * 2 + lane / 2 % 2) * c.kv_heads + kh;
   auto look_up = [&](int j) __attribute__((always_inline)) {
-    const int t = min(j, stop - 1) * kWide;
-#pragma unroll
-    for (int k = 0; k < PER; ++k) page[k] = entry_of(t + unit_tile(k) * kKvTile);
-    scale_page = entry_of(t + threadIdx.x % 2 * kKvTile);
+    page = entry_of(min(j, stop - 1) * kWide + lane % 2 * kKvTile);
   };
   // (all threads load and store one of the four scales: no branch)
   auto fetch = [&](int j, uint4 (&to)[PER], float& sc) __attribute__((always_inline)) {
     const int t0 = min(j, stop - 1) * kWide;
-    int64_t at[PER];
-#pragma unroll
-    for (int k = 0; k < PER; ++k) at[k] = checked(page[k]);
-    const int64_t at_scale = checked(scale_page);
+    const uint32_t mine = checked(page);
+    const uint32_t both[2] = {(uint32_t)__builtin_amdgcn_readlane((int)mine, 0),
+                              (uint32_t)__builtin_amdgcn_readlane((int)mine, 1)};
     // the next look-up goes first: loads return in order, and the next step
     // needs it before these
     look_up(j + 1);
-    sc = c.scale[((at_scale * c.layers + a.layer) * 2 + threadIdx.x / 2 % 2) * c.kv_heads + kh];
+    sc = scale_at[(int64_t)mine * c.page_scales];
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
       const int t = t0 + unit_tile(k) * kKvTile;
-      to[k] = *reinterpret_cast<const uint4*>(c.data + at[k] * c.page_bytes + (t & in_page) * D +
-                                              unit_off[k]);
+      const uint8_t* p = c.data + (int64_t)both[unit_tile(k)] * c.page_bytes +
+                         (t & in_page) * D + unit_off[k];
+      to[k] = reinterpret_cast<const uint4*>(p)[lane];
     }
   };
   auto stage = [&](auto mask, int j, const uint4 (&from)[PER], float sc)
       __attribute__((always_inline)) {
-    scales[(j & 3) * 4 + threadIdx.x % 4] = sc;
+    scales[(j & 3) * 4 + lane % 4] = sc;
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
       uint4 w = from[k];
@@ -794,9 +787,9 @@ __global__ __launch_bounds__(NW* kWave, 1) void kv_attend_tile(KvAttendArgs a) {
         for (int y = 0; y < DY; ++y) {
           // one after the other: all of them at once in the vector registers
           // would push out other values
-          asm volatile("" : "+a"(acc[t][y]));
+          if (PINNED) asm volatile("" : "+a"(acc[t][y]));
           acc[t][y] *= fade[t];
-          asm volatile("" : "+a"(acc[t][y]));
+          if (PINNED) asm volatile("" : "+a"(acc[t][y]));
         }
       }
     }
@@ -884,9 +877,11 @@ __global__ __launch_bounds__(256) void kv_attend_join(KvAttendArgs a, int tile_r
   if (row < rows) join_row<D>(a, q.row0 + row / a.group, kh * a.group + row % a.group, parts);
 }
 
-constexpr int kTileWaves = 4;
+// Waves of the tile kernel's workgroups, each with one tile of 32 rows.
 template <int D>
-constexpr int tile_rows() { return kTileWaves * (D > 128 ? 1 : 2) * kWide; }
+constexpr int tile_waves() { return D > 128 ? 4 : 8; }
+template <int D>
+constexpr int tile_rows() { return tile_waves<D>() * kWide; }
 
 template <int D, int FMT>
 void launch_rows(const KvAttendArgs& a, dim3 grid, hipStream_t st) {
@@ -902,9 +897,9 @@ hipError_t launch(const KvAttendArgs& a, hipStream_t st) {
   const int64_t tiles = a.cu ? a.tokens * a.group / rows + a.n
                              : a.n * ((a.group + rows - 1) / rows);
   if (a.tiled)
-    hipLaunchKernelGGL((kv_attend_tile<D, FMT, kTileWaves, D <= 128 ? 2 : 1>),
+    hipLaunchKernelGGL((kv_attend_tile<D, FMT, tile_waves<D>(), 1>),
                        dim3((unsigned)(tiles * a.c.kv_heads), (unsigned)a.parts),
-                       dim3(kTileWaves * kWave), 0, st, a);
+                       dim3(tile_waves<D>() * kWave), 0, st, a);
   else
     launch_rows<D, FMT>(a, dim3((unsigned)tiles, (unsigned)a.c.kv_heads, (unsigned)a.parts), st);
   if (a.tiled && a.parts > 1)
@@ -927,16 +922,17 @@ KvSplit kv_attend_split(int dim, int64_t n, int64_t tokens, int heads, int kv_he
   const int group = heads / kv_heads;
   s.tiled = max_new * group > 2 * kRows;
   const int rows = s.tiled ? (dim == 256 ? tile_rows<256>() : tile_rows<128>()) : kRows;
-  const int64_t groups = std::max<int64_t>((tokens * group / rows + n) * kv_heads, 1);
+  const int64_t tiles = tokens == n ? n * ((group + rows - 1) / rows) : tokens * group / rows + n;
+  const int64_t groups = std::max<int64_t>(tiles * kv_heads, 1);
   const int64_t chunks = std::max<int64_t>((max_len + kChunk - 1) / kChunk, 1);
-  int64_t want = s.tiled ? 512 : 2048;
+  int64_t want = s.tiled ? 512 : 256;
   int64_t least = 32;  // chunks of a part
   if (!s.tiled) {
     s.waves = groups < 256 && dim <= 128 ? 8 : 4;
     least = 2 * s.waves;
     if (chunks <= 3 * s.waves) want = 1;
     // (their counters lie in the workspace's first bytes)
-    static_assert(2048 / 2 <= kKvCounts, "a counter for every tile with parts");
+    static_assert(256 / 2 <= kKvCounts, "a counter for every tile with parts");
   }
   const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(want / groups, kMostParts));
   s.part_chunks = (int)std::max<int64_t>(least, (chunks + parts - 1) / parts);
