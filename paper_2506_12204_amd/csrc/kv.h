@@ -9,7 +9,7 @@
 
 namespace semsched {
 
-constexpr int kKvCounts = 1024;      // counters of attention's tiles with several parts
+constexpr int kKvCounts = 8192;      // counters of attention's tiles with several parts
 constexpr int kKvTile = 16;          // tokens per tile of a page's block
 
 // The cache as the kernels see it: the caller's arrays and the derived sizes.
@@ -76,7 +76,7 @@ struct KvAttendArgs {
   const int32_t *seqs, *cu;
   int64_t n, tokens;
   int32_t layer, heads, group;
-  int32_t bf16, wide;
+  int32_t bf16, wide, wide_out;  // 16-byte accesses to q, to out, are aligned
   int32_t causal, window;
   float scale_log2;  // softmax scale * log2(e)
   int32_t tiled;       // the kernel for many rows per sequence

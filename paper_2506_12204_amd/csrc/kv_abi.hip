@@ -197,7 +197,7 @@ int check_attend(const sem_kv_cache* c, int32_t layer, const sem_kv_query* q, co
   if (reinterpret_cast<uintptr_t>(q->q) % 2 != 0 || reinterpret_cast<uintptr_t>(q->out) % 2 != 0)
     return SEM_EINVAL;
   // one row tile per workgroup column of the grid, one row per wave of the join
-  if (q->heads > 65536 || q->tokens * (int64_t)q->heads + n > INT32_MAX) return SEM_ENOTIMPL;
+  if (q->heads > 65536 || (q->tokens + n) * (int64_t)q->heads > INT32_MAX) return SEM_ENOTIMPL;
   return SEM_OK;
 }
 
@@ -376,6 +376,7 @@ int sem_kv_attend_async(const sem_kv_cache* cache, int32_t layer, const sem_kv_q
   a.group = query->heads / cache->kv_heads;
   a.bf16 = query->dtype == SEM_KV_BF16;
   a.wide = aligned16(query->q, query->q_token_stride, query->q_head_stride);
+  a.wide_out = aligned16(query->out, query->out_token_stride, query->out_head_stride);
   a.causal = query->causal != 0;
   a.window = query->window;
   a.scale_log2 = query->scale * 1.4426950408889634f;

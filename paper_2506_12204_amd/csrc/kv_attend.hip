@@ -36,39 +36,57 @@ constexpr int kMostParts = 128;      // of the key axis
 // outputs. Weights stay below kLift * 2^kSlack, which half precision holds.
 constexpr float kSlack = 8.0f;
 
-// Row tiles are numbered without reading the lengths: those of sequence i start
-// at cu[i] * group / rows + i, which leaves room for a partly filled one. Without
-// offsets, one token each, every sequence has the same number of them.
-__device__ __forceinline__ int64_t tile_start(const KvAttendArgs& a, int64_t i, int rows) {
-  return (int64_t)a.cu[i] * a.group / rows + i;
-}
-
 struct Sequence {
   const int32_t* table;
   int64_t row0;     // first query token
   int fresh, len;   // query tokens, keys
 };
 
-// The sequence of row tile u and u's number in it; false if there is none.
-__device__ __forceinline__ bool find_sequence(const KvAttendArgs& a, int64_t u, int rows,
+// The sequence of row tile u and the tile's number in it; false if there is no
+// such tile. Tiles are numbered sequence by sequence, LATE ones (whose causal
+// rows see most keys) first where that is asked for. The grid's size is a bound,
+// and its workgroups without work have to be the last or first ones: the device
+// deals workgroups to its parts in turn, and idle ones at regular places would
+// leave the same parts without work. So every wave counts the tiles of all
+// sequences, 64 at a time (n / 64 rounds of independent loads, where a search
+// would take log n dependent ones).
+template <bool LATE>
+__device__ __forceinline__ bool find_sequence(const KvAttendArgs& a, uint32_t u, int rows,
                                               Sequence& q, int64_t& tile) {
   const KvView& c = a.c;
-  int64_t i;
+  int64_t i = -1;
   if (a.cu) {
-    int64_t end = a.n;
-    i = 0;
-    while (end - i > 1) {
-      const int64_t mid = (i + end) / 2;
-      if (tile_start(a, mid, rows) <= u) i = mid;
-      else end = mid;
+    const int lane = lane_id();
+    auto count = [&](int64_t at) __attribute__((always_inline)) -> uint32_t {
+      if (at >= a.n) return 0;
+      const int64_t fresh = (int64_t)a.cu[at + 1] - a.cu[at];
+      return fresh > 0 && fresh <= a.tokens ? (uint32_t)((fresh * a.group + rows - 1) / rows) : 0u;
+    };
+    uint32_t total = 0;
+    if (LATE) {
+      for (int64_t at = 0; at < a.n; at += kWave) total += wave_add_u32(count(at + lane));
+      if (u >= total) return false;
+      u = total - 1 - u;
     }
-    tile = u - tile_start(a, i, rows);
-    if (u == 0 && (a.cu[0] != 0 || a.cu[a.n] != a.tokens) && threadIdx.x == 0)
+    uint32_t before = 0;
+    for (int64_t at = 0; at < a.n; at += kWave) {
+      const uint32_t mine = count(at + lane), upto = before + wave_incl_scan_u32(mine);
+      const uint64_t beyond = __ballot(upto > u);
+      if (beyond) {
+        const int first = __ffsll((unsigned long long)beyond) - 1;
+        i = at + first;
+        tile = u - (uint32_t)__builtin_amdgcn_readlane((int)(upto - mine), first);
+        break;
+      }
+      before = (uint32_t)__builtin_amdgcn_readlane((int)upto, kWave - 1);
+    }
+    if (blockIdx.x == 0 && (a.cu[0] != 0 || a.cu[a.n] != a.tokens) && threadIdx.x == 0)
       atomicOr(c.flags, kFlagInval);
+    if (i < 0) return false;
   } else {
     const uint32_t each = (uint32_t)(a.group + rows - 1) / (uint32_t)rows;
-    i = (uint32_t)u / each;
-    tile = (uint32_t)u % each;
+    i = u / each;
+    tile = u % each;
   }
   q.row0 = a.cu ? a.cu[i] : i;
   const int64_t fresh = a.cu ? (int64_t)a.cu[i + 1] - q.row0 : 1;
@@ -76,7 +94,6 @@ __device__ __forceinline__ bool find_sequence(const KvAttendArgs& a, int64_t u, 
     if (threadIdx.x == 0) atomicOr(c.flags, kFlagInval);
     return false;
   }
-  if (tile < 0 || tile * rows >= fresh * a.group) return false;
   q.fresh = (int)fresh;
   const int32_t s = a.seqs[i];
   q.len = 0;
@@ -102,19 +119,27 @@ __device__ __forceinline__ void visible(const KvAttendArgs& a, const Sequence& q
   low = a.window > 0 ? max(pos + 1 - a.window, 0) : 0;
 }
 
-// Parts that chunks [c0, c1) of the keys are split into (the last one takes
-// what is beyond the parts that the caller's bound on the length allows for).
+// Parts that chunks [c0, c1) of the keys are split into, of equal sizes (larger
+// ones where the caller's bound on the length does not hold).
 __device__ __forceinline__ int parts_of(const KvAttendArgs& a, int c0, int c1) {
   return max(1, min((c1 - c0 + a.part_chunks - 1) / a.part_chunks, a.parts));
 }
+__device__ __forceinline__ int part_start(int c0, int c1, int parts, int part) {
+  return c0 + (int)((uint32_t)max(c1 - c0, 0) * (uint64_t)part / (uint32_t)parts);
+}
 
-__device__ __forceinline__ uint16_t to16(float x, int bf16) {
-  if (bf16) {
-    const uint32_t u = __float_as_uint(x);
-    if (x != x) return 0x7fc0;
-    return (uint16_t)((u + 0x7fffu + ((u >> 16) & 1u)) >> 16);
+// Two values in the outputs' type, rounded to the nearest.
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack_pair(float x, float y) {
+  const float2_t v = {x, y};
+  if (BF16) {
+    typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2_t));
   }
-  return __builtin_bit_cast(uint16_t, (_Float16)x);
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, half2_t));
+}
+__device__ __forceinline__ uint32_t pack_pair(float x, float y, int bf16) {
+  return bf16 ? pack_pair<true>(x, y) : pack_pair<false>(x, y);
 }
 
 // A row's query in halves, as the lane's D / (8 G) operands of eight: of G = 4
@@ -200,14 +225,25 @@ __device__ __forceinline__ void finish_row(const KvAttendArgs& a, int64_t token,
   const float inv = some ? 1.0f / total : 0.0f;
   uint16_t* out = a.out + token * a.out_token + head * a.out_head + lane_id() * W;
 #pragma unroll
-  for (int j = 0; j < W; ++j) out[j] = to16(o[j] * inv, a.bf16);
+  for (int j = 0; j < W; j += 2) {
+    const uint32_t p = pack_pair(o[j] * inv, W > 1 ? o[(j + 1) % W] * inv : 0.0f, a.bf16);
+    if (W == 1) {
+      out[0] = (uint16_t)p;
+    } else if (a.wide_out) {
+      *reinterpret_cast<uint32_t*>(out + j) = p;
+    } else {
+      out[j] = (uint16_t)p;
+      out[j + 1] = (uint16_t)(p >> 16);
+    }
+  }
   if (a.lse && lane_id() == 0)
     a.lse[token * a.heads + head] =
         some ? (most + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : kNone;
 }
 
 // Joins a row's parts with one wave.
-template <int D>
+// ALIVE: written by workgroups of this kernel, to be read past the L2 caches.
+template <int D, bool ALIVE>
 __device__ __forceinline__ void join_row(const KvAttendArgs& a, int64_t token, int64_t head,
                                          int parts) {
   constexpr int W = D / 64;
@@ -217,10 +253,13 @@ __device__ __forceinline__ void join_row(const KvAttendArgs& a, int64_t token, i
   static_assert(kMostParts == 2 * kWave, "two parts per lane");
   const int far = kWave + lane;
   const float* ml = a.part_ml + 2 * at;
-  const float m0 = lane < parts ? load_agent(ml + 2 * lane * all) : kNone;
-  const float l0 = lane < parts ? load_agent(ml + 2 * lane * all + 1) : 0.0f;
-  const float m1 = far < parts ? load_agent(ml + 2 * far * all) : kNone;
-  const float l1 = far < parts ? load_agent(ml + 2 * far * all + 1) : 0.0f;
+  auto load = [](const float* p) __attribute__((always_inline)) {
+    return ALIVE ? load_agent(p) : *p;
+  };
+  const float m0 = lane < parts ? load(ml + 2 * lane * all) : kNone;
+  const float l0 = lane < parts ? load(ml + 2 * lane * all + 1) : 0.0f;
+  const float m1 = far < parts ? load(ml + 2 * far * all) : kNone;
+  const float l1 = far < parts ? load(ml + 2 * far * all + 1) : 0.0f;
   float most = fmaxf(m0, m1);
 #pragma unroll
   for (int off = 32; off > 0; off /= 2) most = fmaxf(most, __shfl_xor(most, off, kWave));
@@ -237,7 +276,7 @@ __device__ __forceinline__ void join_row(const KvAttendArgs& a, int64_t token, i
   for (int k = 0; k < parts; ++k) {
     const float w = __shfl(k < kWave ? w0 : w1, k % kWave, kWave);
 #pragma unroll
-    for (int j = 0; j < W; ++j) o[j] += load_agent(from + k * all * D + j) * w;
+    for (int j = 0; j < W; ++j) o[j] += load(from + k * all * D + j) * w;
   }
   finish_row<D>(a, token, head, most, total, o);
 }
@@ -263,10 +302,12 @@ __global__ __launch_bounds__(NW* kWave) void kv_attend_rows(KvAttendArgs a) {
   const KvView& c = a.c;
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int r = lane % 16, g = lane / 16;
-  const int kh = blockIdx.y;
+  // heads side by side: the dies take workgroups in turn, and so get an equal
+  // share of every sequence
+  const int kh = blockIdx.x % c.kv_heads;
   Sequence q;
   int64_t tile;
-  if (!find_sequence(a, blockIdx.x, kRows, q, tile)) return;
+  if (!find_sequence<false>(a, blockIdx.x / c.kv_heads, kRows, q, tile)) return;
   const int64_t rows = (int64_t)q.fresh * a.group;
   const int64_t row = tile * kRows + r;
   const bool live = row < rows;
@@ -282,10 +323,9 @@ __global__ __launch_bounds__(NW* kWave) void kv_attend_rows(KvAttendArgs a) {
   visible(a, q, (int)(tile * kRows / a.group), from, all_to);
   visible(a, q, (int)((min(tile * kRows + kRows, rows) - 1) / a.group), all_from, to);
   const int c0 = from / kChunk, c1 = (to + kChunk - 1) / kChunk;
-  const int parts = parts_of(a, c0, c1), part = blockIdx.z;
+  const int parts = parts_of(a, c0, c1), part = blockIdx.y;
   if (part >= parts) return;
-  const int begin = c0 + part * a.part_chunks;
-  const int stop = part == parts - 1 ? c1 : begin + a.part_chunks;
+  const int begin = part_start(c0, c1, parts, part), stop = part_start(c0, c1, parts, part + 1);
 
   float m = kNone, l = 0.0f, vref = 0.0f;
   float4_t acc[D / 16];
@@ -467,7 +507,7 @@ __global__ __launch_bounds__(NW* kWave) void kv_attend_rows(KvAttendArgs a) {
   wait_stores();
   block_sync();
   if (threadIdx.x == 0) {
-    uint32_t* count = a.counts + (int64_t)blockIdx.x * c.kv_heads + kh;
+    uint32_t* count = a.counts + blockIdx.x;
     last = atomicAdd(count, 1u) == (uint32_t)parts - 1;
     if (last) store_agent(count, 0u);  // for the next call
   }
@@ -476,7 +516,7 @@ __global__ __launch_bounds__(NW* kWave) void kv_attend_rows(KvAttendArgs a) {
   for (int i = wave; i < kRows; i += NW) {
     const int64_t rr = tile * kRows + i;
     if (rr >= rows) break;
-    join_row<D>(a, q.row0 + rr / a.group, kh * a.group + rr % a.group, parts);
+    join_row<D, true>(a, q.row0 + rr / a.group, kh * a.group + rr % a.group, parts);
   }
 }
 
@@ -523,8 +563,13 @@ __global__ __launch_bounds__(NW* kWave, NW / 4) void kv_attend_tile(KvAttendArgs
   constexpr bool PINNED = NW == 4;
   constexpr int ROWS = NW * RT * kWide;
   static_assert(NT * PER % UNITS == 0, "whole rounds of units");
-  __shared__ half8_t keys[2 * KS * kWave];      // [buffer][step][lane]
-  __shared__ half8_t vals[4 * 2 * DY * kWave];  // [buffer][8 keys of either half][tile][lane]
+  constexpr int KEYS = 2 * KS * kWave;      // [buffer][step][lane]
+  constexpr int VALS = 4 * 2 * DY * kWave;  // [buffer][8 keys of either half][tile][lane]
+  constexpr int PITCH = D / 8 + 1;          // of an output row at the end
+  constexpr int OUTS = NW * kWide * PITCH;
+  __shared__ half8_t pool[KEYS + VALS > OUTS ? KEYS + VALS : OUTS];
+  half8_t* const keys = pool;
+  half8_t* const vals = pool + KEYS;
   __shared__ float scales[4 * 4];               // [buffer][K tile 0, 1, V tile 0, 1]
   const KvView& c = a.c;
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -532,9 +577,7 @@ __global__ __launch_bounds__(NW* kWave, NW / 4) void kv_attend_tile(KvAttendArgs
   const int kh = blockIdx.x % c.kv_heads;
   Sequence q;
   int64_t tile;
-  if (!find_sequence(a, (int64_t)(gridDim.x / c.kv_heads) - 1 - blockIdx.x / c.kv_heads, ROWS, q,
-                     tile))
-    return;
+  if (!find_sequence<true>(a, blockIdx.x / c.kv_heads, ROWS, q, tile)) return;
   const int64_t rows = (int64_t)q.fresh * a.group;
   // the keys that the workgroup's rows see
   int from, to, unused;
@@ -543,8 +586,8 @@ __global__ __launch_bounds__(NW* kWave, NW / 4) void kv_attend_tile(KvAttendArgs
   const int c0 = from / kChunk, c1 = (to + kChunk - 1) / kChunk;
   const int parts = parts_of(a, c0, c1), part = blockIdx.y;
   if (part >= parts) return;
-  const int begin = 2 * (c0 + part * a.part_chunks);
-  const int stop = part == parts - 1 ? 2 * c1 : begin + 2 * a.part_chunks;
+  const int begin = 2 * part_start(c0, c1, parts, part);
+  const int stop = 2 * part_start(c0, c1, parts, part + 1);
 
   const int64_t row0 = tile * ROWS + wave * (RT * kWide);
   half8_t query[RT][KS];
@@ -731,9 +774,9 @@ __global__ __launch_bounds__(NW* kWave, NW / 4) void kv_attend_tile(KvAttendArgs
     const float f = fmaxf(z.ks * factor[t], 1e-30f);
     float top = s[0];
 #pragma unroll
-    for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+    for (int i = 1; i < 16; ++i) top = __builtin_elementwise_maximum(top, s[i]);
     top *= f;
-    top = fmaxf(top, other_half(top));
+    top = __builtin_elementwise_maximum(top, other_half(top));
     const bool raise = top > m[t] + kSlack;
     const float next = raise ? top : m[t];
     const float shrink = raise ? __builtin_amdgcn_exp2f(m[t] - next) : 1.0f;
@@ -822,13 +865,14 @@ __global__ __launch_bounds__(NW* kWave, NW / 4) void kv_attend_tile(KvAttendArgs
     read_vals(stop - 1, vf);
     output(vf, w1);
   }
+  block_sync();  // the buffers are free
   if (__ballot(wrong) && lane == 0) atomicOr(c.flags, kFlagInval);
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
-    l[t] += __shfl_xor(l[t], 32, kWave);
-    if (token[t] < 0) continue;
-    const int64_t at = (q.row0 + token[t]) * a.heads + head[t];
+    l[t] += other_half(l[t]);
     if (parts > 1) {
+      if (token[t] < 0) continue;
+      const int64_t at = (q.row0 + token[t]) * a.heads + head[t];
       const int64_t slot = (int64_t)part * a.tokens * a.heads + at;
       const float by = vref * (1.0f / kLift);
       float* o = a.part_o + slot * D;
@@ -848,33 +892,69 @@ __global__ __launch_bounds__(NW* kWave, NW / 4) void kv_attend_tile(KvAttendArgs
     }
     const bool some = l[t] > 0.0f || l[t] != l[t];
     const float inv = some ? vref * (1.0f / kLift) / l[t] : 0.0f;
-    uint16_t* o = a.out + (q.row0 + token[t]) * a.out_token + head[t] * a.out_head;
+    // through LDS, so that rows are written whole
+    uint2* const row = reinterpret_cast<uint2*>(pool + (wave * kWide + r) * PITCH);
+    if (a.bf16) {
 #pragma unroll
-    for (int y = 0; y < DY; ++y)
+      for (int y = 0; y < DY; ++y)
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-        o[y * 32 + i / 4 * 8 + h * 4 + i % 4] = to16(acc[t][y][i] * inv, a.bf16);
-    if (a.lse && h == 0)
-      a.lse[at] = some ? (m[t] + __builtin_amdgcn_logf(l[t])) * 0.6931471805599453f : kNone;
+        for (int k = 0; k < 4; ++k)
+          row[y * 8 + k * 2 + h] =
+              make_uint2(pack_pair<true>(acc[t][y][4 * k] * inv, acc[t][y][4 * k + 1] * inv),
+                         pack_pair<true>(acc[t][y][4 * k + 2] * inv, acc[t][y][4 * k + 3] * inv));
+    } else {
+#pragma unroll
+      for (int y = 0; y < DY; ++y)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          row[y * 8 + k * 2 + h] =
+              make_uint2(pack_pair<false>(acc[t][y][4 * k] * inv, acc[t][y][4 * k + 1] * inv),
+                         pack_pair<false>(acc[t][y][4 * k + 2] * inv, acc[t][y][4 * k + 3] * inv));
+    }
+    if (a.lse && h == 0 && token[t] >= 0)
+      a.lse[(q.row0 + token[t]) * a.heads + head[t]] =
+          some ? (m[t] + __builtin_amdgcn_logf(l[t])) * 0.6931471805599453f : kNone;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (a wave reads what it wrote)
+    constexpr int LANES = D / 8;  // of a row
+#pragma unroll 2
+    for (int i = lane / LANES; i < kWide; i += kWave / LANES) {
+      const int64_t rr = row0 + t * kWide + i;
+      if (rr >= rows) break;
+      const uint32_t tok = (uint32_t)rr / (uint32_t)a.group;
+      const int64_t hd = kh * a.group + (int)((uint32_t)rr - tok * a.group);
+      uint16_t* o = a.out + (q.row0 + tok) * a.out_token + hd * a.out_head + lane % LANES * 8;
+      const uint4 x = __builtin_bit_cast(uint4, pool[(wave * kWide + i) * PITCH + lane % LANES]);
+      if (a.wide_out) {
+        *reinterpret_cast<uint4*>(o) = x;
+      } else {
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o[j] = (uint16_t)(w[j / 2] >> (16 * (j % 2)));
+      }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // before the next row tile's writes
   }
 }
 
-// Joins the parts of the key axis: one workgroup per row tile that has several,
-// a wave per row.
+// Joins the parts of the key axis of the tile kernel: a wave per row.
+constexpr int kJoinRows = 32;  // of a workgroup
 template <int D>
 __global__ __launch_bounds__(256) void kv_attend_join(KvAttendArgs a, int tile_rows) {
   Sequence q;
   int64_t tile;
-  if (!find_sequence(a, blockIdx.x, tile_rows, q, tile)) return;
+  if (!find_sequence<false>(a, blockIdx.x / a.c.kv_heads, tile_rows, q, tile)) return;
   const int64_t rows = (int64_t)q.fresh * a.group;
-  const int kh = blockIdx.y;
+  const int kh = blockIdx.x % a.c.kv_heads;
   int from, to, unused;
   visible(a, q, (int)(tile * tile_rows / a.group), from, unused);
   visible(a, q, (int)((min(tile * tile_rows + tile_rows, rows) - 1) / a.group), unused, to);
   const int parts = parts_of(a, from / kChunk, (to + kChunk - 1) / kChunk);
   if (parts == 1) return;
-  const int64_t row = tile * tile_rows + (int64_t)blockIdx.z * 4 + threadIdx.x / kWave;
-  if (row < rows) join_row<D>(a, q.row0 + row / a.group, kh * a.group + row % a.group, parts);
+  const int64_t row0 = tile * tile_rows + (int64_t)blockIdx.y * kJoinRows;
+  for (int i = threadIdx.x / kWave; i < kJoinRows && row0 + i < rows; i += 4) {
+    const int64_t row = row0 + i;
+    join_row<D, false>(a, q.row0 + row / a.group, kh * a.group + row % a.group, parts);
+  }
 }
 
 // Waves of the tile kernel's workgroups, each with one tile of 32 rows.
@@ -896,16 +976,16 @@ hipError_t launch(const KvAttendArgs& a, hipStream_t st) {
   const int rows = a.tiled ? tile_rows<D>() : kRows;
   const int64_t tiles = a.cu ? a.tokens * a.group / rows + a.n
                              : a.n * ((a.group + rows - 1) / rows);
+  const dim3 grid((unsigned)(tiles * a.c.kv_heads), (unsigned)a.parts);
   if (a.tiled)
-    hipLaunchKernelGGL((kv_attend_tile<D, FMT, tile_waves<D>(), 1>),
-                       dim3((unsigned)(tiles * a.c.kv_heads), (unsigned)a.parts),
+    hipLaunchKernelGGL((kv_attend_tile<D, FMT, tile_waves<D>(), 1>), grid,
                        dim3(tile_waves<D>() * kWave), 0, st, a);
   else
-    launch_rows<D, FMT>(a, dim3((unsigned)tiles, (unsigned)a.c.kv_heads, (unsigned)a.parts), st);
+    launch_rows<D, FMT>(a, grid, st);
   if (a.tiled && a.parts > 1)
     hipLaunchKernelGGL(kv_attend_join<D>,
-                       dim3((unsigned)tiles, (unsigned)a.c.kv_heads, (unsigned)(rows / 4)),
-                       dim3(256), 0, st, a, rows);
+                       dim3((unsigned)(tiles * a.c.kv_heads), (unsigned)(rows / kJoinRows)), dim3(256), 0, st,
+                       a, rows);
   return hipGetLastError();
 }
 
