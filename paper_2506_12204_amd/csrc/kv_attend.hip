@@ -14,7 +14,6 @@
 // largest vs seen, 2^14 above, so that weights down to 2^-28 of the largest
 // keep 11 bits.
 #include <algorithm>
-#include <type_traits>
 
 #include "device_common.h"
 #include "kv.h"
@@ -38,12 +37,12 @@ constexpr float kSlack = 8.0f;
 
 struct Sequence {
   const int32_t* table;
-  int64_t row0;     // first query token
-  int fresh, len;   // query tokens, keys
+  int64_t row0;           // first query token
+  int index, fresh, len;  // its number in the call, query tokens, keys
 };
 
-// The sequence of row tile u and the tile's number in it; false if there is no
-// such tile. Tiles are numbered sequence by sequence, LATE ones (whose causal
+// The sequence of row tile u (all but its keys) and the tile's number in it;
+// false if there is no such tile. Tiles are numbered sequence by sequence, LATE ones (whose causal
 // rows see most keys) first where that is asked for. The grid's size is a bound,
 // and its workgroups without work have to be the last or first ones: the device
 // deals workgroups to its parts in turn, and idle ones at regular places would
@@ -51,8 +50,8 @@ struct Sequence {
 // sequences, 64 at a time (n / 64 rounds of independent loads, where a search
 // would take log n dependent ones).
 template <bool LATE>
-__device__ __forceinline__ bool find_sequence(const KvAttendArgs& a, uint32_t u, int rows,
-                                              Sequence& q, int64_t& tile) {
+__device__ __forceinline__ bool find_tile(const KvAttendArgs& a, uint32_t u, int rows, Sequence& q,
+                                          int& tile) {
   const KvView& c = a.c;
   int64_t i = -1;
   if (a.cu) {
@@ -75,7 +74,7 @@ __device__ __forceinline__ bool find_sequence(const KvAttendArgs& a, uint32_t u,
       if (beyond) {
         const int first = __ffsll((unsigned long long)beyond) - 1;
         i = at + first;
-        tile = u - (uint32_t)__builtin_amdgcn_readlane((int)(upto - mine), first);
+        tile = (int)u - __builtin_amdgcn_readlane((int)(upto - mine), first);
         break;
       }
       before = (uint32_t)__builtin_amdgcn_readlane((int)upto, kWave - 1);
@@ -86,7 +85,7 @@ __device__ __forceinline__ bool find_sequence(const KvAttendArgs& a, uint32_t u,
   } else {
     const uint32_t each = (uint32_t)(a.group + rows - 1) / (uint32_t)rows;
     i = u / each;
-    tile = u % each;
+    tile = (int)(u % each);
   }
   q.row0 = a.cu ? a.cu[i] : i;
   const int64_t fresh = a.cu ? (int64_t)a.cu[i + 1] - q.row0 : 1;
@@ -95,20 +94,21 @@ __device__ __forceinline__ bool find_sequence(const KvAttendArgs& a, uint32_t u,
     return false;
   }
   q.fresh = (int)fresh;
-  const int32_t s = a.seqs[i];
-  q.len = 0;
-  q.table = c.tables;
-  if ((uint32_t)s >= (uint32_t)c.slots) {
-    if (threadIdx.x == 0) atomicOr(c.flags, kFlagInval);
-    return true;  // its rows see no key
-  }
-  q.table += (int64_t)s * c.max_blocks;
-  q.len = c.lens[s];
+  q.index = (int)i;
+  return true;
+}
+
+// The sequence's keys; none if the cache cannot hold them.
+__device__ __forceinline__ void find_keys(const KvAttendArgs& a, Sequence& q) {
+  const KvView& c = a.c;
+  const int32_t s = a.seqs[q.index];
+  const bool known = (uint32_t)s < (uint32_t)c.slots;
+  q.table = c.tables + (known ? (int64_t)s * c.max_blocks : 0);
+  q.len = known ? c.lens[s] : -1;
   if (q.len < 0 || (int64_t)q.len > ((int64_t)c.max_blocks << c.page_shift)) {
     if (threadIdx.x == 0) atomicOr(c.flags, kFlagInval);
     q.len = 0;
   }
-  return true;
 }
 
 // Keys [low, high) that query token i of the sequence sees.
@@ -142,49 +142,55 @@ __device__ __forceinline__ uint32_t pack_pair(float x, float y, int bf16) {
   return bf16 ? pack_pair<true>(x, y) : pack_pair<false>(x, y);
 }
 
-// A row's query in halves, as the lane's D / (8 G) operands of eight: of G = 4
-// lane groups, group g holds channels (4 j + g) * 16 .. + 15 in operands 2 j and
-// 2 j + 1; of G = 2, channels 16 j + 8 g .. + 7 in operand j. Returns what the
-// scores have to be multiplied by, which is not negative (a negative scale
-// changes the query's sign).
+// A row's query, as the lane's D / (8 G) operands of eight: of G = 4 lane groups,
+// group g holds channels (4 j + g) * 16 .. + 15 in operands 2 j and 2 j + 1; of
+// G = 2, channels 16 j + 8 g .. + 7 in operand j. Loaded first, so that finding
+// the keys and their pages takes place meanwhile.
 template <int D, int G>
-__device__ __forceinline__ float load_query(const KvAttendArgs& a, const uint16_t* row, int g,
-                                            half8_t (&q)[D / (8 * G)]) {
-  constexpr int N = D / (8 * G);
+struct Query {
+  static constexpr int N = D / (8 * G);
   uint16_t e[N][8];
+
+  __device__ __forceinline__ void load(const KvAttendArgs& a, const uint16_t* row, int g) {
 #pragma unroll
-  for (int j = 0; j < N; ++j) {
-    const uint16_t* p = row + (G == 4 ? (4 * (j / 2) + g) * 16 + j % 2 * 8 : 16 * j + 8 * g);
-    if (a.wide) {
-      *reinterpret_cast<uint4*>(e[j]) = *reinterpret_cast<const uint4*>(p);
-    } else {
+    for (int j = 0; j < N; ++j) {
+      const uint16_t* p = row + (G == 4 ? (4 * (j / 2) + g) * 16 + j % 2 * 8 : 16 * j + 8 * g);
+      if (a.wide) {
+        *reinterpret_cast<uint4*>(e[j]) = *reinterpret_cast<const uint4*>(p);
+      } else {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) e[j][k] = p[k];
+        for (int k = 0; k < 8; ++k) e[j][k] = p[k];
+      }
     }
   }
-  const float sign = a.scale_log2 < 0.0f ? -1.0f : 1.0f;
-  float up = 1.0f, undo = 1.0f;
-  if (a.bf16) {
-    float top = 0.0f;
+
+  // In halves. Returns what the scores have to be multiplied by, which is not
+  // negative (a negative scale changes the query's sign).
+  __device__ __forceinline__ float convert(const KvAttendArgs& a, half8_t (&q)[N]) const {
+    const float sign = a.scale_log2 < 0.0f ? -1.0f : 1.0f;
+    float up = 1.0f, undo = 1.0f;
+    if (a.bf16) {
+      float top = 0.0f;
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) top = fmaxf(top, fabsf(load16(e[j][k], 1)));
+      if (G == 4) top = fmaxf(top, __shfl_xor(top, 16, kWave));
+      top = fmaxf(top, __shfl_xor(top, 32, kWave));
+      // 2^(14 - exponent), between 2^-126 and 2^126; rows of zeros or with an
+      // infinity stay as they are
+      const int e2 = (int)(__float_as_uint(top) >> 23);
+      const int shift = top > 0.0f && e2 < 255 ? min(max(14 - (e2 - 127), -126), 126) : 0;
+      up = __uint_as_float((uint32_t)(127 + shift) << 23);
+      undo = __uint_as_float((uint32_t)(127 - shift) << 23);
+    }
 #pragma unroll
     for (int j = 0; j < N; ++j)
 #pragma unroll
-      for (int k = 0; k < 8; ++k) top = fmaxf(top, fabsf(load16(e[j][k], 1)));
-    if (G == 4) top = fmaxf(top, __shfl_xor(top, 16, kWave));
-    top = fmaxf(top, __shfl_xor(top, 32, kWave));
-    // 2^(14 - exponent), between 2^-126 and 2^126; rows of zeros or with an
-    // infinity stay as they are
-    const int e2 = (int)(__float_as_uint(top) >> 23);
-    const int shift = top > 0.0f && e2 < 255 ? min(max(14 - (e2 - 127), -126), 126) : 0;
-    up = __uint_as_float((uint32_t)(127 + shift) << 23);
-    undo = __uint_as_float((uint32_t)(127 - shift) << 23);
+      for (int k = 0; k < 8; ++k) q[j][k] = (_Float16)(load16(e[j][k], a.bf16) * (up * sign));
+    return undo * fabsf(a.scale_log2);
   }
-#pragma unroll
-  for (int j = 0; j < N; ++j)
-#pragma unroll
-    for (int k = 0; k < 8; ++k) q[j][k] = (_Float16)(load16(e[j][k], a.bf16) * (up * sign));
-  return undo * fabsf(a.scale_log2);
-}
+};
 
 // Sixteen codes as two operands of eight halves.
 template <int FMT>
@@ -241,9 +247,9 @@ __device__ __forceinline__ void finish_row(const KvAttendArgs& a, int64_t token,
         some ? (most + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : kNone;
 }
 
-// Joins a row's parts with one wave.
-// ALIVE: written by workgroups of this kernel, to be read past the L2 caches.
-template <int D, bool ALIVE>
+// Joins a row's parts with one wave. They were written by workgroups of this
+// kernel, and are read past the L2 caches.
+template <int D>
 __device__ __forceinline__ void join_row(const KvAttendArgs& a, int64_t token, int64_t head,
                                          int parts) {
   constexpr int W = D / 64;
@@ -253,13 +259,10 @@ __device__ __forceinline__ void join_row(const KvAttendArgs& a, int64_t token, i
   static_assert(kMostParts == 2 * kWave, "two parts per lane");
   const int far = kWave + lane;
   const float* ml = a.part_ml + 2 * at;
-  auto load = [](const float* p) __attribute__((always_inline)) {
-    return ALIVE ? load_agent(p) : *p;
-  };
-  const float m0 = lane < parts ? load(ml + 2 * lane * all) : kNone;
-  const float l0 = lane < parts ? load(ml + 2 * lane * all + 1) : 0.0f;
-  const float m1 = far < parts ? load(ml + 2 * far * all) : kNone;
-  const float l1 = far < parts ? load(ml + 2 * far * all + 1) : 0.0f;
+  const float m0 = lane < parts ? load_agent(ml + 2 * lane * all) : kNone;
+  const float l0 = lane < parts ? load_agent(ml + 2 * lane * all + 1) : 0.0f;
+  const float m1 = far < parts ? load_agent(ml + 2 * far * all) : kNone;
+  const float l1 = far < parts ? load_agent(ml + 2 * far * all + 1) : 0.0f;
   float most = fmaxf(m0, m1);
 #pragma unroll
   for (int off = 32; off > 0; off /= 2) most = fmaxf(most, __shfl_xor(most, off, kWave));
@@ -276,7 +279,7 @@ __device__ __forceinline__ void join_row(const KvAttendArgs& a, int64_t token, i
   for (int k = 0; k < parts; ++k) {
     const float w = __shfl(k < kWave ? w0 : w1, k % kWave, kWave);
 #pragma unroll
-    for (int j = 0; j < W; ++j) o[j] += load(from + k * all * D + j) * w;
+    for (int j = 0; j < W; ++j) o[j] += load_agent(from + k * all * D + j) * w;
   }
   finish_row<D>(a, token, head, most, total, o);
 }
@@ -306,22 +309,23 @@ __global__ __launch_bounds__(NW* kWave) void kv_attend_rows(KvAttendArgs a) {
   // share of every sequence
   const int kh = blockIdx.x % c.kv_heads;
   Sequence q;
-  int64_t tile;
-  if (!find_sequence<false>(a, blockIdx.x / c.kv_heads, kRows, q, tile)) return;
-  const int64_t rows = (int64_t)q.fresh * a.group;
-  const int64_t row = tile * kRows + r;
-  const bool live = row < rows;
-  const int token = (int)((live ? row : rows - 1) / a.group);
-  const int head = kh * a.group + (int)((live ? row : rows - 1) % a.group);
-  half8_t query[D / 32];
-  const float factor = load_query<D, 4>(
-      a, a.q + (q.row0 + token) * a.q_token + head * a.q_head, g, query);
+  int tile;
+  if (!find_tile<false>(a, blockIdx.x / c.kv_heads, kRows, q, tile)) return;
+  const int rows = q.fresh * a.group;
+  const uint32_t row = (uint32_t)min(tile * kRows + r, rows - 1);
+  const bool live = tile * kRows + r < rows;
+  const int token = (int)(row / (uint32_t)a.group);
+  const int head = kh * a.group + (int)(row % (uint32_t)a.group);
+  Query<D, 4> raw;
+  raw.load(a, a.q + (q.row0 + token) * a.q_token + head * a.q_head, g);
+  find_keys(a, q);
   int low, high;
   visible(a, q, token, low, high);
   // the keys that any row of the tile sees, and those that all see
   int from, to, all_from, all_to;
-  visible(a, q, (int)(tile * kRows / a.group), from, all_to);
-  visible(a, q, (int)((min(tile * kRows + kRows, rows) - 1) / a.group), all_from, to);
+  visible(a, q, (int)((uint32_t)(tile * kRows) / (uint32_t)a.group), from, all_to);
+  visible(a, q, (int)((uint32_t)(min(tile * kRows + kRows, rows) - 1) / (uint32_t)a.group),
+          all_from, to);
   const int c0 = from / kChunk, c1 = (to + kChunk - 1) / kChunk;
   const int parts = parts_of(a, c0, c1), part = blockIdx.y;
   if (part >= parts) return;
@@ -380,6 +384,8 @@ __global__ __launch_bounds__(NW* kWave) void kv_attend_rows(KvAttendArgs a) {
     load_k(begin + wave, kpage, vpage);
     load_v(begin + wave, vpage);
   }
+  half8_t query[D / 32];
+  const float factor = raw.convert(a, query);
   for (int ch = begin + wave; ch < stop; ch += NW) {
     const int t0 = ch * kChunk, vt = t0 + g * kKvTile;
     const bool more = ch + NW < stop;
@@ -475,7 +481,7 @@ __global__ __launch_bounds__(NW* kWave) void kv_attend_rows(KvAttendArgs a) {
   // a wave joins every NW-th row, a lane its W channels of it
   const int64_t all = a.tokens * a.heads;
   for (int i = wave; i < kRows; i += NW) {
-    const int64_t rr = tile * kRows + i;
+    const int rr = tile * kRows + i;
     if (rr >= rows) break;
     float most = kNone;
     for (int w = 0; w < busy; ++w) most = fmaxf(most, join_m[w][i]);
@@ -489,7 +495,8 @@ __global__ __launch_bounds__(NW* kWave) void kv_attend_rows(KvAttendArgs a) {
 #pragma unroll
       for (int j = 0; j < W; ++j) o[j] += join_o[w][i][lane * W + j] * e;
     }
-    const int64_t tok = q.row0 + rr / a.group, hd = kh * a.group + rr % a.group;
+    const int64_t tok = q.row0 + (uint32_t)rr / (uint32_t)a.group;
+    const int64_t hd = kh * a.group + (uint32_t)rr % (uint32_t)a.group;
     if (parts == 1) {
       finish_row<D>(a, tok, hd, most, total, o);
     } else {
@@ -514,16 +521,17 @@ __global__ __launch_bounds__(NW* kWave) void kv_attend_rows(KvAttendArgs a) {
   block_sync();
   if (!last) return;
   for (int i = wave; i < kRows; i += NW) {
-    const int64_t rr = tile * kRows + i;
+    const int rr = tile * kRows + i;
     if (rr >= rows) break;
-    join_row<D, true>(a, q.row0 + rr / a.group, kh * a.group + rr % a.group, parts);
+    join_row<D>(a, q.row0 + (uint32_t)rr / (uint32_t)a.group,
+                kh * a.group + (uint32_t)rr % (uint32_t)a.group, parts);
   }
 }
 
 // ---------------------------------------------------------------------------
-// Many rows: tiles of NW * RT * 32 rows of one KV head.
+// Many rows: tiles of NW * 32 rows of one KV head.
 //
-// A wave holds RT * 32 rows (their queries and outputs in registers) and goes
+// A wave holds 32 rows (their queries and outputs in registers) and goes
 // through the keys 32 at a time; the workgroup turns their codes into halves
 // once and keeps them in LDS in operand order, so that every operand is one
 // 16-byte LDS read without bank conflicts. As above, scores are taken as K q^T:
@@ -538,88 +546,59 @@ __global__ __launch_bounds__(NW* kWave) void kv_attend_rows(KvAttendArgs a) {
 constexpr int kWide = 32;  // rows of a matrix tile, and keys of a step
 typedef float float16_t __attribute__((ext_vector_type(16)));
 
-// The order of a step's instructions: every matrix instruction is followed by
-// vector ones that run beside it, an operand read and an exponential.
-template <int MATRIX, int VECTOR>
-__device__ __forceinline__ void interleave() {
-#pragma unroll
-  for (int i = 0; i < MATRIX; ++i) {
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);       // matrix
-    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);       // LDS reads
-    __builtin_amdgcn_sched_group_barrier(0x002, VECTOR, 0);  // vector
-    __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);       // exponentials
-  }
-}
-
-template <int D, int FMT, int NW, int RT>
+template <int D, int FMT, int NW>
 __global__ __launch_bounds__(NW* kWave, NW / 4) void kv_attend_tile(KvAttendArgs a) {
   constexpr int NT = NW * kWave;
   constexpr int KS = D / 16;       // matrix steps of the score product
   constexpr int DY = D / 32;       // output tiles
   constexpr int UNITS = 4 * D;     // 16-byte units of a step's K and V
   constexpr int PER = UNITS > NT ? UNITS / NT : 1;  // of them per thread
+  constexpr int ROWS = NW * kWide;
+  static_assert(NT * PER % UNITS == 0, "whole rounds of units");
   // Two waves per SIMD hold everything in vector registers; one has to keep
   // outputs and queries in the accumulation registers.
   constexpr bool PINNED = NW == 4;
-  constexpr int ROWS = NW * RT * kWide;
-  static_assert(NT * PER % UNITS == 0, "whole rounds of units");
   constexpr int KEYS = 2 * KS * kWave;      // [buffer][step][lane]
   constexpr int VALS = 4 * 2 * DY * kWave;  // [buffer][8 keys of either half][tile][lane]
   constexpr int PITCH = D / 8 + 1;          // of an output row at the end
-  constexpr int OUTS = NW * kWide * PITCH;
+  constexpr int OUTS = ROWS * PITCH;
   __shared__ half8_t pool[KEYS + VALS > OUTS ? KEYS + VALS : OUTS];
+  __shared__ float scales[4 * 4];  // [buffer][K tile 0, 1, V tile 0, 1]
   half8_t* const keys = pool;
   half8_t* const vals = pool + KEYS;
-  __shared__ float scales[4 * 4];               // [buffer][K tile 0, 1, V tile 0, 1]
   const KvView& c = a.c;
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int r = lane % kWide, h = lane / kWide;
   const int kh = blockIdx.x % c.kv_heads;
   Sequence q;
-  int64_t tile;
-  if (!find_sequence<true>(a, blockIdx.x / c.kv_heads, ROWS, q, tile)) return;
-  const int64_t rows = (int64_t)q.fresh * a.group;
+  int tile;
+  if (!find_tile<true>(a, blockIdx.x / c.kv_heads, ROWS, q, tile)) return;
+  const int rows = q.fresh * a.group;
+  const int row0 = tile * ROWS + wave * kWide;
+  const uint32_t row = (uint32_t)min(row0 + r, rows - 1);
+  const bool live = row0 + r < rows;
+  const int token = (int)(row / (uint32_t)a.group);
+  const int head = kh * a.group + (int)(row % (uint32_t)a.group);
+  Query<D, 2> asked;
+  asked.load(a, a.q + (q.row0 + token) * a.q_token + head * a.q_head, h);
+  find_keys(a, q);
   // the keys that the workgroup's rows see
   int from, to, unused;
-  visible(a, q, (int)(tile * ROWS / a.group), from, unused);
-  visible(a, q, (int)((min(tile * ROWS + ROWS, rows) - 1) / a.group), unused, to);
+  visible(a, q, (int)((uint32_t)(tile * ROWS) / (uint32_t)a.group), from, unused);
+  visible(a, q, (int)((uint32_t)(min(tile * ROWS + ROWS, rows) - 1) / (uint32_t)a.group), unused, to);
   const int c0 = from / kChunk, c1 = (to + kChunk - 1) / kChunk;
   const int parts = parts_of(a, c0, c1), part = blockIdx.y;
   if (part >= parts) return;
   const int begin = 2 * part_start(c0, c1, parts, part);
   const int stop = 2 * part_start(c0, c1, parts, part + 1);
-
-  const int64_t row0 = tile * ROWS + wave * (RT * kWide);
-  half8_t query[RT][KS];
-  float factor[RT];
-  int low[RT], high[RT], token[RT], head[RT];
-#pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    const int64_t row = row0 + t * kWide + r;
-    const bool live = row < rows;
-    const int64_t at = live ? row : rows - 1;
-    token[t] = (int)(at / a.group);
-    head[t] = kh * a.group + (int)(at % a.group);
-    factor[t] = load_query<D, 2>(
-        a, a.q + (q.row0 + token[t]) * a.q_token + head[t] * a.q_head, h, query[t]);
-    visible(a, q, token[t], low[t], high[t]);
-    if (!live) {
-      low[t] = 0;
-      high[t] = 0;
-      token[t] = -1;
-    }
-  }
-  if (PINNED) {
-#pragma unroll
-    for (int t = 0; t < RT; ++t)
-#pragma unroll
-      for (int k = 0; k < KS; ++k) asm volatile("" : "+a"(query[t][k]));
-  }
+  int low, high;
+  visible(a, q, token, low, high);
+  if (!live) high = 0;
   // the keys that all of this wave's rows see
   int all_from = 0, all_to = 0;
-  if (row0 + RT * kWide <= rows) {
-    visible(a, q, (int)(row0 / a.group), unused, all_to);
-    visible(a, q, (int)((row0 + RT * kWide - 1) / a.group), all_from, unused);
+  if (row0 + kWide <= rows) {
+    visible(a, q, (int)((uint32_t)row0 / (uint32_t)a.group), unused, all_to);
+    visible(a, q, (int)((uint32_t)(row0 + kWide - 1) / (uint32_t)a.group), all_from, unused);
     if (all_from >= all_to) all_to = 0;
   }
 
@@ -629,9 +608,6 @@ __global__ __launch_bounds__(NW* kWave, NW / 4) void kv_attend_tile(KvAttendArgs
   const int in_page = c.page_tokens - 1;
   const int last_block = (q.len - 1) >> c.page_shift;
   bool wrong = false;
-  auto entry_of = [&](int t) __attribute__((always_inline)) {
-    return q.table[min(t >> c.page_shift, last_block)];
-  };
   auto checked = [&](int32_t entry) __attribute__((always_inline)) -> uint32_t {
     const bool bad = (uint32_t)entry >= (uint32_t)c.num_pages;
     wrong |= bad;
@@ -657,23 +633,18 @@ __global__ __launch_bounds__(NW* kWave, NW / 4) void kv_attend_tile(KvAttendArgs
     unit_to[k] = is_key(k) ? in / 16 * kWave + tok / 4 * 8 + tl * 4 + tok % 4
                            : in / 32 * kWave + tl * kWide + in % 32;
   }
-  uint4 raw[2][PER];
-  float sraw[2] = {0.0f, 0.0f};
-  int32_t page = 0;
   const float* const scale_at =
       c.scale + ((int64_t)a.layer * 2 + lane / 2 % 2) * c.kv_heads + kh;
   auto look_up = [&](int j) __attribute__((always_inline)) {
-    page = entry_of(min(j, stop - 1) * kWide + lane % 2 * kKvTile);
+    return q.table[min((min(j, stop - 1) * kWide + lane % 2 * kKvTile) >> c.page_shift, last_block)];
   };
   // (all threads load and store one of the four scales: no branch)
-  auto fetch = [&](int j, uint4 (&to)[PER], float& sc) __attribute__((always_inline)) {
+  auto fetch = [&](int j, int32_t entry, uint4 (&to)[PER], float& sc)
+      __attribute__((always_inline)) {
     const int t0 = min(j, stop - 1) * kWide;
-    const uint32_t mine = checked(page);
+    const uint32_t mine = checked(entry);
     const uint32_t both[2] = {(uint32_t)__builtin_amdgcn_readlane((int)mine, 0),
                               (uint32_t)__builtin_amdgcn_readlane((int)mine, 1)};
-    // the next look-up goes first: loads return in order, and the next step
-    // needs it before these
-    look_up(j + 1);
     sc = scale_at[(int64_t)mine * c.page_scales];
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
@@ -683,278 +654,310 @@ __global__ __launch_bounds__(NW* kWave, NW / 4) void kv_attend_tile(KvAttendArgs
       to[k] = reinterpret_cast<const uint4*>(p)[lane];
     }
   };
-  auto stage = [&](auto mask, int j, const uint4 (&from)[PER], float sc)
-      __attribute__((always_inline)) {
+  // V codes beyond the length may be anything (K ones are hidden later).
+  auto hide = [&](int j, uint4 (&w)[PER]) __attribute__((always_inline)) {
+    if ((j + 1) * kWide <= q.len) return;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      const int n = is_key(k) ? 16 : q.len - j * kWide - unit_tile(k) * kKvTile;
+      w[k].x = keep_bytes(w[k].x, n);
+      w[k].y = keep_bytes(w[k].y, n - 4);
+      w[k].z = keep_bytes(w[k].z, n - 8);
+      w[k].w = keep_bytes(w[k].w, n - 12);
+    }
+  };
+  auto stage = [&](int j, const uint4 (&from)[PER], float sc) __attribute__((always_inline)) {
     scales[(j & 3) * 4 + lane % 4] = sc;
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
-      uint4 w = from[k];
-      // V codes beyond the length may be anything; K ones are hidden later
-      if (decltype(mask)::value && !is_key(k)) {
-        const int n = q.len - j * kWide - unit_tile(k) * kKvTile;
-        w.x = keep_bytes(w.x, n);
-        w.y = keep_bytes(w.y, n - 4);
-        w.z = keep_bytes(w.z, n - 8);
-        w.w = keep_bytes(w.w, n - 12);
-      }
       half8_t lo, hi;
-      codes_to_operands<FMT>(w, lo, hi);
+      codes_to_operands<FMT>(from[k], lo, hi);
       half8_t* to = is_key(k) ? keys + (j & 1) * (KS * kWave) : vals + (j & 3) * (2 * DY * kWave);
       to[unit_to[k]] = lo;
       to[unit_to[k] + (is_key(k) ? kWide : DY * kWave)] = hi;
     }
   };
 
-  float m[RT], l[RT], vref = 0.0f;
-  float16_t acc[RT][DY], s0[RT], s1[RT];
-  half8_t w0[RT][2], w1[RT][2];
+  half8_t query[KS];
+  float factor = 0.0f;
+  float m = kNone, l = 0.0f, vref = 0.0f;
+  float16_t acc[DY], s0, s1;
+  half8_t w0[2], w1[2];
 #pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    m[t] = kNone;
-    l[t] = 0.0f;
+  for (int y = 0; y < DY; ++y)
 #pragma unroll
-    for (int y = 0; y < DY; ++y)
+    for (int i = 0; i < 16; ++i) acc[y][i] = 0.0f;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) acc[t][y][i] = 0.0f;
+  for (int x = 0; x < 2; ++x)
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) w1[t][x][i] = (_Float16)0.0f;
-  }
-  auto score = [&](int j, float16_t (&s)[RT]) __attribute__((always_inline)) {
-    const half8_t* from = keys + (j & 1) * (KS * kWave) + lane;
-#pragma unroll
-    for (int t = 0; t < RT; ++t)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
-#pragma unroll
-    for (int k = 0; k < KS; ++k) {
-      const half8_t kf = from[k * kWave];
-#pragma unroll
-      for (int t = 0; t < RT; ++t)
-        s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, query[t][k], s[t], 0, 0, 0);
-    }
+    for (int i = 0; i < 8; ++i) w1[x][i] = (_Float16)0.0f;
+  auto read_key = [&](int j, int k) __attribute__((always_inline)) {
+    return keys[(j & 1) * (KS * kWave) + k * kWave + lane];
   };
-  auto output = [&](const half8_t (&vf)[2][DY], const half8_t (&w)[RT][2])
+  auto score = [&](int k, half8_t key, float16_t& s) __attribute__((always_inline)) {
+    s = __builtin_amdgcn_mfma_f32_32x32x16_f16(key, query[k], s, 0, 0, 0);
+  };
+  auto output = [&](int x, const half8_t (&vf)[DY], const half8_t (&w)[2])
       __attribute__((always_inline)) {
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
-#pragma unroll
-      for (int y = 0; y < DY; ++y)
-#pragma unroll
-        for (int t = 0; t < RT; ++t)
-          acc[t][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[x][y], w[t][x], acc[t][y], 0, 0, 0);
+    for (int y = 0; y < DY; ++y)
+      acc[y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[y], w[x], acc[y], 0, 0, 0);
   };
-  auto read_vals = [&](int j, half8_t (&vf)[2][DY]) __attribute__((always_inline)) {
+  auto read_vals = [&](int j, int x, half8_t (&vf)[DY]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
+    for (int y = 0; y < DY; ++y)
+      vf[y] = vals[(j & 3) * (2 * DY * kWave) + (x * DY + y) * kWave + lane];
+  };
+
+  int32_t page = 0;  // of the next step's loads
+  // Step j: scores of keys j + 1 into nxt, weights of keys j from cur, outputs of
+  // keys j - 1. The first half's matrix instructions each get a share of the
+  // weights' vector ones (the compiler would put them all behind).
+  auto step = [&](int j, float16_t& cur, float16_t& nxt, const half8_t (&wp)[2], half8_t (&wc)[2],
+                  uint4 (&rw)[PER], float& sc) __attribute__((always_inline)) {
+    if (j * kWide < all_from || (j + 1) * kWide > all_to) {  // keys that some rows do not see
+      const int t0 = j * kWide + h * kKvTile;
 #pragma unroll
-      for (int y = 0; y < DY; ++y)
-        vf[x][y] = vals[(j & 3) * (2 * DY * kWave) + (x * DY + y) * kWave + lane];
-  };
-  // Scores of a row tile become weights; its outputs so far are to be multiplied
-  // by `fade`.
-  struct Scales {
-    float ks, bias, unrel, older;
-  };
-  auto scales_of = [&](int j) __attribute__((always_inline)) {
+      for (int i = 0; i < 16; ++i)
+        cur[i] = t0 + i >= low && t0 + i < high ? cur[i] : kNone;
+    }
+    hide(j + 2, rw);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) nxt[i] = 0.0f;
+    __builtin_amdgcn_sched_barrier(0);
+    half8_t kf[KS];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) kf[k] = read_key(j + 1, k);
     const float ks = scales[(j & 3) * 4 + h];
     const float vs0 = scales[(j & 3) * 4 + 2], vs1 = scales[(j & 3) * 4 + 3];
+    float top = cur[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) top = __builtin_elementwise_maximum(top, cur[i]);
+    __builtin_amdgcn_sched_barrier(0);
+    score(0, kf[0], nxt);
     // weights are relative to the largest V scale so far (the same in all lanes)
     const float vmax = fmaxf(fmaxf(vs0, vs1), vref);
     const float inv = vmax > 0.0f ? __builtin_amdgcn_rcpf(vmax) : 0.0f;
-    const float older = vmax > vref ? vref * inv : 1.0f;
-    vref = vmax;
     const float rel = fmaxf((h ? vs1 : vs0) * inv, 9.3e-10f) * kLift;  // (2^-30)
-    return Scales{ks, __builtin_amdgcn_logf(rel), __builtin_amdgcn_rcpf(rel), older};
-  };
-  auto weigh = [&](int t, const Scales& z, const float16_t& s, half8_t (&w)[2], float& fade)
-      __attribute__((always_inline)) {
+    const float unrel = __builtin_amdgcn_rcpf(rel);
     // (not zero, so that a hidden key's minus infinity stays one)
-    const float f = fmaxf(z.ks * factor[t], 1e-30f);
-    float top = s[0];
-#pragma unroll
-    for (int i = 1; i < 16; ++i) top = __builtin_elementwise_maximum(top, s[i]);
+    const float f = fmaxf(ks * factor, 1e-30f);
     top *= f;
     top = __builtin_elementwise_maximum(top, other_half(top));
-    const bool raise = top > m[t] + kSlack;
-    const float next = raise ? top : m[t];
-    const float shrink = raise ? __builtin_amdgcn_exp2f(m[t] - next) : 1.0f;
-    m[t] = next;
-    const float b = z.bias - (next == kNone ? 0.0f : next);
+    __builtin_amdgcn_sched_barrier(0);
+    score(1, kf[1], nxt);
+    const bool raise = top > m + kSlack;
+    const float next = raise ? top : m;
+    const float shrink = raise ? __builtin_amdgcn_exp2f(m - next) : 1.0f;
+    const float fade = vmax > vref ? shrink * (vref * inv) : shrink;
+    vref = vmax;
+    m = next;
+    const float b = __builtin_amdgcn_logf(rel) - (next == kNone ? 0.0f : next);
     float sum[2] = {0.0f, 0.0f};
+    half8_t vf[DY], vg[DY];
+    constexpr int SHARES = KS / 2 - 1;  // of the weights
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], f, b));
-      sum[i % 2] += p;
-      w[i / 8][i % 8] = (_Float16)p;
+    for (int i = 0; i < SHARES; ++i) {
+      __builtin_amdgcn_sched_barrier(0);
+      score(2 * i + 2, kf[2 * i + 2], nxt);
+      score(2 * i + 3, kf[2 * i + 3], nxt);
+      if (2 * i + 4 < KS) {
+        kf[2 * i + 4] = read_key(j + 1, 2 * i + 4);
+        kf[2 * i + 5] = read_key(j + 1, 2 * i + 5);
+      } else {
+        read_vals(max(j - 1, begin), 0, vf);
+      }
+#pragma unroll
+      for (int k = 16 * i / SHARES; k < 16 * (i + 1) / SHARES; ++k) {
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(cur[k], f, b));
+        sum[k % 2] += p;
+        wc[k / 8][k % 8] = (_Float16)p;
+      }
     }
-    l[t] = l[t] * shrink + (sum[0] + sum[1]) * z.unrel;
-    fade = z.older * shrink;
-    asm volatile("" : "+v"(w[0]), "+v"(w[1]));  // here, not where they are used
-  };
-  auto step = [&](auto mask, int j, float16_t (&cur)[RT], float16_t (&nxt)[RT],
-                  const half8_t (&wp)[RT][2], half8_t (&wc)[RT][2], uint4 (&rw)[PER], float& sc)
-      __attribute__((always_inline)) {
-    if (decltype(mask)::value) {
-      const int t0 = j * kWide + h * kKvTile;
+    l = l * shrink + (sum[0] + sum[1]) * unrel;
+    asm volatile("" : "+v"(wc[0]), "+v"(wc[1]), "+v"(l));  // here, not where they are used
+    __builtin_amdgcn_sched_barrier(0);
+    read_vals(max(j - 1, begin), 1, vg);
+    output(0, vf, wp);
+    output(1, vg, wp);
+    stage(j + 2, rw, sc);
+    // the next look-up goes first: loads return in order, and the next step
+    // needs it before these
+    const int32_t entry = page;
+    page = look_up(j + 5);
+    fetch(j + 4, entry, rw, sc);
 #pragma unroll
-      for (int t = 0; t < RT; ++t)
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          cur[t][i] = t0 + i >= low[t] && t0 + i < high[t] ? cur[t][i] : kNone;
+    for (int i = 0; i < 2 * DY; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a matrix instruction,
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // an operand read
+      __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);  // and vector ones
     }
-    float fade[RT];
-    half8_t vf[2][DY];
     __builtin_amdgcn_sched_barrier(0);
-    const Scales z = scales_of(j);
-    score(j + 1, nxt);
-    weigh(0, z, cur[0], wc[0], fade[0]);
-    read_vals(max(j - 1, begin), vf);
-    __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
-    interleave<RT * KS, 6>();
-    __builtin_amdgcn_sched_barrier(0);
-    output(vf, wp);
-    if (RT > 1) weigh(RT - 1, z, cur[RT - 1], wc[RT - 1], fade[RT - 1]);
-    stage(mask, j + 2, rw, sc);
-    fetch(j + 4, rw, sc);
-    interleave<RT * 2 * DY, 8>();
-    __builtin_amdgcn_sched_barrier(0);
-    bool any = false;
+    if (__ballot(fade != 1.0f)) {
 #pragma unroll
-    for (int t = 0; t < RT; ++t) any |= fade[t] != 1.0f;
-    if (__ballot(any)) {
-#pragma unroll
-      for (int t = 0; t < RT; ++t) {
-#pragma unroll
-        for (int y = 0; y < DY; ++y) {
-          // one after the other: all of them at once in the vector registers
-          // would push out other values
-          if (PINNED) asm volatile("" : "+a"(acc[t][y]));
-          acc[t][y] *= fade[t];
-          if (PINNED) asm volatile("" : "+a"(acc[t][y]));
-        }
+      for (int y = 0; y < DY; ++y) {
+        // one after the other: all of them at once in the vector registers
+        // would push out other values
+        if (PINNED) asm volatile("" : "+a"(acc[y]));
+        acc[y] *= fade;
+        if (PINNED) asm volatile("" : "+a"(acc[y]));
       }
     }
     block_sync();
   };
   if (begin < stop) {
-    constexpr std::false_type plain{};
-    constexpr std::true_type masked{};
-    look_up(begin);
-    fetch(begin, raw[0], sraw[0]);
-    fetch(begin + 1, raw[1], sraw[1]);
-    stage(masked, begin, raw[0], sraw[0]);
-    stage(masked, begin + 1, raw[1], sraw[1]);
-    fetch(begin + 2, raw[0], sraw[0]);
-    fetch(begin + 3, raw[1], sraw[1]);
+    int32_t entry[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) entry[i] = look_up(begin + i);
+    page = look_up(begin + 4);
+    factor = asked.convert(a, query);
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      if (PINNED) asm volatile("" : "+a"(query[k]));
+      else asm volatile("" : "+v"(query[k]));
+    }
+    uint4 early[2][PER], raw[2][PER];
+    float searly[2], sraw[2];
+    fetch(begin, entry[0], early[0], searly[0]);
+    fetch(begin + 1, entry[1], early[1], searly[1]);
+    fetch(begin + 2, entry[2], raw[0], sraw[0]);
+    fetch(begin + 3, entry[3], raw[1], sraw[1]);
+    hide(begin, early[0]);
+    hide(begin + 1, early[1]);
+    stage(begin, early[0], searly[0]);
+    stage(begin + 1, early[1], searly[1]);
     block_sync();
-    score(begin, s0);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s0[i] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) score(k, read_key(begin, k), s0);
     block_sync();  // step `begin` puts keys begin + 2 where these were
     for (int j = begin; j < stop; j += 2) {
-      // keys that all rows see, and codes that all are there
-      if (j * kWide >= all_from && (j + 2) * kWide <= all_to && (j + 4) * kWide <= q.len) {
-        step(plain, j, s0, s1, w1, w0, raw[0], sraw[0]);
-        step(plain, j + 1, s1, s0, w0, w1, raw[1], sraw[1]);
-      } else {
-        step(masked, j, s0, s1, w1, w0, raw[0], sraw[0]);
-        step(masked, j + 1, s1, s0, w0, w1, raw[1], sraw[1]);
-      }
+      step(j, s0, s1, w1, w0, raw[0], sraw[0]);
+      step(j + 1, s1, s0, w0, w1, raw[1], sraw[1]);
     }
-    half8_t vf[2][DY];
-    read_vals(stop - 1, vf);
-    output(vf, w1);
+    half8_t vf[DY], vg[DY];
+    read_vals(stop - 1, 0, vf);
+    read_vals(stop - 1, 1, vg);
+    output(0, vf, w1);
+    output(1, vg, w1);
   }
   block_sync();  // the buffers are free
   if (__ballot(wrong) && lane == 0) atomicOr(c.flags, kFlagInval);
+  l += other_half(l);
+  if (parts > 1) {
+    if (!live) return;
+    const int64_t slot = ((int64_t)part * a.tokens + q.row0 + token) * a.heads + head;
+    const float by = vref * (1.0f / kLift);
+    float* o = a.part_o + slot * D;
 #pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    l[t] += other_half(l[t]);
-    if (parts > 1) {
-      if (token[t] < 0) continue;
-      const int64_t at = (q.row0 + token[t]) * a.heads + head[t];
-      const int64_t slot = (int64_t)part * a.tokens * a.heads + at;
-      const float by = vref * (1.0f / kLift);
-      float* o = a.part_o + slot * D;
+    for (int y = 0; y < DY; ++y)
 #pragma unroll
-      for (int y = 0; y < DY; ++y)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const float4_t x = {acc[t][y][4 * k] * by, acc[t][y][4 * k + 1] * by,
-                              acc[t][y][4 * k + 2] * by, acc[t][y][4 * k + 3] * by};
-          *reinterpret_cast<float4_t*>(o + y * 32 + k * 8 + h * 4) = x;
-        }
-      if (h == 0) {
-        a.part_ml[2 * slot] = m[t];
-        a.part_ml[2 * slot + 1] = l[t];
+      for (int k = 0; k < 4; ++k) {
+        const float4_t x = {acc[y][4 * k] * by, acc[y][4 * k + 1] * by, acc[y][4 * k + 2] * by,
+                            acc[y][4 * k + 3] * by};
+        *reinterpret_cast<float4_t*>(o + y * 32 + k * 8 + h * 4) = x;
       }
-      continue;
+    if (h == 0) {
+      a.part_ml[2 * slot] = m;
+      a.part_ml[2 * slot + 1] = l;
     }
-    const bool some = l[t] > 0.0f || l[t] != l[t];
-    const float inv = some ? vref * (1.0f / kLift) / l[t] : 0.0f;
-    // through LDS, so that rows are written whole
-    uint2* const row = reinterpret_cast<uint2*>(pool + (wave * kWide + r) * PITCH);
-    if (a.bf16) {
+    return;
+  }
+  const bool some = l > 0.0f || l != l;
+  const float inv = some ? vref * (1.0f / kLift) / l : 0.0f;
+  // through LDS, so that rows are written whole
+  uint2* const mine = reinterpret_cast<uint2*>(pool + (wave * kWide + r) * PITCH);
 #pragma unroll
-      for (int y = 0; y < DY; ++y)
+  for (int y = 0; y < DY; ++y)
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          row[y * 8 + k * 2 + h] =
-              make_uint2(pack_pair<true>(acc[t][y][4 * k] * inv, acc[t][y][4 * k + 1] * inv),
-                         pack_pair<true>(acc[t][y][4 * k + 2] * inv, acc[t][y][4 * k + 3] * inv));
-    } else {
-#pragma unroll
-      for (int y = 0; y < DY; ++y)
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          row[y * 8 + k * 2 + h] =
-              make_uint2(pack_pair<false>(acc[t][y][4 * k] * inv, acc[t][y][4 * k + 1] * inv),
-                         pack_pair<false>(acc[t][y][4 * k + 2] * inv, acc[t][y][4 * k + 3] * inv));
-    }
-    if (a.lse && h == 0 && token[t] >= 0)
-      a.lse[(q.row0 + token[t]) * a.heads + head[t]] =
-          some ? (m[t] + __builtin_amdgcn_logf(l[t])) * 0.6931471805599453f : kNone;
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (a wave reads what it wrote)
-    constexpr int LANES = D / 8;  // of a row
+    for (int k = 0; k < 4; ++k)
+      mine[y * 8 + k * 2 + h] =
+          make_uint2(pack_pair(acc[y][4 * k] * inv, acc[y][4 * k + 1] * inv, a.bf16),
+                     pack_pair(acc[y][4 * k + 2] * inv, acc[y][4 * k + 3] * inv, a.bf16));
+  if (a.lse && h == 0 && live)
+    a.lse[(q.row0 + token) * a.heads + head] =
+        some ? (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : kNone;
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (a wave reads what it wrote)
+  constexpr int LANES = D / 8;  // of a row
 #pragma unroll 2
-    for (int i = lane / LANES; i < kWide; i += kWave / LANES) {
-      const int64_t rr = row0 + t * kWide + i;
-      if (rr >= rows) break;
-      const uint32_t tok = (uint32_t)rr / (uint32_t)a.group;
-      const int64_t hd = kh * a.group + (int)((uint32_t)rr - tok * a.group);
-      uint16_t* o = a.out + (q.row0 + tok) * a.out_token + hd * a.out_head + lane % LANES * 8;
-      const uint4 x = __builtin_bit_cast(uint4, pool[(wave * kWide + i) * PITCH + lane % LANES]);
-      if (a.wide_out) {
-        *reinterpret_cast<uint4*>(o) = x;
-      } else {
-        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  for (int i = lane / LANES; i < kWide; i += kWave / LANES) {
+    const int rr = row0 + i;
+    if (rr >= rows) break;
+    const uint32_t tok = (uint32_t)rr / (uint32_t)a.group;
+    const int64_t hd = kh * a.group + (int)((uint32_t)rr - tok * a.group);
+    uint16_t* o = a.out + (q.row0 + tok) * a.out_token + hd * a.out_head + lane % LANES * 8;
+    const uint4 x = __builtin_bit_cast(uint4, pool[(wave * kWide + i) * PITCH + lane % LANES]);
+    if (a.wide_out) {
+      *reinterpret_cast<uint4*>(o) = x;
+    } else {
+      const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-        for (int j = 0; j < 8; ++j) o[j] = (uint16_t)(w[j / 2] >> (16 * (j % 2)));
-      }
+      for (int j = 0; j < 8; ++j) o[j] = (uint16_t)(w[j / 2] >> (16 * (j % 2)));
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // before the next row tile's writes
   }
 }
 
-// Joins the parts of the key axis of the tile kernel: a wave per row.
-constexpr int kJoinRows = 32;  // of a workgroup
+// Joins the parts of the key axis of the tile kernel: sixteen lanes per row.
+constexpr int kJoinRows = 16;  // of a workgroup
 template <int D>
-__global__ __launch_bounds__(256) void kv_attend_join(KvAttendArgs a, int tile_rows) {
+__global__ __launch_bounds__(kJoinRows * 16) void kv_attend_join(KvAttendArgs a, int tile_rows) {
+  constexpr int W = D / 16;  // channels of a lane
+  const KvView& c = a.c;
   Sequence q;
-  int64_t tile;
-  if (!find_sequence<false>(a, blockIdx.x / a.c.kv_heads, tile_rows, q, tile)) return;
-  const int64_t rows = (int64_t)q.fresh * a.group;
-  const int kh = blockIdx.x % a.c.kv_heads;
+  int tile;
+  if (!find_tile<false>(a, blockIdx.x / c.kv_heads, tile_rows, q, tile)) return;
+  const int rows = q.fresh * a.group;
+  const int row = tile * tile_rows + blockIdx.y * kJoinRows + threadIdx.x / 16;
+  if (tile * tile_rows + (int)blockIdx.y * kJoinRows >= rows) return;
+  find_keys(a, q);
   int from, to, unused;
-  visible(a, q, (int)(tile * tile_rows / a.group), from, unused);
-  visible(a, q, (int)((min(tile * tile_rows + tile_rows, rows) - 1) / a.group), unused, to);
+  visible(a, q, (int)((uint32_t)(tile * tile_rows) / (uint32_t)a.group), from, unused);
+  visible(a, q, (int)((uint32_t)(min(tile * tile_rows + tile_rows, rows) - 1) / (uint32_t)a.group),
+          unused, to);
   const int parts = parts_of(a, from / kChunk, (to + kChunk - 1) / kChunk);
-  if (parts == 1) return;
-  const int64_t row0 = tile * tile_rows + (int64_t)blockIdx.y * kJoinRows;
-  for (int i = threadIdx.x / kWave; i < kJoinRows && row0 + i < rows; i += 4) {
-    const int64_t row = row0 + i;
-    join_row<D, false>(a, q.row0 + row / a.group, kh * a.group + row % a.group, parts);
+  if (parts == 1 || row >= rows) return;
+  const int64_t token = q.row0 + (uint32_t)row / (uint32_t)a.group;
+  const int64_t head = blockIdx.x % c.kv_heads * a.group + (uint32_t)row % (uint32_t)a.group;
+  const int64_t all = a.tokens * a.heads, at = token * a.heads + head;
+  const int lane = threadIdx.x % 16;
+  const float2_t* ml = reinterpret_cast<const float2_t*>(a.part_ml) + at;
+  float most = kNone;
+#pragma unroll 4
+  for (int k = 0; k < parts; ++k) most = fmaxf(most, ml[k * all][0]);
+  const float base = most == kNone ? 0.0f : most;
+  float total = 0.0f;
+  float4_t o[W / 4];
+#pragma unroll
+  for (int j = 0; j < W / 4; ++j) o[j] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+  const float* part = a.part_o + at * D + lane * W;
+#pragma unroll 4
+  for (int k = 0; k < parts; ++k) {
+    const float2_t p = ml[k * all];
+    const float w = __builtin_amdgcn_exp2f(p[0] - base);
+    total += p[1] * w;
+#pragma unroll
+    for (int j = 0; j < W / 4; ++j)
+      o[j] += *reinterpret_cast<const float4_t*>(part + k * all * D + 4 * j) * w;
   }
+  const bool some = total > 0.0f || total != total;
+  const float inv = some ? 1.0f / total : 0.0f;
+  uint16_t* out = a.out + token * a.out_token + head * a.out_head + lane * W;
+#pragma unroll
+  for (int j = 0; j < W / 4; ++j) {
+    const uint32_t x = pack_pair(o[j][0] * inv, o[j][1] * inv, a.bf16);
+    const uint32_t y = pack_pair(o[j][2] * inv, o[j][3] * inv, a.bf16);
+    if (a.wide_out) {
+      *reinterpret_cast<uint2*>(out + 4 * j) = make_uint2(x, y);
+    } else {
+      out[4 * j] = (uint16_t)x;
+      out[4 * j + 1] = (uint16_t)(x >> 16);
+      out[4 * j + 2] = (uint16_t)y;
+      out[4 * j + 3] = (uint16_t)(y >> 16);
+    }
+  }
+  if (a.lse && lane == 0)
+    a.lse[at] = some ? (most + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : kNone;
 }
 
 // Waves of the tile kernel's workgroups, each with one tile of 32 rows.
@@ -978,7 +981,7 @@ hipError_t launch(const KvAttendArgs& a, hipStream_t st) {
                              : a.n * ((a.group + rows - 1) / rows);
   const dim3 grid((unsigned)(tiles * a.c.kv_heads), (unsigned)a.parts);
   if (a.tiled)
-    hipLaunchKernelGGL((kv_attend_tile<D, FMT, tile_waves<D>(), 1>), grid,
+    hipLaunchKernelGGL((kv_attend_tile<D, FMT, tile_waves<D>()>), grid,
                        dim3(tile_waves<D>() * kWave), 0, st, a);
   else
     launch_rows<D, FMT>(a, grid, st);
