@@ -469,7 +469,7 @@ int sem_schedule_static(const uint8_t *priority, const int32_t *length, int64_t 
  * the cache (no memory outside the arguments is accessed); SEM_ERANGE for a
  * negative token count.
  */
-#define SEM_KV_ZEROED_BYTES 33024
+#define SEM_KV_ZEROED_BYTES 4352
 #define SEM_KV_INT8 0
 #define SEM_KV_FP8 1
 #define SEM_KV_BF16 0

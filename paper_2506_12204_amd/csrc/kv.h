@@ -9,7 +9,7 @@
 
 namespace semsched {
 
-constexpr int kKvCounts = 8192;      // counters of attention's tiles with several parts
+constexpr int kKvCounts = 1024;      // counters of attention's tiles with several parts
 constexpr int kKvTile = 16;          // tokens per tile of a page's block
 
 // The cache as the kernels see it: the caller's arrays and the derived sizes.

@@ -999,23 +999,44 @@ hipError_t launch_dim(const KvAttendArgs& a, hipStream_t st) {
 
 }  // namespace
 
+// Which kernel, and how many parts of the key axis. Rules measured on MI355X:
+//   * The kernel of few rows takes cost_few ns of the whole device per tile of 16
+//     rows and chunk of 64 keys, the tile kernel cost_tile ns per tile and 32 keys
+//     (256 rows, 128 for 256 channels), and 20 us more for its longer start and
+//     end: 16 sequences of 128 rows over 4096 keys (8 KV heads, 128 channels) take
+//     74 us with the one and 91 us with the other, of 256 rows 137 and 99 us.
+//   * Few rows: parts only where there are fewer workgroups than compute units,
+//     then as many as those; each is eight waves with long runs of keys (four
+//     contexts of 131072 tokens take 175 us with 256 workgroups, 187 us with 768),
+//     and not for fewer than 24 chunks (a single token over 1024 keys takes 10 us
+//     in one part; two add 3 us of joining). With more workgroups than compute
+//     units four waves each, without parts (256 ragged requests: 87 us, 95 us with
+//     parts of 2048 keys).
+//   * Tiles: two rounds of workgroups of unequal length, parts of 512 keys at
+//     least (a prompt of 512 rows over 2048 keys takes 34 us, 72 us without).
 KvSplit kv_attend_split(int dim, int64_t n, int64_t tokens, int heads, int kv_heads,
                         int64_t max_new, int64_t max_len) {
   KvSplit s = {};
   const int group = heads / kv_heads;
-  s.tiled = max_new * group > 2 * kRows;
-  const int rows = s.tiled ? (dim == 256 ? tile_rows<256>() : tile_rows<128>()) : kRows;
-  const int64_t tiles = tokens == n ? n * ((group + rows - 1) / rows) : tokens * group / rows + n;
-  const int64_t groups = std::max<int64_t>(tiles * kv_heads, 1);
   const int64_t chunks = std::max<int64_t>((max_len + kChunk - 1) / kChunk, 1);
-  int64_t want = s.tiled ? 512 : 256;
-  int64_t least = 32;  // chunks of a part
+  // row tiles of the grid, and what there are of them if max_new holds
+  auto grid_of = [&](int64_t rows) { return tokens * group / rows + n; };
+  auto tiles_of = [&](int64_t rows) {
+    return std::min(grid_of(rows), n * ((max_new * group + rows - 1) / rows));
+  };
+  const int tile = dim == 256 ? tile_rows<256>() : tile_rows<128>();
+  const double cost_few = dim == 64 ? 0.7 : dim == 128 ? 1.0 : 2.8;
+  const double cost_tile = dim == 64 ? 3.7 : dim == 128 ? 4.6 : 5.4;
+  const double each = (double)kv_heads * (double)chunks;
+  s.tiled = cost_tile * 2 * each * (double)tiles_of(tile) + 20e3 <
+            cost_few * each * (double)tiles_of(kRows);
+  const int64_t groups = std::max<int64_t>(tiles_of(s.tiled ? tile : kRows) * kv_heads, 1);
+  int64_t want = 512, least = 8;  // workgroups, chunks of a part
   if (!s.tiled) {
     s.waves = groups < 256 && dim <= 128 ? 8 : 4;
     least = 2 * s.waves;
-    if (chunks <= 3 * s.waves) want = 1;
-    // (their counters lie in the workspace's first bytes)
-    static_assert(256 / 2 <= kKvCounts, "a counter for every tile with parts");
+    // (a tile with parts needs a counter)
+    want = chunks <= 3 * s.waves || grid_of(kRows) * kv_heads > kKvCounts ? 1 : 256;
   }
   const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(want / groups, kMostParts));
   s.part_chunks = (int)std::max<int64_t>(least, (chunks + parts - 1) / parts);
