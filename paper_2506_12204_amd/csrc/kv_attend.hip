@@ -14,6 +14,7 @@
 // largest vs seen, 2^14 above, so that weights down to 2^-28 of the largest
 // keep 11 bits.
 #include <algorithm>
+#include <cstdlib>
 
 #include "device_common.h"
 #include "kv.h"
@@ -1030,6 +1031,10 @@ KvSplit kv_attend_split(int dim, int64_t n, int64_t tokens, int heads, int kv_he
   const double each = (double)kv_heads * (double)chunks;
   s.tiled = cost_tile * 2 * each * (double)tiles_of(tile) + 20e3 <
             cost_few * each * (double)tiles_of(kRows);
+  // SEMSCHED_KV_TILES=0 or 1 takes one kernel for all sizes, so that both stay
+  // testable on small ones.
+  const char* forced = std::getenv("SEMSCHED_KV_TILES");
+  if (forced && (forced[0] == '0' || forced[0] == '1')) s.tiled = forced[0] == '1';
   const int64_t groups = std::max<int64_t>(tiles_of(s.tiled ? tile : kRows) * kv_heads, 1);
   int64_t want = 512, least = 8;  // workgroups, chunks of a part
   if (!s.tiled) {

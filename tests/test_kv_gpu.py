@@ -29,6 +29,13 @@ def ss():
     return mod
 
 
+@pytest.fixture(params=["few", "tile"])
+def kernel(request, monkeypatch):
+    """Attention's two kernels, each at sizes that the other is chosen for."""
+    monkeypatch.setenv("SEMSCHED_KV_TILES", "1" if request.param == "tile" else "0")
+    return request.param
+
+
 def i32(x):
     import torch
     return torch.tensor(np.asarray(x, dtype=np.int32), device="cuda")
@@ -159,7 +166,7 @@ DIMS = [(64, 16), (64, 64), (128, 16), (128, 32), (128, 64), (128, 256), (256, 6
 @pytest.mark.parametrize("dim,pt", DIMS)
 @pytest.mark.parametrize("fmt", [ko.INT8, ko.FP8])
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
-def test_single_tokens(ss, dim, pt, fmt, dtype):
+def test_single_tokens(ss, dim, pt, fmt, dtype, kernel):
     # one key, tile and chunk borders, a page that ends inside a chunk, an idle slot
     lens = [1, 15, 16, 17, 63, 64, 65, 0, 200, 129]
     print("decode", dim, pt, fmt, dtype, flush=True)
@@ -169,7 +176,7 @@ def test_single_tokens(ss, dim, pt, fmt, dtype):
 
 @pytest.mark.parametrize("heads,kv_heads", [(1, 1), (3, 1), (16, 1), (17, 1), (40, 1), (6, 3),
                                             (5, 5)])
-def test_head_groups(ss, heads, kv_heads):
+def test_head_groups(ss, heads, kv_heads, kernel):
     print("groups", heads, kv_heads, flush=True)
     run_attend(ss, [70, 5, 130], [1, 1, 1], heads=heads, kv_heads=kv_heads, fmt=ko.FP8)
     run_attend(ss, [70, 5, 130], [9, 5, 33], heads=heads, kv_heads=kv_heads, dtype="f16")
@@ -177,7 +184,7 @@ def test_head_groups(ss, heads, kv_heads):
 
 @pytest.mark.parametrize("split", [0, 1, 4000])
 @pytest.mark.parametrize("fmt", [ko.INT8, ko.FP8])
-def test_long_contexts(ss, split, fmt):
+def test_long_contexts(ss, split, fmt, kernel):
     # few rows: the key axis is split, by a bound that may be wrong either way
     print("long", split, fmt, flush=True)
     run_attend(ss, [3001, 17, 4000, 0], [1] * 4, heads=2, kv_heads=1, fmt=fmt, max_len=split,
@@ -188,7 +195,7 @@ def test_long_contexts(ss, split, fmt):
 @pytest.mark.parametrize("causal,window", [(True, 0), (True, 1), (True, 50), (False, 0),
                                            (False, 40)])
 @pytest.mark.parametrize("fmt,dtype", [(ko.INT8, "bf16"), (ko.FP8, "f16")])
-def test_several_tokens(ss, dim, pt, causal, window, fmt, dtype):
+def test_several_tokens(ss, dim, pt, causal, window, fmt, dtype, kernel):
     # whole prompts, chunks on a context, drafts, a sequence without queries
     lens, new = [100, 300, 65, 40, 1, 333], [100, 70, 3, 0, 1, 129]
     print("several", dim, pt, causal, window, fmt, flush=True)
@@ -197,7 +204,7 @@ def test_several_tokens(ss, dim, pt, causal, window, fmt, dtype):
 
 
 @pytest.mark.parametrize("causal", [True, False])
-def test_more_queries_than_keys(ss, causal):
+def test_more_queries_than_keys(ss, causal, kernel):
     # rows before the first key see nothing: zeros, and a sum of minus infinity
     print("empty rows", causal, flush=True)
     run_attend(ss, [3, 0, 70], [20, 4, 200], heads=3, kv_heads=1, causal=causal, fmt=ko.FP8)
@@ -205,13 +212,13 @@ def test_more_queries_than_keys(ss, causal):
 
 @pytest.mark.parametrize("fmt", [ko.INT8, ko.FP8])
 @pytest.mark.parametrize("new", [1, 40])
-def test_bytes_beyond_the_length_do_not_count(ss, fmt, new):
+def test_bytes_beyond_the_length_do_not_count(ss, fmt, new, kernel):
     print("dirty", fmt, new, flush=True)
     lens = [41, 100, 64, 77]
     run_attend(ss, lens, [new] * 4, heads=4, kv_heads=2, fmt=fmt, dirty=True, pt=32)
 
 
-def test_magnitudes_and_strides(ss):
+def test_magnitudes_and_strides(ss, kernel):
     print("magnitudes", flush=True)
     run_attend(ss, [90, 33], [2, 30], heads=4, kv_heads=2, big=True)
     # rows that are not 16-byte aligned, an output with a stride
@@ -221,7 +228,7 @@ def test_magnitudes_and_strides(ss):
     run_attend(ss, [90, 33], [1, 9], heads=4, kv_heads=2, scale=-0.3)
 
 
-def test_scales_of_very_different_pages(ss):
+def test_scales_of_very_different_pages(ss, kernel):
     """Weights are rounded relative to the largest V scale, zero scales included."""
     import torch
     print("page scales", flush=True)
@@ -241,7 +248,7 @@ def test_scales_of_very_different_pages(ss):
     assert (case.c.attend(1, q, i32([0, 1]), i32([0, new, 2 * new])) == 0).all()
 
 
-def test_nan_and_infinity_of_a_query_stay_in_its_row(ss):
+def test_nan_and_infinity_of_a_query_stay_in_its_row(ss, kernel):
     import torch
     print("nan rows", flush=True)
     case = Case(ss, [130], fmt=ko.FP8, dim=64, pt=32, kv_heads=1)
@@ -281,6 +288,93 @@ def test_page_offsets_beyond_32_bits(ss):
         want, _, mag = ko.attend(q[:, h].double().cpu().numpy(), k[:, h], v[:, h], 1 / 16, True, 0)
         # int8 keys and values: half a step of 1/127 of the largest each
         assert np.abs(again[0, h].double().cpu().numpy() - want).max() < 0.1
+
+
+@pytest.mark.parametrize("dim,heads,kv_heads", [(64, 6, 2), (128, 5, 1), (256, 4, 4)])
+@pytest.mark.parametrize("max_len,max_new", [(0, 0), (1, 1), (100000, 3)])
+def test_parts_of_longer_contexts(ss, kernel, dim, heads, kv_heads, max_len, max_new):
+    """Ragged chunks over contexts that are split into parts, by bounds that hold
+    or do not; a sum of each row."""
+    print("parts", kernel, dim, max_len, max_new, flush=True)
+    run_attend(ss, [2500, 700, 0, 4100, 1300], [37, 3, 0, 1, 80], heads=heads, kv_heads=kv_heads,
+               dim=dim, pt=128, fmt=ko.FP8, dtype="f16", max_len=max_len, max_new=max_new, seed=11)
+
+
+def test_many_sequences(ss, kernel):
+    """More sequences than a wave counts at a time, some without queries."""
+    print("many sequences", kernel, flush=True)
+    rng = np.random.default_rng(12)
+    lens = rng.integers(0, 60, 150).tolist()
+    new = [int(rng.integers(0, n + 1)) if rng.random() < 0.7 else 0 for n in lens]
+    run_attend(ss, lens, new, heads=2, kv_heads=1, dim=64, pt=16, fmt=ko.INT8, seed=12)
+    # one token each, through offsets and without
+    lens = rng.integers(1, 90, 200).tolist()
+    for with_cu in (True, False):
+        run_attend(ss, lens, [1] * 200, heads=2, kv_heads=2, dim=64, pt=16, fmt=ko.FP8,
+                   with_cu=with_cu, max_new=1, seed=13)
+
+
+def test_all_queries_hidden(ss, kernel):
+    """A call in which no row sees a key."""
+    import torch
+    print("hidden", kernel, flush=True)
+    case, q, out = run_attend(ss, [0, 0], [3, 40], heads=4, kv_heads=2)
+    assert (out == 0).all() and not torch.signbit(out).any()
+
+
+def test_rows_of_equal_scores_are_means(ss, kernel):
+    """Zero keys (blocks of scale zero): every visible value has the same weight."""
+    import torch
+    print("means", kernel, flush=True)
+    case = Case(ss, [500, 33], fmt=ko.INT8, dim=64, pt=16, kv_heads=1, seed=4)
+    case.scale[:, :, 0] = 0
+    case.c.scale.copy_(torch.from_numpy(case.scale))
+    q = case.queries([60, 33], 2, torch.float16)
+    lse = torch.empty(93, 2, device="cuda")
+    out = case.c.attend(1, q, i32([0, 1]), i32([0, 60, 93]), lse=lse)
+    case.c.check()
+    case.check(q, [60, 33], out, lse, 0.125, True, 0)
+
+
+def test_scores_that_rise_along_the_keys(ss, kernel):
+    """The running maximum is raised again and again; late keys dominate."""
+    import torch
+    print("rising", kernel, flush=True)
+    for sign in (1, -1):
+        case = Case(ss, [400], fmt=ko.INT8, dim=64, pt=64, kv_heads=1, seed=5)
+        data = np.zeros_like(case.data)
+        for b in range(7):
+            page = case.tables[0, b]
+            block = data[page].reshape(2, 2, 1, 64 * 64)
+            k = np.zeros((64, 64), np.int8)
+            k[:, 0] = np.clip(sign * (np.arange(b * 64, b * 64 + 64) - 200) // 2, -127, 127)
+            block[1, 0, 0][ko.block_index(0, 64, 64)] = k.view(np.uint8)
+            block[1, 1] = case.data[page].reshape(2, 2, 1, 64 * 64)[1, 1]
+        case.data = data
+        case.scale[:, :, 0] = 1.0
+        case.c.data.copy_(torch.from_numpy(data))
+        case.c.scale.copy_(torch.from_numpy(case.scale))
+        q = torch.zeros(70, 1, 64, dtype=torch.bfloat16, device="cuda")
+        q[:, 0, 0] = 1.0
+        lse = torch.empty(70, 1, device="cuda")
+        out = case.c.attend(1, q, i32([0]), i32([0, 70]), scale=1.0, lse=lse)
+        case.c.check()
+        case.check(q, [70], out, lse, 1.0, True, 0)
+
+
+def test_an_output_may_be_a_slice(ss, kernel):
+    """Rows of the output that lie apart, 16-byte aligned and not."""
+    import torch
+    print("slices", kernel, flush=True)
+    case = Case(ss, [90, 33], fmt=ko.FP8, dim=128, pt=32, kv_heads=2, seed=6)
+    q = case.queries([40, 33], 4, torch.bfloat16)
+    ref = case.c.attend(1, q, i32([0, 1]), i32([0, 40, 73])).clone()
+    for pad in (8, 2, 1):
+        wide = torch.zeros(73, 4 * 128 + pad, dtype=torch.bfloat16, device="cuda")
+        out = wide[:, pad:].view(73, 4, 128)
+        case.c.attend(1, q, i32([0, 1]), i32([0, 40, 73]), out=out)
+        case.c.check()
+        assert torch.equal(out, ref) and (wide[:, :pad] == 0).all()
 
 
 @pytest.mark.parametrize("dim,pt,kv_heads", [(64, 16, 1), (128, 64, 2), (256, 32, 3),
@@ -651,7 +745,7 @@ def test_blocking_forms(ss):
     assert L.sem_kv_compact(ref) == 0  # the status does not outlive its call
 
 
-def test_results_do_not_depend_on_the_run(ss):
+def test_results_do_not_depend_on_the_run(ss, kernel):
     import torch
     print("repeat", flush=True)
     case = Case(ss, [700, 300, 5], fmt=ko.FP8, dim=128, pt=64, kv_heads=2)
