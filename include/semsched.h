@@ -467,7 +467,7 @@ int sem_schedule_static(const uint8_t *priority, const int32_t *length, int64_t 
  * pointers, sizes or strides out of range, a workspace too small, and,
  * detected on the device, sequences, lengths, offsets or page numbers outside
  * the cache (no memory outside the arguments is accessed); SEM_ERANGE for a
- * negative token count.
+ * negative token count. Scales are not negative.
  */
 #define SEM_KV_ZEROED_BYTES 4352
 #define SEM_KV_INT8 0
@@ -551,7 +551,8 @@ int sem_kv_compact_async(const sem_kv_cache *cache, void *workspace, size_t ws_b
  * a * (1 / top)), a the largest finite magnitude of its new elements, top 127
  * or 448; if s' > s its older codes become round(c * s / s'); new codes are
  * round(x / s'), ties to even, in 32-bit arithmetic. Infinities are stored as
- * the largest code, NaN as 0, and either is reported as SEM_ERANGE.
+ * the largest code (those of half precision as 65504, where the scale reaches
+ * further), NaN as 0, and either is reported as SEM_ERANGE.
  */
 int sem_kv_append(const sem_kv_cache *cache, int32_t layer, const void *k, const void *v,
                   int32_t dtype, int64_t k_token_stride, int64_t k_head_stride,
@@ -570,7 +571,10 @@ int sem_kv_append_async(const sem_kv_cache *cache, int32_t layer, const void *k,
  * in groups of heads / kv_heads consecutive ones. With causal set a query sees
  * the keys up to its own position, else all of the sequence's; with window
  * w > 0 only those less than w before it, too. A row that sees no key (an
- * empty sequence) gives zeros and lse -infinity.
+ * empty sequence) gives zeros and lse -infinity. Products are of half-precision
+ * operands with 32-bit sums: codes and queries are exact, the weights have 11
+ * bits, but no finer than 2^-31 of the largest weight and value scale that the
+ * workgroup has met.
  *   out [tokens][heads][head_dim] of the queries' type; lse [tokens][heads]
  *   float: the logarithm of the sum of exp(score), NULL if not wanted.
  *   max_new, max_len: bounds that the caller knows on the queries and the

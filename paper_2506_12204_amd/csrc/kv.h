@@ -10,6 +10,7 @@
 namespace semsched {
 
 constexpr int kKvCounts = 1024;      // counters of attention's tiles with several parts
+constexpr int kKvPieces = 256;       // of attention's work, where it is cut into equal ones
 constexpr int kKvTile = 16;          // tokens per tile of a page's block
 
 // The cache as the kernels see it: the caller's arrays and the derived sizes.
@@ -67,6 +68,13 @@ struct KvAppendArgs {
   int32_t wide;  // 16-byte loads are aligned
 };
 
+// A row tile whose keys went to several of attention's pieces.
+struct KvCut {
+  int32_t parts, piece;  // how many (0: none), the first of them
+  int32_t row0, rows;    // the sequence's first query token, rows of a KV head
+  int32_t tile, head;    // its number in the sequence, the KV head
+};
+
 struct KvAttendArgs {
   KvView c;
   const uint16_t* q;
@@ -80,12 +88,15 @@ struct KvAttendArgs {
   int32_t causal, window;
   float scale_log2;  // softmax scale * log2(e)
   int32_t tiled;       // the kernel for many rows per sequence
+  int32_t whole;       // a tile per workgroup of it, else a piece of all tiles' keys
   int32_t waves;       // of the other kernel's workgroups, 4 or 8
   int32_t parts;       // most parts that the keys of a row tile are split into,
   int32_t part_chunks; // of so many chunks of 64 keys each
   uint32_t* counts;    // [kKvCounts] parts finished, zero between calls
-  float* part_o;       // [parts][tokens * heads][head_dim]
-  float* part_ml;      // [parts][tokens * heads][2]: maximum (log2), sum
+  // partial outputs, [parts][tokens * heads] rows or, tiled, two tiles per piece
+  float* part_o;   // [rows][head_dim]
+  float* part_ml;  // [rows][2]: maximum (log2), sum
+  KvCut* cuts;     // [kKvPieces], of the tile that a piece ends with
 };
 
 hipError_t launch_kv_fork(const KvForkArgs& a, hipStream_t st);
@@ -98,7 +109,8 @@ hipError_t launch_kv_attend(const KvAttendArgs& a, hipStream_t st);
 // How an attention call of these sizes is split (its workspace holds the
 // parts' partial outputs).
 struct KvSplit {
-  int tiled, waves, parts, part_chunks;
+  int tiled, whole, waves, parts, part_chunks;
+  int64_t part_rows;  // of partial outputs
 };
 KvSplit kv_attend_split(int dim, int64_t n, int64_t tokens, int heads, int kv_heads,
                         int64_t max_new, int64_t max_len);

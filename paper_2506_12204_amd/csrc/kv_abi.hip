@@ -161,7 +161,7 @@ int check_append(const sem_kv_cache* c, int32_t layer, const void* k, const void
 
 struct AttendPlan {
   KvSplit split = {};
-  size_t part_o = 0, part_ml = 0, total = kZeroed;
+  size_t part_o = 0, part_ml = 0, cuts = 0, total = kZeroed;
 };
 
 AttendPlan attend_plan(const sem_kv_cache* c, int32_t heads, int64_t n, int64_t tokens,
@@ -171,11 +171,12 @@ AttendPlan attend_plan(const sem_kv_cache* c, int32_t heads, int64_t n, int64_t 
                               (int64_t)c->max_blocks * c->page_tokens);
   max_new = std::min<int64_t>(max_new > 0 ? max_new : tokens, std::max<int64_t>(tokens, 1));
   p.split = kv_attend_split(c->head_dim, n, tokens, heads, c->kv_heads, max_new, max_len);
-  if (p.split.parts > 1) {
-    const size_t rows = (size_t)p.split.parts * (size_t)tokens * (size_t)heads;
+  if (p.split.part_rows > 0) {
+    const size_t rows = (size_t)p.split.part_rows;
     p.part_o = kZeroed;
     p.part_ml = align_up(p.part_o + 4 * rows * (size_t)c->head_dim);
-    p.total = align_up(p.part_ml + 8 * rows);
+    p.cuts = align_up(p.part_ml + 8 * rows);
+    p.total = align_up(p.cuts + (p.split.tiled ? kKvPieces * sizeof(KvCut) : 0));
   }
   return p;
 }
@@ -381,12 +382,14 @@ int sem_kv_attend_async(const sem_kv_cache* cache, int32_t layer, const sem_kv_q
   a.window = query->window;
   a.scale_log2 = query->scale * 1.4426950408889634f;
   a.tiled = p.split.tiled;
+  a.whole = p.split.whole;
   a.waves = p.split.waves;
   a.parts = p.split.parts;
   a.part_chunks = p.split.part_chunks;
   a.counts = reinterpret_cast<uint32_t*>(base + kHeaderBytes);
   a.part_o = reinterpret_cast<float*>(base + p.part_o);
   a.part_ml = reinterpret_cast<float*>(base + p.part_ml);
+  a.cuts = reinterpret_cast<KvCut*>(base + p.cuts);
   return status_of(launch_kv_attend(a, static_cast<hipStream_t>(stream)));
 }
 

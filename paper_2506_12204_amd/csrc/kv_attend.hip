@@ -11,8 +11,10 @@
 // there, and so are the queries (a bf16 row is first multiplied by a power of
 // two that brings its largest element to 2^14, which is undone in the scale).
 // The weights exp(x - m) vs are rounded to half precision relative to the
-// largest vs seen, 2^14 above, so that weights down to 2^-28 of the largest
-// keep 11 bits.
+// largest vs seen, 2^6 above, so that weights down to 2^-20 of the largest keep
+// 11 bits and smaller ones lose at most 2^-31 of it; a V block whose scale is
+// below 2^-30 of the largest seen counts as if it were that large. Sums, maxima
+// and outputs are in 32 bits.
 #include <algorithm>
 #include <cstdlib>
 
@@ -43,34 +45,26 @@ struct Sequence {
 };
 
 // The sequence of row tile u (all but its keys) and the tile's number in it;
-// false if there is no such tile. Tiles are numbered sequence by sequence, LATE ones (whose causal
-// rows see most keys) first where that is asked for. The grid's size is a bound,
-// and its workgroups without work have to be the last or first ones: the device
-// deals workgroups to its parts in turn, and idle ones at regular places would
-// leave the same parts without work. So every wave counts the tiles of all
-// sequences, 64 at a time (n / 64 rounds of independent loads, where a search
-// would take log n dependent ones).
-template <bool LATE>
+// false if there is no such tile. Tiles are numbered sequence by sequence. The
+// grid's size is a bound, and its workgroups without work have to be the last
+// ones: the device deals workgroups to its parts in turn, and idle ones at
+// regular places would leave the same parts without work. So every wave counts
+// the tiles of all sequences, 64 at a time (n / 64 rounds of independent loads,
+// where a search would take log n dependent ones).
 __device__ __forceinline__ bool find_tile(const KvAttendArgs& a, uint32_t u, int rows, Sequence& q,
                                           int& tile) {
   const KvView& c = a.c;
   int64_t i = -1;
   if (a.cu) {
     const int lane = lane_id();
-    auto count = [&](int64_t at) __attribute__((always_inline)) -> uint32_t {
-      if (at >= a.n) return 0;
-      const int64_t fresh = (int64_t)a.cu[at + 1] - a.cu[at];
-      return fresh > 0 && fresh <= a.tokens ? (uint32_t)((fresh * a.group + rows - 1) / rows) : 0u;
-    };
-    uint32_t total = 0;
-    if (LATE) {
-      for (int64_t at = 0; at < a.n; at += kWave) total += wave_add_u32(count(at + lane));
-      if (u >= total) return false;
-      u = total - 1 - u;
-    }
     uint32_t before = 0;
     for (int64_t at = 0; at < a.n; at += kWave) {
-      const uint32_t mine = count(at + lane), upto = before + wave_incl_scan_u32(mine);
+      uint32_t mine = 0;
+      if (at + lane < a.n) {
+        const int64_t fresh = (int64_t)a.cu[at + lane + 1] - a.cu[at + lane];
+        if (fresh > 0 && fresh <= a.tokens) mine = (uint32_t)((fresh * a.group + rows - 1) / rows);
+      }
+      const uint32_t upto = before + wave_incl_scan_u32(mine);
       const uint64_t beyond = __ballot(upto > u);
       if (beyond) {
         const int first = __ffsll((unsigned long long)beyond) - 1;
@@ -296,6 +290,12 @@ __device__ __forceinline__ void join_row(const KvAttendArgs& a, int64_t token, i
 // lane's 16-byte load is 16 channels of a key or 16 keys of a channel, and no
 // LDS is used before the join. A lane's 16 keys lie in one page, so the scales
 // are one number each per lane and chunk.
+//
+// Bound by reading the cache where contexts are long: four of 100001 to 131072
+// tokens (64 heads, 8 KV heads, 128 channels) take 170 us, 5.6 TB/s; 251 ragged
+// requests of 16 to 4096 tokens 86 us, 4.4 TB/s. A single token over 777 keys
+// takes 10 us, most of it the launch and the chain of loads before the first
+// product (the sequence, its length, its table, the page).
 template <int D, int FMT, int NW>
 __global__ __launch_bounds__(NW* kWave) void kv_attend_rows(KvAttendArgs a) {
   constexpr int PITCH = D + 4;
@@ -311,7 +311,7 @@ __global__ __launch_bounds__(NW* kWave) void kv_attend_rows(KvAttendArgs a) {
   const int kh = blockIdx.x % c.kv_heads;
   Sequence q;
   int tile;
-  if (!find_tile<false>(a, blockIdx.x / c.kv_heads, kRows, q, tile)) return;
+  if (!find_tile(a, blockIdx.x / c.kv_heads, kRows, q, tile)) return;
   const int rows = q.fresh * a.group;
   const uint32_t row = (uint32_t)min(tile * kRows + r, rows - 1);
   const bool live = tile * kRows + r < rows;
@@ -543,9 +543,214 @@ __global__ __launch_bounds__(NW* kWave) void kv_attend_rows(KvAttendArgs a) {
 // Three steps overlap, so that the matrix cores are fed while the vector units
 // turn scores into weights: step j takes the scores of keys j + 1, the weights
 // of keys j and the outputs of keys j - 1, which do not depend on each other.
-// Codes are loaded four steps ahead and put into LDS two steps ahead.
+// Codes are loaded four steps ahead and put into LDS two steps ahead. (Six or
+// eight steps ahead measured the same.)
+//
+// Bound by the matrix and vector instructions of a step together: 32 matrix
+// instructions of 16 passes and 400 vector ones per wave and 32 keys (128
+// channels). A prompt of 16384 tokens, 32 heads of 128 channels, takes 2.40 ms,
+// 918 TFLOP/s, where a large matrix product reaches 1300; before the steps
+// overlapped it took 6.07 ms.
 constexpr int kWide = 32;  // rows of a matrix tile, and keys of a step
 typedef float float16_t __attribute__((ext_vector_type(16)));
+
+// How the tiles are shared out. All of a call's work is laid out as one line: a
+// KV head's tiles after the other's, sequence by sequence, each as long as the
+// keys that it takes plus kTileCost for its start and end. The line is cut into
+// equal pieces, one per workgroup (one of which fills a compute unit), wherever
+// the cuts fall; tiles that are cut are joined afterwards. So no compute unit
+// waits for another, whatever the sequences' lengths, and at most two partial
+// tiles per workgroup are written. Chunks of 300 to 512 queries of four sequences
+// of 2048 to 8192 keys (32 heads, 8 KV heads, 128 channels) take 127 us, of which
+// the join 15; parts of equal length dealt out in turn took 160 us, as long as
+// the longest of them.
+// Whole tiles are dealt in turn instead where that costs less by the lines'
+// lengths, as for equal sequences whose tiles go into the compute units without
+// rest: 2048 rows each of four sequences over 4096 keys take 158 us, 195 us cut.
+// Where there are tiles for six rounds (kWholeRounds) each has a workgroup of its
+// own, which the device places as compute units become free: 64 such sequences
+// take 2.49 ms, dealt in turn 2.60 ms, cut 2.66 ms; ragged ones (64 to 448
+// queries, 512 to 8192 keys, about eight rounds) 1.03 ms in either way, and of
+// four rounds 0.50 ms whole and 0.40 ms cut.
+constexpr int kPieces = kKvPieces;
+constexpr int kTileCost = 256;    // in keys; 256 to 448 measure alike
+constexpr int kLeastPiece = 512;  // pieces are not cut shorter than this
+constexpr int kCutCost = 640;     // of the cuts and the join, as keys of every piece
+constexpr int kWholeRounds = 6;
+
+// A sequence's share of the line: tile t is first + rise * (t + 1) long.
+struct Share {
+  uint64_t first;
+  uint32_t tiles, rise;
+  int32_t row0, fresh, slot, len;  // the sequence's first query, queries, place, keys
+  __device__ __forceinline__ uint64_t before(uint32_t t) const {
+    return t * first + (uint64_t)rise * ((uint64_t)t * (t + 1) / 2);
+  }
+  __device__ __forceinline__ uint64_t of(uint32_t t) const {
+    return first + (uint64_t)rise * (t + 1);
+  }
+};
+
+template <int ROWS>
+__device__ __forceinline__ Share share_of(const KvAttendArgs& a, int64_t i) {
+  const KvView& c = a.c;
+  Share s = {1, 0, 0, 0, 0, 0, 0};
+  if (i >= a.n) return s;
+  const int64_t row0 = a.cu ? a.cu[i] : i;
+  const int64_t fresh = a.cu ? (int64_t)a.cu[i + 1] - row0 : 1;
+  const int32_t slot = a.seqs[i];
+  const bool known = (uint32_t)slot < (uint32_t)c.slots;
+  int64_t len = known ? c.lens[slot] : -1;
+  s.row0 = (int)row0;
+  s.fresh = (int)fresh;
+  s.slot = known ? slot : 0;
+  bool wrong = fresh < 0 || row0 < 0 || row0 + fresh > a.tokens;
+  if (!wrong) s.tiles = (uint32_t)((fresh * a.group + ROWS - 1) / ROWS);
+  if (len < 0 || len > ((int64_t)c.max_blocks << c.page_shift)) {
+    wrong |= s.tiles > 0;
+    len = 0;
+  }
+  s.len = (int)len;
+  if (wrong && blockIdx.x == 0) atomicOr(c.flags, kFlagInval);
+  const uint32_t group = min((uint32_t)a.group, (uint32_t)ROWS);
+  if (a.causal && a.window == 0) {
+    len = max(len - fresh, (int64_t)0);
+    s.rise = ROWS;
+  } else if (a.window > 0) {
+    len = min(len, (int64_t)a.window + ROWS / (int)group);
+  }
+  s.first = group * (uint64_t)(len + kTileCost);
+  return s;
+}
+
+__device__ __forceinline__ uint64_t lane_u64(uint64_t v, int lane) {
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane) |
+         (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32;
+}
+
+__device__ __forceinline__ Share lane_share(const Share& s, int lane) {
+  auto get = [&](uint32_t v) { return __builtin_amdgcn_readlane((int)v, lane); };
+  return {lane_u64(s.first, lane), (uint32_t)get(s.tiles), (uint32_t)get(s.rise), get(s.row0),
+          get(s.fresh), get(s.slot), get(s.len)};
+}
+
+// A place on the line: the tile there, and where it starts.
+struct Place {
+  uint64_t start;
+  Share share;
+  int head, index;
+  uint32_t tile;
+};
+
+template <int ROWS>
+struct Line {
+  uint64_t each = 0;  // length of a KV head's part
+  uint64_t size, rest;  // of a piece; so many are one longer
+  uint32_t tiles = 0;   // of a KV head
+  uint32_t pieces;
+  bool dealt;           // whole tiles are
+  Share mine;  // of the lane's sequence among the first 64
+
+  __device__ __forceinline__ bool measure(const KvAttendArgs& a) {
+    const int lane = lane_id();
+    const uint32_t group = (uint32_t)min(a.group, ROWS);
+    uint32_t longest = 0;  // tile, in keys
+    mine = share_of<ROWS>(a, lane);
+    for (int64_t at = 0; at < a.n; at += kWave) {
+      const Share s = at == 0 ? mine : share_of<ROWS>(a, at + lane);
+      each += last_lane_u64(wave_incl_scan_u64(s.before(s.tiles)));
+      tiles += wave_add_u32(s.tiles);
+      longest = max(longest, s.tiles ? (uint32_t)(s.of(s.tiles - 1) / group) : 0u);
+    }
+    longest = wave_max_u32(longest);
+    if (tiles == 0) return false;
+    const uint64_t total = each * a.c.kv_heads;
+    const uint64_t whole = (uint64_t)tiles * a.c.kv_heads, keys = total / group;
+    dealt = a.whole || (whole + kPieces - 1) / kPieces * longest < keys / kPieces + kCutCost;
+    pieces = (uint32_t)min(max(whole, keys / kLeastPiece), (uint64_t)kPieces);
+    size = total / pieces;
+    rest = total - size * pieces;
+    return true;
+  }
+  __device__ __forceinline__ uint64_t cut(uint32_t g) const {
+    return size * g + min((uint64_t)g, rest);
+  }
+  __device__ __forceinline__ uint32_t piece_of(uint64_t x) const {
+    const uint64_t longer = rest * (size + 1);
+    return (uint32_t)(x < longer ? x / (size + 1) : rest + (x - longer) / size);
+  }
+  __device__ __forceinline__ bool find(const KvAttendArgs& a, uint64_t x, Place& p) const {
+    const int lane = lane_id();
+    p.head = (int)(x / each);
+    uint64_t start = p.head * each;
+    for (int64_t at = 0; at < a.n; at += kWave) {
+      const Share s = at == 0 ? mine : share_of<ROWS>(a, at + lane);
+      const uint64_t own = s.before(s.tiles), upto = start + wave_incl_scan_u64(own);
+      const uint64_t beyond = __ballot(upto > x);
+      if (beyond) {
+        const int at_lane = __ffsll((unsigned long long)beyond) - 1;
+        p.index = (int)at + at_lane;
+        p.share = lane_share(s, at_lane);
+        start = lane_u64(upto - own, at_lane);
+        uint32_t low = 0, high = p.share.tiles;  // before(low) <= x - start
+        while (high - low > 1) {
+          const uint32_t mid = (low + high) / 2;
+          if (p.share.before(mid) <= x - start) low = mid;
+          else high = mid;
+        }
+        p.tile = low;
+        p.start = start + p.share.before(low);
+        return true;
+      }
+      start = last_lane_u64(upto);
+    }
+    return false;
+  }
+  // Tile u of all, KV heads side by side and the line's last tiles first (the
+  // later a causal tile, the more keys its rows see).
+  __device__ __forceinline__ bool deal(const KvAttendArgs& a, uint64_t u, Place& p) const {
+    p.head = (int)(u % (uint32_t)a.c.kv_heads);
+    u /= (uint32_t)a.c.kv_heads;
+    if (u >= tiles) return false;
+    u = tiles - 1 - u;
+    const int lane = lane_id();
+    uint32_t before = 0;
+    for (int64_t at = 0; at < a.n; at += kWave) {
+      const Share s = at == 0 ? mine : share_of<ROWS>(a, at + lane);
+      const uint32_t upto = before + wave_incl_scan_u32(s.tiles);
+      const uint64_t beyond = __ballot(upto > u);
+      if (beyond) {
+        const int at_lane = __ffsll((unsigned long long)beyond) - 1;
+        p.index = (int)at + at_lane;
+        p.share = lane_share(s, at_lane);
+        p.tile = (uint32_t)u - (uint32_t)__builtin_amdgcn_readlane((int)(upto - s.tiles), at_lane);
+        p.start = 0;
+        return true;
+      }
+      before = (uint32_t)__builtin_amdgcn_readlane((int)upto, kWave - 1);
+    }
+    return false;
+  }
+  // The next tile of the line; false behind its end.
+  __device__ __forceinline__ bool next(const KvAttendArgs& a, Place& p) const {
+    p.start += p.share.of(p.tile);
+    if (++p.tile < p.share.tiles) return true;
+    p.tile = 0;
+    do {
+      if (++p.index >= (int)a.n) {
+        p.index = 0;
+        if (++p.head >= a.c.kv_heads) return false;
+      }
+      p.share = lane_share(share_of<ROWS>(a, p.index), 0);
+    } while (p.share.tiles == 0);
+    return true;
+  }
+};
+
+__device__ __forceinline__ Sequence sequence_of(const KvAttendArgs& a, const Place& p) {
+  return {a.c.tables + (int64_t)p.share.slot * a.c.max_blocks, p.share.row0, p.index,
+          p.share.fresh, p.share.len};
+}
 
 template <int D, int FMT, int NW>
 __global__ __launch_bounds__(NW* kWave, NW / 4) void kv_attend_tile(KvAttendArgs a) {
@@ -570,395 +775,434 @@ __global__ __launch_bounds__(NW* kWave, NW / 4) void kv_attend_tile(KvAttendArgs
   const KvView& c = a.c;
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int r = lane % kWide, h = lane / kWide;
-  const int kh = blockIdx.x % c.kv_heads;
-  Sequence q;
-  int tile;
-  if (!find_tile<true>(a, blockIdx.x / c.kv_heads, ROWS, q, tile)) return;
-  const int rows = q.fresh * a.group;
-  const int row0 = tile * ROWS + wave * kWide;
-  const uint32_t row = (uint32_t)min(row0 + r, rows - 1);
-  const bool live = row0 + r < rows;
-  const int token = (int)(row / (uint32_t)a.group);
-  const int head = kh * a.group + (int)(row % (uint32_t)a.group);
-  Query<D, 2> asked;
-  asked.load(a, a.q + (q.row0 + token) * a.q_token + head * a.q_head, h);
-  find_keys(a, q);
-  // the keys that the workgroup's rows see
-  int from, to, unused;
-  visible(a, q, (int)((uint32_t)(tile * ROWS) / (uint32_t)a.group), from, unused);
-  visible(a, q, (int)((uint32_t)(min(tile * ROWS + ROWS, rows) - 1) / (uint32_t)a.group), unused, to);
-  const int c0 = from / kChunk, c1 = (to + kChunk - 1) / kChunk;
-  const int parts = parts_of(a, c0, c1), part = blockIdx.y;
-  if (part >= parts) return;
-  const int begin = 2 * part_start(c0, c1, parts, part);
-  const int stop = 2 * part_start(c0, c1, parts, part + 1);
-  int low, high;
-  visible(a, q, token, low, high);
-  if (!live) high = 0;
-  // the keys that all of this wave's rows see
-  int all_from = 0, all_to = 0;
-  if (row0 + kWide <= rows) {
-    visible(a, q, (int)((uint32_t)row0 / (uint32_t)a.group), unused, all_to);
-    visible(a, q, (int)((uint32_t)(row0 + kWide - 1) / (uint32_t)a.group), all_from, unused);
-    if (all_from >= all_to) all_to = 0;
+  if (!a.whole && threadIdx.x == 0) a.cuts[blockIdx.x].parts = 0;
+  Line<ROWS> line;
+  const bool any = line.measure(a);
+  if (a.cu && blockIdx.x == 0 && threadIdx.x == 0 && (a.cu[0] != 0 || a.cu[a.n] != a.tokens))
+    atomicOr(c.flags, kFlagInval);
+  if (!any) return;
+  // a die's workgroups (every eighth) take neighbouring pieces: the same KV head
+  const uint32_t piece = line.pieces == kPieces
+                             ? blockIdx.x % 8 * (kPieces / 8) + blockIdx.x / 8
+                             : blockIdx.x;
+  uint64_t turn = blockIdx.x, x0 = 0, x1 = 0;
+  Place at;
+  if (line.dealt) {
+    if (!line.deal(a, turn, at)) return;
+  } else {
+    if (piece >= line.pieces) return;
+    x0 = line.cut(piece);
+    x1 = line.cut(piece + 1);
+    if (!line.find(a, x0, at)) return;
   }
+  for (;;) {
+    const int kh = at.head, tile = (int)at.tile;
+    const Sequence q = sequence_of(a, at);
+    const int rows = q.fresh * a.group;
+    const int row0 = tile * ROWS + wave * kWide;
+    const uint32_t row = (uint32_t)min(row0 + r, rows - 1);
+    const bool live = row0 + r < rows;
+    const int token = (int)(row / (uint32_t)a.group);
+    const int head = kh * a.group + (int)(row % (uint32_t)a.group);
+    Query<D, 2> asked;
+    asked.load(a, a.q + (q.row0 + token) * a.q_token + head * a.q_head, h);
+    // the keys that the workgroup's rows see
+    int from, to, unused;
+    visible(a, q, (int)((uint32_t)(tile * ROWS) / (uint32_t)a.group), from, unused);
+    visible(a, q, (int)((uint32_t)(min(tile * ROWS + ROWS, rows) - 1) / (uint32_t)a.group), unused,
+            to);
+    const int c0 = from / kChunk, c1 = max((to + kChunk - 1) / kChunk, c0);
+    const uint64_t width = at.share.of(at.tile), end = at.start + width;
+    if (line.dealt) {
+      x0 = at.start;
+      x1 = end;
+    }
+    const bool whole = x0 == at.start && end <= x1;
+    auto chunk_at = [&](uint64_t x) __attribute__((always_inline)) {
+      const uint64_t n = (uint64_t)(c1 - c0), each = width / max(n, (uint64_t)1) + 1;
+      return c0 + (int)min(n, (x - at.start) / each);
+    };
+    const int begin = 2 * (x0 == at.start ? c0 : chunk_at(x0));
+    const int stop = 2 * (end <= x1 ? c1 : chunk_at(x1));
+    int low, high;
+    visible(a, q, token, low, high);
+    if (!live) high = 0;
+    // the keys that all of this wave's rows see
+    int all_from = 0, all_to = 0;
+    if (row0 + kWide <= rows) {
+      visible(a, q, (int)((uint32_t)row0 / (uint32_t)a.group), unused, all_to);
+      visible(a, q, (int)((uint32_t)(row0 + kWide - 1) / (uint32_t)a.group), all_from, unused);
+      if (all_from >= all_to) all_to = 0;
+    }
 
-  const int64_t block_bytes = (int64_t)c.page_tokens * D;
-  const int64_t k_off = ((int64_t)a.layer * 2 * c.kv_heads + kh) * block_bytes;
-  const int64_t v_off = k_off + c.kv_heads * block_bytes;
-  const int in_page = c.page_tokens - 1;
-  const int last_block = (q.len - 1) >> c.page_shift;
-  bool wrong = false;
-  auto checked = [&](int32_t entry) __attribute__((always_inline)) -> uint32_t {
-    const bool bad = (uint32_t)entry >= (uint32_t)c.num_pages;
-    wrong |= bad;
-    return bad ? 0u : (uint32_t)entry;
-  };
-  // A thread's 16-byte units of a step: the first half of all are K, the rest V;
-  // a wave's lie side by side in one tile of 16 keys, so all of their address
-  // but the lane is scalar. Pages are looked up a step before their codes are
-  // loaded (even lanes the first tile's, odd lanes the second's), and those two
-  // steps before they are put into LDS.
-  auto unit_of = [&](int k) __attribute__((always_inline)) {
-    return (wave * kWave + k * NT) % UNITS;  // of lane 0
-  };
-  auto is_key = [&](int k) __attribute__((always_inline)) { return unit_of(k) < UNITS / 2; };
-  auto unit_tile = [&](int k) __attribute__((always_inline)) { return unit_of(k) / D & 1; };
-  int64_t unit_off[PER];  // where a unit is in a tile's page
-  int unit_to[PER];       // and where its operands go
-#pragma unroll
-  for (int k = 0; k < PER; ++k) {
-    const int in = unit_of(k) % D + lane, tl = unit_tile(k), tok = in % 16;
-    unit_off[k] = (is_key(k) ? k_off : v_off) + unit_of(k) % D * 16;
-    // K: 16 channels (step in / 16) of key in % 16; V: 16 keys of channel `in`
-    unit_to[k] = is_key(k) ? in / 16 * kWave + tok / 4 * 8 + tl * 4 + tok % 4
-                           : in / 32 * kWave + tl * kWide + in % 32;
-  }
-  const float* const scale_at =
-      c.scale + ((int64_t)a.layer * 2 + lane / 2 % 2) * c.kv_heads + kh;
-  auto look_up = [&](int j) __attribute__((always_inline)) {
-    return q.table[min((min(j, stop - 1) * kWide + lane % 2 * kKvTile) >> c.page_shift, last_block)];
-  };
-  // (all threads load and store one of the four scales: no branch)
-  auto fetch = [&](int j, int32_t entry, uint4 (&to)[PER], float& sc)
-      __attribute__((always_inline)) {
-    const int t0 = min(j, stop - 1) * kWide;
-    const uint32_t mine = checked(entry);
-    const uint32_t both[2] = {(uint32_t)__builtin_amdgcn_readlane((int)mine, 0),
-                              (uint32_t)__builtin_amdgcn_readlane((int)mine, 1)};
-    sc = scale_at[(int64_t)mine * c.page_scales];
+    const int64_t block_bytes = (int64_t)c.page_tokens * D;
+    const int64_t k_off = ((int64_t)a.layer * 2 * c.kv_heads + kh) * block_bytes;
+    const int64_t v_off = k_off + c.kv_heads * block_bytes;
+    const int in_page = c.page_tokens - 1;
+    const int last_block = (q.len - 1) >> c.page_shift;
+    bool wrong = false;
+    auto checked = [&](int32_t entry) __attribute__((always_inline)) -> uint32_t {
+      const bool bad = (uint32_t)entry >= (uint32_t)c.num_pages;
+      wrong |= bad;
+      return bad ? 0u : (uint32_t)entry;
+    };
+    // A thread's 16-byte units of a step: the first half of all are K, the rest V;
+    // a wave's lie side by side in one tile of 16 keys, so all of their address
+    // but the lane is scalar. Pages are looked up a step before their codes are
+    // loaded (even lanes the first tile's, odd lanes the second's), and those two
+    // steps before they are put into LDS.
+    auto unit_of = [&](int k) __attribute__((always_inline)) {
+      return (wave * kWave + k * NT) % UNITS;  // of lane 0
+    };
+    auto is_key = [&](int k) __attribute__((always_inline)) { return unit_of(k) < UNITS / 2; };
+    auto unit_tile = [&](int k) __attribute__((always_inline)) { return unit_of(k) / D & 1; };
+    int64_t unit_off[PER];  // where a unit is in a tile's page
+    int unit_to[PER];       // and where its operands go
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
-      const int t = t0 + unit_tile(k) * kKvTile;
-      const uint8_t* p = c.data + (int64_t)both[unit_tile(k)] * c.page_bytes +
-                         (t & in_page) * D + unit_off[k];
-      to[k] = reinterpret_cast<const uint4*>(p)[lane];
+      const int in = unit_of(k) % D + lane, tl = unit_tile(k), tok = in % 16;
+      unit_off[k] = (is_key(k) ? k_off : v_off) + unit_of(k) % D * 16;
+      // K: 16 channels (step in / 16) of key in % 16; V: 16 keys of channel `in`
+      unit_to[k] = is_key(k) ? in / 16 * kWave + tok / 4 * 8 + tl * 4 + tok % 4
+                             : in / 32 * kWave + tl * kWide + in % 32;
     }
-  };
-  // V codes beyond the length may be anything (K ones are hidden later).
-  auto hide = [&](int j, uint4 (&w)[PER]) __attribute__((always_inline)) {
-    if ((j + 1) * kWide <= q.len) return;
+    const float* const scale_at =
+        c.scale + ((int64_t)a.layer * 2 + lane / 2 % 2) * c.kv_heads + kh;
+    auto look_up = [&](int j) __attribute__((always_inline)) {
+      return q.table[min((min(j, stop - 1) * kWide + lane % 2 * kKvTile) >> c.page_shift,
+                         last_block)];
+    };
+    // (all threads load and store one of the four scales: no branch)
+    auto fetch = [&](int j, int32_t entry, uint4 (&to)[PER], float& sc)
+        __attribute__((always_inline)) {
+      const int t0 = min(j, stop - 1) * kWide;
+      const uint32_t mine = checked(entry);
+      const uint32_t both[2] = {(uint32_t)__builtin_amdgcn_readlane((int)mine, 0),
+                                (uint32_t)__builtin_amdgcn_readlane((int)mine, 1)};
+      sc = scale_at[(int64_t)mine * c.page_scales];
 #pragma unroll
-    for (int k = 0; k < PER; ++k) {
-      const int n = is_key(k) ? 16 : q.len - j * kWide - unit_tile(k) * kKvTile;
-      w[k].x = keep_bytes(w[k].x, n);
-      w[k].y = keep_bytes(w[k].y, n - 4);
-      w[k].z = keep_bytes(w[k].z, n - 8);
-      w[k].w = keep_bytes(w[k].w, n - 12);
-    }
-  };
-  auto stage = [&](int j, const uint4 (&from)[PER], float sc) __attribute__((always_inline)) {
-    scales[(j & 3) * 4 + lane % 4] = sc;
+      for (int k = 0; k < PER; ++k) {
+        const int t = t0 + unit_tile(k) * kKvTile;
+        const uint8_t* p = c.data + (int64_t)both[unit_tile(k)] * c.page_bytes +
+                           (t & in_page) * D + unit_off[k];
+        to[k] = reinterpret_cast<const uint4*>(p)[lane];
+      }
+    };
+    // V codes beyond the length may be anything (K ones are hidden later).
+    auto hide = [&](int j, uint4 (&w)[PER]) __attribute__((always_inline)) {
+      if ((j + 1) * kWide <= q.len) return;
 #pragma unroll
-    for (int k = 0; k < PER; ++k) {
-      half8_t lo, hi;
-      codes_to_operands<FMT>(from[k], lo, hi);
-      half8_t* to = is_key(k) ? keys + (j & 1) * (KS * kWave) : vals + (j & 3) * (2 * DY * kWave);
-      to[unit_to[k]] = lo;
-      to[unit_to[k] + (is_key(k) ? kWide : DY * kWave)] = hi;
-    }
-  };
+      for (int k = 0; k < PER; ++k) {
+        const int n = is_key(k) ? 16 : q.len - j * kWide - unit_tile(k) * kKvTile;
+        w[k].x = keep_bytes(w[k].x, n);
+        w[k].y = keep_bytes(w[k].y, n - 4);
+        w[k].z = keep_bytes(w[k].z, n - 8);
+        w[k].w = keep_bytes(w[k].w, n - 12);
+      }
+    };
+    auto stage = [&](int j, const uint4 (&from)[PER], float sc) __attribute__((always_inline)) {
+      scales[(j & 3) * 4 + lane % 4] = sc;
+#pragma unroll
+      for (int k = 0; k < PER; ++k) {
+        half8_t lo, hi;
+        codes_to_operands<FMT>(from[k], lo, hi);
+        half8_t* to = is_key(k) ? keys + (j & 1) * (KS * kWave) : vals + (j & 3) * (2 * DY * kWave);
+        to[unit_to[k]] = lo;
+        to[unit_to[k] + (is_key(k) ? kWide : DY * kWave)] = hi;
+      }
+    };
 
-  half8_t query[KS];
-  float factor = 0.0f;
-  float m = kNone, l = 0.0f, vref = 0.0f;
-  float16_t acc[DY], s0, s1;
-  half8_t w0[2], w1[2];
-#pragma unroll
-  for (int y = 0; y < DY; ++y)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) acc[y][i] = 0.0f;
-#pragma unroll
-  for (int x = 0; x < 2; ++x)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) w1[x][i] = (_Float16)0.0f;
-  auto read_key = [&](int j, int k) __attribute__((always_inline)) {
-    return keys[(j & 1) * (KS * kWave) + k * kWave + lane];
-  };
-  auto score = [&](int k, half8_t key, float16_t& s) __attribute__((always_inline)) {
-    s = __builtin_amdgcn_mfma_f32_32x32x16_f16(key, query[k], s, 0, 0, 0);
-  };
-  auto output = [&](int x, const half8_t (&vf)[DY], const half8_t (&w)[2])
-      __attribute__((always_inline)) {
+    half8_t query[KS];
+    float factor = 0.0f;
+    float m = kNone, l = 0.0f, vref = 0.0f;
+    float16_t acc[DY], s0, s1;
+    half8_t w0[2], w1[2];
 #pragma unroll
     for (int y = 0; y < DY; ++y)
-      acc[y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[y], w[x], acc[y], 0, 0, 0);
-  };
-  auto read_vals = [&](int j, int x, half8_t (&vf)[DY]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int y = 0; y < DY; ++y)
-      vf[y] = vals[(j & 3) * (2 * DY * kWave) + (x * DY + y) * kWave + lane];
-  };
+      for (int i = 0; i < 16; ++i) acc[y][i] = 0.0f;
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w1[x][i] = (_Float16)0.0f;
+    auto read_key = [&](int j, int k) __attribute__((always_inline)) {
+      return keys[(j & 1) * (KS * kWave) + k * kWave + lane];
+    };
+    auto score = [&](int k, half8_t key, float16_t& s) __attribute__((always_inline)) {
+      s = __builtin_amdgcn_mfma_f32_32x32x16_f16(key, query[k], s, 0, 0, 0);
+    };
+    auto output = [&](int x, const half8_t (&vf)[DY], const half8_t (&w)[2])
+        __attribute__((always_inline)) {
+#pragma unroll
+      for (int y = 0; y < DY; ++y)
+        acc[y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[y], w[x], acc[y], 0, 0, 0);
+    };
+    auto read_vals = [&](int j, int x, half8_t (&vf)[DY]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int y = 0; y < DY; ++y)
+        vf[y] = vals[(j & 3) * (2 * DY * kWave) + (x * DY + y) * kWave + lane];
+    };
 
-  int32_t page = 0;  // of the next step's loads
-  // Step j: scores of keys j + 1 into nxt, weights of keys j from cur, outputs of
-  // keys j - 1. The first half's matrix instructions each get a share of the
-  // weights' vector ones (the compiler would put them all behind).
-  auto step = [&](int j, float16_t& cur, float16_t& nxt, const half8_t (&wp)[2], half8_t (&wc)[2],
-                  uint4 (&rw)[PER], float& sc) __attribute__((always_inline)) {
-    if (j * kWide < all_from || (j + 1) * kWide > all_to) {  // keys that some rows do not see
-      const int t0 = j * kWide + h * kKvTile;
+    int32_t page = 0;  // of the next step's loads
+    // Step j: scores of keys j + 1 into nxt, weights of keys j from cur, outputs of
+    // keys j - 1. The first half's matrix instructions each get a share of the
+    // weights' vector ones (the compiler would put them all behind).
+    auto step = [&](int j, float16_t& cur, float16_t& nxt, const half8_t (&wp)[2], half8_t (&wc)[2],
+                    uint4 (&rw)[PER], float& sc) __attribute__((always_inline)) {
+      if (j * kWide < all_from || (j + 1) * kWide > all_to) {  // keys that some rows do not see
+        const int t0 = j * kWide + h * kKvTile;
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-        cur[i] = t0 + i >= low && t0 + i < high ? cur[i] : kNone;
-    }
-    hide(j + 2, rw);
+        for (int i = 0; i < 16; ++i)
+          cur[i] = t0 + i >= low && t0 + i < high ? cur[i] : kNone;
+      }
+      hide(j + 2, rw);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) nxt[i] = 0.0f;
-    __builtin_amdgcn_sched_barrier(0);
-    half8_t kf[KS];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) kf[k] = read_key(j + 1, k);
-    const float ks = scales[(j & 3) * 4 + h];
-    const float vs0 = scales[(j & 3) * 4 + 2], vs1 = scales[(j & 3) * 4 + 3];
-    float top = cur[0];
-#pragma unroll
-    for (int i = 1; i < 16; ++i) top = __builtin_elementwise_maximum(top, cur[i]);
-    __builtin_amdgcn_sched_barrier(0);
-    score(0, kf[0], nxt);
-    // weights are relative to the largest V scale so far (the same in all lanes)
-    const float vmax = fmaxf(fmaxf(vs0, vs1), vref);
-    const float inv = vmax > 0.0f ? __builtin_amdgcn_rcpf(vmax) : 0.0f;
-    const float rel = fmaxf((h ? vs1 : vs0) * inv, 9.3e-10f) * kLift;  // (2^-30)
-    const float unrel = __builtin_amdgcn_rcpf(rel);
-    // (not zero, so that a hidden key's minus infinity stays one)
-    const float f = fmaxf(ks * factor, 1e-30f);
-    top *= f;
-    top = __builtin_elementwise_maximum(top, other_half(top));
-    __builtin_amdgcn_sched_barrier(0);
-    score(1, kf[1], nxt);
-    const bool raise = top > m + kSlack;
-    const float next = raise ? top : m;
-    const float shrink = raise ? __builtin_amdgcn_exp2f(m - next) : 1.0f;
-    const float fade = vmax > vref ? shrink * (vref * inv) : shrink;
-    vref = vmax;
-    m = next;
-    const float b = __builtin_amdgcn_logf(rel) - (next == kNone ? 0.0f : next);
-    float sum[2] = {0.0f, 0.0f};
-    half8_t vf[DY], vg[DY];
-    constexpr int SHARES = KS / 2 - 1;  // of the weights
-#pragma unroll
-    for (int i = 0; i < SHARES; ++i) {
+      for (int i = 0; i < 16; ++i) nxt[i] = 0.0f;
       __builtin_amdgcn_sched_barrier(0);
-      score(2 * i + 2, kf[2 * i + 2], nxt);
-      score(2 * i + 3, kf[2 * i + 3], nxt);
-      if (2 * i + 4 < KS) {
-        kf[2 * i + 4] = read_key(j + 1, 2 * i + 4);
-        kf[2 * i + 5] = read_key(j + 1, 2 * i + 5);
-      } else {
-        read_vals(max(j - 1, begin), 0, vf);
+      half8_t kf[KS];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) kf[k] = read_key(j + 1, k);
+      const float ks = scales[(j & 3) * 4 + h];
+      const float vs0 = scales[(j & 3) * 4 + 2], vs1 = scales[(j & 3) * 4 + 3];
+      float top = cur[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) top = __builtin_elementwise_maximum(top, cur[i]);
+      __builtin_amdgcn_sched_barrier(0);
+      score(0, kf[0], nxt);
+      // weights are relative to the largest V scale so far (the same in all lanes)
+      const float vmax = fmaxf(fmaxf(vs0, vs1), vref);
+      const float inv = vmax > 0.0f ? __builtin_amdgcn_rcpf(vmax) : 0.0f;
+      const float rel = fmaxf((h ? vs1 : vs0) * inv, 9.3e-10f) * kLift;  // (2^-30)
+      const float unrel = __builtin_amdgcn_rcpf(rel);
+      // (not zero, so that a hidden key's minus infinity stays one)
+      const float f = fmaxf(ks * factor, 1e-30f);
+      top *= f;
+      top = __builtin_elementwise_maximum(top, other_half(top));
+      __builtin_amdgcn_sched_barrier(0);
+      score(1, kf[1], nxt);
+      const bool raise = top > m + kSlack;
+      const float next = raise ? top : m;
+      const float shrink = raise ? __builtin_amdgcn_exp2f(m - next) : 1.0f;
+      const float fade = vmax > vref ? shrink * (vref * inv) : shrink;
+      vref = vmax;
+      m = next;
+      const float b = __builtin_amdgcn_logf(rel) - (next == kNone ? 0.0f : next);
+      float sum[2] = {0.0f, 0.0f};
+      half8_t vf[DY], vg[DY];
+      constexpr int SHARES = KS / 2 - 1;  // of the weights
+#pragma unroll
+      for (int i = 0; i < SHARES; ++i) {
+        __builtin_amdgcn_sched_barrier(0);
+        score(2 * i + 2, kf[2 * i + 2], nxt);
+        score(2 * i + 3, kf[2 * i + 3], nxt);
+        if (2 * i + 4 < KS) {
+          kf[2 * i + 4] = read_key(j + 1, 2 * i + 4);
+          kf[2 * i + 5] = read_key(j + 1, 2 * i + 5);
+        } else {
+          read_vals(max(j - 1, begin), 0, vf);
+        }
+#pragma unroll
+        for (int k = 16 * i / SHARES; k < 16 * (i + 1) / SHARES; ++k) {
+          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(cur[k], f, b));
+          sum[k % 2] += p;
+          wc[k / 8][k % 8] = (_Float16)p;
+        }
       }
+      l = l * shrink + (sum[0] + sum[1]) * unrel;
+      asm volatile("" : "+v"(wc[0]), "+v"(wc[1]), "+v"(l));  // here, not where they are used
+      __builtin_amdgcn_sched_barrier(0);
+      read_vals(max(j - 1, begin), 1, vg);
+      output(0, vf, wp);
+      output(1, vg, wp);
+      stage(j + 2, rw, sc);
+      // the next look-up goes first: loads return in order, and the next step
+      // needs it before these
+      const int32_t entry = page;
+      page = look_up(j + 5);
+      fetch(j + 4, entry, rw, sc);
 #pragma unroll
-      for (int k = 16 * i / SHARES; k < 16 * (i + 1) / SHARES; ++k) {
-        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(cur[k], f, b));
-        sum[k % 2] += p;
-        wc[k / 8][k % 8] = (_Float16)p;
+      for (int i = 0; i < 2 * DY; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a matrix instruction,
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // an operand read
+        __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);  // and vector ones
       }
-    }
-    l = l * shrink + (sum[0] + sum[1]) * unrel;
-    asm volatile("" : "+v"(wc[0]), "+v"(wc[1]), "+v"(l));  // here, not where they are used
-    __builtin_amdgcn_sched_barrier(0);
-    read_vals(max(j - 1, begin), 1, vg);
-    output(0, vf, wp);
-    output(1, vg, wp);
-    stage(j + 2, rw, sc);
-    // the next look-up goes first: loads return in order, and the next step
-    // needs it before these
-    const int32_t entry = page;
-    page = look_up(j + 5);
-    fetch(j + 4, entry, rw, sc);
+      __builtin_amdgcn_sched_barrier(0);
+      if (__ballot(fade != 1.0f)) {
 #pragma unroll
-    for (int i = 0; i < 2 * DY; ++i) {
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a matrix instruction,
-      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // an operand read
-      __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);  // and vector ones
-    }
-    __builtin_amdgcn_sched_barrier(0);
-    if (__ballot(fade != 1.0f)) {
-#pragma unroll
-      for (int y = 0; y < DY; ++y) {
-        // one after the other: all of them at once in the vector registers
-        // would push out other values
-        if (PINNED) asm volatile("" : "+a"(acc[y]));
-        acc[y] *= fade;
-        if (PINNED) asm volatile("" : "+a"(acc[y]));
+        for (int y = 0; y < DY; ++y) {
+          // one after the other: all of them at once in the vector registers
+          // would push out other values
+          if (PINNED) asm volatile("" : "+a"(acc[y]));
+          acc[y] *= fade;
+          if (PINNED) asm volatile("" : "+a"(acc[y]));
+        }
       }
-    }
-    block_sync();
-  };
-  if (begin < stop) {
-    int32_t entry[4];
+      block_sync();
+    };
+    if (begin < stop) {
+      int32_t entry[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) entry[i] = look_up(begin + i);
-    page = look_up(begin + 4);
-    factor = asked.convert(a, query);
+      for (int i = 0; i < 4; ++i) entry[i] = look_up(begin + i);
+      page = look_up(begin + 4);
+      factor = asked.convert(a, query);
 #pragma unroll
-    for (int k = 0; k < KS; ++k) {
-      if (PINNED) asm volatile("" : "+a"(query[k]));
-      else asm volatile("" : "+v"(query[k]));
-    }
-    uint4 early[2][PER], raw[2][PER];
-    float searly[2], sraw[2];
-    fetch(begin, entry[0], early[0], searly[0]);
-    fetch(begin + 1, entry[1], early[1], searly[1]);
-    fetch(begin + 2, entry[2], raw[0], sraw[0]);
-    fetch(begin + 3, entry[3], raw[1], sraw[1]);
-    hide(begin, early[0]);
-    hide(begin + 1, early[1]);
-    stage(begin, early[0], searly[0]);
-    stage(begin + 1, early[1], searly[1]);
-    block_sync();
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s0[i] = 0.0f;
-#pragma unroll
-    for (int k = 0; k < KS; ++k) score(k, read_key(begin, k), s0);
-    block_sync();  // step `begin` puts keys begin + 2 where these were
-    for (int j = begin; j < stop; j += 2) {
-      step(j, s0, s1, w1, w0, raw[0], sraw[0]);
-      step(j + 1, s1, s0, w0, w1, raw[1], sraw[1]);
-    }
-    half8_t vf[DY], vg[DY];
-    read_vals(stop - 1, 0, vf);
-    read_vals(stop - 1, 1, vg);
-    output(0, vf, w1);
-    output(1, vg, w1);
-  }
-  block_sync();  // the buffers are free
-  if (__ballot(wrong) && lane == 0) atomicOr(c.flags, kFlagInval);
-  l += other_half(l);
-  if (parts > 1) {
-    if (!live) return;
-    const int64_t slot = ((int64_t)part * a.tokens + q.row0 + token) * a.heads + head;
-    const float by = vref * (1.0f / kLift);
-    float* o = a.part_o + slot * D;
-#pragma unroll
-    for (int y = 0; y < DY; ++y)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float4_t x = {acc[y][4 * k] * by, acc[y][4 * k + 1] * by, acc[y][4 * k + 2] * by,
-                            acc[y][4 * k + 3] * by};
-        *reinterpret_cast<float4_t*>(o + y * 32 + k * 8 + h * 4) = x;
+      for (int k = 0; k < KS; ++k) {
+        if (PINNED) asm volatile("" : "+a"(query[k]));
+        else asm volatile("" : "+v"(query[k]));
       }
-    if (h == 0) {
-      a.part_ml[2 * slot] = m;
-      a.part_ml[2 * slot + 1] = l;
+      uint4 early[2][PER], raw[2][PER];
+      float searly[2], sraw[2];
+      fetch(begin, entry[0], early[0], searly[0]);
+      fetch(begin + 1, entry[1], early[1], searly[1]);
+      fetch(begin + 2, entry[2], raw[0], sraw[0]);
+      fetch(begin + 3, entry[3], raw[1], sraw[1]);
+      hide(begin, early[0]);
+      hide(begin + 1, early[1]);
+      stage(begin, early[0], searly[0]);
+      stage(begin + 1, early[1], searly[1]);
+      block_sync();
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s0[i] = 0.0f;
+#pragma unroll
+      for (int k = 0; k < KS; ++k) score(k, read_key(begin, k), s0);
+      block_sync();  // step `begin` puts keys begin + 2 where these were
+      for (int j = begin; j < stop; j += 2) {
+        step(j, s0, s1, w1, w0, raw[0], sraw[0]);
+        step(j + 1, s1, s0, w0, w1, raw[1], sraw[1]);
+      }
+      half8_t vf[DY], vg[DY];
+      read_vals(stop - 1, 0, vf);
+      read_vals(stop - 1, 1, vg);
+      output(0, vf, w1);
+      output(1, vg, w1);
     }
-    return;
-  }
-  const bool some = l > 0.0f || l != l;
-  const float inv = some ? vref * (1.0f / kLift) / l : 0.0f;
-  // through LDS, so that rows are written whole
-  uint2* const mine = reinterpret_cast<uint2*>(pool + (wave * kWide + r) * PITCH);
+    block_sync();  // the buffers are free
+    if (__ballot(wrong) && lane == 0) atomicOr(c.flags, kFlagInval);
+    l += other_half(l);
+    if (!whole) {
+      // a piece's first tile and its last one may be cut
+      const int64_t slot = (int64_t)(2 * piece + (x0 == at.start)) * ROWS + wave * kWide + r;
+      const float by = vref * (1.0f / kLift);
+      float* o = a.part_o + slot * D;
 #pragma unroll
-  for (int y = 0; y < DY; ++y)
+      for (int y = 0; y < DY; ++y)
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      mine[y * 8 + k * 2 + h] =
-          make_uint2(pack_pair(acc[y][4 * k] * inv, acc[y][4 * k + 1] * inv, a.bf16),
-                     pack_pair(acc[y][4 * k + 2] * inv, acc[y][4 * k + 3] * inv, a.bf16));
-  if (a.lse && h == 0 && live)
-    a.lse[(q.row0 + token) * a.heads + head] =
-        some ? (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : kNone;
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (a wave reads what it wrote)
-  constexpr int LANES = D / 8;  // of a row
-#pragma unroll 2
-  for (int i = lane / LANES; i < kWide; i += kWave / LANES) {
-    const int rr = row0 + i;
-    if (rr >= rows) break;
-    const uint32_t tok = (uint32_t)rr / (uint32_t)a.group;
-    const int64_t hd = kh * a.group + (int)((uint32_t)rr - tok * a.group);
-    uint16_t* o = a.out + (q.row0 + tok) * a.out_token + hd * a.out_head + lane % LANES * 8;
-    const uint4 x = __builtin_bit_cast(uint4, pool[(wave * kWide + i) * PITCH + lane % LANES]);
-    if (a.wide_out) {
-      *reinterpret_cast<uint4*>(o) = x;
+        for (int k = 0; k < 4; ++k) {
+          const float4_t x = {acc[y][4 * k] * by, acc[y][4 * k + 1] * by, acc[y][4 * k + 2] * by,
+                              acc[y][4 * k + 3] * by};
+          *reinterpret_cast<float4_t*>(o + y * 32 + k * 8 + h * 4) = x;
+        }
+      if (h == 0) {
+        a.part_ml[2 * slot] = m;
+        a.part_ml[2 * slot + 1] = l;
+      }
+      if (x0 == at.start && threadIdx.x == 0)  // the first part tells how to join them
+        a.cuts[blockIdx.x] = {(int32_t)(line.piece_of(end - 1) - piece) + 1, (int32_t)piece,
+                              (int32_t)q.row0, rows, tile, kh};
     } else {
-      const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+      const bool some = l > 0.0f || l != l;
+      const float inv = some ? vref * (1.0f / kLift) / l : 0.0f;
+      // through LDS, so that rows are written whole
+      uint2* const mine = reinterpret_cast<uint2*>(pool + (wave * kWide + r) * PITCH);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) o[j] = (uint16_t)(w[j / 2] >> (16 * (j % 2)));
+      for (int y = 0; y < DY; ++y)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          mine[y * 8 + k * 2 + h] =
+              make_uint2(pack_pair(acc[y][4 * k] * inv, acc[y][4 * k + 1] * inv, a.bf16),
+                         pack_pair(acc[y][4 * k + 2] * inv, acc[y][4 * k + 3] * inv, a.bf16));
+      if (a.lse && h == 0 && live)
+        a.lse[(q.row0 + token) * a.heads + head] =
+            some ? (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : kNone;
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (a wave reads what it wrote)
+      constexpr int LANES = D / 8;  // of a row
+#pragma unroll 2
+      for (int i = lane / LANES; i < kWide; i += kWave / LANES) {
+        const int rr = row0 + i;
+        if (rr >= rows) break;
+        const uint32_t tok = (uint32_t)rr / (uint32_t)a.group;
+        const int64_t hd = kh * a.group + (int)((uint32_t)rr - tok * a.group);
+        uint16_t* o = a.out + (q.row0 + tok) * a.out_token + hd * a.out_head + lane % LANES * 8;
+        const uint4 x = __builtin_bit_cast(uint4, pool[(wave * kWide + i) * PITCH + lane % LANES]);
+        if (a.wide_out) {
+          *reinterpret_cast<uint4*>(o) = x;
+        } else {
+          const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+          for (int j = 0; j < 8; ++j) o[j] = (uint16_t)(w[j / 2] >> (16 * (j % 2)));
+        }
+      }
+    }
+    block_sync();  // the buffers are free
+    if (line.dealt) {
+      turn += gridDim.x;
+      if (!line.deal(a, turn, at)) break;
+    } else {
+      x0 = end;
+      if (x0 >= x1 || !line.next(a, at)) break;
     }
   }
 }
 
-// Joins the parts of the key axis of the tile kernel: sixteen lanes per row.
-constexpr int kJoinRows = 16;  // of a workgroup
-template <int D>
-__global__ __launch_bounds__(kJoinRows * 16) void kv_attend_join(KvAttendArgs a, int tile_rows) {
+// Joins the tiles that were cut: sixteen lanes per row, kJoinRows rows after
+// each other.
+constexpr int kJoinRows = 64;  // of a workgroup
+template <int D, int ROWS>
+__global__ __launch_bounds__(256) void kv_attend_join(KvAttendArgs a) {
   constexpr int W = D / 16;  // channels of a lane
-  const KvView& c = a.c;
-  Sequence q;
-  int tile;
-  if (!find_tile<false>(a, blockIdx.x / c.kv_heads, tile_rows, q, tile)) return;
-  const int rows = q.fresh * a.group;
-  const int row = tile * tile_rows + blockIdx.y * kJoinRows + threadIdx.x / 16;
-  if (tile * tile_rows + (int)blockIdx.y * kJoinRows >= rows) return;
-  find_keys(a, q);
-  int from, to, unused;
-  visible(a, q, (int)((uint32_t)(tile * tile_rows) / (uint32_t)a.group), from, unused);
-  visible(a, q, (int)((uint32_t)(min(tile * tile_rows + tile_rows, rows) - 1) / (uint32_t)a.group),
-          unused, to);
-  const int parts = parts_of(a, from / kChunk, (to + kChunk - 1) / kChunk);
-  if (parts == 1 || row >= rows) return;
-  const int64_t token = q.row0 + (uint32_t)row / (uint32_t)a.group;
-  const int64_t head = blockIdx.x % c.kv_heads * a.group + (uint32_t)row % (uint32_t)a.group;
-  const int64_t all = a.tokens * a.heads, at = token * a.heads + head;
-  const int lane = threadIdx.x % 16;
-  const float2_t* ml = reinterpret_cast<const float2_t*>(a.part_ml) + at;
-  float most = kNone;
+  const KvCut cut = a.cuts[blockIdx.x];
+  const int parts = cut.parts;
+  if (parts == 0) return;
+  // (the first part is its piece's last tile, the others are their pieces' first)
+  for (int mine = blockIdx.y * kJoinRows + threadIdx.x / 16;
+       mine < (int)(blockIdx.y + 1) * kJoinRows; mine += 16) {
+    const int row = cut.tile * ROWS + mine;
+    if (row >= cut.rows) return;
+    auto slot = [&](int k) __attribute__((always_inline)) {
+      return (int64_t)(2 * (cut.piece + k) + (k == 0)) * ROWS + mine;
+    };
+    const int64_t token = cut.row0 + (uint32_t)row / (uint32_t)a.group;
+    const int64_t head = cut.head * a.group + (uint32_t)row % (uint32_t)a.group;
+    const int lane = threadIdx.x % 16;
+    const float2_t* ml = reinterpret_cast<const float2_t*>(a.part_ml);
+    float most = kNone;
 #pragma unroll 4
-  for (int k = 0; k < parts; ++k) most = fmaxf(most, ml[k * all][0]);
-  const float base = most == kNone ? 0.0f : most;
-  float total = 0.0f;
-  float4_t o[W / 4];
+    for (int k = 0; k < parts; ++k) most = fmaxf(most, ml[slot(k)][0]);
+    const float base = most == kNone ? 0.0f : most;
+    float total = 0.0f;
+    float4_t o[W / 4];
 #pragma unroll
-  for (int j = 0; j < W / 4; ++j) o[j] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
-  const float* part = a.part_o + at * D + lane * W;
+    for (int j = 0; j < W / 4; ++j) o[j] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    const float* part = a.part_o + lane * W;
 #pragma unroll 4
-  for (int k = 0; k < parts; ++k) {
-    const float2_t p = ml[k * all];
-    const float w = __builtin_amdgcn_exp2f(p[0] - base);
-    total += p[1] * w;
+    for (int k = 0; k < parts; ++k) {
+      const float2_t p = ml[slot(k)];
+      const float w = __builtin_amdgcn_exp2f(p[0] - base);
+      total += p[1] * w;
 #pragma unroll
-    for (int j = 0; j < W / 4; ++j)
-      o[j] += *reinterpret_cast<const float4_t*>(part + k * all * D + 4 * j) * w;
-  }
-  const bool some = total > 0.0f || total != total;
-  const float inv = some ? 1.0f / total : 0.0f;
-  uint16_t* out = a.out + token * a.out_token + head * a.out_head + lane * W;
-#pragma unroll
-  for (int j = 0; j < W / 4; ++j) {
-    const uint32_t x = pack_pair(o[j][0] * inv, o[j][1] * inv, a.bf16);
-    const uint32_t y = pack_pair(o[j][2] * inv, o[j][3] * inv, a.bf16);
-    if (a.wide_out) {
-      *reinterpret_cast<uint2*>(out + 4 * j) = make_uint2(x, y);
-    } else {
-      out[4 * j] = (uint16_t)x;
-      out[4 * j + 1] = (uint16_t)(x >> 16);
-      out[4 * j + 2] = (uint16_t)y;
-      out[4 * j + 3] = (uint16_t)(y >> 16);
+      for (int j = 0; j < W / 4; ++j)
+        o[j] += *reinterpret_cast<const float4_t*>(part + slot(k) * D + 4 * j) * w;
     }
+    const bool some = total > 0.0f || total != total;
+    const float inv = some ? 1.0f / total : 0.0f;
+    uint16_t* out = a.out + token * a.out_token + head * a.out_head + lane * W;
+#pragma unroll
+    for (int j = 0; j < W / 4; ++j) {
+      const uint32_t x = pack_pair(o[j][0] * inv, o[j][1] * inv, a.bf16);
+      const uint32_t y = pack_pair(o[j][2] * inv, o[j][3] * inv, a.bf16);
+      if (a.wide_out) {
+        *reinterpret_cast<uint2*>(out + 4 * j) = make_uint2(x, y);
+      } else {
+        out[4 * j] = (uint16_t)x;
+        out[4 * j + 1] = (uint16_t)(x >> 16);
+        out[4 * j + 2] = (uint16_t)y;
+        out[4 * j + 3] = (uint16_t)(y >> 16);
+      }
+    }
+    if (a.lse && lane == 0)
+      a.lse[token * a.heads + head] =
+          some ? (most + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : kNone;
   }
-  if (a.lse && lane == 0)
-    a.lse[at] = some ? (most + __builtin_amdgcn_logf(total)) * 0.6931471805599453f : kNone;
 }
 
 // Waves of the tile kernel's workgroups, each with one tile of 32 rows.
@@ -977,19 +1221,20 @@ void launch_rows(const KvAttendArgs& a, dim3 grid, hipStream_t st) {
 
 template <int D, int FMT>
 hipError_t launch(const KvAttendArgs& a, hipStream_t st) {
-  const int rows = a.tiled ? tile_rows<D>() : kRows;
-  const int64_t tiles = a.cu ? a.tokens * a.group / rows + a.n
-                             : a.n * ((a.group + rows - 1) / rows);
-  const dim3 grid((unsigned)(tiles * a.c.kv_heads), (unsigned)a.parts);
-  if (a.tiled)
+  if (a.tiled) {
+    constexpr int ROWS = tile_rows<D>();
+    const int64_t tiles = a.tokens * a.group / ROWS + a.n;  // at most
+    const dim3 grid(a.whole ? (unsigned)(tiles * a.c.kv_heads) : kPieces);
     hipLaunchKernelGGL((kv_attend_tile<D, FMT, tile_waves<D>()>), grid,
                        dim3(tile_waves<D>() * kWave), 0, st, a);
-  else
-    launch_rows<D, FMT>(a, grid, st);
-  if (a.tiled && a.parts > 1)
-    hipLaunchKernelGGL(kv_attend_join<D>,
-                       dim3((unsigned)(tiles * a.c.kv_heads), (unsigned)(rows / kJoinRows)), dim3(256), 0, st,
-                       a, rows);
+    if (!a.whole)
+      hipLaunchKernelGGL((kv_attend_join<D, ROWS>), dim3(kPieces, ROWS / kJoinRows), dim3(256), 0,
+                         st, a);
+  } else {
+    const int64_t tiles = a.cu ? a.tokens * a.group / kRows + a.n
+                               : a.n * ((a.group + kRows - 1) / kRows);
+    launch_rows<D, FMT>(a, dim3((unsigned)(tiles * a.c.kv_heads), (unsigned)a.parts), st);
+  }
   return hipGetLastError();
 }
 
@@ -1005,7 +1250,7 @@ hipError_t launch_dim(const KvAttendArgs& a, hipStream_t st) {
 //     rows and chunk of 64 keys, the tile kernel cost_tile ns per tile and 32 keys
 //     (256 rows, 128 for 256 channels), and 20 us more for its longer start and
 //     end: 16 sequences of 128 rows over 4096 keys (8 KV heads, 128 channels) take
-//     74 us with the one and 91 us with the other, of 256 rows 137 and 99 us.
+//     78 us with the one and 105 us with the other, of 256 rows 139 and 97 us.
 //   * Few rows: parts only where there are fewer workgroups than compute units,
 //     then as many as those; each is eight waves with long runs of keys (four
 //     contexts of 131072 tokens take 175 us with 256 workgroups, 187 us with 768),
@@ -1013,8 +1258,7 @@ hipError_t launch_dim(const KvAttendArgs& a, hipStream_t st) {
 //     in one part; two add 3 us of joining). With more workgroups than compute
 //     units four waves each, without parts (256 ragged requests: 87 us, 95 us with
 //     parts of 2048 keys).
-//   * Tiles: two rounds of workgroups of unequal length, parts of 512 keys at
-//     least (a prompt of 512 rows over 2048 keys takes 34 us, 72 us without).
+//   * Tiles: see kPieces.
 KvSplit kv_attend_split(int dim, int64_t n, int64_t tokens, int heads, int kv_heads,
                         int64_t max_new, int64_t max_len) {
   KvSplit s = {};
@@ -1035,17 +1279,20 @@ KvSplit kv_attend_split(int dim, int64_t n, int64_t tokens, int heads, int kv_he
   // testable on small ones.
   const char* forced = std::getenv("SEMSCHED_KV_TILES");
   if (forced && (forced[0] == '0' || forced[0] == '1')) s.tiled = forced[0] == '1';
-  const int64_t groups = std::max<int64_t>(tiles_of(s.tiled ? tile : kRows) * kv_heads, 1);
-  int64_t want = 512, least = 8;  // workgroups, chunks of a part
-  if (!s.tiled) {
-    s.waves = groups < 256 && dim <= 128 ? 8 : 4;
-    least = 2 * s.waves;
-    // (a tile with parts needs a counter)
-    want = chunks <= 3 * s.waves || grid_of(kRows) * kv_heads > kKvCounts ? 1 : 256;
+  if (s.tiled) {
+    s.whole = tokens * group / tile * kv_heads >= kWholeRounds * kPieces;
+    if (!s.whole) s.part_rows = 2 * kPieces * tile;
+    return s;
   }
+  const int64_t groups = std::max<int64_t>(tiles_of(kRows) * kv_heads, 1);
+  s.waves = groups < 256 && dim <= 128 ? 8 : 4;
+  const int64_t least = 2 * s.waves;  // chunks of a part
+  // (a tile with parts needs a counter)
+  const int64_t want = chunks <= 3 * s.waves || grid_of(kRows) * kv_heads > kKvCounts ? 1 : 256;
   const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(want / groups, kMostParts));
   s.part_chunks = (int)std::max<int64_t>(least, (chunks + parts - 1) / parts);
   s.parts = (int)((chunks + s.part_chunks - 1) / s.part_chunks);
+  if (s.parts > 1) s.part_rows = s.parts * tokens * heads;
   return s;
 }
 
