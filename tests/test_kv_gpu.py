@@ -314,6 +314,18 @@ def test_many_sequences(ss, kernel):
                    with_cu=with_cu, max_new=1, seed=13)
 
 
+def test_rounds_of_tiles(ss, kernel):
+    """More row tiles than the device has compute units, many times over, and
+    as many equal ones as it has."""
+    print("rounds", kernel, flush=True)
+    rng = np.random.default_rng(14)
+    new = [int(x) for x in rng.integers(60, 72, 24)]
+    lens = [n + int(x) for n, x in zip(new, rng.integers(0, 40, 24))]
+    run_attend(ss, lens, new, heads=256, kv_heads=16, dim=64, pt=32, fmt=ko.INT8, seed=14)
+    run_attend(ss, [900] * 8, [16] * 8, heads=256, kv_heads=16, dim=64, pt=128, fmt=ko.FP8,
+               seed=15)
+
+
 def test_all_queries_hidden(ss, kernel):
     """A call in which no row sees a key."""
     import torch
