@@ -546,11 +546,12 @@ __global__ __launch_bounds__(NW* kWave) void kv_attend_rows(KvAttendArgs a) {
 // Codes are loaded four steps ahead and put into LDS two steps ahead. (Six or
 // eight steps ahead measured the same.)
 //
-// Bound by the matrix and vector instructions of a step together: 32 matrix
-// instructions of 16 passes and 400 vector ones per wave and 32 keys (128
-// channels). A prompt of 16384 tokens, 32 heads of 128 channels, takes 2.40 ms,
-// 918 TFLOP/s, where a large matrix product reaches 1300; before the steps
-// overlapped it took 6.07 ms.
+// Bound by the matrix and vector instructions of a step together: 16 matrix
+// instructions (512 cycles) and 150 vector ones (about 800, the 16 exponentials
+// at a quarter of the rate) per wave and 32 keys (128 channels), two waves on a
+// SIMD. The matrix cores are busy in 42% of the cycles of a prompt of 16384
+// tokens (32 heads of 128 channels): 2.40 ms, 918 TFLOP/s, where a large matrix
+// product reaches 1300; before the steps overlapped it took 6.07 ms.
 constexpr int kWide = 32;  // rows of a matrix tile, and keys of a step
 typedef float float16_t __attribute__((ext_vector_type(16)));
 
@@ -561,7 +562,7 @@ typedef float float16_t __attribute__((ext_vector_type(16)));
 // the cuts fall; tiles that are cut are joined afterwards. So no compute unit
 // waits for another, whatever the sequences' lengths, and at most two partial
 // tiles per workgroup are written. Chunks of 300 to 512 queries of four sequences
-// of 2048 to 8192 keys (32 heads, 8 KV heads, 128 channels) take 127 us, of which
+// of 2048 to 8192 keys (32 heads, 8 KV heads, 128 channels) take 118 us, of which
 // the join 15; parts of equal length dealt out in turn took 160 us, as long as
 // the longest of them.
 // Whole tiles are dealt in turn instead where that costs less by the lines'
@@ -785,6 +786,9 @@ __global__ __launch_bounds__(NW* kWave, NW / 4) void kv_attend_tile(KvAttendArgs
   const uint32_t piece = line.pieces == kPieces
                              ? blockIdx.x % 8 * (kPieces / 8) + blockIdx.x / 8
                              : blockIdx.x;
+  // One of a SIMD's two waves goes first, so that they drift into different halves
+  // of a step (the chunks at kPieces 118 us, 125 us without).
+  if (wave >= 4) __builtin_amdgcn_s_setprio(1);
   uint64_t turn = blockIdx.x, x0 = 0, x1 = 0;
   Place at;
   if (line.dealt) {
