@@ -345,6 +345,9 @@ __global__ __launch_bounds__(AW* kWave) void kv_append(KvAppendArgs a) {
   const int64_t fresh = a.cu ? (int64_t)a.cu[i + 1] - row : 1;
   const int32_t s = a.seqs[i];
   const bool leader = threadIdx.x == 0 && blockIdx.y == 0;
+  if (a.cu && u == 0 && leader && (a.cu[0] != 0 || a.cu[a.n] != a.tokens))
+    atomicOr(c.flags, kFlagInval);
+  if (a.cu && u < append_start(a, i)) return;  // offsets that do not begin with 0
   if (fresh <= 0) {
     if (fresh < 0 && leader) atomicOr(c.flags, kFlagInval);
     return;

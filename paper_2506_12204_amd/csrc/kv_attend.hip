@@ -63,6 +63,7 @@ __device__ __forceinline__ bool find_tile(const KvAttendArgs& a, uint32_t u, int
       if (at + lane < a.n) {
         const int64_t fresh = (int64_t)a.cu[at + lane + 1] - a.cu[at + lane];
         if (fresh > 0 && fresh <= a.tokens) mine = (uint32_t)((fresh * a.group + rows - 1) / rows);
+        else if (fresh != 0 && blockIdx.x == 0) atomicOr(c.flags, kFlagInval);
       }
       const uint32_t upto = before + wave_incl_scan_u32(mine);
       const uint64_t beyond = __ballot(upto > u);
@@ -100,7 +101,8 @@ __device__ __forceinline__ void find_keys(const KvAttendArgs& a, Sequence& q) {
   const bool known = (uint32_t)s < (uint32_t)c.slots;
   q.table = c.tables + (known ? (int64_t)s * c.max_blocks : 0);
   q.len = known ? c.lens[s] : -1;
-  if (q.len < 0 || (int64_t)q.len > ((int64_t)c.max_blocks << c.page_shift)) {
+  if (q.len < 0 || (int64_t)q.len > ((int64_t)c.max_blocks << c.page_shift) ||
+      (q.len > 0 && c.num_pages == 0)) {
     if (threadIdx.x == 0) atomicOr(c.flags, kFlagInval);
     q.len = 0;
   }
@@ -607,7 +609,8 @@ __device__ __forceinline__ Share share_of(const KvAttendArgs& a, int64_t i) {
   s.slot = known ? slot : 0;
   bool wrong = fresh < 0 || row0 < 0 || row0 + fresh > a.tokens;
   if (!wrong) s.tiles = (uint32_t)((fresh * a.group + ROWS - 1) / ROWS);
-  if (len < 0 || len > ((int64_t)c.max_blocks << c.page_shift)) {
+  if (len < 0 || len > ((int64_t)c.max_blocks << c.page_shift) ||
+      (len > 0 && c.num_pages == 0)) {
     wrong |= s.tiles > 0;
     len = 0;
   }

@@ -306,8 +306,13 @@ __global__ __launch_bounds__(ST) void kv_compact_plan(KvCompactArgs a) {
   const KvView& c = a.c;
   const int t = threadIdx.x;
   const int64_t words = (c.num_pages + 31) >> 5;
+  // (bits past the last page are not pages, whatever they hold)
+  auto live_word = [&](int64_t w) {
+    const uint32_t all = (w + 1) * 32 > c.num_pages ? (1u << (c.num_pages & 31)) - 1u : ~0u;
+    return c.live[w] & all;
+  };
   uint32_t mine = 0;
-  for (int64_t w = t; w < words; w += ST) mine += (uint32_t)__popc(c.live[w]);
+  for (int64_t w = t; w < words; w += ST) mine += (uint32_t)__popc(live_word(w));
   uint32_t alive;
   block_excl_scan_u32<ST>(mine, scratch, alive);
   uint32_t holes = 0, far = 0;
@@ -317,7 +322,7 @@ __global__ __launch_bounds__(ST) void kv_compact_plan(KvCompactArgs a) {
     const int64_t w = w0 + t;
     uint32_t hole = 0, high = 0, dead = 0;
     if (w < words) {
-      const uint32_t live = c.live[w];
+      const uint32_t live = live_word(w);
       const int64_t first = w * 32;
       const uint32_t below = first + 32 <= (int64_t)alive ? ~0u
                              : first >= (int64_t)alive    ? 0u

@@ -796,3 +796,83 @@ def test_eviction_carried_out(ss):
     assert c.lens.tolist() == want
     used = sum(-(-n // 16) for n in want)
     assert c.refs.tolist() == [1] * used + [0] * (24 - used)
+
+
+def test_errors_of_either_attention_kernel(ss, kernel):
+    """Sequences, offsets, page numbers and lengths outside the cache."""
+    import torch
+    print("attention errors", kernel, flush=True)
+    q = torch.ones(40, 2, 64, dtype=torch.float16, device="cuda")
+
+    def fresh():
+        c = ss.KVCache(8, 4, 4, layers=1, kv_heads=1, head_dim=64, page_tokens=16)
+        c.data.zero_()
+        c.reserve(i32([0, 1]), i32([50, 40]))
+        c.check()
+        return c
+
+    for name, seqs, cu in (("a slot beyond", [0, 9], [0, 10, 40]),
+                           ("a negative slot", [-1, 1], [0, 10, 40]),
+                           ("offsets past the rows", [0, 1], [0, 10, 90]),
+                           ("offsets that fall", [0, 1], [0, 50, 40]),
+                           ("offsets from 5", [0, 1], [5, 10, 40]),
+                           ("negative offsets", [0, 1], [-5, 10, 40]),
+                           ("offsets that end early", [0, 1], [0, 10, 30])):
+        print(" ", name, flush=True)
+        c = fresh()
+        c.attend(0, q, i32(seqs), i32(cu))
+        with pytest.raises(ss.SemschedError):
+            c.check()
+    for name, change in (("page", lambda c: c.tables[0, 1].fill_(1 << 30)),
+                         ("negative page", lambda c: c.tables[0, 1].fill_(-7)),
+                         ("length", lambda c: c.lens[0].fill_(65)),
+                         ("negative length", lambda c: c.lens[0].fill_(-1))):
+        print(" ", name, flush=True)
+        c = fresh()
+        change(c)
+        c.attend(0, q, i32([0, 1]), i32([0, 20, 40]))
+        with pytest.raises(ss.SemschedError):
+            c.check()
+    # a cache without pages
+    c = ss.KVCache(0, 2, 2, layers=1, kv_heads=1, head_dim=64, page_tokens=16)
+    out = c.attend(0, q, i32([0, 1]), i32([0, 20, 40]))
+    c.check()
+    assert (out == 0).all()
+    c.lens.fill_(3)
+    c.attend(0, q, i32([0, 1]), i32([0, 20, 40]))
+    with pytest.raises(ss.SemschedError):
+        c.check()
+
+
+@pytest.mark.parametrize("cu", [[33, 38], [3, 5], [0, 1], [0, 45], [-2, 5], [5, 0]])
+def test_append_of_bad_offsets(ss, cu):
+    """Reported, with nothing written outside the sequences' own pages."""
+    import torch
+    print("append offsets", cu, flush=True)
+    c = ss.KVCache(8, 3, 4, layers=1, kv_heads=1, head_dim=64, page_tokens=16)
+    c.data.zero_()
+    c.reserve(i32([0, 1, 2]), i32([20, 20, 20]))
+    c.check()
+    x = torch.ones(40, 1, 64, dtype=torch.bfloat16, device="cuda")
+    c.append(0, x, x, i32([1]), i32(cu))
+    with pytest.raises(ss.SemschedError):
+        c.check()
+    own = set(c.tables[1].tolist())
+    for page in range(8):
+        if page not in own:
+            assert (c.data[page] == 0).all() and (c.scale[page] == 0).all(), page
+
+
+def test_compact_reads_no_bits_past_the_pages(ss):
+    import torch
+    print("live bits", flush=True)
+    c = ss.KVCache(5, 3, 4, layers=1, kv_heads=1, head_dim=64, page_tokens=16)
+    c.data.copy_(torch.arange(5, dtype=torch.uint8, device="cuda")[:, None].expand_as(c.data))
+    c.reserve(i32([0, 1, 2]), i32([16, 32, 16]))
+    c.free(i32([1]))
+    c.live[0] |= 0x00f00000
+    c.compact()
+    c.check()
+    assert c.tables[0, 0].item() == 0 and c.tables[2, 0].item() == 1
+    assert c.refs.tolist() == [1, 1, 0, 0, 0] and c.live[0].item() & 31 == 3
+    assert (c.data[1] == 3).all()
