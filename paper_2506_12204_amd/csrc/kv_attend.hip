@@ -32,6 +32,10 @@ constexpr int kRows = 16;            // rows of a tile: a token and a head each
 constexpr int kChunk = 64;           // keys a wave takes at a time
 constexpr float kLift = 64.0f;       // 2^6
 constexpr float kNone = -__builtin_inff();
+// What the largest V scale met starts from, the least normal number: the
+// reciprocal of a smaller one is not finite, and blocks of such scales (of values
+// below 3.7e-37) count relative to this one.
+constexpr float kLeastScale = 0x1p-126f;
 constexpr int kMostParts = 128;      // of the key axis
 // The running maximum is raised only when a score passes it by this much (in
 // powers of two), which is seldom: most steps then need no rescaling of the
@@ -334,7 +338,7 @@ __global__ __launch_bounds__(NW* kWave) void kv_attend_rows(KvAttendArgs a) {
   if (part >= parts) return;
   const int begin = part_start(c0, c1, parts, part), stop = part_start(c0, c1, parts, part + 1);
 
-  float m = kNone, l = 0.0f, vref = 0.0f;
+  float m = kNone, l = 0.0f, vref = kLeastScale;
   float4_t acc[D / 16];
 #pragma unroll
   for (int y = 0; y < D / 16; ++y) acc[y] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
@@ -433,7 +437,7 @@ __global__ __launch_bounds__(NW* kWave) void kv_attend_rows(KvAttendArgs a) {
     // weights are relative to the largest V scale so far
     float vmax = fmaxf(vs, __shfl_xor(vs, 16, kWave));
     vmax = fmaxf(fmaxf(vmax, other_half(vmax)), vref);
-    const float inv = vmax > 0.0f ? __builtin_amdgcn_rcpf(vmax) : 0.0f;
+    const float inv = __builtin_amdgcn_rcpf(vmax);
     const bool raise = top > m + kSlack;
     const float next = raise ? top : m;
     const float shrink = raise ? __builtin_amdgcn_exp2f(m - next) : 1.0f;
@@ -473,10 +477,9 @@ __global__ __launch_bounds__(NW* kWave) void kv_attend_rows(KvAttendArgs a) {
       join_m[wave][r] = m;
       join_l[wave][r] = l;
     }
-    const float by = vref * (1.0f / kLift);
 #pragma unroll
     for (int y = 0; y < D / 16; ++y) {
-      const float4_t o = acc[y] * by;
+      const float4_t o = acc[y] * (1.0f / kLift) * vref;  // (their product may not be normal)
       *reinterpret_cast<float4_t*>(&join_o[wave][r][y * 16 + g * 4]) = o;
     }
   }
@@ -921,7 +924,7 @@ __global__ __launch_bounds__(NW* kWave, NW / 4) void kv_attend_tile(KvAttendArgs
 
     half8_t query[KS];
     float factor = 0.0f;
-    float m = kNone, l = 0.0f, vref = 0.0f;
+    float m = kNone, l = 0.0f, vref = kLeastScale;
     float16_t acc[DY], s0, s1;
     half8_t w0[2], w1[2];
 #pragma unroll
@@ -978,7 +981,7 @@ __global__ __launch_bounds__(NW* kWave, NW / 4) void kv_attend_tile(KvAttendArgs
       score(0, kf[0], nxt);
       // weights are relative to the largest V scale so far (the same in all lanes)
       const float vmax = fmaxf(fmaxf(vs0, vs1), vref);
-      const float inv = vmax > 0.0f ? __builtin_amdgcn_rcpf(vmax) : 0.0f;
+      const float inv = __builtin_amdgcn_rcpf(vmax);
       const float rel = fmaxf((h ? vs1 : vs0) * inv, 9.3e-10f) * kLift;  // (2^-30)
       const float unrel = __builtin_amdgcn_rcpf(rel);
       // (not zero, so that a hidden key's minus infinity stays one)
@@ -1089,15 +1092,14 @@ __global__ __launch_bounds__(NW* kWave, NW / 4) void kv_attend_tile(KvAttendArgs
     if (!whole) {
       // a piece's first tile and its last one may be cut
       const int64_t slot = (int64_t)(2 * piece + (x0 == at.start)) * ROWS + wave * kWide + r;
-      const float by = vref * (1.0f / kLift);
       float* o = a.part_o + slot * D;
 #pragma unroll
       for (int y = 0; y < DY; ++y)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const float4_t x = {acc[y][4 * k] * by, acc[y][4 * k + 1] * by, acc[y][4 * k + 2] * by,
-                              acc[y][4 * k + 3] * by};
-          *reinterpret_cast<float4_t*>(o + y * 32 + k * 8 + h * 4) = x;
+          const float4_t x = {acc[y][4 * k], acc[y][4 * k + 1], acc[y][4 * k + 2],
+                              acc[y][4 * k + 3]};
+          *reinterpret_cast<float4_t*>(o + y * 32 + k * 8 + h * 4) = x * (1.0f / kLift) * vref;
         }
       if (h == 0) {
         a.part_ml[2 * slot] = m;
@@ -1108,7 +1110,7 @@ __global__ __launch_bounds__(NW* kWave, NW / 4) void kv_attend_tile(KvAttendArgs
                               (int32_t)q.row0, rows, tile, kh};
     } else {
       const bool some = l > 0.0f || l != l;
-      const float inv = some ? vref * (1.0f / kLift) / l : 0.0f;
+      const float inv = some ? (1.0f / kLift) / l : 0.0f;
       // through LDS, so that rows are written whole
       uint2* const mine = reinterpret_cast<uint2*>(pool + (wave * kWide + r) * PITCH);
 #pragma unroll
@@ -1116,8 +1118,9 @@ __global__ __launch_bounds__(NW* kWave, NW / 4) void kv_attend_tile(KvAttendArgs
 #pragma unroll
         for (int k = 0; k < 4; ++k)
           mine[y * 8 + k * 2 + h] =
-              make_uint2(pack_pair(acc[y][4 * k] * inv, acc[y][4 * k + 1] * inv, a.bf16),
-                         pack_pair(acc[y][4 * k + 2] * inv, acc[y][4 * k + 3] * inv, a.bf16));
+              make_uint2(pack_pair(acc[y][4 * k] * inv * vref, acc[y][4 * k + 1] * inv * vref, a.bf16),
+                         pack_pair(acc[y][4 * k + 2] * inv * vref, acc[y][4 * k + 3] * inv * vref,
+                                   a.bf16));
       if (a.lse && h == 0 && live)
         a.lse[(q.row0 + token) * a.heads + head] =
             some ? (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : kNone;

@@ -876,3 +876,56 @@ def test_compact_reads_no_bits_past_the_pages(ss):
     assert c.tables[0, 0].item() == 0 and c.tables[2, 0].item() == 1
     assert c.refs.tolist() == [1, 1, 0, 0, 0] and c.live[0].item() & 31 == 3
     assert (c.data[1] == 3).all()
+
+
+@pytest.mark.parametrize("fmt", [ko.INT8, ko.FP8])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("tiny", [2.0 ** -128, 1e-40, 2.0 ** -149])
+def test_scales_without_a_finite_reciprocal(ss, kernel, fmt, dim, tiny):
+    """V scales that are not normal numbers, on the first pages of a sequence, on
+    all of them, on its only key. An output is then off by what it is of normal
+    scales, and by the least normal number, which is what outputs may be cut to."""
+    import torch
+    print("tiny scales", kernel, fmt, dim, tiny, flush=True)
+    for new in (1, 40):
+        lens = [300, 260, max(new, 1), 90]
+        case = Case(ss, lens, fmt=fmt, dim=dim, pt=32, kv_heads=1, seed=21)
+        case.scale[case.tables[0, :3], :, 1] = tiny
+        case.scale[case.tables[1, :9], :, 1] = tiny
+        case.scale[case.tables[2, :2], :, 1] = tiny
+        case.scale[case.tables[3, 2], :, 1] = tiny
+        case.c.scale.copy_(torch.from_numpy(case.scale))
+        q = case.queries([new] * 4, 4, torch.bfloat16)
+        lse = torch.empty(4 * new, 4, device="cuda")
+        out = case.c.attend(1, q, i32(range(4)), i32(np.arange(5) * new), lse=lse)
+        case.c.check()
+        case.check(q, [new] * 4, out, lse, dim ** -0.5, True, 0)
+        for s in (1, 2):  # what check's absolute term hides: the tiny values themselves
+            k, v = (ko.read(case.data, case.scale, case.geom, case.tables[s], lens[s], 1, w, 0)
+                    for w in (0, 1))
+            for h in range(4):
+                rows = slice(s * new, (s + 1) * new)
+                want, _, mag = ko.attend(q[rows, h].double().cpu().numpy(), k, v, dim ** -0.5,
+                                         True, 0)
+                tol = 2 * (2.0 ** -9 * np.abs(want) + (2.0 ** -12 + 2.0 ** -14) * mag) + 2.0 ** -126
+                assert (np.abs(out[rows, h].double().cpu().numpy() - want) <= tol).all(), (s, h)
+
+
+def test_appended_values_below_the_normal_scales(ss, kernel):
+    """What append writes for values of 2^-121 at most, read back."""
+    import torch
+    print("tiny values", kernel, flush=True)
+    for fmt in (ss.KV_INT8, ss.KV_FP8):
+        c = ss.KVCache(8, 1, 8, layers=1, kv_heads=1, head_dim=64, page_tokens=16, format=fmt)
+        gen = torch.Generator("cuda").manual_seed(7)
+        k = torch.randn(50, 1, 64, generator=gen, device="cuda").bfloat16()
+        v = (torch.rand(50, 1, 64, generator=gen, device="cuda") * 2.0 ** -121).bfloat16()
+        c.reserve(i32([0]), i32([50]))
+        c.append(0, k, v, i32([0]), i32([0, 50]))
+        assert (c.scale[c.tables[0, :4].long(), 0, 1] < 2.0 ** -126).all()
+        out = c.attend(0, torch.zeros_like(k), i32([0]), i32([0, 50]))  # means of the values
+        c.check()
+        want = v.double().cumsum(0) / torch.arange(1, 51, device="cuda")[:, None, None]
+        # half a code's step (of 127, or of 8 to the power of two), the output's rounding, the least normal
+        step = 2.0 ** -121 * (2.0 ** -8 if fmt == ss.KV_INT8 else 2.0 ** -4)
+        assert ((out.double() - want).abs() <= step + 2.0 ** -8 * want + 2.0 ** -126).all()
