@@ -618,6 +618,11 @@ class KVCache:
     the last check. A step is: ``reserve`` room for the new tokens, then for
     every layer ``append`` their keys and values and ``attend``. Lists of
     sequences are int32 GPU tensors that name each at most once.
+
+    Operations may be captured into a graph. ``attend`` takes a larger workspace
+    where its sizes need one, which it refuses to do while capturing: call it
+    with the same sizes once before. A workspace that was replaced stays
+    allocated, for the graphs that were captured with it.
     """
 
     def __init__(self, num_pages: int, slots: int, max_blocks: int, *, layers: int, kv_heads: int,
@@ -671,6 +676,7 @@ class KVCache:
         self.ws_bytes = int(lib.sem_kv_workspace_bytes(self._ref))
         self.workspace = torch.zeros(self.ws_bytes, dtype=torch.uint8, device=self.device)
         self._ws, self._index = self.workspace.data_ptr(), data.get_device()
+        self._replaced = []  # earlier workspaces, whose addresses captured graphs may hold
         self._needs = {}  # workspace bytes of attention by its sizes
 
     # The operations are called for every layer of every step, so their checks
@@ -701,14 +707,18 @@ class KVCache:
         return dtype
 
     def _room(self, need: int) -> None:
-        """A larger workspace, the status word carried over."""
-        if need > self.ws_bytes:
-            ws = torch.zeros(need, dtype=torch.uint8, device=self.device)
-            ws[:4].copy_(self.workspace[:4])  # (the rest of its first bytes is zero between calls)
-            # (work in flight on another stream than the old one's may still use it)
-            self.workspace.record_stream(torch.cuda.current_stream(self.device))
-            self.workspace, self.ws_bytes = ws, need
-            self._ws = ws.data_ptr()
+        """A larger workspace, at least twice as large (so that all that were
+        replaced take no more than the last)."""
+        if need <= self.ws_bytes:
+            return
+        if torch.cuda.is_current_stream_capturing():
+            # (it would lie in the graph's pool, and be zeroed by replays only)
+            raise RuntimeError(f"attention of these sizes needs a workspace of {need} bytes, which "
+                               "cannot be taken while a graph is captured: call it once before")
+        ws = torch.zeros(max(need, 2 * self.ws_bytes), dtype=torch.uint8, device=self.device)
+        self._replaced.append(self.workspace)
+        self.workspace, self.ws_bytes = ws, ws.numel()
+        self._ws = ws.data_ptr()
 
     def reserve(self, seqs: torch.Tensor, tokens: torch.Tensor) -> None:
         """Room for tokens[i] more tokens of seqs[i] (their lengths grow)."""
@@ -811,7 +821,10 @@ class KVCache:
     def check(self) -> None:
         """Waits for the current stream; raises on an error of any operation
         since the last check."""
-        code = lib.sem_check(self._ws, _raw_stream(self._index))
-        if code != SEM_OK:
-            self.workspace[:4].zero_()
+        code = SEM_OK
+        for ws in (*self._replaced, self.workspace):  # (graphs report to the one they know)
+            rc = lib.sem_check(ws.data_ptr(), _raw_stream(self._index))
+            if rc != SEM_OK:
+                ws[:4].zero_()
+                code = code or rc
         _raise(code, "KVCache")

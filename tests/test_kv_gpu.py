@@ -929,3 +929,103 @@ def test_appended_values_below_the_normal_scales(ss, kernel):
         # half a code's step (of 127, or of 8 to the power of two), the output's rounding, the least normal
         step = 2.0 ** -121 * (2.0 ** -8 if fmt == ss.KV_INT8 else 2.0 ** -4)
         assert ((out.double() - want).abs() <= step + 2.0 ** -8 * want + 2.0 ** -126).all()
+
+
+def test_a_graph_outlives_a_larger_workspace(ss, monkeypatch):
+    """Steps of a captured graph before and after an eager call that needs a larger
+    workspace: the graph's results stay right, nobody else's memory changes, and
+    its errors are still reported."""
+    import torch
+    print("graph and growth", flush=True)
+
+    def fresh():
+        c = ss.KVCache(512, 3, 128, layers=1, kv_heads=1, head_dim=64, page_tokens=16)
+        gen = torch.Generator("cuda").manual_seed(8)
+        kv = torch.randn(2, 3000, 1, 64, generator=gen, device="cuda").bfloat16()
+        c.reserve(seqs, i32([1900, 1000, 100]))
+        c.append(0, kv[0], kv[1], seqs, i32([0, 1900, 2900, 3000]))
+        return c
+
+    seqs, one = i32([0, 1, 2]), i32([1, 1, 1])
+    x = torch.randn(3, 4, 64, device="cuda").bfloat16()
+    prompt = torch.randn(600, 2, 64, device="cuda").bfloat16()
+    out = torch.empty(3, 2, 64, dtype=torch.bfloat16, device="cuda")
+
+    def step(c):  # (the key axis is split: counters and parts lie in the workspace)
+        c.reserve(seqs, one)
+        c.append(0, x[:, 2:3], x[:, 3:], seqs)
+        c.attend(0, x[:, :2], seqs, out=out)
+
+    want, c = [], fresh()
+    for _ in range(6):
+        step(c)
+        want.append((out.clone(), c.book.clone()))
+
+    def by_tiles(c):  # its partial outputs need more
+        with monkeypatch.context() as m:
+            m.setenv("SEMSCHED_KV_TILES", "1")
+            return c.attend(0, prompt, i32([0]), i32([0, 600])).clone()
+
+    large = by_tiles(c)
+    c.check()
+
+    c = fresh()
+    step(c)  # takes the workspace that the graph is captured with
+    torch.cuda.synchronize()
+    assert torch.equal(out, want[0][0])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(c)
+    others, small = [], c.ws_bytes
+    for k in range(1, 6):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[k][0]) and torch.equal(c.book, want[k][1]), k
+        if k == 2:
+            by_tiles(c)
+            assert c.ws_bytes > small
+        # the program's own tensors, of the sizes of either workspace
+        others += [torch.full((n,), 3, dtype=torch.uint8, device="cuda")
+                   for n in (small, small // 2, c.ws_bytes)]
+    assert torch.equal(by_tiles(c), large)
+    c.check()
+    assert all((t == 3).all() for t in others)
+    c.lens[2] = 128 * 16  # its table is full: the graph's reserve has no room
+    graph.replay()
+    with pytest.raises(ss.SemschedError) as e:
+        c.check()
+    assert e.value.code == ss.SEM_EINVAL
+    c.check()  # reported once
+
+
+def test_no_larger_workspace_while_capturing(ss, monkeypatch):
+    """Refused with the capture unharmed; the call goes into a graph once its
+    workspace is there."""
+    import torch
+    print("growth in capture", flush=True)
+    monkeypatch.setenv("SEMSCHED_KV_TILES", "1")  # (partial outputs for every compute unit)
+    c = ss.KVCache(64, 1, 64, layers=1, kv_heads=1, head_dim=64, page_tokens=16)
+    q = torch.randn(900, 2, 64, device="cuda").bfloat16()
+    c.reserve(i32([0]), i32([900]))
+    c.append(0, q[:, :1], q[:, 1:], i32([0]), i32([0, 900]))
+    seqs, cu, out, x = i32([0]), i32([0, 900]), torch.empty_like(q), torch.zeros(4, device="cuda")
+    torch.cuda.synchronize()
+    before, graph = c.workspace, torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        x += 1
+        with pytest.raises(RuntimeError, match="captured"):
+            c.attend(0, q, seqs, cu, out=out)
+    assert c.workspace is before
+    graph.replay()
+    assert (x == 1).all()
+    want = c.attend(0, q, seqs, cu).clone()
+    c.check()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.attend(0, q, seqs, cu, out=out)
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+    c.check()

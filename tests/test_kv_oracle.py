@@ -2,7 +2,9 @@
 checks of KV cache arguments (no GPU is touched by any call here)."""
 
 import ctypes
+import gc
 import math
+import weakref
 
 import numpy as np
 import pytest
@@ -158,3 +160,32 @@ def test_binding_refuses_cpu_tensors_and_sizes(ss):
     with pytest.raises(TypeError):
         ss.KVCache(4, 2, 2, layers=1, kv_heads=1, head_dim=64, device="cpu",
                    book=torch.zeros(4, dtype=torch.int64))
+
+
+def test_a_replaced_workspace_stays_allocated(ss, monkeypatch):
+    """Graphs hold the address of the workspace that they were captured with; a
+    larger one is not taken while capturing."""
+    torch = pytest.importorskip("torch")
+    capturing = False
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing)
+    c = ss.KVCache.__new__(ss.KVCache)  # (no device here: the workspace alone)
+    c.device, c.ws_bytes, c._replaced = torch.device("cpu"), 8192, []
+    c.workspace = torch.full((8192,), 5, dtype=torch.uint8)
+    c._ws = c.workspace.data_ptr()
+    first = weakref.ref(c.workspace)
+    capturing = True
+    with pytest.raises(RuntimeError):
+        c._room(8193)
+    assert c.workspace is first() and c.ws_bytes == 8192
+    c._room(8192)  # large enough: nothing is taken
+    assert c.workspace is first()
+    capturing = False
+    need = 8192
+    for _ in range(5):
+        need += 1000
+        c._room(need)
+        assert c.ws_bytes == c.workspace.numel() >= need and c._ws == c.workspace.data_ptr()
+        assert (c.workspace == 0).all()
+    gc.collect()
+    assert first() is not None and (first() == 5).all()
+    assert sum(w.numel() for w in c._replaced) <= c.ws_bytes
