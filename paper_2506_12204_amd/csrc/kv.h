@@ -66,6 +66,7 @@ struct KvAppendArgs {
   int32_t layer;
   int32_t bf16;  // else IEEE half
   int32_t wide;  // 16-byte loads are aligned
+  uint32_t units;  // of work (set by the launch); workgroups behind them check offsets
 };
 
 // A row tile whose keys went to several of attention's pieces.

@@ -1029,3 +1029,23 @@ def test_no_larger_workspace_while_capturing(ss, monkeypatch):
         torch.cuda.synchronize()
         assert torch.equal(out, want)
     c.check()
+
+
+@pytest.mark.parametrize("cu", [[0, 100, 50, 120], [0, 100, 100, 20, 120], [0, 40, 10, 30, 120],
+                                [0, 60, 120, 119, 120], list(range(0, 71)) + [10, 40, 120]])
+def test_append_of_offsets_that_fall(ss, cu):
+    """Wherever they do, with the ends and every other sequence's rows in order."""
+    print("append, falling offsets", len(cu), flush=True)
+    import torch
+    n = len(cu) - 1
+    c = ss.KVCache(16 * n, n, 16, layers=1, kv_heads=1, head_dim=64, page_tokens=16)
+    c.reserve(i32(range(n)), i32([120] * n))
+    c.check()
+    x = torch.ones(120, 1, 64, dtype=torch.bfloat16, device="cuda")
+    c.append(0, x, x, i32(range(n)), i32(cu))
+    with pytest.raises(ss.SemschedError) as e:
+        c.check()
+    assert e.value.code == ss.SEM_EINVAL
+    # the same cache takes offsets that do not
+    c.append(0, x, x, i32(range(n)), i32(sorted(cu)))
+    c.check()
