@@ -93,6 +93,7 @@ struct KvAttendArgs {
   int32_t waves;       // of the other kernel's workgroups, 4 or 8
   int32_t parts;       // most parts that the keys of a row tile are split into,
   int32_t part_chunks; // of so many chunks of 64 keys each
+  uint32_t tiles;      // its row tiles (set by the launch); workgroups behind them check offsets
   uint32_t* counts;    // [kKvCounts] parts finished, zero between calls
   // partial outputs, [parts][tokens * heads] rows or, tiled, two tiles per piece
   float* part_o;   // [rows][head_dim]

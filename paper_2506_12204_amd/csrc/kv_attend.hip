@@ -67,7 +67,6 @@ __device__ __forceinline__ bool find_tile(const KvAttendArgs& a, uint32_t u, int
       if (at + lane < a.n) {
         const int64_t fresh = (int64_t)a.cu[at + lane + 1] - a.cu[at + lane];
         if (fresh > 0 && fresh <= a.tokens) mine = (uint32_t)((fresh * a.group + rows - 1) / rows);
-        else if (fresh != 0 && blockIdx.x == 0) atomicOr(c.flags, kFlagInval);
       }
       const uint32_t upto = before + wave_incl_scan_u32(mine);
       const uint64_t beyond = __ballot(upto > u);
@@ -312,6 +311,14 @@ __global__ __launch_bounds__(NW* kWave) void kv_attend_rows(KvAttendArgs a) {
   const KvView& c = a.c;
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int r = lane % 16, g = lane / 16;
+  // The workgroups behind the tiles look for offsets that fall, as a tile's own
+  // search ends where it finds the tile.
+  if (blockIdx.x >= a.tiles) {
+    const int64_t pair = (int64_t)(blockIdx.x - a.tiles) * (NW * kWave) + threadIdx.x;
+    if (blockIdx.y == 0 && pair < a.n && a.cu[pair + 1] < a.cu[pair])
+      atomicOr(c.flags, kFlagInval);
+    return;
+  }
   // heads side by side: the dies take workgroups in turn, and so get an equal
   // share of every sequence
   const int kh = blockIdx.x % c.kv_heads;
@@ -1222,7 +1229,12 @@ template <int D>
 constexpr int tile_rows() { return tile_waves<D>() * kWide; }
 
 template <int D, int FMT>
-void launch_rows(const KvAttendArgs& a, dim3 grid, hipStream_t st) {
+void launch_rows(KvAttendArgs a, hipStream_t st) {
+  const int64_t tiles = a.cu ? a.tokens * a.group / kRows + a.n  // at most
+                             : a.n * ((a.group + kRows - 1) / kRows);
+  const int64_t checks = a.cu ? (a.n + a.waves * kWave - 1) / (a.waves * kWave) : 0;
+  a.tiles = (uint32_t)(tiles * a.c.kv_heads);
+  const dim3 grid((unsigned)(a.tiles + checks), (unsigned)a.parts);
   if (D <= 128 && a.waves == 8)
     hipLaunchKernelGGL((kv_attend_rows<D, FMT, D <= 128 ? 8 : 4>), grid, dim3(8 * kWave), 0, st, a);
   else
@@ -1241,9 +1253,7 @@ hipError_t launch(const KvAttendArgs& a, hipStream_t st) {
       hipLaunchKernelGGL((kv_attend_join<D, ROWS>), dim3(kPieces, ROWS / kJoinRows), dim3(256), 0,
                          st, a);
   } else {
-    const int64_t tiles = a.cu ? a.tokens * a.group / kRows + a.n
-                               : a.n * ((a.group + kRows - 1) / kRows);
-    launch_rows<D, FMT>(a, dim3((unsigned)(tiles * a.c.kv_heads), (unsigned)a.parts), st);
+    launch_rows<D, FMT>(a, st);
   }
   return hipGetLastError();
 }

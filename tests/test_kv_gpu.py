@@ -1049,3 +1049,25 @@ def test_append_of_offsets_that_fall(ss, cu):
     # the same cache takes offsets that do not
     c.append(0, x, x, i32(range(n)), i32(sorted(cu)))
     c.check()
+
+
+@pytest.mark.parametrize("at", [1, 40, 63, 64, 65, 70, 149, 299])
+@pytest.mark.parametrize("by", [1, 30])
+def test_attention_of_offsets_that_fall(ss, kernel, at, by):
+    """At any sequence of many, with the ends in order."""
+    import torch
+    print("attention, falling offsets", kernel, at, by, flush=True)
+    n = 300
+    c = ss.KVCache(n, n, 1, layers=1, kv_heads=1, head_dim=64, page_tokens=16)
+    c.data.zero_()
+    c.reserve(i32(range(n)), i32([16] * n))
+    cu = np.arange(n + 1)
+    cu[at] = max(cu[at + 1] + by if at < n - 1 else cu[at - 1] - by, 0)
+    assert (np.diff(cu) < 0).any()
+    q = torch.ones(n, 2, 64, dtype=torch.float16, device="cuda")
+    c.attend(0, q, i32(range(n)), i32(np.arange(n + 1)))
+    c.check()
+    c.attend(0, q, i32(range(n)), i32(cu))
+    with pytest.raises(ss.SemschedError) as e:
+        c.check()
+    assert e.value.code == ss.SEM_EINVAL
