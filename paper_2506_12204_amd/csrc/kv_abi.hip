@@ -128,6 +128,7 @@ int check_rows(const sem_kv_cache* c, int32_t layer, const int32_t* seqs, const 
   if (rc != SEM_OK) return rc;
   if (layer < 0 || layer >= c->layers || tokens < 0 || tokens > INT32_MAX) return SEM_EINVAL;
   if (!cu && tokens != n) return SEM_EINVAL;  // without offsets one token each
+  if (n == 0 && tokens > 0) return SEM_EINVAL;  // rows of no sequence
   return SEM_OK;
 }
 

@@ -416,7 +416,7 @@ void launch_format(const KvAppendArgs& a, dim3 grid, hipStream_t st) {
 }  // namespace
 
 hipError_t launch_kv_append(const KvAppendArgs& args, hipStream_t st) {
-  if (args.n == 0 || args.tokens == 0) return hipSuccess;
+  if (args.n == 0) return hipSuccess;  // (without tokens the offsets are looked at)
   KvAppendArgs a = args;
   const int64_t units = a.cu ? (a.tokens >> a.c.page_shift) + 2 * a.n : a.n;
   const int64_t checks = a.cu ? (a.n + AW * kWave - 1) / (AW * kWave) : 0;

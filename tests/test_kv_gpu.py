@@ -1071,3 +1071,28 @@ def test_attention_of_offsets_that_fall(ss, kernel, at, by):
     with pytest.raises(ss.SemschedError) as e:
         c.check()
     assert e.value.code == ss.SEM_EINVAL
+
+
+def test_rows_and_sequences_that_do_not_match(ss, kernel):
+    """Rows of no sequence; sequences without rows whose offsets say otherwise."""
+    import torch
+    print("rows and sequences", kernel, flush=True)
+    c = ss.KVCache(8, 4, 4, layers=1, kv_heads=1, head_dim=64, page_tokens=16)
+    c.data.zero_()
+    c.reserve(i32([0, 1]), i32([20, 5]))
+    x = torch.ones(3, 2, 64, dtype=torch.float16, device="cuda")
+    calls = (lambda m, seqs, cu: c.attend(0, x[:m], i32(seqs), i32(cu)),
+             lambda m, seqs, cu: c.append(0, x[:m, :1], x[:m, 1:], i32(seqs), i32(cu)))
+    for call in calls:
+        with pytest.raises(ss.SemschedError) as e:
+            call(3, [], [0])
+        assert e.value.code == ss.SEM_EINVAL
+        for cu in ([0, 0, 3], [0, 5, 0], [-2, 0, 0], [3, 3, 3]):
+            call(0, [0, 1], cu)
+            with pytest.raises(ss.SemschedError) as e:
+                c.check()
+            assert e.value.code == ss.SEM_EINVAL, cu
+        call(0, [0, 1], [0, 0, 0])
+        call(0, [], [0])
+        c.check()
+    assert (c.data == 0).all() and (c.scale == 0).all()

@@ -189,3 +189,12 @@ def test_a_replaced_workspace_stays_allocated(ss, monkeypatch):
     gc.collect()
     assert first() is not None and (first() == 5).all()
     assert sum(w.numel() for w in c._replaced) <= c.ws_bytes
+
+
+def test_rows_of_no_sequence_are_refused(ss):
+    fake = ctypes.c_void_p(1 << 40)
+    c = cache(ss)
+    q = ss.KVQueryC(1 << 40, 1 << 40, None, 1024, 128, 1024, 128, 5, 0, 0, 8, 0, 1, 0, 0.1)
+    assert ss.lib.sem_kv_attend(c, 0, ctypes.byref(q), fake, fake, 0) == ss.SEM_EINVAL
+    assert ss.lib.sem_kv_append(c, 0, fake, fake, 0, 512, 128, 512, 128, fake, fake, 0,
+                                5) == ss.SEM_EINVAL
