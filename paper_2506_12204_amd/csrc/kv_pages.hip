@@ -162,6 +162,7 @@ __device__ __forceinline__ Growth growth_of(const KvReserveArgs& a, int64_t i) {
 // 11 us for 256 that grow by up to 64 tokens. Up to 1024 sequences keep their
 // needs in registers.
 __global__ __launch_bounds__(ST) void kv_reserve_plan(KvReserveArgs a) {
+  __shared__ uint64_t sums[ST / kWave + 1];
   __shared__ uint32_t scratch[ST / kWave + 1];
   __shared__ uint32_t bad;
   const KvView& c = a.c;
@@ -185,8 +186,8 @@ __global__ __launch_bounds__(ST) void kv_reserve_plan(KvReserveArgs a) {
         mine.need = 0;
       }
     }
-    uint32_t sum;
-    first = (uint32_t)total + block_excl_scan_u32<ST>(mine.need, scratch, sum);
+    uint64_t sum;  // (a need may be 2^27 pages, and there are 1024 of them)
+    first = (uint32_t)(total + block_excl_scan_u64<ST>(mine.need, sums, sum));
     if (i < a.n) a.begin[i] = first | (mine.shared << 31);
     total += sum;
     if (total > (uint64_t)a.room) break;  // more than the pool has; uniform

@@ -1096,3 +1096,27 @@ def test_rows_and_sequences_that_do_not_match(ss, kernel):
         call(0, [], [0])
         c.check()
     assert (c.data == 0).all() and (c.scale == 0).all()
+
+
+def test_needs_that_pass_32_bits(ss):
+    """33 sequences that ask for 2^32 pages in all: too few are free, and nothing
+    changes (a sum of 32 bits would be 0)."""
+    import torch
+    print("needs beyond 32 bits", flush=True)
+    mb, n = (1 << 27) - 1, 33
+    if torch.cuda.mem_get_info()[0] < 48 << 30:
+        pytest.skip("the tables of this size take 18 GB")
+    c = ss.KVCache(4, n, mb, layers=1, kv_heads=1, head_dim=64, page_tokens=16)
+    grow = [mb * 16] * 32 + [32 * 16]
+    assert sum(g // 16 for g in grow) == 1 << 32
+    c.reserve(i32(range(n)), i32(grow))
+    with pytest.raises(ss.SemschedError) as e:
+        c.check()
+    assert e.value.code == ss.SEM_ENOMEM
+    assert (c.lens == 0).all() and (c.refs == 0).all() and (c.live == 0).all()
+    assert (c.tables[:, :64] == -1).all()
+    c.reserve(i32([3, 1]), i32([33, 16]))
+    c.check()
+    assert c.tables[3, :4].tolist() == [0, 1, 2, -1] and c.tables[1, :2].tolist() == [3, -1]
+    del c
+    torch.cuda.empty_cache()
