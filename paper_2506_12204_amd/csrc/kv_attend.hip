@@ -12,9 +12,8 @@
 // two that brings its largest element to 2^14, which is undone in the scale).
 // The weights exp(x - m) vs are rounded to half precision relative to the
 // largest vs seen, 2^6 above, so that weights down to 2^-20 of the largest keep
-// 11 bits and smaller ones lose at most 2^-31 of it; a V block whose scale is
-// below 2^-30 of the largest seen counts as if it were that large. Sums, maxima
-// and outputs are in 32 bits.
+// 11 bits and smaller ones lose at most 2^-31 of it. Sums, maxima and outputs are
+// in 32 bits.
 #include <algorithm>
 #include <cstdlib>
 
@@ -986,10 +985,11 @@ __global__ __launch_bounds__(NW* kWave, NW / 4) void kv_attend_tile(KvAttendArgs
       for (int i = 1; i < 16; ++i) top = __builtin_elementwise_maximum(top, cur[i]);
       __builtin_amdgcn_sched_barrier(0);
       score(0, kf[0], nxt);
-      // weights are relative to the largest V scale so far (the same in all lanes)
+      // weights are relative to the largest V scale so far (the same in all lanes); one
+      // of zero is taken for 2^-60 of it, whose weights are 0 in half precision
       const float vmax = fmaxf(fmaxf(vs0, vs1), vref);
       const float inv = __builtin_amdgcn_rcpf(vmax);
-      const float rel = fmaxf((h ? vs1 : vs0) * inv, 9.3e-10f) * kLift;  // (2^-30)
+      const float rel = fmaxf((h ? vs1 : vs0) * inv, 0x1p-60f) * kLift;
       const float unrel = __builtin_amdgcn_rcpf(rel);
       // (not zero, so that a hidden key's minus infinity stays one)
       const float f = fmaxf(ks * factor, 1e-30f);

@@ -1120,3 +1120,29 @@ def test_needs_that_pass_32_bits(ss):
     assert c.tables[3, :4].tolist() == [0, 1, 2, -1] and c.tables[1, :2].tolist() == [3, -1]
     del c
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_blocks_of_scale_zero_count_nothing(ss, kernel, new):
+    """V codes under a scale of zero, on the keys of almost all the weight."""
+    import torch
+    print("scale zero", kernel, new, flush=True)
+    case = Case(ss, [128], fmt=ko.INT8, dim=64, pt=16, kv_heads=1, seed=33)
+    null = case.tables[0, 3:6]
+    data = case.data.reshape(-1, 2, 2, 1, 16 * 64)
+    data[:, 1, 0] = 0
+    data[null, 1, 0] = 1  # these keys' scores are 14 above the others' 0
+    case.scale[:, 1, 0] = 14 / 64
+    case.scale[null, 1, 1] = 0
+    case.scale[case.tables[0, [0, 1, 2, 6, 7]], 1, 1] = 2.0 ** 16
+    case.c.scale.copy_(torch.from_numpy(case.scale))
+    q = torch.ones(new, 1, 64, dtype=torch.float16, device="cuda")
+    got = []
+    for value in (0, 100, 156):  # 156: -100
+        data[null, 1, 1] = value
+        case.c.data.copy_(torch.from_numpy(case.data))
+        got.append(case.c.attend(1, q, i32([0]), i32([0, new]), scale=1.0).clone())
+        case.c.check()
+    assert (got[0] != 0).any()
+    for x in got[1:]:
+        assert torch.equal(x, got[0])
