@@ -574,7 +574,7 @@ int sem_kv_append_async(const sem_kv_cache *cache, int32_t layer, const void *k,
  * empty sequence) gives zeros and lse -infinity. Products are of half-precision
  * operands with 32-bit sums: codes and queries are exact (the elements of a bf16
  * row down to 2^-31 of its largest), the weights have 11 bits, but no finer than
- * 2^-31 of the largest weight and value scale that the workgroup has met.
+ * 2^-31 of the largest weight and value scale of the keys that the row sees.
  *   out [tokens][heads][head_dim] of the queries' type; lse [tokens][heads]
  *   float: the logarithm of the sum of exp(score), NULL if not wanted.
  *   max_new, max_len: bounds that the caller knows on the queries and the

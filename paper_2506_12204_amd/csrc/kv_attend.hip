@@ -11,9 +11,9 @@
 // there, and so are the queries (a bf16 row is first multiplied by a power of
 // two that brings its largest element to 2^14, which is undone in the scale).
 // The weights exp(x - m) vs are rounded to half precision relative to the
-// largest vs seen, 2^6 above, so that weights down to 2^-20 of the largest keep
-// 11 bits and smaller ones lose at most 2^-31 of it. Sums, maxima and outputs are
-// in 32 bits.
+// largest vs of the keys that the row has seen, 2^6 above, so that weights down to
+// 2^-20 of the largest keep 11 bits and smaller ones lose at most 2^-31 of it. Sums,
+// maxima and outputs are in 32 bits.
 #include <algorithm>
 #include <cstdlib>
 
@@ -403,7 +403,8 @@ __global__ __launch_bounds__(NW* kWave) void kv_attend_rows(KvAttendArgs a) {
     const int t0 = ch * kChunk, vt = t0 + g * kKvTile;
     const bool more = ch + NW < stop;
     // (not zero, so that a hidden key's minus infinity stays one)
-    const float f = fmaxf(kscale * factor, 1e-30f), vs = vscale;
+    const float f = fmaxf(kscale * factor, 1e-30f);
+    float vs = vscale;
     const int64_t kpage = checked(kentry), vpage = checked(ventry);
     look_up(ch + 2 * NW);
     float s[16];
@@ -425,6 +426,7 @@ __global__ __launch_bounds__(NW* kWave) void kv_attend_rows(KvAttendArgs a) {
       // keys that some rows do not see (whatever is held there)
 #pragma unroll
       for (int k = 0; k < 16; ++k) s[k] = vt + k >= low && vt + k < high ? s[k] : kNone;
+      if (vt >= high || vt + kKvTile <= low) vs = vref;  // the row sees none of these 16
       const int n = q.len - vt;
 #pragma unroll
       for (int y = 0; y < D / 16; ++y) {
@@ -440,7 +442,7 @@ __global__ __launch_bounds__(NW* kWave) void kv_attend_rows(KvAttendArgs a) {
     top *= f;
     top = fmaxf(top, __shfl_xor(top, 16, kWave));
     top = fmaxf(top, other_half(top));
-    // weights are relative to the largest V scale so far
+    // weights are relative to the largest V scale that the row has seen
     float vmax = fmaxf(vs, __shfl_xor(vs, 16, kWave));
     vmax = fmaxf(fmaxf(vmax, other_half(vmax)), vref);
     const float inv = __builtin_amdgcn_rcpf(vmax);
@@ -965,11 +967,15 @@ __global__ __launch_bounds__(NW* kWave, NW / 4) void kv_attend_tile(KvAttendArgs
     // weights' vector ones (the compiler would put them all behind).
     auto step = [&](int j, float16_t& cur, float16_t& nxt, const half8_t (&wp)[2], half8_t (&wc)[2],
                     uint4 (&rw)[PER], float& sc) __attribute__((always_inline)) {
+      const float ks = scales[(j & 3) * 4 + h];
+      float vs0 = scales[(j & 3) * 4 + 2], vs1 = scales[(j & 3) * 4 + 3];
       if (j * kWide < all_from || (j + 1) * kWide > all_to) {  // keys that some rows do not see
-        const int t0 = j * kWide + h * kKvTile;
+        const int t0 = j * kWide, t1 = t0 + kKvTile, t = h ? t1 : t0;
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          cur[i] = t0 + i >= low && t0 + i < high ? cur[i] : kNone;
+          cur[i] = t + i >= low && t + i < high ? cur[i] : kNone;
+        if (t0 >= high || t1 <= low) vs0 = vref;  // none of these 16
+        if (t1 >= high || t1 + kKvTile <= low) vs1 = vref;
       }
       hide(j + 2, rw);
 #pragma unroll
@@ -978,15 +984,13 @@ __global__ __launch_bounds__(NW* kWave, NW / 4) void kv_attend_tile(KvAttendArgs
       half8_t kf[KS];
 #pragma unroll
       for (int k = 0; k < 4; ++k) kf[k] = read_key(j + 1, k);
-      const float ks = scales[(j & 3) * 4 + h];
-      const float vs0 = scales[(j & 3) * 4 + 2], vs1 = scales[(j & 3) * 4 + 3];
       float top = cur[0];
 #pragma unroll
       for (int i = 1; i < 16; ++i) top = __builtin_elementwise_maximum(top, cur[i]);
       __builtin_amdgcn_sched_barrier(0);
       score(0, kf[0], nxt);
-      // weights are relative to the largest V scale so far (the same in all lanes); one
-      // of zero is taken for 2^-60 of it, whose weights are 0 in half precision
+      // weights are relative to the largest V scale that the row has seen; one of
+      // zero is taken for 2^-60 of it, whose weights are 0 in half precision
       const float vmax = fmaxf(fmaxf(vs0, vs1), vref);
       const float inv = __builtin_amdgcn_rcpf(vmax);
       const float rel = fmaxf((h ? vs1 : vs0) * inv, 0x1p-60f) * kLift;

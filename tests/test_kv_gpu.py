@@ -1122,6 +1122,47 @@ def test_needs_that_pass_32_bits(ss):
     torch.cuda.empty_cache()
 
 
+@pytest.mark.parametrize("fmt,dim", [(ko.INT8, 64), (ko.FP8, 128), (ko.INT8, 256)])
+@pytest.mark.parametrize("grow", [1e3, 1e-3])
+@pytest.mark.parametrize("window", [0, 20])
+def test_hidden_pages_take_no_bits(ss, kernel, fmt, dim, grow, window):
+    """V scales that rise or fall a thousand times from page to page: what a row
+    does not see, by the window or because it is later, does not count."""
+    import torch
+    if not window and grow < 1:
+        return  # (a row sees the first and largest scale then)
+    print("hidden pages", kernel, fmt, dim, grow, window, flush=True)
+    for new in (1, 60):
+        lens = [160, 150, 60]
+        case = Case(ss, lens, fmt=fmt, dim=dim, pt=16, kv_heads=1, seed=31)
+        for s in range(3):
+            for b in range(-(-lens[s] // 16)):
+                case.scale[case.tables[s, b], :, 1] *= np.float32(grow ** (b - 5))
+        case.c.scale.copy_(torch.from_numpy(case.scale))
+        q = case.queries([new] * 3, 2, torch.bfloat16)
+        out = case.c.attend(1, q, i32(range(3)), i32(np.arange(4) * new), window=window)
+        case.c.check()
+        # (check's absolute term would hide the small ones)
+        o = out.double().cpu().numpy()
+        for s in range(3):
+            k, v = (ko.read(case.data, case.scale, case.geom, case.tables[s], lens[s], 1, w, 0)
+                    for w in (0, 1))
+            for h in range(2):
+                rows = slice(s * new, (s + 1) * new)
+                want, _, mag = ko.attend(q[rows, h].double().cpu().numpy(), k, v, dim ** -0.5,
+                                         True, window)
+                tol = 2 * (2.0 ** -9 * np.abs(want) + (2.0 ** -12 + 2.0 ** -14) * mag)
+                # a weight is no finer than 2^-31 of the row's largest weight and scale
+                for i in range(new):
+                    n = lens[s] - new + i + 1
+                    low = max(n - window, 0) if window else 0
+                    page = case.tables[s, np.arange(low, n) // 16]
+                    vs = case.scale[page, 1, 1, 0].astype(np.float64)
+                    codes = np.abs(v[low:n]) / vs[:, None]
+                    tol[i] += 2.0 ** -31 * vs.max() * codes.sum(0)
+                assert (np.abs(o[rows, h] - want) <= tol).all(), (new, s, h)
+
+
 @pytest.mark.parametrize("new", [1, 40])
 def test_blocks_of_scale_zero_count_nothing(ss, kernel, new):
     """V codes under a scale of zero, on the keys of almost all the weight."""
