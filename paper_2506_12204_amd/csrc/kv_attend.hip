@@ -115,7 +115,8 @@ __device__ __forceinline__ void visible(const KvAttendArgs& a, const Sequence& q
                                         int& high) {
   const int pos = q.len - q.fresh + i;
   high = a.causal ? max(min(pos + 1, q.len), 0) : q.len;
-  low = a.window > 0 ? max(pos + 1 - a.window, 0) : 0;
+  // (a negative position less a large window passes 32 bits)
+  low = a.window > 0 && pos >= a.window ? pos + 1 - a.window : 0;
 }
 
 // Parts that chunks [c0, c1) of the keys are split into, of equal sizes (larger

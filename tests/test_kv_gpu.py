@@ -1187,3 +1187,16 @@ def test_blocks_of_scale_zero_count_nothing(ss, kernel, new):
     assert (got[0] != 0).any()
     for x in got[1:]:
         assert torch.equal(x, got[0])
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("window", [(1 << 31) - 1, (1 << 31) - 17, 1 << 30])
+def test_windows_larger_than_any_length(ss, kernel, causal, window):
+    """As none, for rows before the first key, too."""
+    print("wide windows", kernel, causal, window, flush=True)
+    _, q, out = run_attend(ss, [3, 0, 70, 90], [20, 4, 200, 9], heads=3, kv_heads=1, causal=causal,
+                           fmt=ko.FP8, window=window)
+    _, _, ref = run_attend(ss, [3, 0, 70, 90], [20, 4, 200, 9], heads=3, kv_heads=1, causal=causal,
+                           fmt=ko.FP8)
+    import torch
+    assert torch.equal(out, ref)
