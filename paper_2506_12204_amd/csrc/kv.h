@@ -101,6 +101,12 @@ struct KvAttendArgs {
   KvCut* cuts;     // [kKvPieces], of the tile that a piece ends with
 };
 
+// Whether a grid can be launched: its threads are counted in 32 bits. The launches
+// below return hipErrorInvalidConfiguration where it cannot.
+inline bool grid_fits(int64_t workgroups, int threads) {
+  return workgroups <= (int64_t)(UINT32_MAX / (uint32_t)threads);
+}
+
 hipError_t launch_kv_fork(const KvForkArgs& a, hipStream_t st);
 hipError_t launch_kv_free(const KvFreeArgs& a, hipStream_t st);
 hipError_t launch_kv_reserve(const KvReserveArgs& a, hipStream_t st);

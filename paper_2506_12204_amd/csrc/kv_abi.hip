@@ -100,7 +100,11 @@ bool workspace_ok(const void* ws, size_t have, size_t need) {
   return ws && have >= need && reinterpret_cast<uintptr_t>(ws) % kAlign == 0;
 }
 
-int status_of(hipError_t e) { return e == hipSuccess ? SEM_OK : SEM_EDEVICE; }
+int status_of(hipError_t e) {
+  // (a grid that is too large: the call has launched nothing)
+  if (e == hipErrorInvalidConfiguration) return SEM_ENOTIMPL;
+  return e == hipSuccess ? SEM_OK : SEM_EDEVICE;
+}
 
 // A blocking call: the library's workspace with its first bytes zeroed, the
 // asynchronous form on the blocking calls' stream, the status.
@@ -198,7 +202,7 @@ int check_attend(const sem_kv_cache* c, int32_t layer, const sem_kv_query* q, co
   if (q->tokens > 0 && (!q->q || !q->out)) return SEM_EINVAL;
   if (reinterpret_cast<uintptr_t>(q->q) % 2 != 0 || reinterpret_cast<uintptr_t>(q->out) % 2 != 0)
     return SEM_EINVAL;
-  // one row tile per workgroup column of the grid, one row per wave of the join
+  // (rows are counted in 32 bits)
   if (q->heads > 65536 || (q->tokens + n) * (int64_t)q->heads > INT32_MAX) return SEM_ENOTIMPL;
   return SEM_OK;
 }

@@ -420,6 +420,7 @@ hipError_t launch_kv_append(const KvAppendArgs& args, hipStream_t st) {
   KvAppendArgs a = args;
   const int64_t units = a.cu ? (a.tokens >> a.c.page_shift) + 2 * a.n : a.n;
   const int64_t checks = a.cu ? (a.n + AW * kWave - 1) / (AW * kWave) : 0;
+  if (!grid_fits(units + checks, AW * kWave)) return hipErrorInvalidConfiguration;
   a.units = (uint32_t)units;
   const dim3 grid((unsigned)(units + checks), (unsigned)((2 * a.c.kv_heads + AW - 1) / AW));
   switch (a.c.head_dim) {

@@ -1234,32 +1234,33 @@ template <int D>
 constexpr int tile_rows() { return tile_waves<D>() * kWide; }
 
 template <int D, int FMT>
-void launch_rows(KvAttendArgs a, hipStream_t st) {
+hipError_t launch_rows(KvAttendArgs a, hipStream_t st) {
   const int64_t tiles = a.cu ? a.tokens * a.group / kRows + a.n  // at most
                              : a.n * ((a.group + kRows - 1) / kRows);
   const int64_t checks = a.cu ? (a.n + a.waves * kWave - 1) / (a.waves * kWave) : 0;
+  if (!grid_fits(tiles * a.c.kv_heads + checks, a.waves * kWave))
+    return hipErrorInvalidConfiguration;
   a.tiles = (uint32_t)(tiles * a.c.kv_heads);
   const dim3 grid((unsigned)(a.tiles + checks), (unsigned)a.parts);
   if (D <= 128 && a.waves == 8)
     hipLaunchKernelGGL((kv_attend_rows<D, FMT, D <= 128 ? 8 : 4>), grid, dim3(8 * kWave), 0, st, a);
   else
     hipLaunchKernelGGL((kv_attend_rows<D, FMT, 4>), grid, dim3(4 * kWave), 0, st, a);
+  return hipGetLastError();
 }
 
 template <int D, int FMT>
 hipError_t launch(const KvAttendArgs& a, hipStream_t st) {
-  if (a.tiled) {
-    constexpr int ROWS = tile_rows<D>();
-    const int64_t tiles = a.tokens * a.group / ROWS + a.n;  // at most
-    const dim3 grid(a.whole ? (unsigned)(tiles * a.c.kv_heads) : kPieces);
-    hipLaunchKernelGGL((kv_attend_tile<D, FMT, tile_waves<D>()>), grid,
-                       dim3(tile_waves<D>() * kWave), 0, st, a);
-    if (!a.whole)
-      hipLaunchKernelGGL((kv_attend_join<D, ROWS>), dim3(kPieces, ROWS / kJoinRows), dim3(256), 0,
-                         st, a);
-  } else {
-    launch_rows<D, FMT>(a, st);
-  }
+  if (!a.tiled) return launch_rows<D, FMT>(a, st);
+  constexpr int ROWS = tile_rows<D>(), THREADS = tile_waves<D>() * kWave;
+  const int64_t tiles = a.tokens * a.group / ROWS + a.n;  // at most
+  const int64_t grid = a.whole ? tiles * a.c.kv_heads : kPieces;
+  if (!grid_fits(grid, THREADS)) return hipErrorInvalidConfiguration;
+  hipLaunchKernelGGL((kv_attend_tile<D, FMT, tile_waves<D>()>), dim3((unsigned)grid),
+                     dim3(THREADS), 0, st, a);
+  if (!a.whole)
+    hipLaunchKernelGGL((kv_attend_join<D, ROWS>), dim3(kPieces, ROWS / kJoinRows), dim3(256), 0,
+                       st, a);
   return hipGetLastError();
 }
 

@@ -397,11 +397,13 @@ __global__ __launch_bounds__(PT) void kv_compact_move(KvCompactArgs a) {
 }  // namespace
 
 hipError_t launch_kv_fork(const KvForkArgs& a, hipStream_t st) {
+  if (!grid_fits(a.n, PT)) return hipErrorInvalidConfiguration;
   if (a.n > 0) hipLaunchKernelGGL(kv_fork, dim3((unsigned)a.n), dim3(PT), 0, st, a);
   return hipGetLastError();
 }
 
 hipError_t launch_kv_free(const KvFreeArgs& a, hipStream_t st) {
+  if (!grid_fits(a.n, PT)) return hipErrorInvalidConfiguration;
   if (a.n > 0) hipLaunchKernelGGL(kv_free, dim3((unsigned)a.n), dim3(PT), 0, st, a);
   return hipGetLastError();
 }

@@ -191,6 +191,33 @@ def test_a_replaced_workspace_stays_allocated(ss, monkeypatch):
     assert sum(w.numel() for w in c._replaced) <= c.ws_bytes
 
 
+def test_grids_that_cannot_be_launched_are_refused(ss, monkeypatch):
+    """Calls whose threads pass 32 bits, with every pointer in order; nothing is
+    launched."""
+    L, big = ss.lib, 1 << 24
+    x = ctypes.c_void_p(1 << 40)
+    a = (x, 1 << 50, None)
+    c = cache(ss, slots=big, max_blocks=1, layers=1, kv_heads=1, head_dim=64, page_tokens=16)
+    assert L.sem_kv_fork_async(c, x, x, None, big, *a) == ss.SEM_ENOTIMPL
+    assert L.sem_kv_free_async(c, x, None, big, *a) == ss.SEM_ENOTIMPL
+    rows = (0, 64, 64, 64, 64, x)
+    assert L.sem_kv_append_async(c, 0, x, x, *rows, None, big, big, *a) == ss.SEM_ENOTIMPL
+    assert L.sem_kv_append_async(c, 0, x, x, *rows, x, big // 2, 1 << 20, *a) == ss.SEM_ENOTIMPL
+    assert L.sem_kv_append_async(c, 0, x, x, *rows, x, 1, 1 << 28, *a) == ss.SEM_ENOTIMPL
+
+    def attend(cache, heads, n, tokens, cu, max_new=0):
+        q = ss.KVQueryC(1 << 40, 1 << 40, None, heads * 64, 64, heads * 64, 64, tokens, max_new, 0,
+                        heads, 0, 1, 0, 0.1)
+        return L.sem_kv_attend_async(cache, 0, ctypes.byref(q), x, cu, n, *a)
+
+    assert attend(c, 1, big, big, None) == ss.SEM_ENOTIMPL
+    assert attend(c, 1, big - 1, big, x) == ss.SEM_ENOTIMPL  # with those that check offsets
+    wide = cache(ss, slots=1 << 18, max_blocks=1, layers=1, kv_heads=64, head_dim=64, page_tokens=16)
+    assert attend(wide, 64, 1 << 18, 1 << 18, None) == ss.SEM_ENOTIMPL
+    monkeypatch.setenv("SEMSCHED_KV_TILES", "1")  # tiles of 512 threads
+    assert attend(c, 64, 1 << 23, 1 << 23, None) == ss.SEM_ENOTIMPL
+
+
 def test_rows_of_no_sequence_are_refused(ss):
     fake = ctypes.c_void_p(1 << 40)
     c = cache(ss)
