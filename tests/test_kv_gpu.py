@@ -1200,3 +1200,17 @@ def test_windows_larger_than_any_length(ss, kernel, causal, window):
                            fmt=ko.FP8)
     import torch
     assert torch.equal(out, ref)
+
+
+def test_the_bench_reports_the_kernel_that_it_names(ss, capsys):
+    """The roofline of a serving iteration is one attention's, not the iteration's."""
+    import argparse
+    import json
+
+    import bench
+    print("bench kv", flush=True)
+    assert bench.bench_kv(argparse.Namespace(steps=2, warmup=1, no_cpu_baseline=True)) == 0
+    res = json.loads(capsys.readouterr().out.strip().splitlines()[-1])
+    roof = res["roofline"]
+    assert 0 < roof["avg_launch_ms"] * 8 < res["ms_per_step"]  # 8 layers
+    assert abs(roof["bytes_per_launch"] / roof["avg_launch_ms"] / 1e6 - roof["achieved"]) < 1
