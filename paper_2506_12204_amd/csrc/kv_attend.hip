@@ -327,7 +327,6 @@ __global__ __launch_bounds__(NW* kWave) void kv_attend_rows(KvAttendArgs a) {
   if (!find_tile(a, blockIdx.x / c.kv_heads, kRows, q, tile)) return;
   const int rows = q.fresh * a.group;
   const uint32_t row = (uint32_t)min(tile * kRows + r, rows - 1);
-  const bool live = tile * kRows + r < rows;
   const int token = (int)(row / (uint32_t)a.group);
   const int head = kh * a.group + (int)(row % (uint32_t)a.group);
   Query<D, 4> raw;

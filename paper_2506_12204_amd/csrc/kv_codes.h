@@ -43,16 +43,6 @@ __device__ __forceinline__ float code_to_float(uint32_t byte) {
   return __builtin_amdgcn_cvt_f32_fp8((int)byte, 0);
 }
 
-// The nearest code, ties to even, beyond the range the largest; NaN is 0 (the
-// comparisons of the clamp are written so that it takes neither side).
-template <int FMT>
-__device__ __forceinline__ uint32_t float_to_code(float x) {
-  const float top = code_max<FMT>();
-  x = x != x ? 0.0f : fminf(fmaxf(x, -top), top);
-  if (FMT == SEM_KV_INT8) return (uint32_t)(int)rintf(x) & 0xffu;
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x, x, 0, false) & 0xffu;
-}
-
 __device__ __forceinline__ float load16(uint16_t u, int bf16) {
   return bf16 ? __uint_as_float((uint32_t)u << 16) : (float)__builtin_bit_cast(_Float16, u);
 }
