@@ -1214,3 +1214,18 @@ def test_the_bench_reports_the_kernel_that_it_names(ss, capsys):
     roof = res["roofline"]
     assert 0 < roof["avg_launch_ms"] * 8 < res["ms_per_step"]  # 8 layers
     assert abs(roof["bytes_per_launch"] / roof["avg_launch_ms"] / 1e6 - roof["achieved"]) < 1
+
+
+def test_cut_tiles_do_not_depend_on_the_run(ss, monkeypatch):
+    """Tiles whose keys go to several workgroups give the same bits in every run."""
+    import torch
+    print("repeat, tiles", flush=True)
+    monkeypatch.setenv("SEMSCHED_KV_TILES", "1")
+    for dim, fmt in ((128, ko.FP8), (64, ko.INT8), (256, ko.INT8)):
+        case = Case(ss, [3000, 700, 1900], fmt=fmt, dim=dim, pt=64, kv_heads=2)
+        q = case.queries([200, 1, 333], 8, torch.float16)
+        seqs, cu = i32([0, 1, 2]), i32([0, 200, 201, 534])
+        first = case.c.attend(1, q, seqs, cu).clone()
+        for _ in range(5):
+            assert torch.equal(case.c.attend(1, q, seqs, cu), first)
+        case.c.check()
