@@ -442,12 +442,16 @@ int sem_schedule_static(const uint8_t *priority, const int32_t *length, int64_t 
  *   format SEM_KV_INT8: two's complement in [-127, 127]; SEM_KV_FP8: e4m3
  *         (largest value 448, no infinities). No code that the library writes
  *         is a NaN.
- * Sequences are slots 0 .. slots-1; the bookkeeping is in four arrays, which
- * the caller may copy and put back to undo steps:
+ * Sequences are slots 0 .. slots-1; the bookkeeping is in four arrays:
  *   live   [ceil(num_pages / 32)] bit p % 32 of word p / 32: page p is in use;
  *   refs   [num_pages] number of table entries that name the page;
  *   lens   [slots] tokens of each sequence;
  *   tables [slots][max_blocks] the pages of each sequence, -1 beyond them.
+ * A copy of the four that is put back undoes fork, reserve and free (and the
+ * growth of appended sequences), but not what was written to data and scale: a
+ * page that was given back and has since been taken holds its new owner's
+ * tokens or copies, and a block that append put on a larger scale keeps it (and
+ * its older codes, rounded again). A compact is not undone.
  * All arrays are DEVICE memory of the caller, all zero (tables: -1) for an
  * empty cache; data need not be cleared. The structure itself is a HOST
  * pointer. page_tokens is a power of two from 16 to 1024, head_dim 64, 128 or
@@ -457,17 +461,19 @@ int sem_schedule_static(const uint8_t *priority, const int32_t *length, int64_t 
  * Every call has a blocking form and an asynchronous one that allocates
  * nothing, does not synchronise, and takes a caller-owned DEVICE workspace
  * (256-byte aligned) and the stream; its calls may be captured into a HIP
- * graph. The caller zeroes the workspace's first SEM_KV_ZEROED_BYTES bytes
- * before the first call. The asynchronous calls add their errors to its first
+ * graph, for which the workspace has to outlive the graph. The caller zeroes
+ * the workspace's first SEM_KV_ZEROED_BYTES bytes before the first call. The asynchronous calls add their errors to its first
  * word and never clear it, so that one sem_check covers a whole step; the
  * caller zeroes that word again after an error. A cache and a
  * workspace must not be used by calls in flight on different streams.
  *
  * Lists of sequences name each at most once. Errors: SEM_EINVAL for null
- * pointers, sizes or strides out of range, a workspace too small, and,
- * detected on the device, sequences, lengths, offsets or page numbers outside
- * the cache (no memory outside the arguments is accessed); SEM_ERANGE for a
- * negative token count. Scales are not negative.
+ * pointers, sizes or strides out of range, rows of no sequence, a workspace too
+ * small, and, detected on the device, sequences, lengths, offsets or page numbers
+ * outside the cache, or offsets that fall (no memory outside the arguments is
+ * accessed); SEM_ERANGE for a negative token count; SEM_ENOTIMPL for calls of
+ * more threads than a launch may have (2^32, as for one token each of 2^24
+ * sequences times KV heads). Scales are not negative.
  */
 #define SEM_KV_ZEROED_BYTES 4352
 #define SEM_KV_INT8 0
@@ -611,7 +617,10 @@ int sem_set_stream(void *stream);
 
 /*
  * Synchronise `stream` and return the status recorded in `workspace` by the
- * last asynchronous call that used it (SEM_OK, SEM_ERANGE or SEM_EINVAL).
+ * last asynchronous call that used it (SEM_OK, SEM_ERANGE, SEM_EINVAL or
+ * SEM_EDEVICE), by all of them since it was zeroed for the KV cache's (SEM_ENOMEM,
+ * too; of several errors the one that comes first in EDEVICE, EINVAL, ENOMEM,
+ * ERANGE).
  */
 int sem_check(const void *workspace, void *stream);
 

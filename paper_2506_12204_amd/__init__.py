@@ -609,9 +609,10 @@ class KVCache:
     (float32 [num_pages, layers, 2, kv_heads]) what they are multiplied by.
     ``book`` is one int32 buffer with the views ``live``, ``refs``, ``lens`` and
     ``tables``, each padded to 64 entries: copying it and putting it back
-    undoes reserve, fork and free (and append's growth) of the steps between,
-    though not compact. The three may be passed in; otherwise they are
-    allocated, empty.
+    undoes reserve, fork and free (and append's growth) of the steps between, as
+    long as no page that they gave back has been taken and written since; what
+    append did to scales and older codes stays, and compact is not undone. The
+    three may be passed in; otherwise they are allocated, empty.
 
     Every operation enqueues on the current stream without synchronising;
     ``check`` waits and raises on a device-detected error of any of them since
@@ -784,7 +785,7 @@ class KVCache:
         to that many positions up to its own; ``max_new`` and ``max_len`` bound
         a sequence's queries and length (0: unknown) and only guide how the
         work is split. ``lse`` (float32 [tokens, heads]) receives the log of
-        the softmax sums. Returns ``out``."""
+        the softmax sums. Returns ``out``, which has no gradient."""
         dtype = self._rows(q, "q")
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)

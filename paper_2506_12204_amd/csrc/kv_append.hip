@@ -17,8 +17,11 @@
 // through LDS. Bound by memory: prompts of 24 sequences (500 to 8192 tokens, 8 KV
 // heads of 128 channels) are written at 4.7 TB/s of rows and codes (108 us), what
 // a large copy reaches; one token for each of 256 sequences takes 8.2 us, the
-// launch and the chain from the sequence to its page (13.3 us with offsets, whose
-// search takes 64 at a time; by halves it took 14.2).
+// launch and the chain from the sequence to its page (13.8 us with offsets, whose
+// search takes 64 at a time), for each of 4096 87 us (133 us with offsets: two units
+// a sequence, each with a search of its own). Blocks of more than 64 tokens are read
+// twice, for the maximum and for the codes: the same prompts on pages of 128 take
+// 162 us, of 256 187 us, of 1024 327 us.
 #include <algorithm>
 
 #include "device_common.h"

@@ -553,18 +553,19 @@ __global__ __launch_bounds__(NW* kWave) void kv_attend_rows(KvAttendArgs a) {
 // are fed, of 16 consecutive keys, which the second product takes from
 // registers.
 //
-// Three steps overlap, so that the matrix cores are fed while the vector units
-// turn scores into weights: step j takes the scores of keys j + 1, the weights
-// of keys j and the outputs of keys j - 1, which do not depend on each other.
-// Codes are loaded four steps ahead and put into LDS two steps ahead. (Six or
-// eight steps ahead measured the same.)
+// A step's instructions do not wait for each other: step j takes the scores of
+// keys j + 1, the weights of keys j and the outputs of keys j - 1. Codes are loaded
+// four steps ahead and put into LDS two steps ahead. (Six or eight steps ahead
+// measured the same.)
 //
-// Bound by the matrix and vector instructions of a step together: 16 matrix
-// instructions (512 cycles) and 150 vector ones (about 800, the 16 exponentials
-// at a quarter of the rate) per wave and 32 keys (128 channels), two waves on a
-// SIMD. The matrix cores are busy in 42% of the cycles of a prompt of 16384
-// tokens (32 heads of 128 channels): 2.40 ms, 918 TFLOP/s, where a large matrix
-// product reaches 1300; before the steps overlapped it took 6.07 ms.
+// Bound by the matrix and vector instructions of a step, which still run almost
+// one after the other: 16 matrix instructions (512 cycles) and about 150 vector
+// ones (about 800, the 16 exponentials at a quarter of the rate) per wave and 32
+// keys (128 channels), two waves on a SIMD that meet at a barrier each step. Of
+// the cycles of a prompt of 16384 tokens (32 heads of 128 channels) matrix
+// instructions take 42% and vector ones about 64%: 2.34 to 2.50 ms by card, 880 to
+// 940 TFLOP/s, where a large matrix product reaches 1300; 6.07 ms where the three
+// parts of a step depended on each other.
 constexpr int kWide = 32;  // rows of a matrix tile, and keys of a step
 typedef float float16_t __attribute__((ext_vector_type(16)));
 
@@ -1282,7 +1283,11 @@ hipError_t launch_dim(const KvAttendArgs& a, hipStream_t st) {
 //     and not for fewer than 24 chunks (a single token over 1024 keys takes 10 us
 //     in one part; two add 3 us of joining). With more workgroups than compute
 //     units four waves each, without parts (256 ragged requests: 87 us, 95 us with
-//     parts of 2048 keys).
+//     parts of 2048 keys). Equal contexts of 32768 keys, 8 KV heads, are read at
+//     5.3 to 5.7 TB/s (8 to 17 sequences), 6.0 (24 to 32, 64) and 5.0 (40, a second
+//     round that does not fill the device). Unequal ones are not balanced: 31
+//     sequences of 1024 keys and one of 131072 take 942 us, as long as eight
+//     workgroups need for the long one, where the bytes take 60.
 //   * Tiles: see kPieces.
 KvSplit kv_attend_split(int dim, int64_t n, int64_t tokens, int heads, int kv_heads,
                         int64_t max_new, int64_t max_len) {
