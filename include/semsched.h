@@ -473,7 +473,8 @@ int sem_schedule_static(const uint8_t *priority, const int32_t *length, int64_t 
  * outside the cache, or offsets that fall (no memory outside the arguments is
  * accessed); SEM_ERANGE for a negative token count; SEM_ENOTIMPL for calls of
  * more threads than a launch may have (2^32, as for one token each of 2^24
- * sequences times KV heads). Scales are not negative.
+ * sequences times KV heads). Scales are from 0 to 2^126 (append writes none above
+ * 2^121).
  */
 #define SEM_KV_ZEROED_BYTES 4352
 #define SEM_KV_INT8 0
