@@ -462,10 +462,11 @@ int sem_schedule_static(const uint8_t *priority, const int32_t *length, int64_t 
  * nothing, does not synchronise, and takes a caller-owned DEVICE workspace
  * (256-byte aligned) and the stream; its calls may be captured into a HIP
  * graph, for which the workspace has to outlive the graph. The caller zeroes
- * the workspace's first SEM_KV_ZEROED_BYTES bytes before the first call. The asynchronous calls add their errors to its first
- * word and never clear it, so that one sem_check covers a whole step; the
- * caller zeroes that word again after an error. A cache and a
- * workspace must not be used by calls in flight on different streams.
+ * the workspace's first SEM_KV_ZEROED_BYTES bytes before the first call. The
+ * asynchronous calls add their errors to its first word and never clear it, so
+ * that one sem_check covers a whole step; the caller zeroes that word again after
+ * an error. A cache and a workspace must not be used by calls in flight on
+ * different streams.
  *
  * Lists of sequences name each at most once. Errors: SEM_EINVAL for null
  * pointers, sizes or strides out of range, rows of no sequence, a workspace too
