@@ -614,6 +614,42 @@ int sem_kv_attend_async(const sem_kv_cache *cache, int32_t layer, const sem_kv_q
                         const int32_t *seqs, const int32_t *cu, int64_t n, void *workspace,
                         size_t ws_bytes, void *stream);
 
+/*
+ * Rotate: the norms of queries and keys, head by head, and the rotation of their
+ * positions, what new tokens go through before append and attend. For every row x
+ * (a token and a head) of head_dim channels (64, 128 or 256; SEM_ENOTIMPL for
+ * others):
+ *   y = x * w / sqrt(mean(x^2) + eps), w the q_weight or k_weight [head_dim]; y = x
+ *   where that is NULL;
+ *   pair i < rot_dim / 2, of channels i and i + rot_dim / 2 (interleaved: 2 i and
+ *   2 i + 1), turns by the angle t = positions[token] * inv_freq[i]: (a, b) becomes
+ *   (a cos t - b sin t, b cos t + a sin t); channels from rot_dim on (a multiple of
+ *   16, 0 for norms alone) stay y.
+ * In 32 bits (a row's sum of squares, too: it overflows for elements beyond 2^60)
+ * and rounded once; the angle is the product in 64 bits of the two numbers given,
+ * so any int32 position is exact to 32 bits. Elements (token, head, channel) at
+ * token * token_stride + head * head_stride + channel. The outputs may be the inputs
+ * (with the same strides), but not overlap them in other ways. heads or kv_heads may
+ * be 0: q or k is then not looked at. It needs no workspace and reports no errors
+ * from the device.
+ */
+typedef struct {
+  const void *q, *k;
+  void *q_out, *k_out;
+  int64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride; /* in elements */
+  int64_t q_out_token_stride, q_out_head_stride, k_out_token_stride, k_out_head_stride;
+  const int32_t *positions;         /* [tokens] */
+  const float *inv_freq;            /* [rot_dim / 2] */
+  const float *q_weight, *k_weight; /* [head_dim] or NULL */
+  int64_t tokens;
+  int32_t heads, kv_heads, head_dim, rot_dim;
+  int32_t dtype; /* SEM_KV_BF16 or SEM_KV_F16 */
+  int32_t interleaved;
+  float eps;
+} sem_qk_rotary;
+int sem_qk_rotate(const sem_qk_rotary *rotary);
+int sem_qk_rotate_async(const sem_qk_rotary *rotary, void *stream);
+
 /* Stream used by the blocking calls (NULL = null stream). */
 int sem_set_stream(void *stream);
 

@@ -72,6 +72,26 @@ def attend(q, ks, vs, scale, causal, window):
     return out, lse, mag
 
 
+def rotate(x, w, eps, positions, inv_freq, interleaved):
+    """Rows x [tokens, heads, dim] normed and turned: (y, the two sides' magnitudes that
+    the errors of an element are relative to)."""
+    x = np.asarray(x, np.float64)
+    tokens, _, dim = x.shape
+    half = len(inv_freq)
+    if w is not None:
+        x = x / np.sqrt((x * x).mean(-1, keepdims=True) + eps) * np.asarray(w, np.float64)
+    out, mag = x.copy(), np.abs(x)
+    for t in range(tokens):
+        for i in range(half):
+            a, b = (2 * i, 2 * i + 1) if interleaved else (i, i + half)
+            angle = math.fmod(int(positions[t]) * float(inv_freq[i]), 2 * math.pi)
+            c, s = math.cos(angle), math.sin(angle)
+            out[t, :, a] = x[t, :, a] * c - x[t, :, b] * s
+            out[t, :, b] = x[t, :, b] * c + x[t, :, a] * s
+            mag[t, :, a] = mag[t, :, b] = np.abs(x[t, :, a]) + np.abs(x[t, :, b])
+    return out, mag
+
+
 class Pages:
     """Reference counts, lengths and tables as lists; contents by page number."""
 

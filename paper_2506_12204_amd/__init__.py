@@ -77,6 +77,8 @@ SYMBOLS = (
     "sem_kv_attend_workspace_bytes",
     "sem_kv_attend",
     "sem_kv_attend_async",
+    "sem_qk_rotate",
+    "sem_qk_rotate_async",
 )
 STATIC_MAX_N = 1048576
 STATIC_SCRATCH_BYTES = 33554432
@@ -114,6 +116,21 @@ class KVQueryC(ctypes.Structure):
                                                        "tokens", "max_new", "max_len")]
                 + [(name, ctypes.c_int32) for name in ("heads", "dtype", "causal", "window")]
                 + [("scale", ctypes.c_float)])
+
+
+class QKRotaryC(ctypes.Structure):
+    """sem_qk_rotary."""
+    _fields_ = ([(name, ctypes.c_void_p) for name in ("q", "k", "q_out", "k_out")]
+                + [(name, ctypes.c_int64) for name in (
+                    "q_token_stride", "q_head_stride", "k_token_stride", "k_head_stride",
+                    "q_out_token_stride", "q_out_head_stride", "k_out_token_stride",
+                    "k_out_head_stride")]
+                + [(name, ctypes.c_void_p) for name in ("positions", "inv_freq", "q_weight",
+                                                        "k_weight")]
+                + [("tokens", ctypes.c_int64)]
+                + [(name, ctypes.c_int32) for name in ("heads", "kv_heads", "head_dim", "rot_dim",
+                                                       "dtype", "interleaved")]
+                + [("eps", ctypes.c_float)])
 
 
 def cost_model(model) -> CostModelC:
@@ -190,6 +207,8 @@ def _load() -> ctypes.CDLL:
                        ("attend_workspace_bytes", [kv, i32, i64, i64, i64, i64])):
         fn = getattr(lib, f"sem_kv_{name}")
         fn.argtypes, fn.restype = args, sz
+    lib.sem_qk_rotate.argtypes, lib.sem_qk_rotate.restype = [vp], ctypes.c_int  # (a sem_qk_rotary)
+    lib.sem_qk_rotate_async.argtypes, lib.sem_qk_rotate_async.restype = [vp, vp], ctypes.c_int
     lib.sem_strerror.argtypes = [ctypes.c_int]
     lib.sem_strerror.restype = ctypes.c_char_p
     for name in ("sem_schedule", "sem_schedule_batched", "sem_schedule_async",
@@ -592,6 +611,15 @@ def evict(priority: torch.Tensor, length: torch.Tensor, cached: torch.Tensor, kv
 _raw_stream = torch._C._cuda_getCurrentRawStream
 
 
+def _enqueue(index: int, call, *args) -> int:
+    """The status of an asynchronous call on the current stream of a device, which
+    need not be the current one."""
+    if torch.cuda.current_device() == index:
+        return call(*args, _raw_stream(index))
+    with torch.cuda.device(index):
+        return call(*args, _raw_stream(index))
+
+
 def _round64(n: int) -> int:
     return -(-n // 64) * 64
 
@@ -599,6 +627,59 @@ def _round64(n: int) -> int:
 _KV_DTYPES = {torch.bfloat16: 0, torch.float16: 1}
 _KV_QUERY = struct.Struct("PPPqqqqqqqiiiif4x")  # sem_kv_query
 assert _KV_QUERY.size == ctypes.sizeof(KVQueryC)
+
+
+_QK_ROTARY = struct.Struct("PPPPqqqqqqqqPPPPqiiiiiif4x")  # sem_qk_rotary
+assert _QK_ROTARY.size == ctypes.sizeof(QKRotaryC)
+
+
+def qk_rotate(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor,
+              *, q_weight: Optional[torch.Tensor] = None,
+              k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+              interleaved: bool = False, q_out: Optional[torch.Tensor] = None,
+              k_out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Norms of queries and keys for each head and the rotation of their positions,
+    before ``KVCache.append`` and ``attend`` (definition: semsched.h).
+
+    q [tokens, heads, head_dim] and k [tokens, kv_heads, head_dim] are bfloat16 or
+    float16 with free strides of tokens and heads; ``positions`` int32 [tokens];
+    ``inv_freq`` float32 [rot_dim / 2], of pairs of channels i and i + rot_dim / 2
+    or, interleaved, 2 i and 2 i + 1; ``q_weight`` and ``k_weight`` float32
+    [head_dim] scale the norms, which are left out where they are None. The
+    outputs, which have no gradient, may be the inputs. Enqueues on the current
+    stream without synchronising."""
+    dtype, at = _KV_DTYPES.get(q.dtype), q.get_device()
+    if dtype is None or at < 0 or k.dtype != q.dtype or k.get_device() != at:
+        raise TypeError("q and k must be bfloat16 or float16 on one GPU")
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if k_out is None:
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    tokens, heads, dim = q.shape
+    for x, out in ((q, q_out), (k, k_out)):
+        if x.dim() != 3 or x.shape[0] != tokens or x.shape[2] != dim or x.stride(2) != 1:
+            raise ValueError("q and k must be [tokens, heads, head_dim] with adjacent channels")
+        if out.dtype != q.dtype or out.get_device() != at or out.shape != x.shape \
+                or out.stride(2) != 1:
+            raise ValueError("outputs must have their inputs' type and shape")
+    if positions.dtype != torch.int32 or positions.get_device() != at \
+            or positions.shape != (tokens,) or not positions.is_contiguous():
+        raise TypeError("positions must be contiguous int32 [tokens] on the rows' GPU")
+    for w, size in ((inv_freq, None), (q_weight, dim), (k_weight, dim)):
+        if w is not None and (w.dtype != torch.float32 or w.get_device() != at or w.dim() != 1
+                              or not w.is_contiguous() or w.shape[0] != (size or w.shape[0])):
+            raise TypeError("inv_freq, q_weight and k_weight must be contiguous float32 vectors on "
+                            "the rows' GPU, weights of head_dim entries")
+    rotary = _QK_ROTARY.pack(q.data_ptr(), k.data_ptr(), q_out.data_ptr(), k_out.data_ptr(),
+                             *q.stride()[:2], *k.stride()[:2], *q_out.stride()[:2],
+                             *k_out.stride()[:2], positions.data_ptr(), inv_freq.data_ptr(),
+                             0 if q_weight is None else q_weight.data_ptr(),
+                             0 if k_weight is None else k_weight.data_ptr(), tokens, heads,
+                             k.shape[1], dim, 2 * inv_freq.shape[0], dtype, interleaved, eps)
+    rc = _enqueue(at, lib.sem_qk_rotate_async, rotary)
+    if rc:
+        _raise(rc, "sem_qk_rotate_async")
+    return q_out, k_out
 
 
 class KVCache:

@@ -101,6 +101,19 @@ struct KvAttendArgs {
   KvCut* cuts;     // [kKvPieces], of the tile that a piece ends with
 };
 
+struct QkRotateArgs {
+  const uint16_t *q, *k;  // 16-bit elements
+  uint16_t *q_out, *k_out;
+  int64_t q_token, q_head, k_token, k_head, qo_token, qo_head, ko_token, ko_head;  // strides
+  const int32_t* positions;
+  const float *inv_freq, *q_weight, *k_weight;  // weights may be null: no norm
+  int64_t tokens;
+  int32_t heads, kv_heads, rot_dim;
+  int32_t bf16, pairs, wide;  // neighbours are paired; 16-byte accesses are aligned
+  float eps;
+  int32_t steps, parts;  // of rows per wave, of a token (set by the launch)
+};
+
 // Whether a grid can be launched: its threads are counted in 32 bits. The launches
 // below return hipErrorInvalidConfiguration where it cannot.
 inline bool grid_fits(int64_t workgroups, int threads) {
@@ -112,6 +125,7 @@ hipError_t launch_kv_free(const KvFreeArgs& a, hipStream_t st);
 hipError_t launch_kv_reserve(const KvReserveArgs& a, hipStream_t st);
 hipError_t launch_kv_compact(const KvCompactArgs& a, hipStream_t st);
 hipError_t launch_kv_append(const KvAppendArgs& a, hipStream_t st);
+hipError_t launch_qk_rotate(const QkRotateArgs& a, int head_dim, hipStream_t st);
 hipError_t launch_kv_attend(const KvAttendArgs& a, hipStream_t st);
 
 // How an attention call of these sizes is split (its workspace holds the

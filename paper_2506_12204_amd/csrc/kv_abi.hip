@@ -207,9 +207,75 @@ int check_attend(const sem_kv_cache* c, int32_t layer, const sem_kv_query* q, co
   return SEM_OK;
 }
 
+int check_rotate(const sem_qk_rotary* r) {
+  if (!r || r->tokens < 0 || r->tokens > INT32_MAX || r->heads < 0 || r->kv_heads < 0 ||
+      (r->dtype != SEM_KV_BF16 && r->dtype != SEM_KV_F16) || !std::isfinite(r->eps) || r->eps < 0)
+    return SEM_EINVAL;
+  if (r->rot_dim < 0 || r->rot_dim > r->head_dim || r->rot_dim % 16 != 0) return SEM_EINVAL;
+  for (const int64_t stride : {r->q_token_stride, r->q_head_stride, r->k_token_stride,
+                               r->k_head_stride, r->q_out_token_stride, r->q_out_head_stride,
+                               r->k_out_token_stride, r->k_out_head_stride})
+    if (stride < 0) return SEM_EINVAL;
+  if (r->tokens > 0 && ((r->heads > 0 && (!r->q || !r->q_out)) ||
+                        (r->kv_heads > 0 && (!r->k || !r->k_out)) ||
+                        (r->rot_dim > 0 && (!r->positions || !r->inv_freq))))
+    return SEM_EINVAL;
+  for (const void* p : {r->q, r->k, (const void*)r->q_out, (const void*)r->k_out})
+    if (reinterpret_cast<uintptr_t>(p) % 2 != 0) return SEM_EINVAL;
+  for (const void* p : {(const void*)r->positions, (const void*)r->inv_freq,
+                        (const void*)r->q_weight, (const void*)r->k_weight})
+    if (reinterpret_cast<uintptr_t>(p) % 4 != 0) return SEM_EINVAL;
+  if (r->head_dim != 64 && r->head_dim != 128 && r->head_dim != 256) return SEM_ENOTIMPL;
+  if (r->heads > 65536 || r->kv_heads > 65536) return SEM_ENOTIMPL;
+  return SEM_OK;
+}
+
 }  // namespace
 
 extern "C" {
+
+int sem_qk_rotate_async(const sem_qk_rotary* rotary, void* stream) {
+  const int rc = check_rotate(rotary);
+  if (rc != SEM_OK) return rc;
+  const sem_qk_rotary& r = *rotary;
+  QkRotateArgs a = {};
+  a.q = static_cast<const uint16_t*>(r.q);
+  a.k = static_cast<const uint16_t*>(r.k);
+  a.q_out = static_cast<uint16_t*>(r.q_out);
+  a.k_out = static_cast<uint16_t*>(r.k_out);
+  a.q_token = r.q_token_stride;
+  a.q_head = r.q_head_stride;
+  a.k_token = r.k_token_stride;
+  a.k_head = r.k_head_stride;
+  a.qo_token = r.q_out_token_stride;
+  a.qo_head = r.q_out_head_stride;
+  a.ko_token = r.k_out_token_stride;
+  a.ko_head = r.k_out_head_stride;
+  a.positions = r.positions;
+  a.inv_freq = r.inv_freq;
+  a.q_weight = r.q_weight;
+  a.k_weight = r.k_weight;
+  a.tokens = r.heads + r.kv_heads > 0 ? r.tokens : 0;
+  a.heads = r.heads;
+  a.kv_heads = r.kv_heads;
+  a.rot_dim = r.rot_dim;
+  a.bf16 = r.dtype == SEM_KV_BF16;
+  a.pairs = r.interleaved != 0;
+  a.wide = (r.heads == 0 || (aligned16(r.q, a.q_token, a.q_head) &&
+                             aligned16(r.q_out, a.qo_token, a.qo_head))) &&
+           (r.kv_heads == 0 || (aligned16(r.k, a.k_token, a.k_head) &&
+                                aligned16(r.k_out, a.ko_token, a.ko_head)));
+  a.eps = r.eps;
+  return status_of(launch_qk_rotate(a, r.head_dim, static_cast<hipStream_t>(stream)));
+}
+
+int sem_qk_rotate(const sem_qk_rotary* rotary) {
+  const int rc = check_rotate(rotary);
+  if (rc != SEM_OK) return rc;
+  return blocking(kZeroed, [&](void*, size_t, hipStream_t st) {
+    return sem_qk_rotate_async(rotary, st);
+  });
+}
 
 size_t sem_kv_page_bytes(const sem_kv_cache* cache) {
   return check_sizes(cache) == SEM_OK ? (size_t)page_bytes(cache) : 0;

@@ -128,20 +128,6 @@ __device__ __forceinline__ int part_start(int c0, int c1, int parts, int part) {
   return c0 + (int)((uint32_t)max(c1 - c0, 0) * (uint64_t)part / (uint32_t)parts);
 }
 
-// Two values in the outputs' type, rounded to the nearest.
-template <bool BF16>
-__device__ __forceinline__ uint32_t pack_pair(float x, float y) {
-  const float2_t v = {x, y};
-  if (BF16) {
-    typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2_t));
-  }
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, half2_t));
-}
-__device__ __forceinline__ uint32_t pack_pair(float x, float y, int bf16) {
-  return bf16 ? pack_pair<true>(x, y) : pack_pair<false>(x, y);
-}
-
 // A row's query, as the lane's D / (8 G) operands of eight: of G = 4 lane groups,
 // group g holds channels (4 j + g) * 16 .. + 15 in operands 2 j and 2 j + 1; of
 // G = 2, channels 16 j + 8 g .. + 7 in operand j. Loaded first, so that finding

@@ -47,4 +47,18 @@ __device__ __forceinline__ float load16(uint16_t u, int bf16) {
   return bf16 ? __uint_as_float((uint32_t)u << 16) : (float)__builtin_bit_cast(_Float16, u);
 }
 
+// Two values in the outputs' type, rounded to the nearest.
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack_pair(float x, float y) {
+  const float2_t v = {x, y};
+  if (BF16) {
+    typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2_t));
+  }
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, half2_t));
+}
+__device__ __forceinline__ uint32_t pack_pair(float x, float y, int bf16) {
+  return bf16 ? pack_pair<true>(x, y) : pack_pair<false>(x, y);
+}
+
 }  // namespace semsched
