@@ -615,6 +615,44 @@ int sem_kv_attend_async(const sem_kv_cache *cache, int32_t layer, const sem_kv_q
                         size_t ws_bytes, void *stream);
 
 /*
+ * Trees of drafted tokens. The query tokens of a sequence, whose keys are its last
+ * ones, form trees: parents[t] is the number among them of the token that token t
+ * continues, less than its own, or -1 for one that continues the context, the keys
+ * before them. A token sees the context and those on its path from there, itself
+ * among them.
+ *
+ * sem_kv_tree makes of the parents what a step's calls need:
+ *   mask_out [tokens][mask_words] uint32: bit j % 32 of word j / 32 is set where the
+ *     row's token sees its sequence's query token j;
+ *   positions_out [tokens]: starts[i] plus the token's depth (0 for parents of -1),
+ *     for sem_qk_rotate; starts NULL: the sequence's length less its query tokens.
+ * parents, seqs and cu (NULL: one token each) as for append and attend, starts [n],
+ * all int32 DEVICE. mask_words, from 1 to 128, is a 32nd of the most query tokens of
+ * a sequence, or more. Device-detected SEM_EINVAL: a parent that does not come first
+ * (taken for -1), more query tokens than bits (those beyond see the context alone),
+ * sequences, lengths and offsets as for attend.
+ *
+ * sem_kv_attend_tree is sem_kv_attend with such masks, or any others: a row sees the
+ * context and those of the query tokens' keys whose bits are set; bits of keys that
+ * are not there do not count. query->causal is 1 and query->window 0 (SEM_EINVAL for
+ * others). Its workspace is sem_kv_attend_workspace_bytes.
+ */
+int sem_kv_tree(const sem_kv_cache *cache, const int32_t *parents, const int32_t *starts,
+                const int32_t *seqs, const int32_t *cu, int64_t n, int64_t tokens,
+                int32_t mask_words, uint32_t *mask_out, int32_t *positions_out);
+int sem_kv_tree_async(const sem_kv_cache *cache, const int32_t *parents, const int32_t *starts,
+                      const int32_t *seqs, const int32_t *cu, int64_t n, int64_t tokens,
+                      int32_t mask_words, uint32_t *mask_out, int32_t *positions_out,
+                      void *workspace, size_t ws_bytes, void *stream);
+int sem_kv_attend_tree(const sem_kv_cache *cache, int32_t layer, const sem_kv_query *query,
+                       const uint32_t *mask, int32_t mask_words, const int32_t *seqs,
+                       const int32_t *cu, int64_t n);
+int sem_kv_attend_tree_async(const sem_kv_cache *cache, int32_t layer, const sem_kv_query *query,
+                             const uint32_t *mask, int32_t mask_words, const int32_t *seqs,
+                             const int32_t *cu, int64_t n, void *workspace, size_t ws_bytes,
+                             void *stream);
+
+/*
  * Rotate: the norms of queries and keys, head by head, and the rotation of their
  * positions, what new tokens go through before append and attend. For every row x
  * (a token and a head) of head_dim channels (64, 128 or 256; SEM_ENOTIMPL for

@@ -51,25 +51,53 @@ def read(data, scale, geom, table, n, layer, which, head):
     return out
 
 
-def attend(q, ks, vs, scale, causal, window):
-    """One head's queries [m, dim] at the last positions of keys ks [n, dim].
+def visible(m, n, i, causal, window):
+    """The keys that query i of m sees of n, as a range."""
+    pos = n - m + i
+    hi = max(min(pos + 1, n), 0) if causal else n
+    lo = max(pos + 1 - window, 0) if window else 0
+    return range(lo, max(hi, lo))
+
+
+def attend(q, ks, vs, scale, causal, window, seen=None):
+    """One head's queries [m, dim] at the last positions of keys ks [n, dim]; `seen`
+    lists the keys of each query instead.
 
     Returns the outputs, lse, and sum_j p_j |v_j| (what errors are relative to)."""
     m, n = q.shape[0], ks.shape[0]
     out, lse, mag = np.zeros(q.shape), np.full(m, -np.inf), np.zeros(q.shape)
     for i in range(m):
-        pos = n - m + i
-        hi = max(min(pos + 1, n), 0) if causal else n
-        lo = max(pos + 1 - window, 0) if window else 0
-        if hi <= lo:
+        keys = list(visible(m, n, i, causal, window) if seen is None else seen[i])
+        if not keys:
             continue
-        x = ks[lo:hi] @ q[i] * scale
+        x = ks[keys] @ q[i] * scale
         top = x.max()
         p = np.exp(x - top)
         lse[i] = top + math.log(p.sum())
         p /= p.sum()
-        out[i], mag[i] = p @ vs[lo:hi], p @ np.abs(vs[lo:hi])
+        out[i], mag[i] = p @ vs[keys], p @ np.abs(vs[keys])
     return out, lse, mag
+
+
+def tree(parents):
+    """(the sets of tokens that each of a sequence's drafted tokens continues, itself
+    among them, their depths)."""
+    sets, depth = [], []
+    for t, p in enumerate(parents):
+        sets.append({t} | (sets[p] if p >= 0 else set()))
+        depth.append(depth[p] + 1 if p >= 0 else 0)
+    return sets, depth
+
+
+def tree_words(sets, words):
+    """Masks of such sets, 32 bits to a word."""
+    return [[sum(1 << (j % 32) for j in s if j // 32 == w) for w in range(words)] for s in sets]
+
+
+def tree_keys(sets, n):
+    """The keys of n that tokens of such sets see."""
+    m = len(sets)
+    return [[*range(n - m), *(n - m + j for j in sorted(s) if n - m + j >= 0)] for s in sets]
 
 
 def rotate(x, w, eps, positions, inv_freq, interleaved):

@@ -77,6 +77,10 @@ SYMBOLS = (
     "sem_kv_attend_workspace_bytes",
     "sem_kv_attend",
     "sem_kv_attend_async",
+    "sem_kv_tree",
+    "sem_kv_tree_async",
+    "sem_kv_attend_tree",
+    "sem_kv_attend_tree_async",
     "sem_qk_rotate",
     "sem_qk_rotate_async",
 )
@@ -90,6 +94,7 @@ STAGE_HIST, STAGE_FIRST, STAGE_FINAL, STAGE_MERGE, STAGE_POLICY, STAGE_COST, STA
 # comparison policies (Section 4): the key fields before the id
 POLICY_SEMANTIC, POLICY_FCFS, POLICY_SJF, POLICY_HPJF = 0, 1, 2, 3
 KV_INT8, KV_FP8 = 0, 1  # the codes of a KV cache
+KV_MASK_WORDS = 128  # most words of a drafted token's mask
 
 
 class CostModelC(ctypes.Structure):
@@ -199,7 +204,9 @@ def _load() -> ctypes.CDLL:
     append = [kv, i32, vp, vp, i32, i64, i64, i64, i64] + rows + [i64]
     for name, args in (("fork", [kv, vp, vp, vp, i64]), ("reserve", [kv, vp, vp, i64]),
                        ("free", [kv, vp, vp, i64]), ("compact", [kv]), ("append", append),
-                       ("attend", [kv, i32, vp] + rows)):  # (a sem_kv_query)
+                       ("attend", [kv, i32, vp] + rows),  # (a sem_kv_query)
+                       ("attend_tree", [kv, i32, vp, vp, i32] + rows),
+                       ("tree", [kv, vp, vp] + rows + [i64, i32, vp, vp])):
         for form, more in (("", []), ("_async", tail)):
             fn = getattr(lib, f"sem_kv_{name}{form}")
             fn.argtypes, fn.restype = args + more, ctypes.c_int
@@ -857,8 +864,8 @@ class KVCache:
     def attend(self, layer: int, q: torch.Tensor, seqs: torch.Tensor,
                cu: Optional[torch.Tensor] = None, *, causal: bool = True, window: int = 0,
                scale: Optional[float] = None, max_new: int = 0, max_len: int = 0,
-               out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None
-               ) -> torch.Tensor:
+               out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+               tree: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Attention of q [tokens, heads, head_dim] over the cache of one layer.
 
         Rows belong to sequences as in ``append``. ``scale`` of the scores
@@ -866,7 +873,9 @@ class KVCache:
         to that many positions up to its own; ``max_new`` and ``max_len`` bound
         a sequence's queries and length (0: unknown) and only guide how the
         work is split. ``lse`` (float32 [tokens, heads]) receives the log of
-        the softmax sums. Returns ``out``, which has no gradient."""
+        the softmax sums. With ``tree``, the masks that ``tree`` made (int32 [tokens,
+        words]), a row sees the context and, of its sequence's new tokens, those
+        whose bits are set. Returns ``out``, which has no gradient."""
         dtype = self._rows(q, "q")
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
@@ -893,12 +902,54 @@ class KVCache:
         query = _KV_QUERY.pack(q.data_ptr(), out.data_ptr(), 0 if lse is None else lse.data_ptr(),
                                q0, q1, o0, o1, tokens, max_new, max_len, heads, dtype, causal,
                                window, self.head_dim ** -0.5 if scale is None else scale)
+        if tree is not None:
+            if tree.dtype != torch.int32 or tree.get_device() != self._index or tree.dim() != 2 \
+                    or tree.shape[0] != tokens or not tree.is_contiguous():
+                raise ValueError("tree must be contiguous int32 [tokens, words] on the cache's GPU")
+            rc = _enqueue(self._index, lib.sem_kv_attend_tree_async, self._ref, layer, query,
+                          tree.data_ptr(), tree.shape[1], self._list(seqs, "seqs"),
+                          self._same(cu, n + 1, "cu"), n, self._ws, self.ws_bytes)
+            if rc:
+                _raise(rc, "sem_kv_attend_tree_async")
+            return out
         rc = lib.sem_kv_attend_async(self._ref, layer, query, self._list(seqs, "seqs"),
                                      self._same(cu, n + 1, "cu"), n, self._ws, self.ws_bytes,
                                      _raw_stream(self._index))
         if rc:
             _raise(rc, "sem_kv_attend_async")
         return out
+
+    def tree(self, parents: torch.Tensor, seqs: torch.Tensor, cu: Optional[torch.Tensor] = None,
+             starts: Optional[torch.Tensor] = None, *, max_new: int = 0,
+             mask: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None
+             ) -> Tuple[torch.Tensor, torch.Tensor]:
+        """Masks and positions of drafted tokens that form trees, for ``attend`` of
+        every layer and for ``qk_rotate``.
+
+        Rows belong to sequences as in ``append``. ``parents`` (int32 [tokens]) is
+        the number, among its sequence's new tokens, of the earlier one that a
+        token continues, -1 for the context. A token's position is starts[i]
+        (None: the length without the new tokens) plus its depth. ``max_new``
+        bounds the new tokens of a sequence (0: unknown) and decides the words of
+        a mask, 4096 tokens at most. Returns ``mask`` (int32 [tokens, words]) and
+        ``positions`` (int32 [tokens])."""
+        tokens, n = parents.numel(), seqs.numel()
+        if mask is None:
+            words = min(max(-(-(max_new or tokens) // 32), 1), KV_MASK_WORDS)
+            mask = torch.empty((tokens, words), dtype=torch.int32, device=parents.device)
+        if positions is None:
+            positions = torch.empty(tokens, dtype=torch.int32, device=parents.device)
+        if mask.dtype != torch.int32 or mask.get_device() != self._index or mask.dim() != 2 \
+                or mask.shape[0] != tokens or not mask.is_contiguous():
+            raise ValueError("mask must be contiguous int32 [tokens, words] on the cache's GPU")
+        rc = _enqueue(self._index, lib.sem_kv_tree_async, self._ref,
+                      self._list(parents, "parents"), self._same(starts, n, "starts"),
+                      self._list(seqs, "seqs"), self._same(cu, n + 1, "cu"), n, tokens,
+                      mask.shape[1], mask.data_ptr(), self._same(positions, tokens, "positions"),
+                      self._ws, self.ws_bytes)
+        if rc:
+            _raise(rc, "sem_kv_tree_async")
+        return mask, positions
 
     def check(self) -> None:
         """Waits for the current stream; raises on an error of any operation

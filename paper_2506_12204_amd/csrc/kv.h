@@ -12,6 +12,7 @@ namespace semsched {
 constexpr int kKvCounts = 1024;      // counters of attention's tiles with several parts
 constexpr int kKvPieces = 256;       // of attention's work, where it is cut into equal ones
 constexpr int kKvTile = 16;          // tokens per tile of a page's block
+constexpr int kKvMaskWords = 128;    // most words of a drafted token's mask
 
 // The cache as the kernels see it: the caller's arrays and the derived sizes.
 struct KvView {
@@ -99,6 +100,19 @@ struct KvAttendArgs {
   float* part_o;   // [rows][head_dim]
   float* part_ml;  // [rows][2]: maximum (log2), sum
   KvCut* cuts;     // [kKvPieces], of the tile that a piece ends with
+  // of drafted trees: [tokens][mask_words]
+  const uint32_t* mask;
+  int32_t mask_words;
+};
+
+struct KvTreeArgs {
+  KvView c;
+  const int32_t *parents, *starts;  // starts may be null: the lengths less the tokens
+  const int32_t *seqs, *cu;
+  int64_t n, tokens;
+  int32_t words;
+  uint32_t* mask;      // [tokens][words]
+  int32_t* positions;  // [tokens]
 };
 
 struct QkRotateArgs {
@@ -127,6 +141,8 @@ hipError_t launch_kv_compact(const KvCompactArgs& a, hipStream_t st);
 hipError_t launch_kv_append(const KvAppendArgs& a, hipStream_t st);
 hipError_t launch_qk_rotate(const QkRotateArgs& a, int head_dim, hipStream_t st);
 hipError_t launch_kv_attend(const KvAttendArgs& a, hipStream_t st);
+hipError_t launch_kv_attend_tree(const KvAttendArgs& a, hipStream_t st);
+hipError_t launch_kv_tree(const KvTreeArgs& a, hipStream_t st);
 
 // How an attention call of these sizes is split (its workspace holds the
 // parts' partial outputs).

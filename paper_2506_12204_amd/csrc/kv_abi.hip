@@ -207,6 +207,71 @@ int check_attend(const sem_kv_cache* c, int32_t layer, const sem_kv_query* q, co
   return SEM_OK;
 }
 
+// The arguments of an attention call whose own were checked.
+int attend_args(const sem_kv_cache* cache, int32_t layer, const sem_kv_query* query,
+                const int32_t* seqs, const int32_t* cu, int64_t n, void* workspace,
+                size_t ws_bytes, KvAttendArgs& a) {
+  const AttendPlan p = attend_plan(cache, query->heads, n, query->tokens, query->max_new,
+                                   query->max_len);
+  if (!workspace_ok(workspace, ws_bytes, p.total)) return SEM_EINVAL;
+  char* base = static_cast<char*>(workspace);
+  a.c = view_of(cache, workspace);
+  a.q = static_cast<const uint16_t*>(query->q);
+  a.out = static_cast<uint16_t*>(query->out);
+  a.lse = query->lse;
+  a.q_token = query->q_token_stride;
+  a.q_head = query->q_head_stride;
+  a.out_token = query->out_token_stride;
+  a.out_head = query->out_head_stride;
+  a.seqs = seqs;
+  a.cu = cu;
+  a.n = n;
+  a.tokens = query->tokens;
+  a.layer = layer;
+  a.heads = query->heads;
+  a.group = query->heads / cache->kv_heads;
+  a.bf16 = query->dtype == SEM_KV_BF16;
+  a.wide = aligned16(query->q, query->q_token_stride, query->q_head_stride);
+  a.wide_out = aligned16(query->out, query->out_token_stride, query->out_head_stride);
+  a.causal = query->causal != 0;
+  a.window = query->window;
+  a.scale_log2 = query->scale * 1.4426950408889634f;
+  a.tiled = p.split.tiled;
+  a.whole = p.split.whole;
+  a.waves = p.split.waves;
+  a.parts = p.split.parts;
+  a.part_chunks = p.split.part_chunks;
+  a.counts = reinterpret_cast<uint32_t*>(base + kHeaderBytes);
+  a.part_o = reinterpret_cast<float*>(base + p.part_o);
+  a.part_ml = reinterpret_cast<float*>(base + p.part_ml);
+  a.cuts = reinterpret_cast<KvCut*>(base + p.cuts);
+  return SEM_OK;
+}
+
+int check_words(int32_t mask_words) {
+  return mask_words < 1 || mask_words > kKvMaskWords ? SEM_EINVAL : SEM_OK;
+}
+
+int check_tree(const sem_kv_cache* c, const int32_t* parents, const int32_t* seqs,
+               const int32_t* cu, int64_t n, int64_t tokens, int32_t mask_words,
+               const uint32_t* mask, const int32_t* positions) {
+  int rc = check_cache(c);
+  if (rc == SEM_OK) rc = check_rows(c, 0, seqs, cu, n, tokens);
+  if (rc == SEM_OK) rc = check_words(mask_words);
+  if (rc != SEM_OK) return rc;
+  return tokens > 0 && (!parents || !mask || !positions) ? SEM_EINVAL : SEM_OK;
+}
+
+int check_attend_tree(const sem_kv_cache* c, int32_t layer, const sem_kv_query* q,
+                      const uint32_t* mask, int32_t mask_words, const int32_t* seqs,
+                      const int32_t* cu, int64_t n) {
+  int rc = check_attend(c, layer, q, seqs, cu, n);
+  if (rc == SEM_OK) rc = check_words(mask_words);
+  if (rc != SEM_OK) return rc;
+  // (what a row sees is in its mask)
+  return !q->causal || q->window != 0 || (q->tokens > 0 && !mask) ? SEM_EINVAL : SEM_OK;
+}
+
 int check_rotate(const sem_qk_rotary* r) {
   if (!r || r->tokens < 0 || r->tokens > INT32_MAX || r->heads < 0 || r->kv_heads < 0 ||
       (r->dtype != SEM_KV_BF16 && r->dtype != SEM_KV_F16) || !std::isfinite(r->eps) || r->eps < 0)
@@ -424,44 +489,11 @@ int sem_kv_append(const sem_kv_cache* cache, int32_t layer, const void* k, const
 int sem_kv_attend_async(const sem_kv_cache* cache, int32_t layer, const sem_kv_query* query,
                         const int32_t* seqs, const int32_t* cu, int64_t n, void* workspace,
                         size_t ws_bytes, void* stream) {
-  const int rc = check_attend(cache, layer, query, seqs, cu, n);
+  int rc = check_attend(cache, layer, query, seqs, cu, n);
   if (rc != SEM_OK) return rc;
-  const AttendPlan p = attend_plan(cache, query->heads, n, query->tokens, query->max_new,
-                                   query->max_len);
-  if (!workspace_ok(workspace, ws_bytes, p.total)) return SEM_EINVAL;
-  char* base = static_cast<char*>(workspace);
   KvAttendArgs a = {};
-  a.c = view_of(cache, workspace);
-  a.q = static_cast<const uint16_t*>(query->q);
-  a.out = static_cast<uint16_t*>(query->out);
-  a.lse = query->lse;
-  a.q_token = query->q_token_stride;
-  a.q_head = query->q_head_stride;
-  a.out_token = query->out_token_stride;
-  a.out_head = query->out_head_stride;
-  a.seqs = seqs;
-  a.cu = cu;
-  a.n = n;
-  a.tokens = query->tokens;
-  a.layer = layer;
-  a.heads = query->heads;
-  a.group = query->heads / cache->kv_heads;
-  a.bf16 = query->dtype == SEM_KV_BF16;
-  a.wide = aligned16(query->q, query->q_token_stride, query->q_head_stride);
-  a.wide_out = aligned16(query->out, query->out_token_stride, query->out_head_stride);
-  a.causal = query->causal != 0;
-  a.window = query->window;
-  a.scale_log2 = query->scale * 1.4426950408889634f;
-  a.tiled = p.split.tiled;
-  a.whole = p.split.whole;
-  a.waves = p.split.waves;
-  a.parts = p.split.parts;
-  a.part_chunks = p.split.part_chunks;
-  a.counts = reinterpret_cast<uint32_t*>(base + kHeaderBytes);
-  a.part_o = reinterpret_cast<float*>(base + p.part_o);
-  a.part_ml = reinterpret_cast<float*>(base + p.part_ml);
-  a.cuts = reinterpret_cast<KvCut*>(base + p.cuts);
-  return status_of(launch_kv_attend(a, static_cast<hipStream_t>(stream)));
+  rc = attend_args(cache, layer, query, seqs, cu, n, workspace, ws_bytes, a);
+  return rc == SEM_OK ? status_of(launch_kv_attend(a, static_cast<hipStream_t>(stream))) : rc;
 }
 
 int sem_kv_attend(const sem_kv_cache* cache, int32_t layer, const sem_kv_query* query,
@@ -472,6 +504,68 @@ int sem_kv_attend(const sem_kv_cache* cache, int32_t layer, const sem_kv_query* 
                                   query->max_len).total;
   return blocking(need, [&](void* ws, size_t bytes, hipStream_t st) {
     return sem_kv_attend_async(cache, layer, query, seqs, cu, n, ws, bytes, st);
+  });
+}
+
+int sem_kv_attend_tree_async(const sem_kv_cache* cache, int32_t layer, const sem_kv_query* query,
+                             const uint32_t* mask, int32_t mask_words, const int32_t* seqs,
+                             const int32_t* cu, int64_t n, void* workspace, size_t ws_bytes,
+                             void* stream) {
+  int rc = check_attend_tree(cache, layer, query, mask, mask_words, seqs, cu, n);
+  if (rc != SEM_OK) return rc;
+  KvAttendArgs a = {};
+  rc = attend_args(cache, layer, query, seqs, cu, n, workspace, ws_bytes, a);
+  if (rc != SEM_OK) return rc;
+  a.causal = 0;
+  a.mask = mask;
+  a.mask_words = mask_words;
+  return status_of(launch_kv_attend_tree(a, static_cast<hipStream_t>(stream)));
+}
+
+int sem_kv_attend_tree(const sem_kv_cache* cache, int32_t layer, const sem_kv_query* query,
+                       const uint32_t* mask, int32_t mask_words, const int32_t* seqs,
+                       const int32_t* cu, int64_t n) {
+  const int rc = check_attend_tree(cache, layer, query, mask, mask_words, seqs, cu, n);
+  if (rc != SEM_OK) return rc;
+  const size_t need = attend_plan(cache, query->heads, n, query->tokens, query->max_new,
+                                  query->max_len).total;
+  return blocking(need, [&](void* ws, size_t bytes, hipStream_t st) {
+    return sem_kv_attend_tree_async(cache, layer, query, mask, mask_words, seqs, cu, n, ws, bytes,
+                                    st);
+  });
+}
+
+int sem_kv_tree_async(const sem_kv_cache* cache, const int32_t* parents, const int32_t* starts,
+                      const int32_t* seqs, const int32_t* cu, int64_t n, int64_t tokens,
+                      int32_t mask_words, uint32_t* mask_out, int32_t* positions_out,
+                      void* workspace, size_t ws_bytes, void* stream) {
+  const int rc = check_tree(cache, parents, seqs, cu, n, tokens, mask_words, mask_out,
+                            positions_out);
+  if (rc != SEM_OK) return rc;
+  if (!workspace_ok(workspace, ws_bytes, kZeroed)) return SEM_EINVAL;
+  KvTreeArgs a = {};
+  a.c = view_of(cache, workspace);
+  a.parents = parents;
+  a.starts = starts;
+  a.seqs = seqs;
+  a.cu = cu;
+  a.n = n;
+  a.tokens = tokens;
+  a.words = mask_words;
+  a.mask = mask_out;
+  a.positions = positions_out;
+  return status_of(launch_kv_tree(a, static_cast<hipStream_t>(stream)));
+}
+
+int sem_kv_tree(const sem_kv_cache* cache, const int32_t* parents, const int32_t* starts,
+                const int32_t* seqs, const int32_t* cu, int64_t n, int64_t tokens,
+                int32_t mask_words, uint32_t* mask_out, int32_t* positions_out) {
+  const int rc = check_tree(cache, parents, seqs, cu, n, tokens, mask_words, mask_out,
+                            positions_out);
+  if (rc != SEM_OK) return rc;
+  return blocking(kZeroed, [&](void* ws, size_t bytes, hipStream_t st) {
+    return sem_kv_tree_async(cache, parents, starts, seqs, cu, n, tokens, mask_words, mask_out,
+                             positions_out, ws, bytes, st);
   });
 }
 
