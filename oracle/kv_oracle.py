@@ -120,6 +120,61 @@ def rotate(x, w, eps, positions, inv_freq, interleaved):
     return out, mag
 
 
+def requantized(codes, was, now, fmt):
+    """Bytes of a block of scale `was` on scale `now`: the nearest codes to the 32-bit
+    quotients, ties to the even one."""
+    val = code_values(fmt)
+    x = val[codes].astype(np.float32) * np.float32(was) / np.float32(now)
+    order = [b for b in np.argsort(val, kind="stable") if not math.isnan(val[b])]
+    order = [b for b in order if b != 128]  # -128 is not a code; minus zero counts as zero
+    steps = val[order]
+    x64 = np.clip(x.astype(np.float64), steps[0], steps[-1])
+    hi = np.clip(np.searchsorted(steps, x64), 1, len(steps) - 1)
+    lo = hi - 1
+    up, down = steps[hi] - x64, x64 - steps[lo]
+    even = np.array([b % 2 == 0 for b in order])
+    pick = np.where((up < down) | ((up == down) & even[hi]), hi, lo)
+    return np.array(order, np.uint8)[pick]
+
+
+def keep_tokens(data, scale, geom, table, chosen):
+    """Moves the tokens `chosen` (old positions, ascending) of one sequence to its front,
+    in place; returns the blocks that changed."""
+    layers, heads, pt, dim, fmt = geom
+    moved = [t for t, at in enumerate(chosen) if t != at]
+    if not moved:
+        return range(0)
+    blocks = range(moved[0] // pt, -(-len(chosen) // pt))
+    old_data, old_scale = data.copy(), scale.copy()
+
+    def block(of, page, layer, w, h):
+        return of[page].reshape(layers, 2, heads, pt * dim)[layer, w, h]
+
+    for b in blocks:
+        tokens = chosen[b * pt:(b + 1) * pt]
+        for layer in range(layers):
+            for w in (0, 1):
+                idx = block_index(w, pt, dim)
+                for h in range(heads):
+                    pages = [int(table[at // pt]) for at in tokens]
+                    now = max(float(old_scale[p, layer, w, h]) for p in pages)
+                    scale[int(table[b]), layer, w, h] = now
+                    to = block(data, int(table[b]), layer, w, h)
+                    for t, (at, page) in enumerate(zip(tokens, pages)):
+                        was = float(old_scale[page, layer, w, h])
+                        codes = block(old_data, page, layer, w, h)[idx[at % pt]]
+                        if was != now:
+                            codes = requantized(codes, was, now, fmt)
+                        to[idx[t]] = codes
+    return blocks
+
+
+def same_numbers(a, b, fmt):
+    """Whether bytes stand for the same numbers (either zero, any NaN)."""
+    val = code_values(fmt)
+    return np.array_equal(val[a], val[b], equal_nan=True)
+
+
 class Pages:
     """Reference counts, lengths and tables as lists; contents by page number."""
 

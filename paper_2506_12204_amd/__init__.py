@@ -81,6 +81,9 @@ SYMBOLS = (
     "sem_kv_tree_async",
     "sem_kv_attend_tree",
     "sem_kv_attend_tree_async",
+    "sem_kv_keep",
+    "sem_kv_keep_async",
+    "sem_kv_keep_workspace_bytes",
     "sem_qk_rotate",
     "sem_qk_rotate_async",
 )
@@ -206,12 +209,14 @@ def _load() -> ctypes.CDLL:
                        ("free", [kv, vp, vp, i64]), ("compact", [kv]), ("append", append),
                        ("attend", [kv, i32, vp] + rows),  # (a sem_kv_query)
                        ("attend_tree", [kv, i32, vp, vp, i32] + rows),
-                       ("tree", [kv, vp, vp] + rows + [i64, i32, vp, vp])):
+                       ("tree", [kv, vp, vp] + rows + [i64, i32, vp, vp]),
+                       ("keep", [kv, vp, vp, vp, vp, i64, i64])):
         for form, more in (("", []), ("_async", tail)):
             fn = getattr(lib, f"sem_kv_{name}{form}")
             fn.argtypes, fn.restype = args + more, ctypes.c_int
     for name, args in (("page_bytes", [kv]), ("workspace_bytes", [kv]),
-                       ("attend_workspace_bytes", [kv, i32, i64, i64, i64, i64])):
+                       ("attend_workspace_bytes", [kv, i32, i64, i64, i64, i64]),
+                       ("keep_workspace_bytes", [kv, i64, i64])):
         fn = getattr(lib, f"sem_kv_{name}")
         fn.argtypes, fn.restype = args, sz
     lib.sem_qk_rotate.argtypes, lib.sem_qk_rotate.restype = [vp], ctypes.c_int  # (a sem_qk_rotary)
@@ -802,8 +807,8 @@ class KVCache:
             return
         if torch.cuda.is_current_stream_capturing():
             # (it would lie in the graph's pool, and be zeroed by replays only)
-            raise RuntimeError(f"attention of these sizes needs a workspace of {need} bytes, which "
-                               "cannot be taken while a graph is captured: call it once before")
+            raise RuntimeError(f"a call of these sizes needs a workspace of {need} bytes, which "
+                               "cannot be taken while a graph is captured: make it once before")
         ws = torch.zeros(max(need, 2 * self.ws_bytes), dtype=torch.uint8, device=self.device)
         self._replaced.append(self.workspace)
         self.workspace, self.ws_bytes = ws, ws.numel()
@@ -841,6 +846,30 @@ class KVCache:
         """Moves the pages in use to the lowest numbers."""
         _raise(lib.sem_kv_compact_async(self._ref, self._ws, self.ws_bytes,
                                         _raw_stream(self._index)), "sem_kv_compact_async")
+
+    def _needed(self, what: str, *sizes: int) -> None:
+        """Room for the workspace that a call of these sizes needs."""
+        need = self._needs.get((what, sizes))
+        if need is None:
+            if len(self._needs) > 4096:
+                self._needs.clear()
+            need = int(getattr(lib, f"sem_kv_{what}_workspace_bytes")(self._ref, *sizes))
+            self._needs[what, sizes] = need
+        if need > self.ws_bytes:
+            self._room(need)
+
+    def keep(self, seqs: torch.Tensor, last: torch.Tensor, index: torch.Tensor,
+             cu: torch.Tensor) -> None:
+        """Of the last last[i] tokens of seqs[i], those numbered index[cu[i]..cu[i+1]]
+        (from 0, ascending) stay, in all layers: the accepted path of a drafted tree.
+        The tokens before them stay, too; pages behind are given back."""
+        n, total = seqs.numel(), index.numel()
+        self._needed("keep", n, total)
+        rc = _enqueue(self._index, lib.sem_kv_keep_async, self._ref, self._list(seqs, "seqs"),
+                      self._same(last, n, "last"), self._list(index, "index"),
+                      self._same(cu, n + 1, "cu"), n, total, self._ws, self.ws_bytes)
+        if rc:
+            _raise(rc, "sem_kv_keep_async")
 
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, seqs: torch.Tensor,
                cu: Optional[torch.Tensor] = None) -> None:

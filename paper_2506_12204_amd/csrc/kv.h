@@ -115,6 +115,23 @@ struct KvTreeArgs {
   int32_t* positions;  // [tokens]
 };
 
+// A sequence that keeps some of its tokens.
+struct KvKept {
+  int32_t seq;             // -1: nothing changes
+  int32_t now;             // its new length
+  int32_t begin, end;      // the blocks whose tokens change
+  int64_t source, scales;  // where its tokens' sources and its blocks' scales start
+};
+
+struct KvKeepArgs {
+  KvView c;
+  const int32_t *seqs, *last, *index, *cu;
+  int64_t n, total;
+  KvKept* kept;     // [n]
+  int64_t* source;  // of each token from block `begin` on: page * page_tokens + place
+  float* scales;    // [blocks][page_scales]
+};
+
 struct QkRotateArgs {
   const uint16_t *q, *k;  // 16-bit elements
   uint16_t *q_out, *k_out;
@@ -142,6 +159,7 @@ hipError_t launch_kv_append(const KvAppendArgs& a, hipStream_t st);
 hipError_t launch_qk_rotate(const QkRotateArgs& a, int head_dim, hipStream_t st);
 hipError_t launch_kv_attend(const KvAttendArgs& a, hipStream_t st);
 hipError_t launch_kv_attend_tree(const KvAttendArgs& a, hipStream_t st);
+hipError_t launch_kv_keep(const KvKeepArgs& a, hipStream_t st);
 hipError_t launch_kv_tree(const KvTreeArgs& a, hipStream_t st);
 
 // How an attention call of these sizes is split (its workspace holds the

@@ -248,6 +248,50 @@ int attend_args(const sem_kv_cache* cache, int32_t layer, const sem_kv_query* qu
   return SEM_OK;
 }
 
+// The plan, sources and scales of sequences that keep `total` tokens among their
+// listed ones.
+struct KeepLayout {
+  size_t kept = kZeroed, source = 0, scales = 0, total = 0;
+};
+
+KeepLayout keep_layout(const sem_kv_cache* c, int64_t n, int64_t sources, int64_t blocks) {
+  KeepLayout L;
+  L.source = align_up(L.kept + sizeof(KvKept) * (size_t)n);
+  L.scales = align_up(L.source + 8 * (size_t)sources);
+  L.total = align_up(L.scales + 4 * (size_t)blocks * (size_t)(c->layers * 2 * c->kv_heads));
+  return L;
+}
+
+KeepLayout keep_layout(const sem_kv_cache* c, int64_t n, int64_t total) {
+  // (a sequence's first block may begin a page before its first listed token, and
+  // its last one ends a page after it)
+  return keep_layout(c, n, total + n * c->page_tokens, total / c->page_tokens + 2 * n);
+}
+
+KvKeepArgs keep_args(const sem_kv_cache* c, const KeepLayout& L, const int32_t* seqs, int64_t n,
+                     void* workspace) {
+  char* base = static_cast<char*>(workspace);
+  KvKeepArgs a = {};
+  a.c = view_of(c, workspace);
+  a.seqs = seqs;
+  a.n = n;
+  a.kept = reinterpret_cast<KvKept*>(base + L.kept);
+  a.source = reinterpret_cast<int64_t*>(base + L.source);
+  a.scales = reinterpret_cast<float*>(base + L.scales);
+  return a;
+}
+
+int check_keep(const sem_kv_cache* c, const int32_t* seqs, const int32_t* last,
+               const int32_t* index, const int32_t* cu, int64_t n, int64_t total) {
+  int rc = check_cache(c);
+  if (rc == SEM_OK) rc = check_list(c, seqs, n);
+  if (rc != SEM_OK) return rc;
+  if (total < 0 || total > INT32_MAX || (n == 0 && total > 0) || (n > 0 && (!last || !cu)) ||
+      (total > 0 && !index))
+    return SEM_EINVAL;
+  return SEM_OK;
+}
+
 int check_words(int32_t mask_words) {
   return mask_words < 1 || mask_words > kKvMaskWords ? SEM_EINVAL : SEM_OK;
 }
@@ -566,6 +610,36 @@ int sem_kv_tree(const sem_kv_cache* cache, const int32_t* parents, const int32_t
   return blocking(kZeroed, [&](void* ws, size_t bytes, hipStream_t st) {
     return sem_kv_tree_async(cache, parents, starts, seqs, cu, n, tokens, mask_words, mask_out,
                              positions_out, ws, bytes, st);
+  });
+}
+
+size_t sem_kv_keep_workspace_bytes(const sem_kv_cache* cache, int64_t n, int64_t total) {
+  if (check_sizes(cache) != SEM_OK || n < 0 || n > cache->slots || total < 0 || total > INT32_MAX)
+    return 0;
+  return keep_layout(cache, n, total).total;
+}
+
+int sem_kv_keep_async(const sem_kv_cache* cache, const int32_t* seqs, const int32_t* last,
+                      const int32_t* index, const int32_t* cu, int64_t n, int64_t total,
+                      void* workspace, size_t ws_bytes, void* stream) {
+  const int rc = check_keep(cache, seqs, last, index, cu, n, total);
+  if (rc != SEM_OK) return rc;
+  const KeepLayout L = keep_layout(cache, n, total);
+  if (!workspace_ok(workspace, ws_bytes, L.total)) return SEM_EINVAL;
+  KvKeepArgs a = keep_args(cache, L, seqs, n, workspace);
+  a.last = last;
+  a.index = index;
+  a.cu = cu;
+  a.total = total;
+  return status_of(launch_kv_keep(a, static_cast<hipStream_t>(stream)));
+}
+
+int sem_kv_keep(const sem_kv_cache* cache, const int32_t* seqs, const int32_t* last,
+                const int32_t* index, const int32_t* cu, int64_t n, int64_t total) {
+  const int rc = check_keep(cache, seqs, last, index, cu, n, total);
+  if (rc != SEM_OK) return rc;
+  return blocking(keep_layout(cache, n, total).total, [&](void* ws, size_t bytes, hipStream_t st) {
+    return sem_kv_keep_async(cache, seqs, last, index, cu, n, total, ws, bytes, st);
   });
 }
 

@@ -47,6 +47,44 @@ __device__ __forceinline__ float load16(uint16_t u, int bf16) {
   return bf16 ? __uint_as_float((uint32_t)u << 16) : (float)__builtin_bit_cast(_Float16, u);
 }
 
+// x / by for one `by`, rounded correctly from the reciprocal (rounded correctly,
+// too) by one step with the remainder: Markstein's theorem, as long as nothing
+// underflows, for which x and `by` are first brought to a middle range by the
+// same power of two.
+struct Quotient {
+  float by, inv, lift;
+  __device__ __forceinline__ explicit Quotient(float b) {
+    lift = b < 0x1p-64f ? 0x1p64f : b > 0x1p64f ? 0x1p-64f : 1.0f;
+    by = b * lift;
+    inv = 1.0f / by;
+  }
+  __device__ __forceinline__ float of(float x) const { return of_lifted(x * lift); }
+  __device__ __forceinline__ float of_lifted(float y) const {
+    const float q = y * inv;
+    return __builtin_fmaf(__builtin_fmaf(-q, by, y), inv, q);
+  }
+};
+
+// Four quotients as codes: ties to even, beyond the range the largest code. (NaN
+// does not reach this.)
+template <int FMT>
+__device__ __forceinline__ uint32_t pack_codes(float a, float b, float c, float d) {
+  const float top = code_max<FMT>();
+  a = __builtin_amdgcn_fmed3f(a, -top, top);
+  b = __builtin_amdgcn_fmed3f(b, -top, top);
+  c = __builtin_amdgcn_fmed3f(c, -top, top);
+  d = __builtin_amdgcn_fmed3f(d, -top, top);
+  if (FMT == SEM_KV_INT8) {
+    // 1.5 * 2^23 more: the sum's low byte is the nearest whole number
+    const uint32_t x = __float_as_uint(a + 12582912.0f), y = __float_as_uint(b + 12582912.0f);
+    const uint32_t z = __float_as_uint(c + 12582912.0f), w = __float_as_uint(d + 12582912.0f);
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(w, z, 0x0c0c0400u),
+                                 __builtin_amdgcn_perm(y, x, 0x0c0c0400u), 0x05040100u);
+  }
+  int p = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, p, true);
+}
+
 // Two values in the outputs' type, rounded to the nearest.
 template <bool BF16>
 __device__ __forceinline__ uint32_t pack_pair(float x, float y) {
