@@ -677,6 +677,29 @@ int sem_kv_keep_async(const sem_kv_cache *cache, const int32_t *seqs, const int3
                       void *workspace, size_t ws_bytes, void *stream);
 
 /*
+ * Weigh: adds to every cached token the softmax weights that the query rows give to
+ * its key, over rows and heads: for key j of sequence s,
+ *   mass[s * mass_stride + j] += sum over rows that see j of exp(score - lse)
+ * with the rows, keys, scores and what is seen as for sem_kv_attend of the same query,
+ * whose lse (an input here) that call returned; query->out is not looked at. Called
+ * for every layer (or some) after its attention, with all query rows or only the last
+ * ones, it sums what prune goes by. A row whose lse is not finite (it sees no key, or
+ * holds no numbers) adds nothing. Sums are of 32 bits, the same in every run.
+ *   mass [slots][mass_stride] float DEVICE, mass_stride at least max_blocks *
+ *   page_tokens. Entries of a sequence's keys from its length on are not changed:
+ *   those of a token that is new, or of a slot that is taken again, have to be what
+ *   the caller wants them to start from, 0 as a rule. (prune leaves zeros behind the
+ *   new length, fork and free leave mass alone.)
+ * Its workspace is the first SEM_KV_ZEROED_BYTES.
+ */
+int sem_kv_weigh(const sem_kv_cache *cache, int32_t layer, const sem_kv_query *query,
+                 const int32_t *seqs, const int32_t *cu, int64_t n, float *mass,
+                 int64_t mass_stride);
+int sem_kv_weigh_async(const sem_kv_cache *cache, int32_t layer, const sem_kv_query *query,
+                       const int32_t *seqs, const int32_t *cu, int64_t n, float *mass,
+                       int64_t mass_stride, void *workspace, size_t ws_bytes, void *stream);
+
+/*
  * Rotate: the norms of queries and keys, head by head, and the rotation of their
  * positions, what new tokens go through before append and attend. For every row x
  * (a token and a head) of head_dim channels (64, 128 or 256; SEM_ENOTIMPL for

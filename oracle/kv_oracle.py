@@ -79,6 +79,18 @@ def attend(q, ks, vs, scale, causal, window, seen=None):
     return out, lse, mag
 
 
+def weigh(q, ks, scale, causal, window, lse):
+    """What one head's queries [m, dim] add to the weights of keys ks [n, dim]; rows whose
+    lse is not finite add nothing."""
+    m, n = q.shape[0], ks.shape[0]
+    out = np.zeros(n)
+    for i in range(m):
+        keys = list(visible(m, n, i, causal, window))
+        if keys and math.isfinite(lse[i]):
+            out[keys] += np.exp(ks[keys] @ q[i] * scale - lse[i])
+    return out
+
+
 def tree(parents):
     """(the sets of tokens that each of a sequence's drafted tokens continues, itself
     among them, their depths)."""

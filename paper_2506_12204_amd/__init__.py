@@ -84,6 +84,8 @@ SYMBOLS = (
     "sem_kv_keep",
     "sem_kv_keep_async",
     "sem_kv_keep_workspace_bytes",
+    "sem_kv_weigh",
+    "sem_kv_weigh_async",
     "sem_qk_rotate",
     "sem_qk_rotate_async",
 )
@@ -210,7 +212,8 @@ def _load() -> ctypes.CDLL:
                        ("attend", [kv, i32, vp] + rows),  # (a sem_kv_query)
                        ("attend_tree", [kv, i32, vp, vp, i32] + rows),
                        ("tree", [kv, vp, vp] + rows + [i64, i32, vp, vp]),
-                       ("keep", [kv, vp, vp, vp, vp, i64, i64])):
+                       ("keep", [kv, vp, vp, vp, vp, i64, i64]),
+                       ("weigh", [kv, i32, vp] + rows + [vp, i64])):
         for form, more in (("", []), ("_async", tail)):
             fn = getattr(lib, f"sem_kv_{name}{form}")
             fn.argtypes, fn.restype = args + more, ctypes.c_int
@@ -870,6 +873,40 @@ class KVCache:
                       self._same(cu, n + 1, "cu"), n, total, self._ws, self.ws_bytes)
         if rc:
             _raise(rc, "sem_kv_keep_async")
+
+    def _mass(self, mass: torch.Tensor) -> int:
+        """The row stride of sums [slots, at least max_blocks * page_tokens]."""
+        if mass.dtype != torch.float32 or mass.get_device() != self._index or mass.dim() != 2 \
+                or mass.shape[0] != self.slots or mass.stride(1) != 1 \
+                or mass.shape[1] < self.max_blocks * self.page_tokens:
+            raise ValueError("mass must be float32 [slots, max_blocks * page_tokens or more] on the "
+                             "cache's GPU, its rows' entries side by side")
+        return mass.stride(0)
+
+    def weigh(self, layer: int, q: torch.Tensor, lse: torch.Tensor, mass: torch.Tensor,
+              seqs: torch.Tensor, cu: Optional[torch.Tensor] = None, *, causal: bool = True,
+              window: int = 0, scale: Optional[float] = None, max_new: int = 0, max_len: int = 0
+              ) -> None:
+        """Adds to ``mass`` (float32 [slots, max_blocks * page_tokens]) the softmax
+        weights that the rows of q give to every cached token, over rows and heads.
+        The arguments are those of ``attend`` of the same rows (or of the last ones of
+        each sequence), which returned ``lse`` (float32 [tokens, heads]). Entries of
+        tokens that were not weighed yet have to be zero."""
+        dtype = self._rows(q, "q")
+        tokens, heads, _ = q.shape
+        if lse.dtype != torch.float32 or lse.get_device() != self._index \
+                or lse.shape != (tokens, heads) or not lse.is_contiguous():
+            raise ValueError("lse must be contiguous float32 [tokens, heads] on the cache's GPU")
+        n, stride = seqs.numel(), self._mass(mass)
+        q0, q1, _ = q.stride()
+        query = _KV_QUERY.pack(q.data_ptr(), 0, lse.data_ptr(), q0, q1, 0, 0, tokens, max_new,
+                               max_len, heads, dtype, causal, window,
+                               self.head_dim ** -0.5 if scale is None else scale)
+        rc = _enqueue(self._index, lib.sem_kv_weigh_async, self._ref, layer, query,
+                      self._list(seqs, "seqs"), self._same(cu, n + 1, "cu"), n, mass.data_ptr(),
+                      stride, self._ws, self.ws_bytes)
+        if rc:
+            _raise(rc, "sem_kv_weigh_async")
 
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, seqs: torch.Tensor,
                cu: Optional[torch.Tensor] = None) -> None:

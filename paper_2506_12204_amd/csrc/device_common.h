@@ -203,6 +203,12 @@ __device__ __forceinline__ uint64_t last_lane_u64(uint64_t v) {
   return ((uint64_t)hi << 32) | lo;
 }
 
+// Value of one lane, the same for all.
+__device__ __forceinline__ uint64_t lane_u64(uint64_t v, int lane) {
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane) |
+         (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32;
+}
+
 // Inclusive wave scan of a 64-bit value (modulo 2^64): limbs of 22, 21 and 21
 // bits, each limb's sum staying below 2^28. Lane moves only, where shuffles
 // of 64-bit values are twelve dependent LDS-path operations (0.6 us).

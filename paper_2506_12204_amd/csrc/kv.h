@@ -132,6 +132,21 @@ struct KvKeepArgs {
   float* scales;    // [blocks][page_scales]
 };
 
+struct KvWeighArgs {
+  KvView c;
+  const uint16_t* q;
+  const float* lse;  // [tokens][heads]
+  float* mass;       // [slots][mass_stride]
+  int64_t q_token, q_head, mass_stride;
+  const int32_t *seqs, *cu;
+  int64_t n, tokens;
+  int32_t layer, heads, group;
+  int32_t bf16, wide;  // 16-byte loads of q are aligned
+  int32_t causal, window;
+  float scale_log2;
+  int32_t key_slots;  // of a workgroup's waves (set by the launch)
+};
+
 struct QkRotateArgs {
   const uint16_t *q, *k;  // 16-bit elements
   uint16_t *q_out, *k_out;
@@ -159,6 +174,7 @@ hipError_t launch_kv_append(const KvAppendArgs& a, hipStream_t st);
 hipError_t launch_qk_rotate(const QkRotateArgs& a, int head_dim, hipStream_t st);
 hipError_t launch_kv_attend(const KvAttendArgs& a, hipStream_t st);
 hipError_t launch_kv_attend_tree(const KvAttendArgs& a, hipStream_t st);
+hipError_t launch_kv_weigh(const KvWeighArgs& a, int64_t max_len, hipStream_t st);
 hipError_t launch_kv_keep(const KvKeepArgs& a, hipStream_t st);
 hipError_t launch_kv_tree(const KvTreeArgs& a, hipStream_t st);
 

@@ -292,6 +292,26 @@ int check_keep(const sem_kv_cache* c, const int32_t* seqs, const int32_t* last,
   return SEM_OK;
 }
 
+int64_t most_tokens(const sem_kv_cache* c) { return (int64_t)c->max_blocks * c->page_tokens; }
+
+int check_mass(const sem_kv_cache* c, const float* mass, int64_t mass_stride) {
+  if (mass_stride < most_tokens(c) || reinterpret_cast<uintptr_t>(mass) % 4 != 0)
+    return SEM_EINVAL;
+  return !mass && c->slots > 0 && most_tokens(c) > 0 ? SEM_EINVAL : SEM_OK;
+}
+
+int check_weigh(const sem_kv_cache* c, int32_t layer, const sem_kv_query* q, const int32_t* seqs,
+                const int32_t* cu, int64_t n, const float* mass, int64_t mass_stride) {
+  if (!q) return check_cache(c) == SEM_OK ? SEM_EINVAL : check_cache(c);
+  sem_kv_query asked = *q;  // (its output is not looked at)
+  asked.out = const_cast<void*>(q->q);
+  asked.out_token_stride = asked.out_head_stride = 0;
+  int rc = check_attend(c, layer, &asked, seqs, cu, n);
+  if (rc == SEM_OK) rc = check_mass(c, mass, mass_stride);
+  if (rc != SEM_OK) return rc;
+  return q->tokens > 0 && !q->lse ? SEM_EINVAL : SEM_OK;
+}
+
 int check_words(int32_t mask_words) {
   return mask_words < 1 || mask_words > kKvMaskWords ? SEM_EINVAL : SEM_OK;
 }
@@ -640,6 +660,47 @@ int sem_kv_keep(const sem_kv_cache* cache, const int32_t* seqs, const int32_t* l
   if (rc != SEM_OK) return rc;
   return blocking(keep_layout(cache, n, total).total, [&](void* ws, size_t bytes, hipStream_t st) {
     return sem_kv_keep_async(cache, seqs, last, index, cu, n, total, ws, bytes, st);
+  });
+}
+
+int sem_kv_weigh_async(const sem_kv_cache* cache, int32_t layer, const sem_kv_query* query,
+                       const int32_t* seqs, const int32_t* cu, int64_t n, float* mass,
+                       int64_t mass_stride, void* workspace, size_t ws_bytes, void* stream) {
+  const int rc = check_weigh(cache, layer, query, seqs, cu, n, mass, mass_stride);
+  if (rc != SEM_OK) return rc;
+  if (!workspace_ok(workspace, ws_bytes, kZeroed)) return SEM_EINVAL;
+  KvWeighArgs a = {};
+  a.c = view_of(cache, workspace);
+  a.q = static_cast<const uint16_t*>(query->q);
+  a.lse = query->lse;
+  a.mass = mass;
+  a.q_token = query->q_token_stride;
+  a.q_head = query->q_head_stride;
+  a.mass_stride = mass_stride;
+  a.seqs = seqs;
+  a.cu = cu;
+  a.n = n;
+  a.tokens = query->tokens;
+  a.layer = layer;
+  a.heads = query->heads;
+  a.group = query->heads / cache->kv_heads;
+  a.bf16 = query->dtype == SEM_KV_BF16;
+  a.wide = aligned16(query->q, query->q_token_stride, query->q_head_stride);
+  a.causal = query->causal != 0;
+  a.window = query->window;
+  a.scale_log2 = query->scale * 1.4426950408889634f;
+  const int64_t most = most_tokens(cache);
+  return status_of(launch_kv_weigh(a, query->max_len > 0 ? std::min(query->max_len, most) : most,
+                                   static_cast<hipStream_t>(stream)));
+}
+
+int sem_kv_weigh(const sem_kv_cache* cache, int32_t layer, const sem_kv_query* query,
+                 const int32_t* seqs, const int32_t* cu, int64_t n, float* mass,
+                 int64_t mass_stride) {
+  const int rc = check_weigh(cache, layer, query, seqs, cu, n, mass, mass_stride);
+  if (rc != SEM_OK) return rc;
+  return blocking(kZeroed, [&](void* ws, size_t bytes, hipStream_t st) {
+    return sem_kv_weigh_async(cache, layer, query, seqs, cu, n, mass, mass_stride, ws, bytes, st);
   });
 }
 

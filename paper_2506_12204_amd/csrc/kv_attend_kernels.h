@@ -201,23 +201,6 @@ struct Query {
   }
 };
 
-// Sixteen codes as two operands of eight halves.
-template <int FMT>
-__device__ __forceinline__ void codes_to_operands(uint4 w, half8_t& lo, half8_t& hi) {
-  half2_t p[8];
-  codes_to_half<FMT>(w.x, p[0], p[1]);
-  codes_to_half<FMT>(w.y, p[2], p[3]);
-  codes_to_half<FMT>(w.z, p[4], p[5]);
-  codes_to_half<FMT>(w.w, p[6], p[7]);
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    lo[2 * k] = p[k][0];
-    lo[2 * k + 1] = p[k][1];
-    hi[2 * k] = p[4 + k][0];
-    hi[2 * k + 1] = p[4 + k][1];
-  }
-}
-
 // Zeroes the codes from the n-th on.
 __device__ __forceinline__ uint32_t keep_bytes(uint32_t w, int n) {
   return n >= 4 ? w : n <= 0 ? 0u : w & ((1u << (8 * n)) - 1u);
@@ -661,11 +644,6 @@ __device__ __forceinline__ Share share_of(const KvAttendArgs& a, int64_t i) {
   }
   s.first = group * (uint64_t)(len + kTileCost);
   return s;
-}
-
-__device__ __forceinline__ uint64_t lane_u64(uint64_t v, int lane) {
-  return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane) |
-         (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32;
 }
 
 __device__ __forceinline__ Share lane_share(const Share& s, int lane) {

@@ -36,6 +36,38 @@ __device__ __forceinline__ void codes_to_half(uint32_t w, half2_t& lo, half2_t& 
   }
 }
 
+// Sixteen codes as two operands of eight halves.
+template <int FMT>
+__device__ __forceinline__ void codes_to_operands(uint4 w, half8_t& lo, half8_t& hi) {
+  half2_t p[8];
+  codes_to_half<FMT>(w.x, p[0], p[1]);
+  codes_to_half<FMT>(w.y, p[2], p[3]);
+  codes_to_half<FMT>(w.z, p[4], p[5]);
+  codes_to_half<FMT>(w.w, p[6], p[7]);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    lo[2 * k] = p[k][0];
+    lo[2 * k + 1] = p[k][1];
+    hi[2 * k] = p[4 + k][0];
+    hi[2 * k + 1] = p[4 + k][1];
+  }
+}
+
+// Four codes as two pairs of bf16, exact too.
+template <int FMT>
+__device__ __forceinline__ void codes_to_bf16(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  if (FMT == SEM_KV_INT8) {
+    // (whole numbers up to 128 have eight bits: a float's upper half holds them)
+    const float a = (float)(int8_t)w, b = (float)(int8_t)(w >> 8);
+    const float c = (float)(int8_t)(w >> 16), d = (float)(int8_t)(w >> 24);
+    lo = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+    hi = __builtin_amdgcn_perm(__float_as_uint(d), __float_as_uint(c), 0x07060302u);
+  } else {
+    lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false));
+    hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true));
+  }
+}
+
 // One code as a float.
 template <int FMT>
 __device__ __forceinline__ float code_to_float(uint32_t byte) {
