@@ -700,6 +700,26 @@ int sem_kv_weigh_async(const sem_kv_cache *cache, int32_t layer, const sem_kv_qu
                        int64_t mass_stride, void *workspace, size_t ws_bytes, void *stream);
 
 /*
+ * Prune: eviction of single tokens by what sem_kv_weigh added up. A sequence of
+ * L > budget tokens keeps a = min(sinks, budget) first ones, r = min(recent,
+ * budget - a) last ones and, of those between, the budget - a - r of the largest mass;
+ * of equal ones the earlier (NaN is the smallest mass). They move together in their
+ * order, in all layers, as keep moves them; mass moves with them and is 0 behind them.
+ * A sequence of at most budget tokens stays as it is. Tokens keep the rotation that
+ * their keys have: a sequence's positions go on from where they were, not from its
+ * length (starts of sem_kv_tree, positions of sem_qk_rotate).
+ * seqs [n] int32 DEVICE; mass [slots][mass_stride] as for weigh. Device-detected
+ * SEM_EINVAL as for keep, which leaves the sequence and its mass as they were; pages
+ * whose tokens change must not be shared: prune before fork.
+ */
+size_t sem_kv_prune_workspace_bytes(const sem_kv_cache *cache, int64_t n, int64_t budget);
+int sem_kv_prune(const sem_kv_cache *cache, float *mass, int64_t mass_stride, const int32_t *seqs,
+                 int64_t n, int64_t budget, int64_t sinks, int64_t recent);
+int sem_kv_prune_async(const sem_kv_cache *cache, float *mass, int64_t mass_stride,
+                       const int32_t *seqs, int64_t n, int64_t budget, int64_t sinks,
+                       int64_t recent, void *workspace, size_t ws_bytes, void *stream);
+
+/*
  * Rotate: the norms of queries and keys, head by head, and the rotation of their
  * positions, what new tokens go through before append and attend. For every row x
  * (a token and a head) of head_dim channels (64, 128 or 256; SEM_ENOTIMPL for

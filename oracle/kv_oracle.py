@@ -132,6 +132,18 @@ def rotate(x, w, eps, positions, inv_freq, interleaved):
     return out, mag
 
 
+def prune_choice(mass, n, budget, sinks, recent):
+    """The tokens of n that stay, ascending."""
+    if n <= budget:
+        return list(range(n))
+    a = min(sinks, budget)
+    r = min(recent, budget - a)
+    key = [-math.inf if math.isnan(x) else float(x) for x in mass[:n]]
+    nan = [math.isnan(x) for x in mass[:n]]
+    rest = sorted(range(a, n - r), key=lambda t: (nan[t], -key[t], t))[:budget - a - r]
+    return sorted([*range(a), *rest, *range(n - r, n)])
+
+
 def requantized(codes, was, now, fmt):
     """Bytes of a block of scale `was` on scale `now`: the nearest codes to the 32-bit
     quotients, ties to the even one."""

@@ -86,6 +86,9 @@ SYMBOLS = (
     "sem_kv_keep_workspace_bytes",
     "sem_kv_weigh",
     "sem_kv_weigh_async",
+    "sem_kv_prune",
+    "sem_kv_prune_async",
+    "sem_kv_prune_workspace_bytes",
     "sem_qk_rotate",
     "sem_qk_rotate_async",
 )
@@ -213,13 +216,15 @@ def _load() -> ctypes.CDLL:
                        ("attend_tree", [kv, i32, vp, vp, i32] + rows),
                        ("tree", [kv, vp, vp] + rows + [i64, i32, vp, vp]),
                        ("keep", [kv, vp, vp, vp, vp, i64, i64]),
-                       ("weigh", [kv, i32, vp] + rows + [vp, i64])):
+                       ("weigh", [kv, i32, vp] + rows + [vp, i64]),
+                       ("prune", [kv, vp, i64, vp, i64, i64, i64, i64])):
         for form, more in (("", []), ("_async", tail)):
             fn = getattr(lib, f"sem_kv_{name}{form}")
             fn.argtypes, fn.restype = args + more, ctypes.c_int
     for name, args in (("page_bytes", [kv]), ("workspace_bytes", [kv]),
                        ("attend_workspace_bytes", [kv, i32, i64, i64, i64, i64]),
-                       ("keep_workspace_bytes", [kv, i64, i64])):
+                       ("keep_workspace_bytes", [kv, i64, i64]),
+                       ("prune_workspace_bytes", [kv, i64, i64])):
         fn = getattr(lib, f"sem_kv_{name}")
         fn.argtypes, fn.restype = args, sz
     lib.sem_qk_rotate.argtypes, lib.sem_qk_rotate.restype = [vp], ctypes.c_int  # (a sem_qk_rotary)
@@ -907,6 +912,20 @@ class KVCache:
                       stride, self._ws, self.ws_bytes)
         if rc:
             _raise(rc, "sem_kv_weigh_async")
+
+    def prune(self, mass: torch.Tensor, seqs: torch.Tensor, budget: int, *, sinks: int = 0,
+              recent: int = 0) -> None:
+        """Holds sequences to ``budget`` tokens: the first ``sinks``, the last ``recent``
+        and, of those between, the ones of the largest ``mass`` (what ``weigh`` added
+        up; of equal ones the earlier). They move together in their order, in all
+        layers, and their mass with them; it is zero behind them. Their keys stay
+        rotated as they are: positions go on from the old length."""
+        n, stride = seqs.numel(), self._mass(mass)
+        self._needed("prune", n, budget)
+        rc = _enqueue(self._index, lib.sem_kv_prune_async, self._ref, mass.data_ptr(), stride,
+                      self._list(seqs, "seqs"), n, budget, sinks, recent, self._ws, self.ws_bytes)
+        if rc:
+            _raise(rc, "sem_kv_prune_async")
 
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, seqs: torch.Tensor,
                cu: Optional[torch.Tensor] = None) -> None:

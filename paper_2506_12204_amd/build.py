@@ -24,7 +24,8 @@ SOURCES = ["abi.hip", "batched.hip", "global_sort.hip", "tile_sort.hip", "long_s
            "insert.hip", "policy.hip",
            "cost.hip", "batch.hip",
            "kv_abi.hip", "kv_pages.hip", "kv_append.hip", "kv_attend.hip",
-           "kv_attend_tree.hip", "kv_tree.hip", "kv_keep.hip", "kv_weigh.hip", "qk_rotate.hip"]
+           "kv_attend_tree.hip", "kv_tree.hip", "kv_keep.hip", "kv_weigh.hip", "kv_prune.hip",
+           "qk_rotate.hip"]
 ARCH = os.environ.get("SEMSCHED_ARCH", "gfx950")
 NOISE = "is not a recognized feature for this target"
 

@@ -132,6 +132,12 @@ struct KvKeepArgs {
   float* scales;    // [blocks][page_scales]
 };
 
+struct KvPruneArgs {
+  KvKeepArgs k;  // (its lists are not there)
+  float* mass;
+  int64_t mass_stride, budget, sinks, recent;
+};
+
 struct KvWeighArgs {
   KvView c;
   const uint16_t* q;
@@ -175,6 +181,9 @@ hipError_t launch_qk_rotate(const QkRotateArgs& a, int head_dim, hipStream_t st)
 hipError_t launch_kv_attend(const KvAttendArgs& a, hipStream_t st);
 hipError_t launch_kv_attend_tree(const KvAttendArgs& a, hipStream_t st);
 hipError_t launch_kv_weigh(const KvWeighArgs& a, int64_t max_len, hipStream_t st);
+bool kv_kept_fits(const KvKeepArgs& a);
+hipError_t launch_kv_kept(const KvKeepArgs& a, hipStream_t st);
+hipError_t launch_kv_prune(const KvPruneArgs& a, hipStream_t st);
 hipError_t launch_kv_keep(const KvKeepArgs& a, hipStream_t st);
 hipError_t launch_kv_tree(const KvTreeArgs& a, hipStream_t st);
 

@@ -312,6 +312,21 @@ int check_weigh(const sem_kv_cache* c, int32_t layer, const sem_kv_query* q, con
   return q->tokens > 0 && !q->lse ? SEM_EINVAL : SEM_OK;
 }
 
+// A sequence keeps no more than it can hold.
+KeepLayout prune_layout(const sem_kv_cache* c, int64_t n, int64_t budget) {
+  budget = std::min(budget, most_tokens(c));
+  return keep_layout(c, n, n * budget, n * ((budget + c->page_tokens - 1) / c->page_tokens));
+}
+
+int check_prune(const sem_kv_cache* c, const float* mass, int64_t mass_stride, const int32_t* seqs,
+                int64_t n, int64_t budget, int64_t sinks, int64_t recent) {
+  int rc = check_cache(c);
+  if (rc == SEM_OK) rc = check_list(c, seqs, n);
+  if (rc == SEM_OK) rc = check_mass(c, mass, mass_stride);
+  if (rc != SEM_OK) return rc;
+  return budget < 0 || sinks < 0 || recent < 0 ? SEM_EINVAL : SEM_OK;
+}
+
 int check_words(int32_t mask_words) {
   return mask_words < 1 || mask_words > kKvMaskWords ? SEM_EINVAL : SEM_OK;
 }
@@ -702,6 +717,39 @@ int sem_kv_weigh(const sem_kv_cache* cache, int32_t layer, const sem_kv_query* q
   return blocking(kZeroed, [&](void* ws, size_t bytes, hipStream_t st) {
     return sem_kv_weigh_async(cache, layer, query, seqs, cu, n, mass, mass_stride, ws, bytes, st);
   });
+}
+
+size_t sem_kv_prune_workspace_bytes(const sem_kv_cache* cache, int64_t n, int64_t budget) {
+  if (check_sizes(cache) != SEM_OK || n < 0 || n > cache->slots || budget < 0) return 0;
+  return prune_layout(cache, n, budget).total;
+}
+
+int sem_kv_prune_async(const sem_kv_cache* cache, float* mass, int64_t mass_stride,
+                       const int32_t* seqs, int64_t n, int64_t budget, int64_t sinks,
+                       int64_t recent, void* workspace, size_t ws_bytes, void* stream) {
+  const int rc = check_prune(cache, mass, mass_stride, seqs, n, budget, sinks, recent);
+  if (rc != SEM_OK) return rc;
+  const KeepLayout L = prune_layout(cache, n, budget);
+  if (!workspace_ok(workspace, ws_bytes, L.total)) return SEM_EINVAL;
+  KvPruneArgs a = {};
+  a.k = keep_args(cache, L, seqs, n, workspace);
+  a.mass = mass;
+  a.mass_stride = mass_stride;
+  a.budget = std::min(budget, most_tokens(cache));
+  a.sinks = sinks;
+  a.recent = recent;
+  return status_of(launch_kv_prune(a, static_cast<hipStream_t>(stream)));
+}
+
+int sem_kv_prune(const sem_kv_cache* cache, float* mass, int64_t mass_stride, const int32_t* seqs,
+                 int64_t n, int64_t budget, int64_t sinks, int64_t recent) {
+  const int rc = check_prune(cache, mass, mass_stride, seqs, n, budget, sinks, recent);
+  if (rc != SEM_OK) return rc;
+  return blocking(prune_layout(cache, n, budget).total,
+                  [&](void* ws, size_t bytes, hipStream_t st) {
+                    return sem_kv_prune_async(cache, mass, mass_stride, seqs, n, budget, sinks,
+                                              recent, ws, bytes, st);
+                  });
 }
 
 }  // extern "C"

@@ -98,8 +98,8 @@ __global__ __launch_bounds__(KT) void kv_keep_plan(KvKeepArgs a) {
   }
   const int64_t at = row0 + i * c.page_tokens;
   if (moves) {
-    for (int k = (begin << c.page_shift) + t; k < now; k += KT) {
-      const int from = k < first ? k : first + a.index[row0 + k - first];
+    for (int64_t k = (begin << c.page_shift) + t; k < now; k += KT) {
+      const int from = k < first ? (int)k : first + a.index[row0 + k - first];
       a.source[at + k - (begin << c.page_shift)] =
           ((int64_t)table[from >> c.page_shift] << c.page_shift) + (from & (c.page_tokens - 1));
     }

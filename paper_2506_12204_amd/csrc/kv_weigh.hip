@@ -144,7 +144,8 @@ __global__ __launch_bounds__(WW* kWave) void kv_weigh(KvWeighArgs a) {
     for (int k = 0; k < 16; ++k) sum[k] = 0.0f;
     if (chunk < s.c1) {
       const int32_t* table = c.tables + (int64_t)s.slot * c.max_blocks;
-      const int t0 = chunk * kChunk, vt = t0 + g * kKvTile, rows = s.fresh * a.group;
+      const int t0 = chunk * kChunk, vt = t0 + g * kKvTile;
+      const uint32_t rows = (uint32_t)s.fresh * (uint32_t)a.group;
       const int last_block = (s.len - 1) >> c.page_shift;
       // the pages of this lane's K rows, and of its 16 keys
       const int32_t kentry = table[min((t0 + r / 4 * kKvTile) >> c.page_shift, last_block)];
@@ -167,10 +168,10 @@ __global__ __launch_bounds__(WW* kWave) void kv_weigh(KvWeighArgs a) {
                                                           j * 1024),
                           key[x][2 * j], key[x][2 * j + 1]);
         const float f = scale[kh] * a.scale_log2;
-        for (int row = r; row - r < rows; row += kRows) {
-          const int at = min(row, rows - 1);
-          const int token = (int)((uint32_t)at / (uint32_t)a.group);
-          const int head = kh * a.group + at - token * a.group;
+        for (uint32_t row = r; row - r < rows; row += kRows) {
+          const uint32_t at = min(row, rows - 1);
+          const int token = (int)(at / (uint32_t)a.group);
+          const int head = kh * a.group + (int)(at % (uint32_t)a.group);
           const uint16_t* q = a.q + (int64_t)(s.row0 + token) * a.q_token + head * a.q_head + g * 16;
           const float lse = a.lse[(int64_t)(s.row0 + token) * a.heads + head];
           Operand query[N];
