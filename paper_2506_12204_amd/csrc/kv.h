@@ -182,7 +182,7 @@ hipError_t launch_kv_attend(const KvAttendArgs& a, hipStream_t st);
 hipError_t launch_kv_attend_tree(const KvAttendArgs& a, hipStream_t st);
 hipError_t launch_kv_weigh(const KvWeighArgs& a, int64_t max_len, hipStream_t st);
 bool kv_kept_fits(const KvKeepArgs& a);
-hipError_t launch_kv_kept(const KvKeepArgs& a, hipStream_t st);
+hipError_t launch_kv_kept(const KvKeepArgs& a, int64_t blocks, hipStream_t st);
 hipError_t launch_kv_prune(const KvPruneArgs& a, hipStream_t st);
 hipError_t launch_kv_keep(const KvKeepArgs& a, hipStream_t st);
 hipError_t launch_kv_tree(const KvTreeArgs& a, hipStream_t st);

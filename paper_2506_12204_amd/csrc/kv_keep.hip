@@ -48,6 +48,9 @@ __global__ __launch_bounds__(KT) void kv_keep_plan(KvKeepArgs a) {
   const int64_t i = blockIdx.x;
   const int t = threadIdx.x;
   auto wrong = [&] { atomicOr(c.flags, kFlagInval); };
+  auto blocks_of = [&](int tokens) {
+    return (int)(((uint32_t)tokens + (uint32_t)c.page_tokens - 1) >> c.page_shift);
+  };
   KvKept kept = {-1, 0, 0, 0, 0, 0};
   const int64_t row0 = a.cu[i], count = (int64_t)a.cu[i + 1] - row0;
   const int32_t s = a.seqs[i], last = a.last[i];
@@ -76,9 +79,9 @@ __global__ __launch_bounds__(KT) void kv_keep_plan(KvKeepArgs a) {
   // The blocks that are written: none where only the end leaves.
   const bool moves = lowest < count;
   const int begin = moves ? (first + lowest) >> c.page_shift : 0;
-  const int end = moves ? (now + c.page_tokens - 1) >> c.page_shift : 0;
+  const int end = moves ? blocks_of(now) : 0;
   const int32_t* table = c.tables + (int64_t)(bad ? 0 : s) * c.max_blocks;
-  const int blocks = ((int)len + c.page_tokens - 1) >> c.page_shift;
+  const int blocks = blocks_of((int)len);
   bool shared = false;
   if (!bad && now < len) {
     const int from = moves ? begin : now >> c.page_shift;
@@ -115,11 +118,10 @@ __global__ __launch_bounds__(KT) void kv_keep_plan(KvKeepArgs a) {
   }
 }
 
-// Four codes of a block of scale `was` on the scale that `q` divides by. (The scale is
-// brought to its middle range first, so that no product leaves 32 bits.)
+// Four codes, of a block whose scale times q's power of two is `held`, on the scale that
+// q divides by. (The scale is lifted first, so that no product leaves 32 bits.)
 template <int FMT>
-__device__ __forceinline__ uint32_t again(uint32_t codes, float was, const Quotient& q) {
-  const float held = was * q.lift;
+__device__ __forceinline__ uint32_t again(uint32_t codes, float held, const Quotient& q) {
   float f[4];
 #pragma unroll
   for (int k = 0; k < 4; ++k)
@@ -127,97 +129,203 @@ __device__ __forceinline__ uint32_t again(uint32_t codes, float was, const Quoti
   return pack_codes<FMT>(f[0], f[1], f[2], f[3]);
 }
 
-// A wave: 64 channels (slice `blockIdx.y`) of a block of every page that changes.
-template <int D, int FMT>
+__device__ __forceinline__ int64_t lane_i64(int64_t v, int lane) {
+  return (int64_t)lane_u64((uint64_t)v, lane);
+}
+__device__ __forceinline__ float lane_float(float v, int lane) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), lane));
+}
+
+// The sources of a step of 64 tokens, a lane each, and where they go.
+struct Step {
+  int64_t source;  // page * page_tokens + place; -1: the token is not there
+  int32_t page;    // its new one
+  float was;       // the scale of the block that it comes from
+};
+
+template <int FMT>
+__device__ __forceinline__ uint32_t byte_at(const uint8_t* p) {
+  return FMT == SEM_KV_INT8 ? (uint32_t)(int32_t) * reinterpret_cast<const int8_t*>(p) : *p;
+}
+
+// A wave: P times 64 channels (part blockIdx.y) of a block of every page that changes, 64
+// tokens at a time. Loads run ahead: the next step's sources while this one's codes
+// arrive. A token that stays where it is on the same scale is not touched, and a tile of
+// 16 of them neither.
+//
+// K: a lane has 16 channels of token lane % 16 of a tile. V: a lane has a channel and
+// fetches its tokens' bytes one by one, at addresses whose bases are scalar.
+template <int D, int FMT, int P>
 __global__ __launch_bounds__(MW* kWave) void kv_keep_move(KvKeepArgs a) {
+  constexpr int TILES = kWave / kKvTile;
   const KvView& c = a.c;
   const int64_t unit = (int64_t)blockIdx.x * MW +
                        __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int64_t i = unit / c.page_scales;
   if (i >= a.n) return;
-  const int which = (int)(unit % c.page_scales), lane = lane_id(), slice = blockIdx.y;
+  const int which = (int)(unit % c.page_scales), lane = lane_id();
   const bool value = which / c.kv_heads % 2 != 0;
   const KvKept kept = a.kept[i];
-  if (kept.seq < 0) return;
-  const int64_t block_bytes = (int64_t)c.page_tokens * D;
-  uint8_t* const data = c.data + which * block_bytes;
+  if (kept.seq < 0 || kept.begin >= kept.end) return;
+  uint8_t* const data = c.data + which * ((int64_t)c.page_tokens * D);
   const float* const scale = c.scale + which;
   const int32_t* const table = c.tables + (int64_t)kept.seq * c.max_blocks;
   const int in_page = c.page_tokens - 1;
-  for (int b = kept.begin; b < kept.end; ++b) {
-    const int t0 = b << c.page_shift, n = min(kept.now - t0, c.page_tokens);
-    const int64_t* source = a.source + kept.source + (t0 - (kept.begin << c.page_shift));
-    float now = 0.0f;
-    for (int t = lane; t < n; t += kWave)
-      now = fmaxf(now, scale[(source[t] >> c.page_shift) * c.page_scales]);
-    now = __uint_as_float(wave_max_u32(__float_as_uint(now)));
-    if (lane == 0 && slice == 0)
-      a.scales[(kept.scales + b - kept.begin) * c.page_scales + which] = now;
-    const Quotient q(now > 0.0f ? now : 1.0f);
-    uint8_t* const block = data + table[b] * c.page_bytes;
-    for (int t1 = 0; t1 < n; t1 += kKvTile) {
-      uint8_t* const tile = block + t1 * D;
-      if (!value) {
-        // 16 channels (group lane / 16 of the slice) of token lane % 16
-        const int t = t1 + lane % 16;
-        if (t < n) {
-          const int64_t from = source[t];
-          const int64_t page = from >> c.page_shift;
+  // (rounds of 64 may end past 31 bits)
+  const uint32_t first = (uint32_t)kept.begin << c.page_shift, end = (uint32_t)kept.now;
+  const int64_t* const source = a.source + kept.source - first;
+  const int part0 = blockIdx.y * P;
+
+  auto look_up = [&](uint32_t t0, Step& s) __attribute__((always_inline)) {
+    const uint32_t t = t0 + lane;
+    s.source = -1;
+    s.page = 0;
+    if (t < end) {
+      s.source = source[t];
+      s.page = table[t >> c.page_shift];
+    }
+  };
+  auto scale_of = [&](Step& s) __attribute__((always_inline)) {
+    s.was = s.source >= 0 ? scale[(s.source >> c.page_shift) * c.page_scales] : 0.0f;
+  };
+  Step next;
+  look_up(first, next);
+  scale_of(next);
+  float now = 0.0f;  // of the lane's block
+  for (uint32_t t0 = first; t0 < end; t0 += kWave) {
+    const Step s = next;
+    // the block's scale
+    if (c.page_tokens <= kWave) {
+      now = s.was;
+      for (int off = 1; off < c.page_tokens; off *= 2) now = fmaxf(now, __shfl_xor(now, off, kWave));
+    } else if (((t0 - first) & in_page) == 0) {
+      now = s.was;
+      const uint32_t stop = min(t0 + (uint32_t)c.page_tokens, end);
+      for (uint32_t t = t0 + kWave + lane; t < stop; t += kWave)
+        now = fmaxf(now, scale[(source[t] >> c.page_shift) * c.page_scales]);
+      now = __uint_as_float(wave_max_u32(__float_as_uint(now)));
+    }
+    const uint32_t t = t0 + lane;
+    if (part0 == 0 && (t & in_page) == 0 && t < end)
+      a.scales[(kept.scales + (t >> c.page_shift) - kept.begin) * c.page_scales + which] = now;
+    const int64_t to = ((int64_t)s.page << c.page_shift) + (t & in_page);
+    const bool moves = s.source >= 0 && (s.source != to || s.was != now);
+    const uint64_t moving = __ballot(moves);
+    look_up(t0 + kWave, next);
+    if (!value) {
+      uint4 u[TILES][P];
+#pragma unroll
+      for (int x = 0; x < TILES; ++x) {
+        if ((moving >> (x * 16) & 0xffff) == 0) continue;
+        const int from_lane = x * 16 + lane % 16;
+        const int64_t from = __shfl(s.source, from_lane, kWave);
+        if (moving >> from_lane & 1) {
           const int in = (int)(from & in_page);
-          const int group = (slice * 4 + lane / 16) * 256;
-          const float was = scale[page * c.page_scales];
-          uint4 u = *reinterpret_cast<const uint4*>(data + page * c.page_bytes + in / 16 * 16 * D +
-                                                    group + in % 16 * 16);
-          if (was != now) {
-            u.x = again<FMT>(u.x, was, q);
-            u.y = again<FMT>(u.y, was, q);
-            u.z = again<FMT>(u.z, was, q);
-            u.w = again<FMT>(u.w, was, q);
-          }
-          asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-          *reinterpret_cast<uint4*>(tile + group + lane % 16 * 16) = u;
-        }
-      } else {
-        // 16 tokens of channel `lane` of the slice
-        const int ch = slice * kWave + lane, m = min(n - t1, kKvTile);
-        uint32_t w[4] = {0, 0, 0, 0};
-        for (int k = 0; k < m; ++k) {
-          const int64_t from = source[t1 + k];
-          const int64_t page = from >> c.page_shift;
-          const int in = (int)(from & in_page);
-          const float was = scale[page * c.page_scales];
-          uint32_t code = data[page * c.page_bytes + in / 16 * 16 * D + ch * 16 + in % 16];
-          if (was != now) code = again<FMT>(code, was, q) & 0xffu;
-          w[k / 4] |= code << (8 * (k % 4));
-        }
-        uint8_t* to = tile + ch * 16;
-        if (m == kKvTile) {
-          *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
-        } else {
-          for (int k = 0; k < m; ++k) to[k] = (uint8_t)(w[k / 4] >> (8 * (k % 4)));
+          const uint8_t* p = data + (from >> c.page_shift) * c.page_bytes + in / 16 * (16 * D) +
+                             part0 * 1024 + lane / 16 * 256 + in % 16 * 16;
+#pragma unroll
+          for (int y = 0; y < P; ++y) u[x][y] = *reinterpret_cast<const uint4*>(p + y * 1024);
         }
       }
-      wait_stores();
+      scale_of(next);
+#pragma unroll
+      for (int x = 0; x < TILES; ++x) {
+        if ((moving >> (x * 16) & 0xffff) == 0) continue;
+        const int from_lane = x * 16 + lane % 16;
+        const float was = __shfl(s.was, from_lane, kWave), mine = __shfl(now, from_lane, kWave);
+        const int64_t page = __shfl(s.page, from_lane, kWave);
+        if (moving >> from_lane & 1) {
+          const Quotient q(mine > 0.0f ? mine : 1.0f);
+          const float held = was * q.lift;
+          uint8_t* p = data + page * c.page_bytes + ((t0 + x * 16) & in_page) * D + part0 * 1024 +
+                       lane / 16 * 256 + lane % 16 * 16;
+#pragma unroll
+          for (int y = 0; y < P; ++y) {
+            uint32_t w[4] = {u[x][y].x, u[x][y].y, u[x][y].z, u[x][y].w};
+            if (was != mine) {
+#pragma unroll
+              for (int k = 0; k < 4; ++k) w[k] = again<FMT>(w[k], held, q);
+            }
+            *reinterpret_cast<uint4*>(p + y * 1024) = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+        }
+      }
+    } else {
+      scale_of(next);
+#pragma unroll
+      for (int x = 0; x < TILES; ++x) {
+        if ((moving >> (x * 16) & 0xffff) == 0) continue;
+        const int m = (int)min(end - t0 - x * 16, (uint32_t)kKvTile);
+        uint32_t code[P][16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+          // (tokens that are not there: the last one that is)
+          const int64_t from = lane_i64(s.source, x * 16 + min(k, m - 1));
+          const int in = (int)(from & in_page);
+          const uint8_t* p = data + (from >> c.page_shift) * c.page_bytes + in / 16 * (16 * D) +
+                             in % 16 + (part0 * kWave + lane) * 16;
+#pragma unroll
+          for (int y = 0; y < P; ++y) code[y][k] = byte_at<FMT>(p + y * 1024);
+        }
+        const float mine = lane_float(now, x * 16);
+        const Quotient q(mine > 0.0f ? mine : 1.0f);
+        const uint64_t same = __ballot(s.was == now);
+        const int64_t page = __builtin_amdgcn_readlane(s.page, x * 16);
+        uint8_t* p = data + page * c.page_bytes + ((t0 + x * 16) & in_page) * D +
+                     (part0 * kWave + lane) * 16;
+#pragma unroll
+        for (int y = 0; y < P; ++y) {
+          uint32_t w[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            float f[4];
+            uint32_t raw = 0, still = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const int token = 4 * k + j;
+              const float held = lane_float(s.was, x * 16 + token) * q.lift;
+              const uint32_t b = code[y][token];
+              f[j] = q.of_lifted(
+                  (FMT == SEM_KV_INT8 ? (float)(int32_t)b : code_to_float<FMT>(b)) * held);
+              raw |= (b & 0xffu) << (8 * j);
+              if (same >> (x * 16 + token) & 1) still |= 0xffu << (8 * j);
+            }
+            w[k] = (raw & still) | (pack_codes<FMT>(f[0], f[1], f[2], f[3]) & ~still);
+          }
+          if (m == kKvTile) {
+            *reinterpret_cast<uint4*>(p + y * 1024) = make_uint4(w[0], w[1], w[2], w[3]);
+          } else {  // the bytes behind the sequence stay
+            for (int k = 0; k < m; ++k) {
+              const uint32_t word = k < 8 ? (k < 4 ? w[0] : w[1]) : (k < 12 ? w[2] : w[3]);
+              p[y * 1024 + k] = (uint8_t)(word >> (8 * (k & 3)));
+            }
+          }
+        }
+      }
     }
   }
 }
 
 // The scales of the blocks that changed, the pages behind the sequence, its length.
+// (In parts, blockIdx.y, where there are many scales; the first does the rest.)
 __global__ __launch_bounds__(KT) void kv_keep_finish(KvKeepArgs a) {
   const KvView& c = a.c;
   const KvKept kept = a.kept[blockIdx.x];
   if (kept.seq < 0) return;
   int32_t* table = c.tables + (int64_t)kept.seq * c.max_blocks;
   const int64_t changed = (int64_t)(kept.end - kept.begin) * c.page_scales;
-  for (int64_t k = threadIdx.x; k < changed; k += KT) {
+  for (int64_t k = (int64_t)blockIdx.y * KT + threadIdx.x; k < changed; k += gridDim.y * KT) {
     const int b = (int)(k / c.page_scales), which = (int)(k % c.page_scales);
     c.scale[(int64_t)table[kept.begin + b] * c.page_scales + which] =
         a.scales[(kept.scales + b) * c.page_scales + which];
   }
+  if (blockIdx.y > 0) return;
   const int len = c.lens[kept.seq];
-  const int blocks = (len + c.page_tokens - 1) >> c.page_shift;
+  const int blocks = (int)(((uint32_t)len + (uint32_t)c.page_tokens - 1) >> c.page_shift);
   block_sync();
-  for (int b = ((kept.now + c.page_tokens - 1) >> c.page_shift) + threadIdx.x; b < blocks; b += KT) {
+  for (int b = (int)(((uint32_t)kept.now + (uint32_t)c.page_tokens - 1) >> c.page_shift) +
+               (int)threadIdx.x;
+       b < blocks; b += KT) {
     const int32_t page = table[b];
     const int32_t old = atomicSub(c.refs + page, 1);
     if (old == 1) {
@@ -231,27 +339,38 @@ __global__ __launch_bounds__(KT) void kv_keep_finish(KvKeepArgs a) {
   if (threadIdx.x == 0) c.lens[kept.seq] = kept.now;
 }
 
-template <int D>
-void launch_move(const KvKeepArgs& a, unsigned grid, hipStream_t st) {
-  if (a.c.format == SEM_KV_INT8)
-    hipLaunchKernelGGL((kv_keep_move<D, SEM_KV_INT8>), dim3(grid, D / 64), dim3(MW * kWave), 0, st,
-                       a);
+template <int D, int FMT>
+void launch_move(const KvKeepArgs& a, hipStream_t st) {
+  // A wave for all of a block's channels where there are units for every compute unit,
+  // else one for 64 of them.
+  constexpr int ALL = D / 64;
+  const int64_t units = a.n * a.c.page_scales;
+  const unsigned grid = (unsigned)((units + MW - 1) / MW);
+  if (units >= 4096)
+    hipLaunchKernelGGL((kv_keep_move<D, FMT, ALL>), dim3(grid), dim3(MW * kWave), 0, st, a);
   else
-    hipLaunchKernelGGL((kv_keep_move<D, SEM_KV_FP8>), dim3(grid, D / 64), dim3(MW * kWave), 0, st,
-                       a);
+    hipLaunchKernelGGL((kv_keep_move<D, FMT, 1>), dim3(grid, ALL), dim3(MW * kWave), 0, st, a);
+}
+
+template <int D>
+void launch_format(const KvKeepArgs& a, hipStream_t st) {
+  if (a.c.format == SEM_KV_INT8) launch_move<D, SEM_KV_INT8>(a, st);
+  else launch_move<D, SEM_KV_FP8>(a, st);
 }
 
 }  // namespace
 
 // The moves of a plan and what follows them.
-hipError_t launch_kv_kept(const KvKeepArgs& a, hipStream_t st) {
-  const int64_t grid = (a.n * a.c.page_scales + MW - 1) / MW;
+hipError_t launch_kv_kept(const KvKeepArgs& a, int64_t blocks, hipStream_t st) {
   switch (a.c.head_dim) {
-    case 64: launch_move<64>(a, (unsigned)grid, st); break;
-    case 128: launch_move<128>(a, (unsigned)grid, st); break;
-    default: launch_move<256>(a, (unsigned)grid, st);
+    case 64: launch_format<64>(a, st); break;
+    case 128: launch_format<128>(a, st); break;
+    default: launch_format<256>(a, st);
   }
-  hipLaunchKernelGGL(kv_keep_finish, dim3((unsigned)a.n), dim3(KT), 0, st, a);
+  const int64_t parts = blocks / a.n * a.c.page_scales / (8 * KT);
+  hipLaunchKernelGGL(kv_keep_finish,
+                     dim3((unsigned)a.n, (unsigned)std::max<int64_t>(1, std::min<int64_t>(parts, 64))),
+                     dim3(KT), 0, st, a);
   return hipGetLastError();
 }
 
@@ -263,7 +382,7 @@ hipError_t launch_kv_keep(const KvKeepArgs& a, hipStream_t st) {
   if (a.n == 0) return hipSuccess;
   if (!kv_kept_fits(a)) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL(kv_keep_plan, dim3((unsigned)a.n), dim3(KT), 0, st, a);
-  return launch_kv_kept(a, st);
+  return launch_kv_kept(a, a.total / a.c.page_tokens + 2 * a.n, st);
 }
 
 }  // namespace semsched

@@ -152,8 +152,11 @@ __global__ __launch_bounds__(PT) void kv_prune_plan(KvPruneArgs a) {
   // The blocks that are written, none where only the end leaves.
   const bool moves = gap < budget;
   const int begin = moves ? gap >> c.page_shift : 0;
-  const int end = moves ? (budget + c.page_tokens - 1) >> c.page_shift : 0;
-  const int blocks = (len + c.page_tokens - 1) >> c.page_shift;
+  const auto blocks_of = [&](int tokens) {
+    return (int)(((uint32_t)tokens + (uint32_t)c.page_tokens - 1) >> c.page_shift);
+  };
+  const int end = moves ? blocks_of(budget) : 0;
+  const int blocks = blocks_of(len);
   const int32_t* table = c.tables + (int64_t)s * c.max_blocks;
   for (int b = (moves ? begin : budget >> c.page_shift) + t; b < blocks; b += PT) {
     const int32_t page = table[b];
@@ -194,7 +197,7 @@ __global__ __launch_bounds__(PT) void kv_prune_plan(KvPruneArgs a) {
     kept.begin = begin;
     kept.end = end;
     kept.source = i * budget + (begin << c.page_shift);
-    kept.scales = i * ((budget + c.page_tokens - 1) >> c.page_shift);
+    kept.scales = i * blocks_of(budget);
     a.k.kept[i] = kept;
   }
 }
@@ -205,7 +208,8 @@ hipError_t launch_kv_prune(const KvPruneArgs& a, hipStream_t st) {
   if (a.k.n == 0) return hipSuccess;
   if (!kv_kept_fits(a.k) || !grid_fits(a.k.n, PT)) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL(kv_prune_plan, dim3((unsigned)a.k.n), dim3(PT), 0, st, a);
-  return launch_kv_kept(a.k, st);
+  const int64_t pt = a.k.c.page_tokens;
+  return launch_kv_kept(a.k, a.k.n * ((a.budget + pt - 1) / pt), st);
 }
 
 }  // namespace semsched
