@@ -128,9 +128,19 @@ struct KvKeepArgs {
   const int32_t *seqs, *last, *index, *cu;
   int64_t n, total;
   KvKept* kept;     // [n]
-  int64_t* source;  // of each token from block `begin` on: page * page_tokens + place
+  // of each token from block `begin` on: where it comes from, the byte of its tile in a
+  // block of its page plus its place among the tile's 16 tokens, and that page
+  int64_t* source;
+  int32_t* pages;
   float* scales;    // [blocks][page_scales]
 };
+
+__device__ __forceinline__ void write_source(const KvKeepArgs& a, int64_t at, int32_t page,
+                                             int in_page) {
+  a.source[at] = page * a.c.page_bytes +
+                 (int64_t)(in_page / kKvTile) * (kKvTile * a.c.head_dim) + in_page % kKvTile;
+  a.pages[at] = page;
+}
 
 struct KvPruneArgs {
   KvKeepArgs k;  // (its lists are not there)

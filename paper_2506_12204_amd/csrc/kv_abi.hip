@@ -251,13 +251,14 @@ int attend_args(const sem_kv_cache* cache, int32_t layer, const sem_kv_query* qu
 // The plan, sources and scales of sequences that keep `total` tokens among their
 // listed ones.
 struct KeepLayout {
-  size_t kept = kZeroed, source = 0, scales = 0, total = 0;
+  size_t kept = kZeroed, source = 0, pages = 0, scales = 0, total = 0;
 };
 
 KeepLayout keep_layout(const sem_kv_cache* c, int64_t n, int64_t sources, int64_t blocks) {
   KeepLayout L;
   L.source = align_up(L.kept + sizeof(KvKept) * (size_t)n);
-  L.scales = align_up(L.source + 8 * (size_t)sources);
+  L.pages = align_up(L.source + 8 * (size_t)sources);
+  L.scales = align_up(L.pages + 4 * (size_t)sources);
   L.total = align_up(L.scales + 4 * (size_t)blocks * (size_t)(c->layers * 2 * c->kv_heads));
   return L;
 }
@@ -277,6 +278,7 @@ KvKeepArgs keep_args(const sem_kv_cache* c, const KeepLayout& L, const int32_t* 
   a.n = n;
   a.kept = reinterpret_cast<KvKept*>(base + L.kept);
   a.source = reinterpret_cast<int64_t*>(base + L.source);
+  a.pages = reinterpret_cast<int32_t*>(base + L.pages);
   a.scales = reinterpret_cast<float*>(base + L.scales);
   return a;
 }

@@ -103,8 +103,8 @@ __global__ __launch_bounds__(KT) void kv_keep_plan(KvKeepArgs a) {
   if (moves) {
     for (int64_t k = (begin << c.page_shift) + t; k < now; k += KT) {
       const int from = k < first ? (int)k : first + a.index[row0 + k - first];
-      a.source[at + k - (begin << c.page_shift)] =
-          ((int64_t)table[from >> c.page_shift] << c.page_shift) + (from & (c.page_tokens - 1));
+      write_source(a, at + k - ((int64_t)begin << c.page_shift), table[from >> c.page_shift],
+                   from & (c.page_tokens - 1));
     }
   }
   if (t == 0) {
@@ -138,63 +138,61 @@ __device__ __forceinline__ float lane_float(float v, int lane) {
 
 // The sources of a step of 64 tokens, a lane each, and where they go.
 struct Step {
-  int64_t source;  // page * page_tokens + place; -1: the token is not there
-  int32_t page;    // its new one
-  float was;       // the scale of the block that it comes from
+  int64_t from;  // the place that plans write
+  int32_t page;  // -1: the token is not there
+  int32_t to;    // its new page
+  float was;     // the scale of the block that it comes from
 };
 
 template <int FMT>
-__device__ __forceinline__ uint32_t byte_at(const uint8_t* p) {
-  return FMT == SEM_KV_INT8 ? (uint32_t)(int32_t) * reinterpret_cast<const int8_t*>(p) : *p;
+__device__ __forceinline__ float number_of(int32_t code) {
+  return FMT == SEM_KV_INT8 ? (float)code : code_to_float<FMT>((uint32_t)code);
 }
 
-// A wave: P times 64 channels (part blockIdx.y) of a block of every page that changes, 64
-// tokens at a time. Loads run ahead: the next step's sources while this one's codes
-// arrive. A token that stays where it is on the same scale is not touched, and a tile of
-// 16 of them neither.
-//
-// K: a lane has 16 channels of token lane % 16 of a tile. V: a lane has a channel and
-// fetches its tokens' bytes one by one, at addresses whose bases are scalar.
-template <int D, int FMT, int P>
-__global__ __launch_bounds__(MW* kWave) void kv_keep_move(KvKeepArgs a) {
-  constexpr int TILES = kWave / kKvTile;
-  const KvView& c = a.c;
-  const int64_t unit = (int64_t)blockIdx.x * MW +
-                       __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int64_t i = unit / c.page_scales;
-  if (i >= a.n) return;
-  const int which = (int)(unit % c.page_scales), lane = lane_id();
-  const bool value = which / c.kv_heads % 2 != 0;
-  const KvKept kept = a.kept[i];
-  if (kept.seq < 0 || kept.begin >= kept.end) return;
-  uint8_t* const data = c.data + which * ((int64_t)c.page_tokens * D);
-  const float* const scale = c.scale + which;
-  const int32_t* const table = c.tables + (int64_t)kept.seq * c.max_blocks;
-  const int in_page = c.page_tokens - 1;
+// A wave's block of every page of a sequence that changes, 64 tokens at a time.
+template <int D>
+struct Mover {
+  const KvKeepArgs& a;
+  const KvKept& kept;
+  const int which, lane = lane_id(), in_page = a.c.page_tokens - 1;
   // (rounds of 64 may end past 31 bits)
-  const uint32_t first = (uint32_t)kept.begin << c.page_shift, end = (uint32_t)kept.now;
+  const uint32_t first = (uint32_t)kept.begin << a.c.page_shift, end = (uint32_t)kept.now;
+  const float* const scale = a.c.scale + which;
+  const int32_t* const table = a.c.tables + (int64_t)kept.seq * a.c.max_blocks;
   const int64_t* const source = a.source + kept.source - first;
-  const int part0 = blockIdx.y * P;
+  const int32_t* const pages = a.pages + kept.source - first;
+  Step s, next, later;
+  float now = 0.0f;  // scale of the lane's block
+  // of a step: what its tokens are divided by, what their codes are multiplied by before,
+  // whether they stay on their scale, the tile that they go to
+  Quotient q{1.0f};
+  float held = 0.0f;
+  bool same = false;
+  int64_t to = 0;
+  uint64_t moving = 0;
 
-  auto look_up = [&](uint32_t t0, Step& s) __attribute__((always_inline)) {
+  __device__ __forceinline__ void look_up(uint32_t t0, Step& s) const {
     const uint32_t t = t0 + lane;
-    s.source = -1;
-    s.page = 0;
+    s.from = 0;
+    s.page = -1;
+    s.to = 0;
     if (t < end) {
-      s.source = source[t];
-      s.page = table[t >> c.page_shift];
+      s.page = pages[t];
+      s.from = source[t];
+      s.to = table[t >> a.c.page_shift];
     }
-  };
-  auto scale_of = [&](Step& s) __attribute__((always_inline)) {
-    s.was = s.source >= 0 ? scale[(s.source >> c.page_shift) * c.page_scales] : 0.0f;
-  };
-  Step next;
-  look_up(first, next);
-  scale_of(next);
-  float now = 0.0f;  // of the lane's block
-  for (uint32_t t0 = first; t0 < end; t0 += kWave) {
-    const Step s = next;
-    // the block's scale
+  }
+  __device__ __forceinline__ void scale_of(Step& s) const {
+    s.was = s.page >= 0 ? scale[(int64_t)s.page * a.c.page_scales] : 0.0f;
+  }
+  __device__ __forceinline__ void begin() {
+    look_up(first, s);
+    look_up(first + kWave, next);
+    scale_of(s);
+  }
+  // Step t0: everything but its codes. The next two steps' loads are on their way.
+  __device__ __forceinline__ void step(uint32_t t0) {
+    const KvView& c = a.c;
     if (c.page_tokens <= kWave) {
       now = s.was;
       for (int off = 1; off < c.page_tokens; off *= 2) now = fmaxf(now, __shfl_xor(now, off, kWave));
@@ -202,108 +200,181 @@ __global__ __launch_bounds__(MW* kWave) void kv_keep_move(KvKeepArgs a) {
       now = s.was;
       const uint32_t stop = min(t0 + (uint32_t)c.page_tokens, end);
       for (uint32_t t = t0 + kWave + lane; t < stop; t += kWave)
-        now = fmaxf(now, scale[(source[t] >> c.page_shift) * c.page_scales]);
+        now = fmaxf(now, scale[(int64_t)pages[t] * c.page_scales]);
       now = __uint_as_float(wave_max_u32(__float_as_uint(now)));
     }
     const uint32_t t = t0 + lane;
-    if (part0 == 0 && (t & in_page) == 0 && t < end)
+    if (blockIdx.y == 0 && (t & in_page) == 0 && t < end)
       a.scales[(kept.scales + (t >> c.page_shift) - kept.begin) * c.page_scales + which] = now;
-    const int64_t to = ((int64_t)s.page << c.page_shift) + (t & in_page);
-    const bool moves = s.source >= 0 && (s.source != to || s.was != now);
-    const uint64_t moving = __ballot(moves);
-    look_up(t0 + kWave, next);
-    if (!value) {
-      uint4 u[TILES][P];
+    q = Quotient(now > 0.0f ? now : 1.0f);
+    held = s.was * q.lift;
+    same = s.was == now;
+    to = s.to * c.page_bytes + (int64_t)((t & in_page) / kKvTile * (kKvTile * D));
+    moving = __ballot(s.page >= 0 && (s.from != to + lane % 16 || !same));
+    scale_of(next);
+    look_up(t0 + 2 * kWave, later);
+  }
+  __device__ __forceinline__ void advance() {
+    s = next;
+    next = later;
+  }
+  __device__ __forceinline__ bool moves(int x) const { return (moving >> (x * 16) & 0xffff) != 0; }
+  __device__ __forceinline__ int tokens_of(uint32_t at) const {
+    return at < end ? (int)min(end - at, (uint32_t)kKvTile) : 0;
+  }
+};
+
+// K: a lane has 16 channels of token lane % 16 of a tile.
+template <int D, int FMT, int P>
+__device__ __forceinline__ void move_keys(Mover<D>& m, uint8_t* data) {
+  constexpr int TILES = kWave / kKvTile;
+  const int lane = lane_id();
+  uint4 u[TILES][P], ahead[TILES][P];
+  auto load = [&](const Step& of, uint64_t which, uint4 (&u)[TILES][P])
+      __attribute__((always_inline)) {
 #pragma unroll
-      for (int x = 0; x < TILES; ++x) {
-        if ((moving >> (x * 16) & 0xffff) == 0) continue;
-        const int from_lane = x * 16 + lane % 16;
-        const int64_t from = __shfl(s.source, from_lane, kWave);
-        if (moving >> from_lane & 1) {
-          const int in = (int)(from & in_page);
-          const uint8_t* p = data + (from >> c.page_shift) * c.page_bytes + in / 16 * (16 * D) +
-                             part0 * 1024 + lane / 16 * 256 + in % 16 * 16;
+    for (int x = 0; x < TILES; ++x) {
+      if ((which >> (x * 16) & 0xffff) == 0) continue;
+      const int mine = x * 16 + lane % 16;
+      const int64_t from = __shfl(of.from, mine, kWave);
+      if (which >> mine & 1) {
+        const uint8_t* p = data + (from & ~15ll) + (from & 15) * 16 + lane / 16 * 256;
 #pragma unroll
-          for (int y = 0; y < P; ++y) u[x][y] = *reinterpret_cast<const uint4*>(p + y * 1024);
-        }
+        for (int y = 0; y < P; ++y) u[x][y] = *reinterpret_cast<const uint4*>(p + y * 1024);
       }
-      scale_of(next);
+    }
+  };
+  for (uint32_t t0 = m.first; t0 < m.end; t0 += kWave, m.advance()) {
+    m.step(t0);
+    if (t0 == m.first) load(m.s, m.moving, u);
+    if (m.end - t0 > (uint32_t)kWave) load(m.next, __ballot(m.next.page >= 0), ahead);
 #pragma unroll
-      for (int x = 0; x < TILES; ++x) {
-        if ((moving >> (x * 16) & 0xffff) == 0) continue;
-        const int from_lane = x * 16 + lane % 16;
-        const float was = __shfl(s.was, from_lane, kWave), mine = __shfl(now, from_lane, kWave);
-        const int64_t page = __shfl(s.page, from_lane, kWave);
-        if (moving >> from_lane & 1) {
-          const Quotient q(mine > 0.0f ? mine : 1.0f);
-          const float held = was * q.lift;
-          uint8_t* p = data + page * c.page_bytes + ((t0 + x * 16) & in_page) * D + part0 * 1024 +
-                       lane / 16 * 256 + lane % 16 * 16;
-#pragma unroll
-          for (int y = 0; y < P; ++y) {
-            uint32_t w[4] = {u[x][y].x, u[x][y].y, u[x][y].z, u[x][y].w};
-            if (was != mine) {
-#pragma unroll
-              for (int k = 0; k < 4; ++k) w[k] = again<FMT>(w[k], held, q);
-            }
-            *reinterpret_cast<uint4*>(p + y * 1024) = make_uint4(w[0], w[1], w[2], w[3]);
-          }
-        }
-      }
-    } else {
-      scale_of(next);
-#pragma unroll
-      for (int x = 0; x < TILES; ++x) {
-        if ((moving >> (x * 16) & 0xffff) == 0) continue;
-        const int m = (int)min(end - t0 - x * 16, (uint32_t)kKvTile);
-        uint32_t code[P][16];
-#pragma unroll
-        for (int k = 0; k < 16; ++k) {
-          // (tokens that are not there: the last one that is)
-          const int64_t from = lane_i64(s.source, x * 16 + min(k, m - 1));
-          const int in = (int)(from & in_page);
-          const uint8_t* p = data + (from >> c.page_shift) * c.page_bytes + in / 16 * (16 * D) +
-                             in % 16 + (part0 * kWave + lane) * 16;
-#pragma unroll
-          for (int y = 0; y < P; ++y) code[y][k] = byte_at<FMT>(p + y * 1024);
-        }
-        const float mine = lane_float(now, x * 16);
-        const Quotient q(mine > 0.0f ? mine : 1.0f);
-        const uint64_t same = __ballot(s.was == now);
-        const int64_t page = __builtin_amdgcn_readlane(s.page, x * 16);
-        uint8_t* p = data + page * c.page_bytes + ((t0 + x * 16) & in_page) * D +
-                     (part0 * kWave + lane) * 16;
+    for (int x = 0; x < TILES; ++x) {
+      if (!m.moves(x)) continue;
+      const int mine = x * 16 + lane % 16;
+      Quotient by = m.q;  // the token's
+      by.by = __shfl(m.q.by, mine, kWave);
+      by.inv = __shfl(m.q.inv, mine, kWave);
+      const float was = __shfl(m.held, mine, kWave);
+      const bool stays = __shfl((int)m.same, mine, kWave);
+      uint8_t* p = data + lane_i64(m.to, x * 16) + lane / 16 * 256 + lane % 16 * 16;
+      if (m.moving >> mine & 1) {
 #pragma unroll
         for (int y = 0; y < P; ++y) {
-          uint32_t w[4];
+          uint32_t w[4] = {u[x][y].x, u[x][y].y, u[x][y].z, u[x][y].w};
+          if (!stays) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            float f[4];
-            uint32_t raw = 0, still = 0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const int token = 4 * k + j;
-              const float held = lane_float(s.was, x * 16 + token) * q.lift;
-              const uint32_t b = code[y][token];
-              f[j] = q.of_lifted(
-                  (FMT == SEM_KV_INT8 ? (float)(int32_t)b : code_to_float<FMT>(b)) * held);
-              raw |= (b & 0xffu) << (8 * j);
-              if (same >> (x * 16 + token) & 1) still |= 0xffu << (8 * j);
-            }
-            w[k] = (raw & still) | (pack_codes<FMT>(f[0], f[1], f[2], f[3]) & ~still);
+            for (int k = 0; k < 4; ++k) w[k] = again<FMT>(w[k], was, by);
           }
-          if (m == kKvTile) {
-            *reinterpret_cast<uint4*>(p + y * 1024) = make_uint4(w[0], w[1], w[2], w[3]);
-          } else {  // the bytes behind the sequence stay
-            for (int k = 0; k < m; ++k) {
-              const uint32_t word = k < 8 ? (k < 4 ? w[0] : w[1]) : (k < 12 ? w[2] : w[3]);
-              p[y * 1024 + k] = (uint8_t)(word >> (8 * (k & 3)));
-            }
-          }
+          *reinterpret_cast<uint4*>(p + y * 1024) = make_uint4(w[0], w[1], w[2], w[3]);
         }
       }
     }
+#pragma unroll
+    for (int x = 0; x < TILES; ++x)
+#pragma unroll
+      for (int y = 0; y < P; ++y) u[x][y] = ahead[x][y];
   }
+}
+
+// V: a lane has a channel (of each of P parts) and fetches its tokens' bytes one by one, a
+// tile ahead, at addresses whose bases are scalar.
+template <int D, int FMT, int P>
+__device__ __forceinline__ void move_values(Mover<D>& m, uint8_t* data) {
+  constexpr int TILES = kWave / kKvTile;
+  const int lane = lane_id();
+  int32_t even[P][16], odd[P][16];
+  // (tokens that are not there: the last one that is)
+  auto load = [&](int64_t from, int x, int n, int32_t (&code)[P][16])
+      __attribute__((always_inline)) {
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      const uint8_t* p = data + lane_i64(from, x * 16 + min(k, n - 1)) + lane * 16;
+#pragma unroll
+      for (int y = 0; y < P; ++y)
+        code[y][k] = FMT == SEM_KV_INT8 ? (int32_t) * reinterpret_cast<const int8_t*>(p + y * 1024)
+                                        : (int32_t)p[y * 1024];
+    }
+  };
+  auto store = [&](int x, int n, const int32_t (&code)[P][16]) __attribute__((always_inline)) {
+    Quotient by = m.q;
+    by.by = lane_float(m.q.by, x * 16);
+    by.inv = lane_float(m.q.inv, x * 16);
+    uint8_t* p = data + lane_i64(m.to, x * 16) + lane * 16;
+    const uint32_t still = (uint32_t)(__ballot(m.same) >> (x * 16)) & 0xffffu;
+#pragma unroll
+    for (int y = 0; y < P; ++y) {
+      uint32_t w[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        float f[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          f[j] = by.of_lifted(number_of<FMT>(code[y][4 * k + j]) *
+                              lane_float(m.held, x * 16 + 4 * k + j));
+        w[k] = pack_codes<FMT>(f[0], f[1], f[2], f[3]);
+      }
+      if (still) {  // codes on the same scale stay as they are
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          uint32_t raw = 0, keep = 0;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            raw |= ((uint32_t)code[y][4 * k + j] & 0xffu) << (8 * j);
+            if (still >> (4 * k + j) & 1) keep |= 0xffu << (8 * j);
+          }
+          w[k] = (raw & keep) | (w[k] & ~keep);
+        }
+      }
+      if (n == kKvTile) {
+        *reinterpret_cast<uint4*>(p + y * 1024) = make_uint4(w[0], w[1], w[2], w[3]);
+      } else {  // the bytes behind the sequence stay
+        for (int k = 0; k < n; ++k) {
+          const uint32_t word = k < 8 ? (k < 4 ? w[0] : w[1]) : (k < 12 ? w[2] : w[3]);
+          p[y * 1024 + k] = (uint8_t)(word >> (8 * (k & 3)));
+        }
+      }
+    }
+  };
+  for (uint32_t t0 = m.first; t0 < m.end; t0 += kWave, m.advance()) {
+    m.step(t0);
+    auto n = [&](int x) __attribute__((always_inline)) { return m.tokens_of(t0 + x * 16); };
+    if (t0 == m.first && m.moves(0)) load(m.s.from, 0, n(0), even);
+#pragma unroll 1
+    for (int x = 0; x < TILES; x += 2) {
+      if (m.moves(x + 1)) load(m.s.from, x + 1, n(x + 1), odd);
+      if (m.moves(x)) store(x, n(x), even);
+      if (x + 2 < TILES) {
+        if (m.moves(x + 2)) load(m.s.from, x + 2, n(x + 2), even);
+      } else if (m.end - t0 > (uint32_t)kWave) {
+        load(m.next.from, 0, n(TILES), even);
+      }
+      if (m.moves(x + 1)) store(x + 1, n(x + 1), odd);
+    }
+  }
+}
+
+// A wave: P times 64 channels (part blockIdx.y) of a block of every page that changes. Loads
+// run ahead: sources two steps of 64 tokens, scales and codes one (V: a tile of 16). A
+// token that stays where it is on the same scale is not touched, and a tile of 16 of
+// them neither.
+template <int D, int FMT, int P>
+__global__ __launch_bounds__(MW* kWave, P == 1 ? 4 : 2) void kv_keep_move(KvKeepArgs a) {
+  const KvView& c = a.c;
+  const int64_t unit = (int64_t)blockIdx.x * MW +
+                       __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int64_t i = unit / c.page_scales;
+  if (i >= a.n) return;
+  // K and V of a head side by side: V takes longer, and the dies deal out workgroups in turn
+  const int pair = (int)(unit % c.page_scales), both = 2 * c.kv_heads;
+  const int which = pair / both * both + pair % 2 * c.kv_heads + pair % both / 2;
+  const KvKept kept = a.kept[i];
+  if (kept.seq < 0 || kept.begin >= kept.end) return;
+  uint8_t* const data = c.data + which * ((int64_t)c.page_tokens * D) + blockIdx.y * (P * 1024);
+  Mover<D> m{a, kept, which};
+  m.begin();
+  if (pair % 2 == 0) move_keys<D, FMT, P>(m, data);
+  else move_values<D, FMT, P>(m, data);
 }
 
 // The scales of the blocks that changed, the pages behind the sequence, its length.

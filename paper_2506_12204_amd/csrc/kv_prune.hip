@@ -112,7 +112,7 @@ __global__ __launch_bounds__(PT) void kv_prune_plan(KvPruneArgs a) {
     wrong = 0;
   }
   block_sync();
-  int64_t* const source = a.k.source + i * budget;
+  int32_t* const source = a.k.pages + i * budget;  // (the tokens at first)
   const bool any = budget - sinks - recent > 0;
   uint32_t more = 0, equal = 0;  // before this round
   for (int64_t j0 = 0; j0 < len; j0 += kEach * PT) {
@@ -138,7 +138,7 @@ __global__ __launch_bounds__(PT) void kv_prune_plan(KvPruneArgs a) {
     for (int k = 0; k < kEach; ++k) {
       const int64_t j = first + k;
       const bool stays = (is_more >> k & 1) || ((is_equal >> k & 1) && e < want);
-      if (stays) source[m + min(e, want)] = j;
+      if (stays) source[m + min(e, want)] = (int32_t)j;
       else if (j < len) atomicMin(&gap, (int32_t)j);
       m += is_more >> k & 1;
       e += is_equal >> k & 1;
@@ -178,14 +178,13 @@ __global__ __launch_bounds__(PT) void kv_prune_plan(KvPruneArgs a) {
     int from = 0;
     float x = 0.0f;
     if (j < budget) {
-      from = (int)source[j];
+      from = source[j];
       x = mass[from];
     }
     block_sync();
     if (j < budget) {
       mass[j] = x;
-      source[j] =
-          ((int64_t)table[from >> c.page_shift] << c.page_shift) + (from & (c.page_tokens - 1));
+      write_source(a.k, i * budget + j, table[from >> c.page_shift], from & (c.page_tokens - 1));
     }
   }
   wait_stores();
@@ -196,7 +195,7 @@ __global__ __launch_bounds__(PT) void kv_prune_plan(KvPruneArgs a) {
     kept.now = budget;
     kept.begin = begin;
     kept.end = end;
-    kept.source = i * budget + (begin << c.page_shift);
+    kept.source = i * budget + ((int64_t)begin << c.page_shift);
     kept.scales = i * blocks_of(budget);
     a.k.kept[i] = kept;
   }
