@@ -13,9 +13,10 @@ namespace semsched {
 
 namespace {
 
-constexpr int PT = 1024;
 constexpr int kBins = 2048;
-constexpr int kEach = 4;  // neighbouring tokens of a thread
+constexpr int kCopies = 4;  // of the counters, for lanes in turn: few lanes then meet at one
+constexpr int kEach = 4;    // neighbouring tokens of a thread
+constexpr int kHeld = 4;    // rounds of them whose weights stay in registers
 
 // Numbers in the order of floats; NaN comes before all.
 __device__ __forceinline__ uint32_t order_of(float x) {
@@ -24,9 +25,13 @@ __device__ __forceinline__ uint32_t order_of(float x) {
   return u >> 31 ? ~u : u | 0x80000000u;
 }
 
-__global__ __launch_bounds__(PT) void kv_prune_plan(KvPruneArgs a) {
-  __shared__ uint32_t bins[kBins];
-  __shared__ uint32_t scratch[PT / kWave + 1];
+// NT threads: 256 where no sequence is longer than their registers hold, else 1024.
+template <int NT>
+__global__ __launch_bounds__(NT) void kv_prune_plan(KvPruneArgs a) {
+  constexpr int kRound = kEach * NT;    // tokens
+  constexpr int kMine = kBins / NT;     // digits of a thread
+  __shared__ alignas(16) uint32_t bins[kBins * kCopies];
+  __shared__ uint32_t scratch[NT / kWave + 1];
   __shared__ uint32_t digit_found, above_found, wrong;
   __shared__ int32_t gap;  // the first token that leaves
   const KvView& c = a.k.c;
@@ -49,29 +54,49 @@ __global__ __launch_bounds__(PT) void kv_prune_plan(KvPruneArgs a) {
   float* const mass = a.mass + s * a.mass_stride;
   const int low = sinks, high = len - recent;  // the tokens between
   uint32_t want = (uint32_t)(budget - sinks - recent);
+  const bool any = want > 0;
+  const int64_t rounds = ((int64_t)len + kRound - 1) / kRound;
+
+  // Round r's weights: neighbouring tokens of a thread, the first rounds' from registers.
+  uint32_t held[kHeld][kEach];
+  auto fetch = [&](int64_t r, uint32_t (&key)[kEach]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const int64_t j = r * kRound + kEach * t + k;
+      key[k] = j >= low && j < high ? order_of(mass[j]) : 0u;
+    }
+  };
+  auto each_round = [&](auto work) __attribute__((always_inline)) {
+#pragma unroll
+    for (int r = 0; r < kHeld; ++r)
+      if (r < rounds) work(r, held[r]);
+    for (int64_t r = kHeld; r < rounds; ++r) {
+      uint32_t key[kEach];
+      fetch(r, key);
+      work(r, key);
+    }
+  };
+  if (any) {
+#pragma unroll
+    for (int r = 0; r < kHeld; ++r) fetch(r, held[r]);
+  }
 
   // The want-th largest of them: its digits from the first on.
   uint32_t edge = 0;
-  if (want > 0) {
+  if (any) {
     constexpr int kShift[3] = {21, 10, 0};
     uint32_t known = 0;  // bits of the edge that are found
+    for (int b = t; b < kBins * kCopies; b += NT) bins[b] = 0;
+    block_sync();
 #pragma unroll 1
     for (int p = 0; p < 3; ++p) {
-      const int shift = kShift[p];
+      const int shift = p == 0 ? kShift[0] : p == 1 ? kShift[1] : kShift[2];
       const uint32_t digits = p == 2 ? 1024u : 2048u;
-      bins[t] = 0;
-      bins[t + PT] = 0;
-      block_sync();
-      for (int64_t j0 = low; j0 < high; j0 += kEach * PT) {
-        uint32_t key[kEach];
+      each_round([&](int64_t r, const uint32_t (&key)[kEach]) __attribute__((always_inline)) {
 #pragma unroll
         for (int k = 0; k < kEach; ++k) {
-          const int64_t j = j0 + k * PT + t;
-          key[k] = j < high ? order_of(mass[j]) : 0u;
-        }
-#pragma unroll
-        for (int k = 0; k < kEach; ++k) {
-          const bool mine = j0 + k * PT + t < high && (key[k] & known) == (edge & known);
+          const int64_t j = r * kRound + kEach * t + k;
+          const bool mine = j >= low && j < high && (key[k] & known) == (edge & known);
           const uint32_t digit = (key[k] >> shift) & (digits - 1u);
           // (equal weights are common, and a counter takes one lane at a time)
           const uint64_t all = __ballot(mine);
@@ -79,24 +104,32 @@ __global__ __launch_bounds__(PT) void kv_prune_plan(KvPruneArgs a) {
           const int one = __ffsll((unsigned long long)all) - 1;
           const uint32_t first = (uint32_t)__builtin_amdgcn_readlane((int)digit, one);
           if (__ballot(mine && digit != first) == 0) {
-            if (lane_id() == one) atomicAdd(&bins[first], (uint32_t)__popcll(all));
+            if (lane_id() == one) atomicAdd(&bins[first * kCopies], (uint32_t)__popcll(all));
           } else if (mine) {
-            atomicAdd(&bins[digit], 1u);
+            atomicAdd(&bins[digit * kCopies + lane_id() % kCopies], 1u);
           }
         }
-      }
+      });
       block_sync();
-      // from the largest digit down, two to a thread
-      const uint32_t d1 = kBins - 1u - 2u * t, d0 = d1 - 1u;
-      const uint32_t n1 = bins[d1], n0 = bins[d0];
+      // from the largest digit down, some to a thread
+      uint32_t count[kMine], own = 0;
+#pragma unroll
+      for (int k = 0; k < kMine; ++k) {
+        uint4* at = reinterpret_cast<uint4*>(bins + (kBins - 1 - kMine * t - k) * kCopies);
+        const uint4 n = *at;
+        *at = make_uint4(0, 0, 0, 0);  // for the next digit
+        count[k] = n.x + n.y + n.z + n.w;
+        own += count[k];
+      }
       uint32_t sum;
-      const uint32_t above = block_excl_scan_u32<PT>(n1 + n0, scratch, sum);
-      if (above < want && want <= above + n1) {
-        digit_found = d1;
-        above_found = above;
-      } else if (above + n1 < want && want <= above + n1 + n0) {
-        digit_found = d0;
-        above_found = above + n1;
+      uint32_t above = block_excl_scan_u32<NT>(own, scratch, sum);
+#pragma unroll
+      for (int k = 0; k < kMine; ++k) {
+        if (above < want && want <= above + count[k]) {
+          digit_found = kBins - 1 - kMine * t - k;
+          above_found = above;
+        }
+        above += count[k];
       }
       block_sync();
       edge |= digit_found << shift;
@@ -113,11 +146,11 @@ __global__ __launch_bounds__(PT) void kv_prune_plan(KvPruneArgs a) {
   }
   block_sync();
   int32_t* const source = a.k.pages + i * budget;  // (the tokens at first)
-  const bool any = budget - sinks - recent > 0;
   uint32_t more = 0, equal = 0;  // before this round
-  for (int64_t j0 = 0; j0 < len; j0 += kEach * PT) {
-    const int64_t first = j0 + kEach * t;
-    uint32_t mine = 0, is_more = 0, is_equal = 0;
+  int32_t leaves = INT32_MAX;
+  each_round([&](int64_t r, const uint32_t (&key)[kEach]) __attribute__((always_inline)) {
+    const int64_t first = r * kRound + kEach * t;
+    uint32_t is_more = 0, is_equal = 0;
 #pragma unroll
     for (int k = 0; k < kEach; ++k) {
       const int64_t j = first + k;
@@ -125,27 +158,28 @@ __global__ __launch_bounds__(PT) void kv_prune_plan(KvPruneArgs a) {
       if (j < low || j >= high) {
         is_more |= 1u << k;
       } else if (any) {
-        const uint32_t key = order_of(mass[j]);
-        if (key > edge) is_more |= 1u << k;
-        else if (key == edge) is_equal |= 1u << k;
+        if (key[k] > edge) is_more |= 1u << k;
+        else if (key[k] == edge) is_equal |= 1u << k;
       }
     }
-    mine = (uint32_t)__popc(is_more) | (uint32_t)__popc(is_equal) << 16;
     uint32_t sum;
-    const uint32_t before = block_excl_scan_u32<PT>(mine, scratch, sum);
+    const uint32_t before = block_excl_scan_u32<NT>(
+        (uint32_t)__popc(is_more) | (uint32_t)__popc(is_equal) << 16, scratch, sum);
     uint32_t m = more + (before & 0xffffu), e = equal + (before >> 16);
 #pragma unroll
     for (int k = 0; k < kEach; ++k) {
       const int64_t j = first + k;
       const bool stays = (is_more >> k & 1) || ((is_equal >> k & 1) && e < want);
       if (stays) source[m + min(e, want)] = (int32_t)j;
-      else if (j < len) atomicMin(&gap, (int32_t)j);
+      else if (j < len) leaves = min(leaves, (int32_t)j);
       m += is_more >> k & 1;
       e += is_equal >> k & 1;
     }
     more += sum & 0xffffu;
     equal += sum >> 16;
-  }
+  });
+  const uint32_t lowest = wave_min_u32((uint32_t)leaves);
+  if (lane_id() == 0) atomicMin(&gap, (int32_t)lowest);
   wait_stores();
   block_sync();
 
@@ -158,7 +192,7 @@ __global__ __launch_bounds__(PT) void kv_prune_plan(KvPruneArgs a) {
   const int end = moves ? blocks_of(budget) : 0;
   const int blocks = blocks_of(len);
   const int32_t* table = c.tables + (int64_t)s * c.max_blocks;
-  for (int b = (moves ? begin : budget >> c.page_shift) + t; b < blocks; b += PT) {
+  for (int b = (moves ? begin : budget >> c.page_shift) + t; b < blocks; b += NT) {
     const int32_t page = table[b];
     if ((uint32_t)page >= (uint64_t)c.num_pages) wrong = 1;
     else if (b >= begin && b < end && c.refs[page] != 1) wrong = 1;
@@ -173,23 +207,29 @@ __global__ __launch_bounds__(PT) void kv_prune_plan(KvPruneArgs a) {
   }
   // The tokens' pages and places, and their weights. Sources lie at their tokens or
   // behind, so a round's weights are read before any of them is written.
-  for (int64_t j0 = moves ? begin << c.page_shift : budget; j0 < budget; j0 += PT) {
-    const int64_t j = j0 + t;
-    int from = 0;
-    float x = 0.0f;
-    if (j < budget) {
-      from = source[j];
-      x = mass[from];
+  for (int64_t j0 = moves ? begin << c.page_shift : budget; j0 < budget; j0 += kEach * NT) {
+    int from[kEach];
+    float x[kEach];
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const int64_t j = j0 + k * NT + t;
+      from[k] = j < budget ? source[j] : 0;
     }
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) x[k] = mass[from[k]];
     block_sync();
-    if (j < budget) {
-      mass[j] = x;
-      write_source(a.k, i * budget + j, table[from >> c.page_shift], from & (c.page_tokens - 1));
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const int64_t j = j0 + k * NT + t;
+      if (j >= budget) continue;
+      mass[j] = x[k];
+      write_source(a.k, i * budget + j, table[from[k] >> c.page_shift],
+                   from[k] & (c.page_tokens - 1));
     }
   }
   wait_stores();
   block_sync();
-  for (int64_t j = budget + t; j < len; j += PT) mass[j] = 0.0f;
+  for (int64_t j = budget + t; j < len; j += NT) mass[j] = 0.0f;
   if (t == 0) {
     kept.seq = s;
     kept.now = budget;
@@ -205,8 +245,12 @@ __global__ __launch_bounds__(PT) void kv_prune_plan(KvPruneArgs a) {
 
 hipError_t launch_kv_prune(const KvPruneArgs& a, hipStream_t st) {
   if (a.k.n == 0) return hipSuccess;
-  if (!kv_kept_fits(a.k) || !grid_fits(a.k.n, PT)) return hipErrorInvalidConfiguration;
-  hipLaunchKernelGGL(kv_prune_plan, dim3((unsigned)a.k.n), dim3(PT), 0, st, a);
+  if (!kv_kept_fits(a.k) || !grid_fits(a.k.n, 1024)) return hipErrorInvalidConfiguration;
+  const dim3 grid((unsigned)a.k.n);
+  if ((int64_t)a.k.c.max_blocks * a.k.c.page_tokens <= kHeld * kEach * 256)
+    hipLaunchKernelGGL(kv_prune_plan<256>, grid, dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL(kv_prune_plan<1024>, grid, dim3(1024), 0, st, a);
   const int64_t pt = a.k.c.page_tokens;
   return launch_kv_kept(a.k, a.k.n * ((a.budget + pt - 1) / pt), st);
 }
