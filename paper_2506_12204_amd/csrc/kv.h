@@ -157,10 +157,9 @@ struct KvWeighArgs {
   const int32_t *seqs, *cu;
   int64_t n, tokens;
   int32_t layer, heads, group;
-  int32_t bf16, wide;  // 16-byte loads of q are aligned
-  int32_t causal, window;
+  int32_t bf16, causal, window;
   float scale_log2;
-  int32_t key_slots;  // of a workgroup's waves (set by the launch)
+  int32_t share;       // waves that share a unit's heads (set by the launch)
 };
 
 struct QkRotateArgs {
@@ -190,7 +189,7 @@ hipError_t launch_kv_append(const KvAppendArgs& a, hipStream_t st);
 hipError_t launch_qk_rotate(const QkRotateArgs& a, int head_dim, hipStream_t st);
 hipError_t launch_kv_attend(const KvAttendArgs& a, hipStream_t st);
 hipError_t launch_kv_attend_tree(const KvAttendArgs& a, hipStream_t st);
-hipError_t launch_kv_weigh(const KvWeighArgs& a, int64_t max_len, hipStream_t st);
+hipError_t launch_kv_weigh(const KvWeighArgs& a, int64_t max_new, int64_t max_len, hipStream_t st);
 bool kv_kept_fits(const KvKeepArgs& a);
 hipError_t launch_kv_kept(const KvKeepArgs& a, int64_t blocks, hipStream_t st);
 hipError_t launch_kv_prune(const KvPruneArgs& a, hipStream_t st);

@@ -702,12 +702,13 @@ int sem_kv_weigh_async(const sem_kv_cache* cache, int32_t layer, const sem_kv_qu
   a.heads = query->heads;
   a.group = query->heads / cache->kv_heads;
   a.bf16 = query->dtype == SEM_KV_BF16;
-  a.wide = aligned16(query->q, query->q_token_stride, query->q_head_stride);
   a.causal = query->causal != 0;
   a.window = query->window;
   a.scale_log2 = query->scale * 1.4426950408889634f;
   const int64_t most = most_tokens(cache);
-  return status_of(launch_kv_weigh(a, query->max_len > 0 ? std::min(query->max_len, most) : most,
+  const int64_t max_len = query->max_len > 0 ? std::min(query->max_len, most) : most;
+  const int64_t max_new = !cu ? 1 : query->max_new > 0 ? query->max_new : query->tokens;
+  return status_of(launch_kv_weigh(a, std::min(max_new, query->tokens), max_len,
                                    static_cast<hipStream_t>(stream)));
 }
 

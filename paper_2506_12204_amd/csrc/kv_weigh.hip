@@ -23,14 +23,13 @@ namespace semsched {
 
 namespace {
 
-constexpr int WW = 8;       // waves of a workgroup
+constexpr int WW = 8;       // waves of a workgroup, one of which fills a compute unit
 constexpr int kChunk = 64;  // keys of a wave
 constexpr int kRows = 16;   // of a tile
 typedef float float4_t __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 
-// A listed sequence: its rows, keys, the chunks of keys that its rows see and the
-// units (of several chunks) that they make.
+// A listed sequence: its rows, keys and the chunks of 64 keys that its rows see.
 struct Seen {
   int32_t row0, fresh, slot, len, c0, c1;
   uint32_t units;
@@ -59,7 +58,7 @@ __device__ __forceinline__ Seen seen_of(const KvWeighArgs& a, int64_t i) {
   const int64_t low = a.window > 0 && first >= a.window ? first + 1 - a.window : 0;
   s.c0 = (int)(low / kChunk);
   s.c1 = (int)((len + kChunk - 1) / kChunk);
-  s.units = (uint32_t)((s.c1 - s.c0 + a.key_slots - 1) / a.key_slots);
+  s.units = (uint32_t)(s.c1 - s.c0);
   return s;
 }
 
@@ -91,187 +90,295 @@ __device__ __forceinline__ float4_t product(bf16x8_t a, bf16x8_t b, float4_t c) 
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
-template <int D, int FMT, bool BF16>
-__global__ __launch_bounds__(WW* kWave) void kv_weigh(KvWeighArgs a) {
+// A lane's row: its token and its head in the group, 16 rows further each time.
+struct Row {
+  uint32_t at, token, head;
+  __device__ __forceinline__ Row(uint32_t r, uint32_t group)
+      : at(r), token(r / group), head(r % group) {}
+  __device__ __forceinline__ void next(uint32_t tokens, uint32_t heads, uint32_t group) {
+    at += kRows;
+    token += tokens;
+    head += heads;
+    if (head >= group) {
+      head -= group;
+      ++token;
+    }
+  }
+};
+
+// The sums of sixteen numbers over the sixteen lanes of a group: lane r gets the r-th. In
+// each step a lane gives half of its numbers away and adds what it gets to the others.
+template <int OFF>
+__device__ __forceinline__ void halve(float (&x)[16], int r) {
+  const bool upper = (r & OFF) != 0;
+#pragma unroll
+  for (int k = 0; k < OFF; ++k) {
+    const float give = upper ? x[k] : x[k + OFF], keep = upper ? x[k + OFF] : x[k];
+    x[k] = keep + __shfl_xor(give, OFF, kWave);
+  }
+}
+__device__ __forceinline__ float sum_of_rows(float (&x)[16], int r) {
+  halve<8>(x, r);
+  halve<4>(x, r);
+  halve<2>(x, r);
+  halve<1>(x, r);
+  return x[0];
+}
+
+// Where a wave is on the line of units (64 keys of a sequence each, all heads).
+struct Cursor {
+  Seen s;
+  int64_t index;
+  uint32_t unit;  // of the sequence
+  uint64_t u;     // of the line
+  __device__ __forceinline__ int chunk() const { return s.c0 + (int)unit; }
+  __device__ __forceinline__ void advance(const KvWeighArgs& a, uint64_t stop) {
+    if (++u >= stop) return;
+    ++unit;
+    while (unit >= s.units) {
+      unit = 0;
+      s = lane_seen(seen_of(a, ++index), 0);
+    }
+  }
+};
+
+// The line is cut into equal pieces of neighbours, one for each team of waves; a team's
+// waves share the heads of its units and join through LDS. Loads run ahead: page numbers
+// two units, codes one head or unit, queries one tile.
+//
+// FEW: for one tile of rows a sequence (any number is right): 16 keys at a time are
+// turned into operands and used. Otherwise all 64 are, once for all tiles.
+template <int D, int FMT, bool BF16, bool FEW>
+__global__ __launch_bounds__(WW* kWave, 2) void kv_weigh(KvWeighArgs a) {
   using Operand = std::conditional_t<BF16, bf16x8_t, half8_t>;
-  constexpr int N = D / 32;  // operands of a row or key
-  __shared__ float sums[WW][kChunk];
+  constexpr int N = D / 32;         // operands of a row or key
+  constexpr bool AHEAD = D <= 128;  // (the registers hold no more codes of 256 channels)
+  __shared__ float sums[2][WW][kChunk];
   const KvView& c = a.c;
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int r = lane % 16, g = lane / 16;
-  const int head_slots = WW / a.key_slots;
-  const int key_slot = wave / head_slots, head_slot = wave % head_slots;
+  const int share = a.share, head_slot = wave % share;
   if (a.cu && blockIdx.x == 0 && threadIdx.x == 0 && (a.cu[0] != 0 || a.cu[a.n] != a.tokens))
     atomicOr(c.flags, kFlagInval);
-  // All units as one line, cut into equal pieces of neighbours.
   const Seen mine = seen_of(a, lane);
   uint64_t total = 0;
   for (int64_t at = 0; at < a.n; at += kWave) {
     const Seen s = at == 0 ? mine : seen_of(a, at + lane);
     total += last_lane_u64(wave_incl_scan_u64(s.units));
   }
-  uint64_t u = total * blockIdx.x / gridDim.x;
-  const uint64_t stop = total * (blockIdx.x + 1) / gridDim.x;
-  if (u >= stop) return;
-  Seen s = {};
-  int64_t index = 0;
-  uint32_t unit = 0;  // of the sequence
+  const uint64_t teams = (uint64_t)gridDim.x * (WW / share);
+  const uint64_t self = (uint64_t)blockIdx.x * (WW / share) + wave / share;
+  const uint64_t stop = total * (self + 1) / teams;
+  // (all teams of a workgroup go through as many rounds)
+  const uint32_t rounds = (uint32_t)((total + teams - 1) / teams);
+  Cursor now = {{}, 0, 0, total * self / teams};
   uint64_t before = 0;
-  for (int64_t at = 0; at < a.n; at += kWave) {
+  for (int64_t at = 0; at < a.n && now.u < stop; at += kWave) {
     const Seen x = at == 0 ? mine : seen_of(a, at + lane);
     const uint64_t upto = before + wave_incl_scan_u64(x.units);
-    const uint64_t beyond = __ballot(upto > u);
+    const uint64_t beyond = __ballot(upto > now.u);
     if (beyond) {
       const int first = __ffsll((unsigned long long)beyond) - 1;
-      index = at + first;
-      s = lane_seen(x, first);
-      unit = (uint32_t)(u - (lane_u64(upto, first) - s.units));
+      now.index = at + first;
+      now.s = lane_seen(x, first);
+      now.unit = (uint32_t)(now.u - (lane_u64(upto, first) - now.s.units));
       break;
     }
     before = last_lane_u64(upto);
   }
   const int64_t block_bytes = (int64_t)c.page_tokens * D;
   const int in_page = c.page_tokens - 1;
+  const uint32_t group = (uint32_t)a.group, step_tokens = kRows / group, step_heads = kRows % group;
+  const Row first_row(r, group);
   bool wrong = false;
-  for (; u < stop; ++u, ++unit) {
-    while (unit >= s.units) {
-      unit = 0;
-      s = lane_seen(seen_of(a, ++index), 0);
-    }
-    const int chunk = s.c0 + (int)unit * a.key_slots + key_slot;
+
+  // The pages of a unit: of this lane's K rows, and of its 16 keys.
+  struct Entries {
+    int32_t k, v;
+  };
+  auto entries = [&](const Cursor& at) __attribute__((always_inline)) {
+    const int32_t* table = c.tables + (int64_t)at.s.slot * c.max_blocks;
+    const int t0 = at.chunk() * kChunk, last_block = (at.s.len - 1) >> c.page_shift;
+    return Entries{table[min((t0 + r / 4 * kKvTile) >> c.page_shift, last_block)],
+                   table[min((t0 + g * kKvTile) >> c.page_shift, last_block)]};
+  };
+  const uint8_t* keys = nullptr;  // of the unit whose codes are loaded
+  const float* scale = nullptr;
+  auto find = [&](const Cursor& at, Entries e) __attribute__((always_inline)) {
+    const bool bad =
+        (uint32_t)e.k >= (uint64_t)c.num_pages || (uint32_t)e.v >= (uint64_t)c.num_pages;
+    wrong |= bad;
+    scale = c.scale + ((int64_t)(bad ? 0 : e.v) * c.layers + a.layer) * 2 * c.kv_heads;
+    keys = c.data + (bad ? 0 : e.k) * c.page_bytes +
+           (int64_t)a.layer * 2 * c.kv_heads * block_bytes +
+           ((at.chunk() * kChunk + r / 4 * kKvTile) & in_page) * D + (r % 4) * 16 + g * 256;
+  };
+  uint4 raw[4][D / 64];
+  float ks = 0.0f;
+  auto load = [&](int kh) __attribute__((always_inline)) {
+    ks = scale[kh];
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+#pragma unroll
+      for (int j = 0; j < D / 64; ++j)
+        raw[x][j] = *reinterpret_cast<const uint4*>(keys + kh * block_bytes + x * 64 + j * 1024);
+  };
+  uint4 asked[N];
+  float lse = 0.0f;
+  auto ask = [&](const Seen& s, int kh, const Row& row, uint32_t rows)
+      __attribute__((always_inline)) {
+    const bool there = row.at < rows;  // (else the sequence's first)
+    const int64_t token = s.row0 + (there ? row.token : 0u);
+    const int head = kh * a.group + (int)(there ? row.head : 0u);
+    const uint16_t* q = a.q + token * a.q_token + head * a.q_head + g * 16;
+    lse = a.lse[token * a.heads + head];
+#pragma unroll
+    for (int j = 0; j < N; ++j)  // (rows need not be 16-byte aligned)
+      __builtin_memcpy(&asked[j], q + j / 2 * 64 + j % 2 * 8, 16);
+  };
+  const bool works = head_slot < c.kv_heads;  // (a wave may have no heads)
+  Cursor next = now;
+  Entries ahead = {0, 0};
+  if (now.u < stop && works) {
+    find(now, entries(now));
+    if (AHEAD) load(head_slot);
+    next.advance(a, stop);
+    if (next.u < stop) ahead = entries(next);
+  }
+  for (uint32_t round = 0; round < rounds; ++round) {
     float sum[16];
 #pragma unroll
     for (int k = 0; k < 16; ++k) sum[k] = 0.0f;
-    if (chunk < s.c1) {
-      const int32_t* table = c.tables + (int64_t)s.slot * c.max_blocks;
-      const int t0 = chunk * kChunk, vt = t0 + g * kKvTile;
-      const uint32_t rows = (uint32_t)s.fresh * (uint32_t)a.group;
-      const int last_block = (s.len - 1) >> c.page_shift;
-      // the pages of this lane's K rows, and of its 16 keys
-      const int32_t kentry = table[min((t0 + r / 4 * kKvTile) >> c.page_shift, last_block)];
-      const int32_t ventry = table[min(vt >> c.page_shift, last_block)];
-      const bool bad = (uint32_t)kentry >= (uint64_t)c.num_pages ||
-                       (uint32_t)ventry >= (uint64_t)c.num_pages;
-      wrong |= bad;
-      const int64_t kpage = bad ? 0 : kentry, vpage = bad ? 0 : ventry;
-      const float* scale = c.scale + (vpage * c.layers + a.layer) * 2 * c.kv_heads;
-      const uint8_t* keys = c.data + kpage * c.page_bytes +
-                            (int64_t)a.layer * 2 * c.kv_heads * block_bytes +
-                            ((t0 + r / 4 * kKvTile) & in_page) * D + (r % 4) * 16 + g * 256;
-      for (int kh = head_slot; kh < c.kv_heads; kh += head_slots) {
-        Operand key[4][N];
+    const bool live = now.u < stop;
+    const Seen s = now.s;
+    const int t0 = now.chunk() * kChunk, vt = t0 + g * kKvTile;
+    float* const mass = a.mass + s.slot * a.mass_stride + min(t0 + lane, max(s.len, 1) - 1);
+    float was = 0.0f;
+    if (live && head_slot == 0) was = *mass;
+    if (live && works) {
+      const uint32_t rows = (uint32_t)s.fresh * group;
+      for (int kh = head_slot; kh < c.kv_heads; kh += share) {
+        Row row = first_row;
+        if (!AHEAD) load(kh);
+        ask(s, kh, row, rows);
+        uint4 codes[4][D / 64];
+        Operand key[FEW ? 1 : 4][N];
+        const float f = ks * a.scale_log2;
 #pragma unroll
         for (int x = 0; x < 4; ++x)
 #pragma unroll
-          for (int j = 0; j < D / 64; ++j)
-            operands<FMT>(*reinterpret_cast<const uint4*>(keys + kh * block_bytes + x * 64 +
-                                                          j * 1024),
-                          key[x][2 * j], key[x][2 * j + 1]);
-        const float f = scale[kh] * a.scale_log2;
-        for (uint32_t row = r; row - r < rows; row += kRows) {
-          const uint32_t at = min(row, rows - 1);
-          const int token = (int)(at / (uint32_t)a.group);
-          const int head = kh * a.group + (int)(at % (uint32_t)a.group);
-          const uint16_t* q = a.q + (int64_t)(s.row0 + token) * a.q_token + head * a.q_head + g * 16;
-          const float lse = a.lse[(int64_t)(s.row0 + token) * a.heads + head];
+          for (int j = 0; j < D / 64; ++j) {
+            if (FEW) codes[x][j] = raw[x][j];
+            else operands<FMT>(raw[x][j], key[FEW ? 0 : x][2 * j], key[FEW ? 0 : x][2 * j + 1]);
+          }
+        if (kh + share < c.kv_heads) {
+          if (AHEAD) load(kh + share);
+        } else if (next.u < stop) {
+          find(next, ahead);
+          if (AHEAD) load(head_slot);
+        }
+        for (; row.at - r < rows;) {
           Operand query[N];
 #pragma unroll
-          for (int j = 0; j < N; ++j) {
-            const uint16_t* p = q + j / 2 * 64 + j % 2 * 8;
-            uint4 w;
-            if (a.wide) {
-              w = *reinterpret_cast<const uint4*>(p);
-            } else {
-              w = make_uint4(p[0] | (uint32_t)p[1] << 16, p[2] | (uint32_t)p[3] << 16,
-                             p[4] | (uint32_t)p[5] << 16, p[6] | (uint32_t)p[7] << 16);
-            }
-            query[j] = __builtin_bit_cast(Operand, w);
-          }
+          for (int j = 0; j < N; ++j) query[j] = __builtin_bit_cast(Operand, asked[j]);
           // Rows that see no key, are not numbers, or are not there weigh nothing.
-          const bool live = row < rows && fabsf(lse) < __builtin_inff();
-          if (__ballot(!live)) {
+          const bool counts = row.at < rows && fabsf(lse) < __builtin_inff();
+          if (__ballot(!counts)) {
 #pragma unroll
             for (int j = 0; j < N; ++j)
-              query[j] = live ? query[j] : __builtin_bit_cast(Operand, make_uint4(0, 0, 0, 0));
+              query[j] = counts ? query[j] : __builtin_bit_cast(Operand, make_uint4(0, 0, 0, 0));
           }
-          const float base = live ? lse * 1.4426950408889634f : __builtin_inff();
-          const int pos = s.len - s.fresh + token;
+          const float base = counts ? lse * 1.4426950408889634f : __builtin_inff();
+          const int pos = s.len - s.fresh + (int)row.token;
           const int high = a.causal ? min(pos + 1, s.len) : s.len;
           const int low = a.window > 0 && pos >= a.window ? pos + 1 - a.window : 0;
-          const bool hides = __ballot(low > t0 || high < t0 + kChunk) != 0;
+          const bool hides = __ballot(counts && (low > t0 || high < t0 + kChunk)) != 0;
+          row.next(step_tokens, step_heads, group);
+          if (!FEW) ask(s, kh, row, rows);  // (behind the last row: the first one again)
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
+            if (FEW) {
+#pragma unroll
+              for (int j = 0; j < D / 64; ++j)
+                operands<FMT>(codes[x][j], key[0][2 * j], key[0][2 * j + 1]);
+            }
             float4_t t = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int j = 0; j < N; ++j) t = product(key[x][j], query[j], t);
+            for (int j = 0; j < N; ++j) t = product(key[FEW ? 0 : x][j], query[j], t);
+            float p[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              float p = __builtin_amdgcn_exp2f(__builtin_fmaf(t[i], f, -base));
-              if (hides) p = vt + 4 * x + i >= low && vt + 4 * x + i < high ? p : 0.0f;
-              sum[4 * x + i] += p;
+            for (int i = 0; i < 4; ++i)
+              p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(t[i], f, -base));
+            if (hides) {
+              asm volatile("");  // (a branch: selects in every tile would cost more)
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                p[i] = vt + 4 * x + i >= low && vt + 4 * x + i < high ? p[i] : 0.0f;
             }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[4 * x + i] += p[i];
           }
+          if (FEW && row.at - r < rows) ask(s, kh, row, rows);
         }
       }
     }
+    now = next;
+    next.advance(a, stop);
+    if (works && next.u < stop) ahead = entries(next);
     // the sixteen lanes of a group each hold other rows: lane r gets key r's sum
-#pragma unroll
-    for (int off = 8; off > 0; off /= 2) {
-      const bool upper = (r & off) != 0;
-#pragma unroll
-      for (int k = 0; k < off; ++k) {
-        const float give = upper ? sum[k] : sum[k + off];
-        const float keep = upper ? sum[k + off] : sum[k];
-        sum[k] = keep + __shfl_xor(give, off, kWave);
-      }
-    }
-    if (head_slots > 1) {
-      sums[wave][lane] = sum[0];
+    const float whole = sum_of_rows(sum, r);
+    float (&joined)[WW][kChunk] = sums[round & 1];  // (the other may still be read)
+    if (share > 1) {
+      if (head_slot > 0) joined[wave][lane] = whole;
       block_sync();
     }
-    const int key = chunk * kChunk + lane;
-    if (head_slot == 0 && chunk < s.c1 && key < s.len) {
-      float x = sum[0];
-      for (int k = 1; k < head_slots; ++k) x += sums[wave + k][lane];
-      a.mass[s.slot * a.mass_stride + key] += x;
+    if (live && head_slot == 0) {
+      float x = whole;
+      for (int k = 1; k < share; ++k) x += joined[wave + k][lane];
+      if (t0 + lane < s.len) *mass = was + x;
     }
-    if (head_slots > 1) block_sync();
   }
   if (__ballot(wrong) && lane == 0) atomicOr(c.flags, kFlagInval);
 }
 
-template <int D, int FMT>
-void launch_type(const KvWeighArgs& a, unsigned grid, hipStream_t st) {
-  if (a.bf16)
-    hipLaunchKernelGGL((kv_weigh<D, FMT, true>), dim3(grid), dim3(WW * kWave), 0, st, a);
+template <int D, int FMT, bool BF16>
+void launch_rows(const KvWeighArgs& a, bool few, unsigned grid, hipStream_t st) {
+  if (few)
+    hipLaunchKernelGGL((kv_weigh<D, FMT, BF16, true>), dim3(grid), dim3(WW * kWave), 0, st, a);
   else
-    hipLaunchKernelGGL((kv_weigh<D, FMT, false>), dim3(grid), dim3(WW * kWave), 0, st, a);
+    hipLaunchKernelGGL((kv_weigh<D, FMT, BF16, false>), dim3(grid), dim3(WW * kWave), 0, st, a);
+}
+
+template <int D, int FMT>
+void launch_type(const KvWeighArgs& a, bool few, unsigned grid, hipStream_t st) {
+  if (a.bf16) launch_rows<D, FMT, true>(a, few, grid, st);
+  else launch_rows<D, FMT, false>(a, few, grid, st);
 }
 
 template <int D>
-void launch_dim(const KvWeighArgs& a, unsigned grid, hipStream_t st) {
-  if (a.c.format == SEM_KV_INT8) launch_type<D, SEM_KV_INT8>(a, grid, st);
-  else launch_type<D, SEM_KV_FP8>(a, grid, st);
+void launch_dim(const KvWeighArgs& a, bool few, unsigned grid, hipStream_t st) {
+  if (a.c.format == SEM_KV_INT8) launch_type<D, SEM_KV_INT8>(a, few, grid, st);
+  else launch_type<D, SEM_KV_FP8>(a, few, grid, st);
 }
 
 }  // namespace
 
-hipError_t launch_kv_weigh(const KvWeighArgs& args, int64_t max_len, hipStream_t st) {
+hipError_t launch_kv_weigh(const KvWeighArgs& args, int64_t max_new, int64_t max_len,
+                           hipStream_t st) {
   if (args.n == 0) return hipSuccess;  // (without tokens the offsets are looked at)
   KvWeighArgs a = args;
-  // Waves that share 64 keys and deal out their heads, where there are too few keys
-  // for a wave each.
-  const int64_t chunks = std::max<int64_t>(1, a.n * ((max_len + kChunk - 1) / kChunk));
-  int head_slots = 1;
-  while (head_slots < WW && 2 * head_slots <= a.c.kv_heads && chunks * head_slots < 512 * WW)
-    head_slots *= 2;
-  a.key_slots = WW / head_slots;
-  const unsigned grid =
-      (unsigned)std::min<int64_t>(512, (chunks + a.key_slots - 1) / a.key_slots + a.n);
+  const bool few = max_new * a.group <= kRows;
+  // As many waves to a team as there are heads for: pieces are then short, and the last
+  // one's end is no long wait.
+  const int64_t units = std::max<int64_t>(1, a.n * ((max_len + kChunk - 1) / kChunk));
+  constexpr int64_t kGroups = 256;
+  a.share = 1;
+  while (a.share < WW && 2 * a.share <= a.c.kv_heads) a.share *= 2;
+  const unsigned grid = (unsigned)std::min<int64_t>(kGroups, (units * a.share + WW - 1) / WW);
   switch (a.c.head_dim) {
-    case 64: launch_dim<64>(a, grid, st); break;
-    case 128: launch_dim<128>(a, grid, st); break;
-    default: launch_dim<256>(a, grid, st);
+    case 64: launch_dim<64>(a, few, grid, st); break;
+    case 128: launch_dim<128>(a, few, grid, st); break;
+    default: launch_dim<256>(a, few, grid, st);
   }
   return hipGetLastError();
 }
