@@ -629,12 +629,13 @@ def evict(priority: torch.Tensor, length: torch.Tensor, cached: torch.Tensor, kv
 # The handle of a device's current stream (torch.cuda.current_stream makes an
 # object of it, which takes longer than the rest of a call).
 _raw_stream = torch._C._cuda_getCurrentRawStream
+_current_device = torch._C._cuda_getDevice
 
 
 def _enqueue(index: int, call, *args) -> int:
     """The status of an asynchronous call on the current stream of a device, which
     need not be the current one."""
-    if torch.cuda.current_device() == index:
+    if _current_device() == index:
         return call(*args, _raw_stream(index))
     with torch.cuda.device(index):
         return call(*args, _raw_stream(index))

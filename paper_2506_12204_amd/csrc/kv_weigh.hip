@@ -9,10 +9,16 @@
 // in 32 bits. A key belongs to one workgroup, which adds its weights in an order that
 // the call's sizes alone decide: results do not depend on the run.
 //
-// A wave has 64 keys of a head as operands in registers and goes through the row
-// tiles. As in attention the product is K q^T: a lane ends up with the scores of one
-// row (lane % 16) and 16 consecutive keys, whose weights it adds up in registers over
-// all rows and heads that it takes.
+// A wave has 64 keys of a head in registers and goes through the row tiles. As in
+// attention the product is K q^T: a lane ends up with the scores of one row (lane % 16)
+// and 16 consecutive keys, whose weights it adds up in registers over all rows and heads
+// that it takes.
+//
+// Few rows are bound by memory: 251 requests of 16 to 4096 keys, 32 heads on 8 of 128
+// channels, take 50 us, of which reading the keys (203 MB) at 5 TB/s is 41. Many rows are
+// bound by the vector instructions of a tile (the exponentials a third of them) and the
+// latency of its queries: 32 rows each of four contexts of 8192 to 32768 keys, the same
+// heads, take 81 us where the keys take 17 and the products 21.
 #include <algorithm>
 
 #include "device_common.h"
@@ -30,12 +36,14 @@ typedef float float4_t __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 
 // A listed sequence: its rows, keys and the chunks of 64 keys that its rows see.
+// (units: of those chunks, what work goes by)
 struct Seen {
   int32_t row0, fresh, slot, len, c0, c1;
   uint32_t units;
 };
 
-__device__ __forceinline__ Seen seen_of(const KvWeighArgs& a, int64_t i) {
+// (`bad` where the cache cannot hold it; it then counts as empty)
+__device__ __forceinline__ Seen seen_of(const KvWeighArgs& a, int64_t i, bool& bad) {
   const KvView& c = a.c;
   Seen s = {0, 0, 0, 0, 0, 0, 0};
   if (i >= a.n) return s;
@@ -46,7 +54,7 @@ __device__ __forceinline__ Seen seen_of(const KvWeighArgs& a, int64_t i) {
   const int64_t len = known ? c.lens[slot] : -1;
   if (fresh < 0 || row0 < 0 || row0 + fresh > a.tokens || len < 0 ||
       len > ((int64_t)c.max_blocks << c.page_shift) || (len > 0 && c.num_pages == 0)) {
-    if (blockIdx.x == 0) atomicOr(c.flags, kFlagInval);
+    bad = true;
     return s;
   }
   if (fresh == 0 || len == 0) return s;
@@ -135,9 +143,14 @@ struct Cursor {
   __device__ __forceinline__ void advance(const KvWeighArgs& a, uint64_t stop) {
     if (++u >= stop) return;
     ++unit;
+    bool bad;  // (has been looked at)
     while (unit >= s.units) {
+      if (++index >= a.n) {  // (lengths that change meanwhile end no later)
+        u = stop;
+        return;
+      }
       unit = 0;
-      s = lane_seen(seen_of(a, ++index), 0);
+      s = lane_seen(seen_of(a, index, bad), 0);
     }
   }
 };
@@ -160,31 +173,47 @@ __global__ __launch_bounds__(WW* kWave, 2) void kv_weigh(KvWeighArgs a) {
   const int share = a.share, head_slot = wave % share;
   if (a.cu && blockIdx.x == 0 && threadIdx.x == 0 && (a.cu[0] != 0 || a.cu[a.n] != a.tokens))
     atomicOr(c.flags, kFlagInval);
-  const Seen mine = seen_of(a, lane);
+  // The units of all sequences, 64 at a time; the first ones' are kept for the search.
+  constexpr int kKept = 4;
+  uint32_t units[kKept];
+  bool bad = false;
+#pragma unroll
+  for (int k = 0; k < kKept; ++k) units[k] = seen_of(a, k * kWave + lane, bad).units;
   uint64_t total = 0;
-  for (int64_t at = 0; at < a.n; at += kWave) {
-    const Seen s = at == 0 ? mine : seen_of(a, at + lane);
-    total += last_lane_u64(wave_incl_scan_u64(s.units));
-  }
+#pragma unroll
+  for (int k = 0; k < kKept; ++k) total += wave_add_u32(units[k]);
+  for (int64_t at = kKept * kWave; at < a.n; at += kWave)
+    total += wave_add_u32(seen_of(a, at + lane, bad).units);
+  if (__ballot(bad) && blockIdx.x == 0 && lane == 0) atomicOr(c.flags, kFlagInval);
   const uint64_t teams = (uint64_t)gridDim.x * (WW / share);
   const uint64_t self = (uint64_t)blockIdx.x * (WW / share) + wave / share;
   const uint64_t stop = total * (self + 1) / teams;
   // (all teams of a workgroup go through as many rounds)
   const uint32_t rounds = (uint32_t)((total + teams - 1) / teams);
   Cursor now = {{}, 0, 0, total * self / teams};
-  uint64_t before = 0;
-  for (int64_t at = 0; at < a.n && now.u < stop; at += kWave) {
-    const Seen x = at == 0 ? mine : seen_of(a, at + lane);
-    const uint64_t upto = before + wave_incl_scan_u64(x.units);
-    const uint64_t beyond = __ballot(upto > now.u);
-    if (beyond) {
-      const int first = __ffsll((unsigned long long)beyond) - 1;
-      now.index = at + first;
-      now.s = lane_seen(x, first);
-      now.unit = (uint32_t)(now.u - (lane_u64(upto, first) - now.s.units));
-      break;
-    }
-    before = last_lane_u64(upto);
+  if (now.u < stop) {
+    uint64_t before = 0;
+    // whether the piece starts among 64 sequences from `at` on
+    auto starts = [&](int64_t at, uint32_t mine) __attribute__((always_inline)) {
+      const uint32_t upto = wave_incl_scan_u32(mine);
+      const uint64_t beyond = __ballot(before + upto > now.u);
+      if (beyond) {
+        const int first = __ffsll((unsigned long long)beyond) - 1;
+        now.index = at + first;
+        now.unit = (uint32_t)(now.u - before -
+                              (uint32_t)__builtin_amdgcn_readlane((int)(upto - mine), first));
+      }
+      before += (uint32_t)__builtin_amdgcn_readlane((int)upto, kWave - 1);
+      return beyond != 0;
+    };
+    bool found = false;
+#pragma unroll
+    for (int k = 0; k < kKept; ++k)
+      if (!found) found = starts(k * kWave, units[k]);
+    for (int64_t at = kKept * kWave; !found && at < a.n; at += kWave)
+      found = starts(at, seen_of(a, at + lane, bad).units);
+    if (found) now.s = lane_seen(seen_of(a, now.index, bad), 0);
+    if (now.unit >= now.s.units) now.u = stop;  // (lengths that change meanwhile)
   }
   const int64_t block_bytes = (int64_t)c.page_tokens * D;
   const int in_page = c.page_tokens - 1;
@@ -236,10 +265,9 @@ __global__ __launch_bounds__(WW* kWave, 2) void kv_weigh(KvWeighArgs a) {
     for (int j = 0; j < N; ++j)  // (rows need not be 16-byte aligned)
       __builtin_memcpy(&asked[j], q + j / 2 * 64 + j % 2 * 8, 16);
   };
-  const bool works = head_slot < c.kv_heads;  // (a wave may have no heads)
   Cursor next = now;
   Entries ahead = {0, 0};
-  if (now.u < stop && works) {
+  if (now.u < stop) {
     find(now, entries(now));
     if (AHEAD) load(head_slot);
     next.advance(a, stop);
@@ -255,7 +283,7 @@ __global__ __launch_bounds__(WW* kWave, 2) void kv_weigh(KvWeighArgs a) {
     float* const mass = a.mass + s.slot * a.mass_stride + min(t0 + lane, max(s.len, 1) - 1);
     float was = 0.0f;
     if (live && head_slot == 0) was = *mass;
-    if (live && works) {
+    if (live) {
       const uint32_t rows = (uint32_t)s.fresh * group;
       for (int kh = head_slot; kh < c.kv_heads; kh += share) {
         Row row = first_row;
@@ -289,6 +317,7 @@ __global__ __launch_bounds__(WW* kWave, 2) void kv_weigh(KvWeighArgs a) {
               query[j] = counts ? query[j] : __builtin_bit_cast(Operand, make_uint4(0, 0, 0, 0));
           }
           const float base = counts ? lse * 1.4426950408889634f : __builtin_inff();
+          const float by = counts ? f : 0.0f;
           const int pos = s.len - s.fresh + (int)row.token;
           const int high = a.causal ? min(pos + 1, s.len) : s.len;
           const int low = a.window > 0 && pos >= a.window ? pos + 1 - a.window : 0;
@@ -308,7 +337,7 @@ __global__ __launch_bounds__(WW* kWave, 2) void kv_weigh(KvWeighArgs a) {
             float p[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(t[i], f, -base));
+              p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(t[i], by, -base));
             if (hides) {
               asm volatile("");  // (a branch: selects in every tile would cost more)
 #pragma unroll
@@ -324,7 +353,7 @@ __global__ __launch_bounds__(WW* kWave, 2) void kv_weigh(KvWeighArgs a) {
     }
     now = next;
     next.advance(a, stop);
-    if (works && next.u < stop) ahead = entries(next);
+    if (next.u < stop) ahead = entries(next);
     // the sixteen lanes of a group each hold other rows: lane r gets key r's sum
     const float whole = sum_of_rows(sum, r);
     float (&joined)[WW][kChunk] = sums[round & 1];  // (the other may still be read)
