@@ -12,11 +12,11 @@
 // taken: a code never grows.
 //
 // Three launches: a plan (one workgroup per sequence: the lists are looked at, every
-// token's page and place written down), the codes (a wave per block of every layer
-// and head), and the pages, lengths and scales. A sequence moves within its own
-// pages: a wave takes its blocks one after the other, first reads all sources of a
-// block and then writes it, and the sources of later blocks lie behind it. Different
-// waves share no codes, and the scales that they read are only replaced afterwards.
+// token's page and place written down), the codes (a wave per 64 channels of a block of
+// every layer and head), and the pages, lengths and scales. A sequence moves within its
+// own pages: a wave takes its tokens in order, 16 at a time read before they are
+// written, and later ones' sources lie behind. Different waves share no codes, and the
+// scales that they read are only replaced afterwards.
 #include <algorithm>
 
 #include "block_common.h"
@@ -225,23 +225,21 @@ struct Mover {
 };
 
 // K: a lane has 16 channels of token lane % 16 of a tile.
-template <int D, int FMT, int P>
+template <int D, int FMT>
 __device__ __forceinline__ void move_keys(Mover<D>& m, uint8_t* data) {
   constexpr int TILES = kWave / kKvTile;
   const int lane = lane_id();
-  uint4 u[TILES][P], ahead[TILES][P];
-  auto load = [&](const Step& of, uint64_t which, uint4 (&u)[TILES][P])
+  uint4 u[TILES], ahead[TILES];
+  auto load = [&](const Step& of, uint64_t which, uint4 (&u)[TILES])
       __attribute__((always_inline)) {
 #pragma unroll
     for (int x = 0; x < TILES; ++x) {
       if ((which >> (x * 16) & 0xffff) == 0) continue;
       const int mine = x * 16 + lane % 16;
       const int64_t from = __shfl(of.from, mine, kWave);
-      if (which >> mine & 1) {
-        const uint8_t* p = data + (from & ~15ll) + (from & 15) * 16 + lane / 16 * 256;
-#pragma unroll
-        for (int y = 0; y < P; ++y) u[x][y] = *reinterpret_cast<const uint4*>(p + y * 1024);
-      }
+      if (which >> mine & 1)
+        u[x] = *reinterpret_cast<const uint4*>(data + (from & ~15ll) + (from & 15) * 16 +
+                                               lane / 16 * 256);
     }
   };
   for (uint32_t t0 = m.first; t0 < m.end; t0 += kWave, m.advance()) {
@@ -259,80 +257,69 @@ __device__ __forceinline__ void move_keys(Mover<D>& m, uint8_t* data) {
       const bool stays = __shfl((int)m.same, mine, kWave);
       uint8_t* p = data + lane_i64(m.to, x * 16) + lane / 16 * 256 + lane % 16 * 16;
       if (m.moving >> mine & 1) {
+        uint32_t w[4] = {u[x].x, u[x].y, u[x].z, u[x].w};
+        if (!stays) {
 #pragma unroll
-        for (int y = 0; y < P; ++y) {
-          uint32_t w[4] = {u[x][y].x, u[x][y].y, u[x][y].z, u[x][y].w};
-          if (!stays) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) w[k] = again<FMT>(w[k], was, by);
-          }
-          *reinterpret_cast<uint4*>(p + y * 1024) = make_uint4(w[0], w[1], w[2], w[3]);
+          for (int k = 0; k < 4; ++k) w[k] = again<FMT>(w[k], was, by);
         }
+        *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
       }
     }
 #pragma unroll
-    for (int x = 0; x < TILES; ++x)
-#pragma unroll
-      for (int y = 0; y < P; ++y) u[x][y] = ahead[x][y];
+    for (int x = 0; x < TILES; ++x) u[x] = ahead[x];
   }
 }
 
-// V: a lane has a channel (of each of P parts) and fetches its tokens' bytes one by one, a
-// tile ahead, at addresses whose bases are scalar.
-template <int D, int FMT, int P>
+// V: a lane has a channel and fetches its tokens' bytes one by one, a tile ahead, at
+// addresses whose bases are scalar.
+template <int D, int FMT>
 __device__ __forceinline__ void move_values(Mover<D>& m, uint8_t* data) {
   constexpr int TILES = kWave / kKvTile;
   const int lane = lane_id();
-  int32_t even[P][16], odd[P][16];
+  int32_t even[16], odd[16];
   // (tokens that are not there: the last one that is)
-  auto load = [&](int64_t from, int x, int n, int32_t (&code)[P][16])
+  auto load = [&](int64_t from, int x, int n, int32_t (&code)[16])
       __attribute__((always_inline)) {
 #pragma unroll
     for (int k = 0; k < 16; ++k) {
       const uint8_t* p = data + lane_i64(from, x * 16 + min(k, n - 1)) + lane * 16;
-#pragma unroll
-      for (int y = 0; y < P; ++y)
-        code[y][k] = FMT == SEM_KV_INT8 ? (int32_t) * reinterpret_cast<const int8_t*>(p + y * 1024)
-                                        : (int32_t)p[y * 1024];
+      code[k] = FMT == SEM_KV_INT8 ? (int32_t) * reinterpret_cast<const int8_t*>(p) : (int32_t)*p;
     }
   };
-  auto store = [&](int x, int n, const int32_t (&code)[P][16]) __attribute__((always_inline)) {
+  auto store = [&](int x, int n, const int32_t (&code)[16]) __attribute__((always_inline)) {
     Quotient by = m.q;
     by.by = lane_float(m.q.by, x * 16);
     by.inv = lane_float(m.q.inv, x * 16);
     uint8_t* p = data + lane_i64(m.to, x * 16) + lane * 16;
     const uint32_t still = (uint32_t)(__ballot(m.same) >> (x * 16)) & 0xffffu;
+    uint32_t w[4];
 #pragma unroll
-    for (int y = 0; y < P; ++y) {
-      uint32_t w[4];
+    for (int k = 0; k < 4; ++k) {
+      float f[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        f[j] = by.of_lifted(number_of<FMT>(code[4 * k + j]) *
+                            lane_float(m.held, x * 16 + 4 * k + j));
+      w[k] = pack_codes<FMT>(f[0], f[1], f[2], f[3]);
+    }
+    if (still) {  // codes on the same scale stay as they are
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        float f[4];
+        uint32_t raw = 0, keep = 0;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          f[j] = by.of_lifted(number_of<FMT>(code[y][4 * k + j]) *
-                              lane_float(m.held, x * 16 + 4 * k + j));
-        w[k] = pack_codes<FMT>(f[0], f[1], f[2], f[3]);
-      }
-      if (still) {  // codes on the same scale stay as they are
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          uint32_t raw = 0, keep = 0;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            raw |= ((uint32_t)code[y][4 * k + j] & 0xffu) << (8 * j);
-            if (still >> (4 * k + j) & 1) keep |= 0xffu << (8 * j);
-          }
-          w[k] = (raw & keep) | (w[k] & ~keep);
+        for (int j = 0; j < 4; ++j) {
+          raw |= ((uint32_t)code[4 * k + j] & 0xffu) << (8 * j);
+          if (still >> (4 * k + j) & 1) keep |= 0xffu << (8 * j);
         }
+        w[k] = (raw & keep) | (w[k] & ~keep);
       }
-      if (n == kKvTile) {
-        *reinterpret_cast<uint4*>(p + y * 1024) = make_uint4(w[0], w[1], w[2], w[3]);
-      } else {  // the bytes behind the sequence stay
-        for (int k = 0; k < n; ++k) {
-          const uint32_t word = k < 8 ? (k < 4 ? w[0] : w[1]) : (k < 12 ? w[2] : w[3]);
-          p[y * 1024 + k] = (uint8_t)(word >> (8 * (k & 3)));
-        }
+    }
+    if (n == kKvTile) {
+      *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {  // the bytes behind the sequence stay
+      for (int k = 0; k < n; ++k) {
+        const uint32_t word = k < 8 ? (k < 4 ? w[0] : w[1]) : (k < 12 ? w[2] : w[3]);
+        p[k] = (uint8_t)(word >> (8 * (k & 3)));
       }
     }
   };
@@ -354,12 +341,19 @@ __device__ __forceinline__ void move_values(Mover<D>& m, uint8_t* data) {
   }
 }
 
-// A wave: P times 64 channels (part blockIdx.y) of a block of every page that changes. Loads
-// run ahead: sources two steps of 64 tokens, scales and codes one (V: a tile of 16). A
-// token that stays where it is on the same scale is not touched, and a tile of 16 of
-// them neither.
-template <int D, int FMT, int P>
-__global__ __launch_bounds__(MW* kWave, P == 1 ? 4 : 2) void kv_keep_move(KvKeepArgs a) {
+// A wave: 64 channels (part blockIdx.y) of a block of every page that changes. Loads run
+// ahead: sources two steps of 64 tokens, scales and codes one (V: a tile of 16). A token
+// that stays where it is on the same scale is not touched, and a tile of 16 of them
+// neither.
+//
+// Bound by memory: of the pages that tokens are taken from, every line that one of them
+// lies in is read (128 bytes hold eight tokens' sixteen channels of K, or 16 tokens' eight
+// channels of V). 32 sequences of 2048 to 16384 tokens pruned to 2000, 4 layers of 8 heads
+// of 128 channels: 1.05 GB are moved, 1.97 GB in lines, which a copy's rate takes 418 us
+// for; 524 us (K alone 227, V alone 320 and 303 without its conversions). A tree of 16 to
+// 64 tokens each of 64 sequences and 32 layers: about 0.3 GB in lines, 76 us.
+template <int D, int FMT>
+__global__ __launch_bounds__(MW* kWave, 4) void kv_keep_move(KvKeepArgs a) {
   const KvView& c = a.c;
   const int64_t unit = (int64_t)blockIdx.x * MW +
                        __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -370,11 +364,11 @@ __global__ __launch_bounds__(MW* kWave, P == 1 ? 4 : 2) void kv_keep_move(KvKeep
   const int which = pair / both * both + pair % 2 * c.kv_heads + pair % both / 2;
   const KvKept kept = a.kept[i];
   if (kept.seq < 0 || kept.begin >= kept.end) return;
-  uint8_t* const data = c.data + which * ((int64_t)c.page_tokens * D) + blockIdx.y * (P * 1024);
+  uint8_t* const data = c.data + which * ((int64_t)c.page_tokens * D) + blockIdx.y * 1024;
   Mover<D> m{a, kept, which};
   m.begin();
-  if (pair % 2 == 0) move_keys<D, FMT, P>(m, data);
-  else move_values<D, FMT, P>(m, data);
+  if (pair % 2 == 0) move_keys<D, FMT>(m, data);
+  else move_values<D, FMT>(m, data);
 }
 
 // The scales of the blocks that changed, the pages behind the sequence, its length.
@@ -412,15 +406,8 @@ __global__ __launch_bounds__(KT) void kv_keep_finish(KvKeepArgs a) {
 
 template <int D, int FMT>
 void launch_move(const KvKeepArgs& a, hipStream_t st) {
-  // A wave for all of a block's channels where there are units for every compute unit,
-  // else one for 64 of them.
-  constexpr int ALL = D / 64;
-  const int64_t units = a.n * a.c.page_scales;
-  const unsigned grid = (unsigned)((units + MW - 1) / MW);
-  if (units >= 4096)
-    hipLaunchKernelGGL((kv_keep_move<D, FMT, ALL>), dim3(grid), dim3(MW * kWave), 0, st, a);
-  else
-    hipLaunchKernelGGL((kv_keep_move<D, FMT, 1>), dim3(grid, ALL), dim3(MW * kWave), 0, st, a);
+  const unsigned grid = (unsigned)((a.n * a.c.page_scales + MW - 1) / MW);
+  hipLaunchKernelGGL((kv_keep_move<D, FMT>), dim3(grid, D / 64), dim3(MW * kWave), 0, st, a);
 }
 
 template <int D>
