@@ -159,7 +159,6 @@ struct KvWeighArgs {
   int32_t layer, heads, group;
   int32_t bf16, causal, window;
   float scale_log2;
-  int32_t share;       // waves that share a unit's heads (set by the launch)
 };
 
 struct QkRotateArgs {
@@ -191,7 +190,7 @@ hipError_t launch_kv_attend(const KvAttendArgs& a, hipStream_t st);
 hipError_t launch_kv_attend_tree(const KvAttendArgs& a, hipStream_t st);
 hipError_t launch_kv_weigh(const KvWeighArgs& a, int64_t max_new, int64_t max_len, hipStream_t st);
 bool kv_kept_fits(const KvKeepArgs& a);
-hipError_t launch_kv_kept(const KvKeepArgs& a, int64_t blocks, hipStream_t st);
+hipError_t launch_kv_kept(const KvKeepArgs& a, int64_t tokens, hipStream_t st);
 hipError_t launch_kv_prune(const KvPruneArgs& a, hipStream_t st);
 hipError_t launch_kv_keep(const KvKeepArgs& a, hipStream_t st);
 hipError_t launch_kv_tree(const KvTreeArgs& a, hipStream_t st);

@@ -218,7 +218,10 @@ struct Mover {
     s = next;
     next = later;
   }
-  __device__ __forceinline__ bool moves(int x) const { return (moving >> (x * 16) & 0xffff) != 0; }
+  // The tokens of tile x that are not where they stay.
+  __device__ __forceinline__ uint32_t in_tile(int x) const {
+    return (uint32_t)(moving >> (x * 16)) & 0xffffu;
+  }
   __device__ __forceinline__ int tokens_of(uint32_t at) const {
     return at < end ? (int)min(end - at, (uint32_t)kKvTile) : 0;
   }
@@ -248,7 +251,7 @@ __device__ __forceinline__ void move_keys(Mover<D>& m, uint8_t* data) {
     if (m.end - t0 > (uint32_t)kWave) load(m.next, __ballot(m.next.page >= 0), ahead);
 #pragma unroll
     for (int x = 0; x < TILES; ++x) {
-      if (!m.moves(x)) continue;
+      if (m.in_tile(x) == 0) continue;
       const int mine = x * 16 + lane % 16;
       Quotient by = m.q;  // the token's
       by.by = __shfl(m.q.by, mine, kWave);
@@ -270,9 +273,10 @@ __device__ __forceinline__ void move_keys(Mover<D>& m, uint8_t* data) {
   }
 }
 
-// V: a lane has a channel and fetches its tokens' bytes one by one, a tile ahead, at
-// addresses whose bases are scalar.
-template <int D, int FMT>
+// V: a lane has a channel and fetches its tokens' bytes one by one, at addresses whose
+// bases are scalar: of a tile in which more than SOME tokens move all of them, a tile
+// ahead, of others the ones that move.
+template <int D, int FMT, int SOME>
 __device__ __forceinline__ void move_values(Mover<D>& m, uint8_t* data) {
   constexpr int TILES = kWave / kKvTile;
   const int lane = lane_id();
@@ -323,20 +327,57 @@ __device__ __forceinline__ void move_values(Mover<D>& m, uint8_t* data) {
       }
     }
   };
+  // A tile in which few tokens move: those alone, four at a time.
+  auto some = [&](int x) __attribute__((always_inline)) {
+    uint8_t* p = data + lane_i64(m.to, x * 16) + lane * 16;
+    Quotient by = m.q;
+    by.by = lane_float(m.q.by, x * 16);
+    by.inv = lane_float(m.q.inv, x * 16);
+    const uint64_t still = __ballot(m.same);
+#pragma unroll 1
+    for (uint32_t left = m.in_tile(x); left != 0;) {
+      const int count = min(4, (int)__popc(left));
+      int at[4];
+      int32_t code[4];
+      float f[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        at[j] = left ? x * 16 + __ffs(left) - 1 : at[j ? j - 1 : 0];
+        left &= left - 1;
+        const uint8_t* from = data + lane_i64(m.s.from, at[j]) + lane * 16;
+        code[j] = FMT == SEM_KV_INT8 ? (int32_t) * reinterpret_cast<const int8_t*>(from)
+                                     : (int32_t)*from;
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        f[j] = by.of_lifted(number_of<FMT>(code[j]) * lane_float(m.held, at[j]));
+      }
+      const uint32_t w = pack_codes<FMT>(f[0], f[1], f[2], f[3]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (j < count)
+          p[at[j] % 16] = (uint8_t)(still >> at[j] & 1 ? (uint32_t)code[j] : w >> (8 * j));
+    }
+  };
   for (uint32_t t0 = m.first; t0 < m.end; t0 += kWave, m.advance()) {
     m.step(t0);
     auto n = [&](int x) __attribute__((always_inline)) { return m.tokens_of(t0 + x * 16); };
-    if (t0 == m.first && m.moves(0)) load(m.s.from, 0, n(0), even);
+    auto many = [&](int x) __attribute__((always_inline)) {
+      return __popc(m.in_tile(x)) > SOME;
+    };
+    if (t0 == m.first && many(0)) load(m.s.from, 0, n(0), even);
 #pragma unroll 1
     for (int x = 0; x < TILES; x += 2) {
-      if (m.moves(x + 1)) load(m.s.from, x + 1, n(x + 1), odd);
-      if (m.moves(x)) store(x, n(x), even);
+      if (many(x + 1)) load(m.s.from, x + 1, n(x + 1), odd);
+      if (many(x)) store(x, n(x), even);
+      else some(x);
       if (x + 2 < TILES) {
-        if (m.moves(x + 2)) load(m.s.from, x + 2, n(x + 2), even);
+        if (many(x + 2)) load(m.s.from, x + 2, n(x + 2), even);
       } else if (m.end - t0 > (uint32_t)kWave) {
         load(m.next.from, 0, n(TILES), even);
       }
-      if (m.moves(x + 1)) store(x + 1, n(x + 1), odd);
+      if (many(x + 1)) store(x + 1, n(x + 1), odd);
+      else some(x + 1);
     }
   }
 }
@@ -350,9 +391,10 @@ __device__ __forceinline__ void move_values(Mover<D>& m, uint8_t* data) {
 // lies in is read (128 bytes hold eight tokens' sixteen channels of K, or 16 tokens' eight
 // channels of V). 32 sequences of 2048 to 16384 tokens pruned to 2000, 4 layers of 8 heads
 // of 128 channels: 1.05 GB are moved, 1.97 GB in lines, which a copy's rate takes 418 us
-// for; 524 us (K alone 227, V alone 320 and 303 without its conversions). A tree of 16 to
-// 64 tokens each of 64 sequences and 32 layers: about 0.3 GB in lines, 76 us.
-template <int D, int FMT>
+// for; 522 us (K alone 227, V alone 320 and 303 without its conversions). Short lists are
+// bound by the instructions and the chain of loads of a wave: the accepted tokens of a
+// tree of 16 to 64 each of 64 sequences, 32 layers, 0.14 GB by the counters, 41 us.
+template <int D, int FMT, int SOME>
 __global__ __launch_bounds__(MW* kWave, 4) void kv_keep_move(KvKeepArgs a) {
   const KvView& c = a.c;
   const int64_t unit = (int64_t)blockIdx.x * MW +
@@ -368,7 +410,7 @@ __global__ __launch_bounds__(MW* kWave, 4) void kv_keep_move(KvKeepArgs a) {
   Mover<D> m{a, kept, which};
   m.begin();
   if (pair % 2 == 0) move_keys<D, FMT>(m, data);
-  else move_values<D, FMT>(m, data);
+  else move_values<D, FMT, SOME>(m, data);
 }
 
 // The scales of the blocks that changed, the pages behind the sequence, its length.
@@ -405,27 +447,34 @@ __global__ __launch_bounds__(KT) void kv_keep_finish(KvKeepArgs a) {
 }
 
 template <int D, int FMT>
-void launch_move(const KvKeepArgs& a, hipStream_t st) {
-  const unsigned grid = (unsigned)((a.n * a.c.page_scales + MW - 1) / MW);
-  hipLaunchKernelGGL((kv_keep_move<D, FMT>), dim3(grid, D / 64), dim3(MW * kWave), 0, st, a);
+void launch_move(const KvKeepArgs& a, int64_t tokens, hipStream_t st) {
+  const dim3 grid((unsigned)((a.n * a.c.page_scales + MW - 1) / MW), D / 64);
+  // Without tiles that are loaded ahead a wave holds fewer registers. 4, 16, 32, 64 of 128
+  // tokens of each of 64 sequences, 8 layers of 8 heads of 128 channels: 22, 34, 46, 74 us;
+  // with them (where more than 8 tokens move) 27, 38, 48, 66 us.
+  if (tokens <= 32 * a.n)
+    hipLaunchKernelGGL((kv_keep_move<D, FMT, kKvTile>), grid, dim3(MW * kWave), 0, st, a);
+  else
+    hipLaunchKernelGGL((kv_keep_move<D, FMT, 8>), grid, dim3(MW * kWave), 0, st, a);
 }
 
 template <int D>
-void launch_format(const KvKeepArgs& a, hipStream_t st) {
-  if (a.c.format == SEM_KV_INT8) launch_move<D, SEM_KV_INT8>(a, st);
-  else launch_move<D, SEM_KV_FP8>(a, st);
+void launch_format(const KvKeepArgs& a, int64_t tokens, hipStream_t st) {
+  if (a.c.format == SEM_KV_INT8) launch_move<D, SEM_KV_INT8>(a, tokens, st);
+  else launch_move<D, SEM_KV_FP8>(a, tokens, st);
 }
 
 }  // namespace
 
-// The moves of a plan and what follows them.
-hipError_t launch_kv_kept(const KvKeepArgs& a, int64_t blocks, hipStream_t st) {
+// The moves of a plan of so many kept tokens, and what follows them.
+hipError_t launch_kv_kept(const KvKeepArgs& a, int64_t tokens, hipStream_t st) {
   switch (a.c.head_dim) {
-    case 64: launch_format<64>(a, st); break;
-    case 128: launch_format<128>(a, st); break;
-    default: launch_format<256>(a, st);
+    case 64: launch_format<64>(a, tokens, st); break;
+    case 128: launch_format<128>(a, tokens, st); break;
+    default: launch_format<256>(a, tokens, st);
   }
-  const int64_t parts = blocks / a.n * a.c.page_scales / (8 * KT);
+  const int64_t blocks = tokens / a.n / a.c.page_tokens + 2;  // of a sequence
+  const int64_t parts = blocks * a.c.page_scales / (8 * KT);
   hipLaunchKernelGGL(kv_keep_finish,
                      dim3((unsigned)a.n, (unsigned)std::max<int64_t>(1, std::min<int64_t>(parts, 64))),
                      dim3(KT), 0, st, a);
@@ -440,7 +489,7 @@ hipError_t launch_kv_keep(const KvKeepArgs& a, hipStream_t st) {
   if (a.n == 0) return hipSuccess;
   if (!kv_kept_fits(a)) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL(kv_keep_plan, dim3((unsigned)a.n), dim3(KT), 0, st, a);
-  return launch_kv_kept(a, a.total / a.c.page_tokens + 2 * a.n, st);
+  return launch_kv_kept(a, a.total, st);
 }
 
 }  // namespace semsched

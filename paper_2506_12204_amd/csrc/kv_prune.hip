@@ -6,6 +6,10 @@
 //   the weights as whole numbers of the same order; the k-th largest of them by its
 //   digits, three counts of 11, 11 and 10 bits; then, in the tokens' order, those above
 //   it and the first of those equal to it.
+//
+// Bound by the counts in LDS and the chain of their scans: 2000 of up to 16384 tokens each
+// of 32 sequences take 24 us (67 with 256 threads), 256 of up to 1200 of 8 sequences 13
+// (16 with 256 threads), of 522 and 23 us that the moves take.
 #include "block_common.h"
 #include "kv.h"
 
@@ -14,6 +18,7 @@ namespace semsched {
 namespace {
 
 constexpr int kBins = 2048;
+constexpr int NT = 1024;    // threads of a sequence
 constexpr int kCopies = 4;  // of the counters, for lanes in turn: few lanes then meet at one
 constexpr int kEach = 4;    // neighbouring tokens of a thread
 constexpr int kHeld = 4;    // rounds of them whose weights stay in registers
@@ -25,8 +30,6 @@ __device__ __forceinline__ uint32_t order_of(float x) {
   return u >> 31 ? ~u : u | 0x80000000u;
 }
 
-// NT threads: 256 where no sequence is longer than their registers hold, else 1024.
-template <int NT>
 __global__ __launch_bounds__(NT) void kv_prune_plan(KvPruneArgs a) {
   constexpr int kRound = kEach * NT;    // tokens
   constexpr int kMine = kBins / NT;     // digits of a thread
@@ -245,14 +248,10 @@ __global__ __launch_bounds__(NT) void kv_prune_plan(KvPruneArgs a) {
 
 hipError_t launch_kv_prune(const KvPruneArgs& a, hipStream_t st) {
   if (a.k.n == 0) return hipSuccess;
-  if (!kv_kept_fits(a.k) || !grid_fits(a.k.n, 1024)) return hipErrorInvalidConfiguration;
+  if (!kv_kept_fits(a.k) || !grid_fits(a.k.n, NT)) return hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)a.k.n);
-  if ((int64_t)a.k.c.max_blocks * a.k.c.page_tokens <= kHeld * kEach * 256)
-    hipLaunchKernelGGL(kv_prune_plan<256>, grid, dim3(256), 0, st, a);
-  else
-    hipLaunchKernelGGL(kv_prune_plan<1024>, grid, dim3(1024), 0, st, a);
-  const int64_t pt = a.k.c.page_tokens;
-  return launch_kv_kept(a.k, a.k.n * ((a.budget + pt - 1) / pt), st);
+  hipLaunchKernelGGL(kv_prune_plan, grid, dim3(NT), 0, st, a);
+  return launch_kv_kept(a.k, a.k.n * a.budget, st);
 }
 
 }  // namespace semsched

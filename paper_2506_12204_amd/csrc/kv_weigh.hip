@@ -7,7 +7,7 @@
 // pass over the keys is enough and no values are read. The product runs on the matrix
 // cores in the queries' own type, in which 8-bit codes are exact; sums and weights are
 // in 32 bits. A key belongs to one workgroup, which adds its weights in an order that
-// the call's sizes alone decide: results do not depend on the run.
+// sizes and lengths alone decide: results do not depend on the run.
 //
 // A wave has 64 keys of a head in registers and goes through the row tiles. As in
 // attention the product is K q^T: a lane ends up with the scores of one row (lane % 16)
@@ -15,10 +15,10 @@
 // that it takes.
 //
 // Few rows are bound by memory: 251 requests of 16 to 4096 keys, 32 heads on 8 of 128
-// channels, take 50 us, of which reading the keys (203 MB) at 5 TB/s is 41. Many rows are
+// channels, take 42 us, of which reading the keys (203 MB) at 6 TB/s is 34. Many rows are
 // bound by the vector instructions of a tile (the exponentials a third of them) and the
 // latency of its queries: 32 rows each of four contexts of 8192 to 32768 keys, the same
-// heads, take 81 us where the keys take 17 and the products 21.
+// heads, take 78 us where the keys take 17 and the products 21.
 #include <algorithm>
 
 #include "device_common.h"
@@ -155,12 +155,34 @@ struct Cursor {
   }
 };
 
+// The waves of a team: the more, the shorter the piece that ends last, but each round of
+// units has a join, which takes about half as long as a head. One token each, 32 heads on
+// 8 of 128 channels, teams of 1, 2, 4, 8 waves: a context of 777 keys 20, 13, 9, 8 us;
+// eight of 4096 20, 14, 11, 12 us; 251 of 16 to 4096 45, 41, 45, 50 us; 256 of 4096 204,
+// 217, 236, 272 us.
+__device__ __forceinline__ int team_of(uint64_t units, uint32_t waves, uint32_t heads) {
+  uint32_t least = 0xffffffffu;
+  int best = 1;
+  if (units >= 16ull * waves) return best;  // (many rounds: their number is about the same)
+  for (uint32_t share = 1; share <= WW && share <= heads; share *= 2) {
+    const uint32_t teams = waves / share, rounds = ((uint32_t)units + teams - 1) / teams;
+    const uint32_t cost = rounds * (2 * ((heads + share - 1) / share) + 1);
+    if (cost < least) {
+      best = (int)share;
+      least = cost;
+    }
+  }
+  return best;
+}
+
 // The line is cut into equal pieces of neighbours, one for each team of waves; a team's
 // waves share the heads of its units and join through LDS. Loads run ahead: page numbers
 // two units, codes one head or unit, queries one tile.
 //
 // FEW: for one tile of rows a sequence (any number is right): 16 keys at a time are
-// turned into operands and used. Otherwise all 64 are, once for all tiles.
+// turned into operands and used. Otherwise all 64 are, once for all tiles. (One token of
+// each of 256 contexts of 4096 keys 204 us instead of 214, of 64 of 2048, 256 channels, 33
+// instead of 37; with 32 rows of four long ones 84 instead of 82.)
 template <int D, int FMT, bool BF16, bool FEW>
 __global__ __launch_bounds__(WW* kWave, 2) void kv_weigh(KvWeighArgs a) {
   using Operand = std::conditional_t<BF16, bf16x8_t, half8_t>;
@@ -170,7 +192,6 @@ __global__ __launch_bounds__(WW* kWave, 2) void kv_weigh(KvWeighArgs a) {
   const KvView& c = a.c;
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int r = lane % 16, g = lane / 16;
-  const int share = a.share, head_slot = wave % share;
   if (a.cu && blockIdx.x == 0 && threadIdx.x == 0 && (a.cu[0] != 0 || a.cu[a.n] != a.tokens))
     atomicOr(c.flags, kFlagInval);
   // The units of all sequences, 64 at a time; the first ones' are kept for the search.
@@ -185,6 +206,8 @@ __global__ __launch_bounds__(WW* kWave, 2) void kv_weigh(KvWeighArgs a) {
   for (int64_t at = kKept * kWave; at < a.n; at += kWave)
     total += wave_add_u32(seen_of(a, at + lane, bad).units);
   if (__ballot(bad) && blockIdx.x == 0 && lane == 0) atomicOr(c.flags, kFlagInval);
+  const int share = team_of(total, gridDim.x * WW, (uint32_t)c.kv_heads);
+  const int head_slot = wave % share;
   const uint64_t teams = (uint64_t)gridDim.x * (WW / share);
   const uint64_t self = (uint64_t)blockIdx.x * (WW / share) + wave / share;
   const uint64_t stop = total * (self + 1) / teams;
@@ -397,13 +420,10 @@ hipError_t launch_kv_weigh(const KvWeighArgs& args, int64_t max_new, int64_t max
   if (args.n == 0) return hipSuccess;  // (without tokens the offsets are looked at)
   KvWeighArgs a = args;
   const bool few = max_new * a.group <= kRows;
-  // As many waves to a team as there are heads for: pieces are then short, and the last
-  // one's end is no long wait.
   const int64_t units = std::max<int64_t>(1, a.n * ((max_len + kChunk - 1) / kChunk));
   constexpr int64_t kGroups = 256;
-  a.share = 1;
-  while (a.share < WW && 2 * a.share <= a.c.kv_heads) a.share *= 2;
-  const unsigned grid = (unsigned)std::min<int64_t>(kGroups, (units * a.share + WW - 1) / WW);
+  const int64_t waves = units * std::min<int64_t>(WW, a.c.kv_heads);
+  const unsigned grid = (unsigned)std::min<int64_t>(kGroups, (waves + WW - 1) / WW);
   switch (a.c.head_dim) {
     case 64: launch_dim<64>(a, few, grid, st); break;
     case 128: launch_dim<128>(a, few, grid, st); break;

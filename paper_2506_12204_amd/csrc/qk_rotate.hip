@@ -170,7 +170,7 @@ template <int D>
 hipError_t launch_dim(QkRotateArgs a, hipStream_t st) {
   constexpr int ROWS = 1024 / D;
   // Steps of a wave: all of a token's where there are many tokens, one where there
-  // are few.
+  // are few. (The kernel alone, all or one: 16384 tokens 67 or 74 us, one 5.2 or 3.1.)
   const int64_t steps = (a.heads + a.kv_heads + ROWS - 1) / ROWS;
   constexpr int64_t kWaves = 4096;
   a.steps = (int32_t)std::min(steps, std::max<int64_t>(1, a.tokens * steps / kWaves));
