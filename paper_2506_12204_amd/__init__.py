@@ -719,12 +719,16 @@ class KVCache:
     Every operation enqueues on the current stream without synchronising;
     ``check`` waits and raises on a device-detected error of any of them since
     the last check. A step is: ``reserve`` room for the new tokens, then for
-    every layer ``append`` their keys and values and ``attend``. Lists of
-    sequences are int32 GPU tensors that name each at most once.
+    every layer ``append`` their keys and values (rotated by ``qk_rotate``) and
+    ``attend``. A step of drafted tokens makes masks and positions of their ``tree``
+    first and passes the masks to ``attend``; ``keep`` leaves the accepted path. Where
+    contexts are bounded, ``weigh`` adds up the attention that tokens get and
+    ``prune`` keeps the heaviest. Lists of sequences are int32 GPU tensors that name
+    each at most once.
 
-    Operations may be captured into a graph. ``attend`` takes a larger workspace
-    where its sizes need one, which it refuses to do while capturing: call it
-    with the same sizes once before. A workspace that was replaced stays
+    Operations may be captured into a graph. ``attend``, ``keep`` and ``prune`` take a
+    larger workspace where their sizes need one, which they refuse to do while
+    capturing: call them with the same sizes once before. A workspace that was replaced stays
     allocated, for the graphs that were captured with it.
     """
 
