@@ -666,7 +666,7 @@ int sem_kv_attend_tree_async(const sem_kv_cache *cache, int32_t layer, const sem
  * seqs, last [n], index [total], cu [n + 1] from 0 to total: int32 DEVICE.
  * Device-detected SEM_EINVAL, which leaves the sequence as it was: a list that does
  * not ascend or leaves 0 .. last[i]-1, last[i] beyond the length, sequences, lengths,
- * offsets and page numbers outside the cache, and a page whose tokens change that
+ * offsets and page numbers outside the cache, a sequence that was listed before, and a page whose tokens change that
  * another sequence shares (reserve makes the pages of new tokens a sequence's own).
  */
 size_t sem_kv_keep_workspace_bytes(const sem_kv_cache *cache, int64_t n, int64_t total);

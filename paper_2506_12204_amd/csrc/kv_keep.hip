@@ -69,6 +69,8 @@ __global__ __launch_bounds__(KT) void kv_keep_plan(KvKeepArgs a) {
   block_sync();
   const int first = (int)len - last;  // of the tokens that the list is about
   bool bad = false;
+  // (a sequence is listed once, and lists do not overlap: the first ones count)
+  for (int64_t k = t; k < i; k += KT) bad |= a.seqs[k] == s || a.cu[k + 1] > row0;
   for (int64_t k = t; k < count; k += KT) {
     const int32_t at = a.index[row0 + k];
     bad |= at >= last || at <= (k ? a.index[row0 + k - 1] : -1);

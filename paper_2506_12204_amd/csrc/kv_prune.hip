@@ -51,6 +51,21 @@ __global__ __launch_bounds__(NT) void kv_prune_plan(KvPruneArgs a) {
     }
     return;
   }
+  // (A sequence is listed once; otherwise the first counts. Two would change each other's
+  // weights while they are counted.)
+  bool again = false;
+  for (int64_t k = t; k < i; k += NT) again |= a.k.seqs[k] == s;
+  if (t == 0) wrong = 0;
+  block_sync();
+  if (again) wrong = 1;
+  block_sync();
+  if (wrong) {
+    if (t == 0) {
+      atomicOr(c.flags, kFlagInval);
+      a.k.kept[i] = kept;
+    }
+    return;
+  }
   const int len = (int)len64, budget = (int)a.budget;
   const int sinks = (int)min(a.sinks, (int64_t)budget);
   const int recent = (int)min(a.recent, (int64_t)(budget - sinks));
@@ -143,10 +158,7 @@ __global__ __launch_bounds__(NT) void kv_prune_plan(KvPruneArgs a) {
   }
 
   // `want` of those equal to the edge stay, the first ones.
-  if (t == 0) {
-    gap = INT32_MAX;
-    wrong = 0;
-  }
+  if (t == 0) gap = INT32_MAX;
   block_sync();
   int32_t* const source = a.k.pages + i * budget;  // (the tokens at first)
   uint32_t more = 0, equal = 0;  // before this round

@@ -266,6 +266,32 @@ def test_device_detected_errors(ss):  # noqa: F811
         assert torch.equal(c.book, book)
 
 
+def test_a_sequence_twice_and_lists_that_overlap(ss):  # noqa: F811
+    """The first one counts, the others are refused."""
+    print("keep twice", flush=True)
+    for seqs, last, index, cu in (([0, 1, 0], [40, 20, 40], [0, 3, 2, 5, 7], [0, 2, 3, 5]),
+                                  ([0, 1, 2], [40, 20, 30], [0, 3, 9, 2], [0, 3, 4, 4]),
+                                  ([0, 2, 1], [40, 30, 20], [0, 3, 9, 12], [0, 3, 1, 4])):
+        case = Case(ss, [40, 20, 30], fmt=ko.INT8, dim=64, pt=16, kv_heads=2, seed=2)
+        case.c.keep(i32(seqs), i32(last), i32(index), i32(cu))
+        want, ok, done = Expected(case), True, []
+        for i, s in enumerate(seqs):
+            lo, hi = cu[i], cu[i + 1]
+            if hi < lo or s in done or any(cu[j + 1] > lo for j in range(i)):
+                ok = False
+                continue
+            done.append(s)
+            old = case.lens[s] - last[i]
+            want.keep(s, list(range(old)) + [old + k for k in index[lo:hi]])
+        if ok:
+            case.c.check()
+        else:
+            with pytest.raises(ss.SemschedError) as e:
+                case.c.check()
+            assert e.value.code == ss.SEM_EINVAL
+        want.check()
+
+
 def test_empty_calls_and_many_sequences(ss):  # noqa: F811
     print("many", flush=True)
     c = ss.KVCache(700, 300, 3, layers=1, kv_heads=1, head_dim=64, page_tokens=16)

@@ -180,6 +180,30 @@ def test_errors(ss):  # noqa: F811
     assert c.lens.tolist() == [40, 20, 0, 0]
 
 
+def test_a_sequence_twice(ss):  # noqa: F811
+    """The first one counts, the second is refused."""
+    import torch
+    print("prune twice", flush=True)
+    case = Case(ss, [70, 40], fmt=ko.INT8, dim=64, pt=16, kv_heads=2, seed=4)
+    mass = torch.rand(2, case.c.max_blocks * 16, device="cuda")
+    was = mass.cpu().numpy()
+    case.c.prune(mass, i32([0, 1]), 30, sinks=2)
+    case.c.prune(mass, i32([1, 1]), 20, sinks=2)
+    with pytest.raises(ss.SemschedError) as e:
+        case.c.check()
+    assert e.value.code == ss.SEM_EINVAL
+    want = Expected(case)
+    chosen = [ko.prune_choice(was[s], n, 30, 2, 0) for s, n in enumerate([70, 40])]
+    left = was[1, chosen[1]]
+    then = ko.prune_choice(left, 30, 20, 2, 0)
+    want.keep(0, chosen[0])
+    want.keep(1, chosen[1])
+    want.keep(1, then)
+    want.check()
+    assert mass.cpu()[1, :20].tolist() == left[then].tolist()
+    assert case.c.lens.tolist()[:2] == [30, 20]
+
+
 def test_weighed_and_pruned_contexts(ss):  # noqa: F811
     """Decode steps that rotate, append, attend and weigh, a prune, and attention over
     what stayed: it is that of the kept tokens."""
