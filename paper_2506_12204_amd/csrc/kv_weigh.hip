@@ -334,42 +334,42 @@ __global__ __launch_bounds__(WW* kWave, 2) void kv_weigh(KvWeighArgs a) {
           for (int j = 0; j < N; ++j) query[j] = __builtin_bit_cast(Operand, asked[j]);
           // Rows that see no key, are not numbers, or are not there weigh nothing.
           const bool counts = row.at < rows && fabsf(lse) < __builtin_inff();
-          if (__ballot(!counts)) {
-#pragma unroll
-            for (int j = 0; j < N; ++j)
-              query[j] = counts ? query[j] : __builtin_bit_cast(Operand, make_uint4(0, 0, 0, 0));
-          }
-          const float base = counts ? lse * 1.4426950408889634f : __builtin_inff();
-          const float by = counts ? f : 0.0f;
+          const float base = lse * 1.4426950408889634f;
           const int pos = s.len - s.fresh + (int)row.token;
-          const int high = a.causal ? min(pos + 1, s.len) : s.len;
+          const int seen = a.causal ? min(pos + 1, s.len) : s.len, high = counts ? seen : 0;
           const int low = a.window > 0 && pos >= a.window ? pos + 1 - a.window : 0;
-          const bool hides = __ballot(counts && (low > t0 || high < t0 + kChunk)) != 0;
+          const bool hides = __ballot(low > t0 || high < t0 + kChunk) != 0;
           row.next(step_tokens, step_heads, group);
           if (!FEW) ask(s, kh, row, rows);  // (behind the last row: the first one again)
+          float4_t t[4];
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            if (FEW) {
+          for (int x = 0; x < 4; ++x) t[x] = float4_t{0.0f, 0.0f, 0.0f, 0.0f};
+          if (FEW) {
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
 #pragma unroll
               for (int j = 0; j < D / 64; ++j)
                 operands<FMT>(codes[x][j], key[0][2 * j], key[0][2 * j + 1]);
+#pragma unroll
+              for (int j = 0; j < N; ++j) t[x] = product(key[0][j], query[j], t[x]);
             }
-            float4_t t = {0.0f, 0.0f, 0.0f, 0.0f};
+          } else {
 #pragma unroll
-            for (int j = 0; j < N; ++j) t = product(key[FEW ? 0 : x][j], query[j], t);
-            float p[4];
+            for (int j = 0; j < N; ++j)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(t[i], by, -base));
-            if (hides) {
-              asm volatile("");  // (a branch: selects in every tile would cost more)
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                p[i] = vt + 4 * x + i >= low && vt + 4 * x + i < high ? p[i] : 0.0f;
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sum[4 * x + i] += p[i];
+              for (int x = 0; x < 4; ++x) t[x] = product(key[FEW ? 0 : x][j], query[j], t[x]);
           }
+          float p[16];
+#pragma unroll
+          for (int k = 0; k < 16; ++k)
+            p[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(t[k / 4][k % 4], f, -base));
+          if (hides) {
+            asm volatile("");  // (a branch: selects in every tile would cost more)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) p[k] = vt + k >= low && vt + k < high ? p[k] : 0.0f;
+          }
+#pragma unroll
+          for (int k = 0; k < 16; ++k) sum[k] += p[k];
           if (FEW && row.at - r < rows) ask(s, kh, row, rows);
         }
       }
