@@ -395,17 +395,18 @@ __device__ __forceinline__ void move_values(Mover<D>& m, uint8_t* data) {
 // of 128 channels: 1.05 GB are moved, 1.97 GB in lines, which a copy's rate takes 418 us
 // for; 522 us (K alone 227, V alone 320 and 303 without its conversions). Short lists are
 // bound by the instructions and the chain of loads of a wave: the accepted tokens of a
-// tree of 16 to 64 each of 64 sequences, 32 layers, 0.14 GB by the counters, 41 us.
+// tree of 16 to 64 each of 64 sequences, 32 layers, 0.12 GB by the counters, 41 us.
 template <int D, int FMT, int SOME>
 __global__ __launch_bounds__(MW* kWave, 4) void kv_keep_move(KvKeepArgs a) {
   const KvView& c = a.c;
-  const int64_t unit = (int64_t)blockIdx.x * MW +
-                       __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int64_t i = unit / c.page_scales;
-  if (i >= a.n) return;
+  const uint32_t scales = (uint32_t)c.page_scales, groups = (scales + MW - 1) / MW;
+  const uint32_t i = blockIdx.x / groups;
+  const uint32_t pair = (blockIdx.x - i * groups) * MW +
+                        (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  if (pair >= scales) return;
   // K and V of a head side by side: V takes longer, and the dies deal out workgroups in turn
-  const int pair = (int)(unit % c.page_scales), both = 2 * c.kv_heads;
-  const int which = pair / both * both + pair % 2 * c.kv_heads + pair % both / 2;
+  const uint32_t both = 2 * (uint32_t)c.kv_heads, first = pair / both * both;
+  const int which = (int)(first + pair % 2 * (uint32_t)c.kv_heads + (pair - first) / 2);
   const KvKept kept = a.kept[i];
   if (kept.seq < 0 || kept.begin >= kept.end) return;
   uint8_t* const data = c.data + which * ((int64_t)c.page_tokens * D) + blockIdx.y * 1024;
@@ -448,9 +449,12 @@ __global__ __launch_bounds__(KT) void kv_keep_finish(KvKeepArgs a) {
   if (threadIdx.x == 0) c.lens[kept.seq] = kept.now;
 }
 
+// Workgroups of a sequence's moves.
+int64_t groups_of(const KvKeepArgs& a) { return ((int64_t)a.c.page_scales + MW - 1) / MW; }
+
 template <int D, int FMT>
 void launch_move(const KvKeepArgs& a, int64_t tokens, hipStream_t st) {
-  const dim3 grid((unsigned)((a.n * a.c.page_scales + MW - 1) / MW), D / 64);
+  const dim3 grid((unsigned)(a.n * groups_of(a)), D / 64);
   // Without tiles that are loaded ahead a wave holds fewer registers. 4, 16, 32, 64 of 128
   // tokens of each of 64 sequences, 8 layers of 8 heads of 128 channels: 22, 34, 46, 74 us;
   // with them (where more than 8 tokens move) 27, 38, 48, 66 us.
@@ -484,7 +488,7 @@ hipError_t launch_kv_kept(const KvKeepArgs& a, int64_t tokens, hipStream_t st) {
 }
 
 bool kv_kept_fits(const KvKeepArgs& a) {
-  return grid_fits((a.n * a.c.page_scales + MW - 1) / MW, MW * kWave) && grid_fits(a.n, KT);
+  return grid_fits(a.n * groups_of(a), MW * kWave) && grid_fits(a.n, KT);
 }
 
 hipError_t launch_kv_keep(const KvKeepArgs& a, hipStream_t st) {

@@ -15,10 +15,11 @@
 // that it takes.
 //
 // Few rows are bound by memory: 251 requests of 16 to 4096 keys, 32 heads on 8 of 128
-// channels, take 42 us, of which reading the keys (203 MB) at 6 TB/s is 34. Many rows are
-// bound by the vector instructions of a tile (the exponentials a third of them) and the
-// latency of its queries: 32 rows each of four contexts of 8192 to 32768 keys, the same
-// heads, take 78 us where the keys take 17 and the products 21.
+// channels, take 41 us, of which reading the keys (203 MB) at 6 TB/s is 34. Many rows are
+// bound by the latency of a tile, whose exponentials (256 cycles) and products (256) wait
+// for its queries with two waves on a SIMD: 32 rows each of four contexts of 8192 to 32768
+// keys, the same heads, take 70 us where the keys take 17 and the products 21. (Queries
+// that run two tiles ahead do not fit the registers and took 75.)
 #include <algorithm>
 
 #include "device_common.h"
@@ -181,8 +182,7 @@ __device__ __forceinline__ int team_of(uint64_t units, uint32_t waves, uint32_t 
 //
 // FEW: for one tile of rows a sequence (any number is right): 16 keys at a time are
 // turned into operands and used. Otherwise all 64 are, once for all tiles. (One token of
-// each of 256 contexts of 4096 keys 204 us instead of 214, of 64 of 2048, 256 channels, 33
-// instead of 37; with 32 rows of four long ones 84 instead of 82.)
+// each of 256 contexts of 4096 keys 204 us instead of 214.)
 template <int D, int FMT, bool BF16, bool FEW>
 __global__ __launch_bounds__(WW* kWave, 2) void kv_weigh(KvWeighArgs a) {
   using Operand = std::conditional_t<BF16, bf16x8_t, half8_t>;
