@@ -889,8 +889,8 @@ class KVCache:
         if mass.dtype != torch.float32 or mass.get_device() != self._index or mass.dim() != 2 \
                 or mass.shape[0] != self.slots or mass.stride(1) != 1 \
                 or mass.shape[1] < self.max_blocks * self.page_tokens:
-            raise ValueError("mass must be float32 [slots, max_blocks * page_tokens or more] on the "
-                             "cache's GPU, its rows' entries side by side")
+            raise ValueError("mass must be float32 [slots, max_blocks * page_tokens or more] on "
+                             "the cache's GPU, its rows' entries side by side")
         return mass.stride(0)
 
     def weigh(self, layer: int, q: torch.Tensor, lse: torch.Tensor, mass: torch.Tensor,

@@ -153,6 +153,15 @@ def test_many_sequences_and_long_ones(ss):  # noqa: F811
     run(ss, [70000, 0, 33000], [1, 0, 17], heads=2, kv_heads=2, dim=64, pt=256, fmt=ko.FP8)
 
 
+@pytest.mark.parametrize("lens", [[800], [20000], [40000, 5], [100000], [9000] * 9])
+def test_teams_of_every_size(ss, lens):  # noqa: F811
+    """From a few pieces, whose heads are shared out, to more than there are waves; several
+    rounds that hardly fill the last one."""
+    print("teams", lens, flush=True)
+    run(ss, lens, [1] * len(lens), heads=8, kv_heads=4, dim=64, pt=1024, max_len=max(lens))
+    run(ss, lens, [3] * len(lens), heads=5, kv_heads=5, dim=64, pt=512, fmt=ko.FP8, dtype="f16")
+
+
 def test_the_last_queries_alone(ss):  # noqa: F811
     """Weights of the last rows of a prompt, whose attention was called with all."""
     import torch
