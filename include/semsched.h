@@ -685,6 +685,8 @@ int sem_kv_keep_async(const sem_kv_cache *cache, const int32_t *seqs, const int3
  * for every layer (or some) after its attention, with all query rows or only the last
  * ones, it sums what prune goes by. A row whose lse is not finite (it sees no key, or
  * holds no numbers) adds nothing. Sums are of 32 bits, the same in every run.
+ * Device-detected SEM_EINVAL: as for attend, and a list that names a sequence twice,
+ * of which nothing is added.
  *   mass [slots][mass_stride] float DEVICE, mass_stride at least max_blocks *
  *   page_tokens. Entries of a sequence's keys from its length on are not changed:
  *   those of a token that is new, or of a slot that is taken again, have to be what

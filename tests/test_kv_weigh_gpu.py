@@ -287,3 +287,49 @@ def test_graph_streams_and_the_blocking_form(ss):  # noqa: F811
     cu[1] = 50
     assert ss.lib.sem_kv_weigh(c._ref, 1, ctypes.byref(query), p(seqs), p(cu), 2, p(mass),
                                mass.stride(0)) == ss.SEM_EINVAL
+
+
+@pytest.mark.parametrize("n,new", [(2, 1), (5, 40), (64, 2), (65, 1), (300, 1), (1200, 1)])
+def test_a_sequence_twice(ss, n, new):  # noqa: F811
+    """Nothing is added and the call is reported; the same list without it is none."""
+    import torch
+    print("weigh twice", n, new, flush=True)
+    rng = np.random.default_rng(n)
+    lens = (new + rng.integers(0, 150, n)).tolist()
+    case = Case(ss, lens, fmt=ko.FP8, dim=64, pt=16, kv_heads=2, seed=n)
+    cu = None if new == 1 else offsets([new] * n)
+    q, lse = case.queries([new] * n, 4, torch.float16), torch.zeros(n * new, 4, device="cuda")
+    order = rng.permutation(n)
+    before = torch.rand(n, case.c.max_blocks * 16, device="cuda")
+    mass = before.clone()
+    for first, other in ((0, 1), (0, n - 1), (n // 2 - 1, n // 2), (n - 2, n - 1)):
+        seqs = order.copy()
+        seqs[other] = seqs[first]
+        case.c.weigh(1, q, lse, mass, i32(seqs), cu)
+        with pytest.raises(ss.SemschedError) as e:
+            case.c.check()
+        assert e.value.code == ss.SEM_EINVAL
+        assert torch.equal(mass, before)
+    case.c.weigh(1, q, lse, mass, i32(order), cu)
+    case.c.check()
+    assert (mass > before).any(1).all()
+
+
+def test_a_sequence_twice_among_very_many(ss):  # noqa: F811
+    import torch
+    print("weigh twice, many slots", flush=True)
+    slots = 300000
+    c = ss.KVCache(4, slots, 1, layers=1, kv_heads=1, head_dim=64, page_tokens=16)
+    c.data.zero_()
+    c.reserve(i32([5, 131077, 299999]), i32([3, 4, 5]))
+    seqs = [5, 131077, 262149, 299999] + list(range(1000, 1096))
+    q, lse = torch.zeros(100, 2, 64, device="cuda").half(), torch.zeros(100, 2, device="cuda")
+    mass = torch.zeros(slots, 16, device="cuda")
+    c.weigh(0, q, lse, mass, i32(seqs))
+    c.check()
+    assert mass[[5, 131077, 299999]].sum(1).tolist() == [6, 8, 10] and mass.sum() == 24
+    for again in (5, 131077, 262149, 299999):
+        c.weigh(0, q, lse, mass, i32(seqs[:-1] + [again]))
+        with pytest.raises(ss.SemschedError) as e:
+            c.check()
+        assert e.value.code == ss.SEM_EINVAL and mass.sum() == 24
