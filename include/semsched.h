@@ -733,8 +733,9 @@ int sem_kv_prune_async(const sem_kv_cache *cache, float *mass, int64_t mass_stri
  *   (a cos t - b sin t, b cos t + a sin t); channels from rot_dim on (a multiple of
  *   16, 0 for norms alone) stay y.
  * In 32 bits (a row's sum of squares, too: it overflows for elements beyond 2^60)
- * and rounded once; the angle is the product in 64 bits of the two numbers given,
- * so any int32 position is exact to 32 bits. Elements (token, head, channel) at
+ * and rounded once; the angle of any int32 position is the product of the two numbers
+ * given, less its whole turns, but for the rounding of that to 32 bits (2^-26 of a
+ * turn). Elements (token, head, channel) at
  * token * token_stride + head * head_stride + channel. The outputs may be the inputs
  * (with the same strides), but not overlap them in other ways. heads or kv_heads may
  * be 0: q or k is then not looked at. It needs no workspace and reports no errors

@@ -180,3 +180,52 @@ def test_streams_graphs_and_the_blocking_form(ss):
                      1e-6)
     assert ss.lib.sem_qk_rotate(ctypes.byref(c)) == 0
     assert torch.equal(qo, now[0]) and torch.equal(ko_, now[1])
+
+
+def crossings(freqs, low, high, seed):
+    """Positions in [low, high) with the frequency whose cosine or sine is below 2^-16 there:
+    (position, frequency, the quarter turns to it, the angle beyond them), from 70 digits."""
+    from decimal import Decimal, getcontext
+    getcontext().prec = 70
+    two_pi = Decimal("6.2831853071795864769252867665590057683943387987502116419498891846156328")
+    rng = np.random.default_rng(seed)
+    found = []
+    for f in freqs:
+        pos = rng.integers(low, high, 1 << 20)
+        # (extended precision finds them: 64 bits of up to 2^29 turns)
+        quarters = 4 * (pos.astype(np.longdouble) * np.longdouble(f)) / np.longdouble(str(two_pi))
+        near = np.abs(quarters - np.rint(quarters)) * 1.6 < 2.0 ** -16
+        for p in pos[near][:12].tolist():
+            turns = 4 * Decimal(p) * Decimal(float(f)) / two_pi
+            whole = turns.to_integral_value()
+            found.append((p, f, int(whole) % 4, float((turns - whole) * two_pi / 4)))
+    return found
+
+
+@pytest.mark.parametrize("low,high", [(1 << 10, 1 << 20), (1 << 30, (1 << 31) - 1),
+                                      (-(1 << 31), -(1 << 30))])
+def test_far_positions_are_as_exact_as_near_ones(ss, low, high):
+    """Angles beside whole quarters of a turn, whose small sines or cosines bfloat16 shows to
+    2^-25: an angle is off by the rounding of its fraction of a turn to 32 bits, 2 pi 2^-26,
+    whatever the position, its small sine by 2^-21 of itself more (the subtraction of the
+    quarter is exact, then come the factor 2 pi and the series' last product), and by the
+    output's rounding: bfloat16 has eight bits, so a step is 2^-7 of the power of two below
+    a value and half of one up to 2^-8 of the value."""
+    import torch
+    print("far", low, flush=True)
+    freqs = (1.0 - np.arange(32) / 37).astype(np.float32)
+    found = crossings(freqs, low, high, 7)
+    assert len(found) > 100
+    x = torch.zeros(len(found), 1, 64, dtype=torch.bfloat16, device="cuda")
+    x[:, :, :32] = 1.0  # (cos t, sin t) of every pair
+    pos = torch.tensor([p for p, *_ in found], dtype=torch.int32, device="cuda")
+    out = ss.qk_rotate(x, x, pos, torch.from_numpy(freqs).cuda())[0].double().cpu().numpy()
+    worst = 0.0
+    for row, (p, f, quarter, beyond) in enumerate(found):
+        i = int(np.flatnonzero(freqs == f)[0])
+        # cos(q pi / 2 + b), sin(q pi / 2 + b): one of them is b, but for its sign
+        got = out[row, 0, i] if quarter % 2 else out[row, 0, 32 + i]
+        want = beyond if quarter in (0, 3) else -beyond
+        tol = 2 * np.pi * 2.0 ** -26 + (2.0 ** -8 + 2.0 ** -21) * abs(want)
+        worst = max(worst, abs(got - want) / tol)
+    assert worst <= 1, worst
