@@ -655,9 +655,10 @@ int sem_kv_attend_tree_async(const sem_kv_cache *cache, int32_t layer, const sem
 /*
  * Keep: of the last last[i] tokens of sequence seqs[i], those numbered
  * index[cu[i]] .. index[cu[i+1]-1] stay (from 0, ascending), the others leave: the
- * accepted path of a drafted tree, whose rejected tokens give their room back. The
- * tokens before them stay where they are. Pages behind the new length are given
- * back, as by free.
+ * accepted path of a drafted tree, whose rejected tokens give their room back. A list
+ * may end in entries of -1, which name no token: where only the GPU knows how many
+ * were accepted, lists have room for the most. The tokens before the last[i] stay
+ * where they are. Pages behind the new length are given back, as by free.
  * In all layers codes move as they are held: a block (a page's K or V of one head)
  * whose tokens change gets as its scale the largest of those of the blocks that its
  * tokens come from, s', and a code of a block of another scale s becomes
@@ -666,8 +667,9 @@ int sem_kv_attend_tree_async(const sem_kv_cache *cache, int32_t layer, const sem
  * seqs, last [n], index [total], cu [n + 1] from 0 to total: int32 DEVICE.
  * Device-detected SEM_EINVAL, which leaves the sequence as it was: a list that does
  * not ascend or leaves 0 .. last[i]-1, last[i] beyond the length, sequences, lengths,
- * offsets and page numbers outside the cache, a sequence that was listed before, and a page whose tokens change that
- * another sequence shares (reserve makes the pages of new tokens a sequence's own).
+ * offsets and page numbers outside the cache, a sequence that was listed before, and a
+ * page whose tokens change that another sequence shares (reserve makes the pages of
+ * new tokens a sequence's own).
  */
 size_t sem_kv_keep_workspace_bytes(const sem_kv_cache *cache, int64_t n, int64_t total);
 int sem_kv_keep(const sem_kv_cache *cache, const int32_t *seqs, const int32_t *last,

@@ -875,7 +875,8 @@ class KVCache:
              cu: torch.Tensor) -> None:
         """Of the last last[i] tokens of seqs[i], those numbered index[cu[i]..cu[i+1]]
         (from 0, ascending) stay, in all layers: the accepted path of a drafted tree.
-        The tokens before them stay, too; pages behind are given back."""
+        The tokens before them stay, too; pages behind are given back. Lists may be
+        filled up with -1 at their ends, where only the GPU knows how many stay."""
         n, total = seqs.numel(), index.numel()
         self._needed("keep", n, total)
         rc = _enqueue(self._index, lib.sem_kv_keep_async, self._ref, self._list(seqs, "seqs"),

@@ -43,7 +43,7 @@ __device__ __forceinline__ bool block_any(bool x, uint32_t* scratch) {
 // Looks at one sequence's list and writes its plan.
 __global__ __launch_bounds__(KT) void kv_keep_plan(KvKeepArgs a) {
   __shared__ uint32_t scratch;
-  __shared__ int32_t lowest;
+  __shared__ int32_t lowest, filled;
   const KvView& c = a.c;
   const int64_t i = blockIdx.x;
   const int t = threadIdx.x;
@@ -52,14 +52,14 @@ __global__ __launch_bounds__(KT) void kv_keep_plan(KvKeepArgs a) {
     return (int)(((uint32_t)tokens + (uint32_t)c.page_tokens - 1) >> c.page_shift);
   };
   KvKept kept = {-1, 0, 0, 0, 0, 0};
-  const int64_t row0 = a.cu[i], count = (int64_t)a.cu[i + 1] - row0;
+  const int64_t row0 = a.cu[i], listed = (int64_t)a.cu[i + 1] - row0;
   const int32_t s = a.seqs[i], last = a.last[i];
   const int64_t room = (int64_t)c.max_blocks << c.page_shift;
   const int64_t len = (uint32_t)s < (uint32_t)c.slots ? c.lens[s] : -1;
   if (i == 0 && t == 0 && (a.cu[0] != 0 || a.cu[a.n] != a.total)) wrong();
-  if (t == 0) lowest = INT32_MAX;
-  if (row0 < 0 || count < 0 || row0 + count > a.total || len < 0 || len > room || last < 0 ||
-      last > len || count > last) {
+  if (t == 0) lowest = filled = INT32_MAX;
+  if (row0 < 0 || listed < 0 || row0 + listed > a.total || len < 0 || len > room || last < 0 ||
+      last > len) {
     if (t == 0) {
       wrong();
       a.kept[i] = kept;
@@ -71,12 +71,18 @@ __global__ __launch_bounds__(KT) void kv_keep_plan(KvKeepArgs a) {
   bool bad = false;
   // (a sequence is listed once, and lists do not overlap: the first ones count)
   for (int64_t k = t; k < i; k += KT) bad |= a.seqs[k] == s || a.cu[k + 1] > row0;
-  for (int64_t k = t; k < count; k += KT) {
-    const int32_t at = a.index[row0 + k];
-    bad |= at >= last || at <= (k ? a.index[row0 + k - 1] : -1);
-    if (at != k) atomicMin(&lowest, (int32_t)k);
+  for (int64_t k = t; k < listed; k += KT) {
+    const int32_t at = a.index[row0 + k], before = k ? a.index[row0 + k - 1] : 0;
+    if (at >= 0) {
+      bad |= at >= last || (k > 0 && (before < 0 || at <= before));
+      if (at != k) atomicMin(&lowest, (int32_t)k);
+    } else {  // the list is filled up from here on
+      bad |= at != -1;
+      if (before >= 0) atomicMin(&filled, (int32_t)k);
+    }
   }
   bad = block_any(bad, &scratch);
+  const int64_t count = min(listed, (int64_t)filled);
   const int now = first + (int)count;
   // The blocks that are written: none where only the end leaves.
   const bool moves = lowest < count;

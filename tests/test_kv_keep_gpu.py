@@ -361,3 +361,71 @@ def test_graph_streams_and_the_blocking_form(ss):  # noqa: F811
         assert torch.equal(a, b)
     last[0] = 1000
     assert ss.lib.sem_kv_keep(c._ref, p(seqs), p(last), p(index), p(cu), 2, 7) == ss.SEM_EINVAL
+
+
+def padded(kept, width):
+    return i32([j for k in kept for j in [*k, *[-1] * (width - len(k))]])
+
+
+@pytest.mark.parametrize("width", [7, 300])
+@pytest.mark.parametrize("fmt", [ko.INT8, ko.FP8])
+def test_lists_of_one_width(ss, width, fmt):  # noqa: F811
+    """Lists that -1 fills up, wider than what they choose from, too."""
+    print("one width", width, flush=True)
+    lens, last = [20, 70, 64, 33, 300, 5], [20, 13, 64, 0, 270, 1]
+    kept = [[0, 3, 4], [0, 1, 2, 3, 4, 9, 12], [], [], path(np.random.default_rng(1), 270, 6), [0]]
+    case = Case(ss, lens, fmt=fmt, dim=64, pt=16, kv_heads=2, seed=width)
+    want = Expected(case)
+    case.c.keep(i32(range(6)), i32(last), padded(kept, width), i32(range(0, 6 * width + 1, width)))
+    case.c.check()
+    for s, (n, m) in enumerate(zip(lens, last)):
+        want.keep(s, list(range(n - m)) + [n - m + j for j in kept[s]])
+    want.check()
+
+
+def test_what_may_fill_a_list(ss):  # noqa: F811
+    import torch
+    print("fillers", flush=True)
+    for row, ok in (([-1, -1, -1], True), ([2, -1, -1], True), ([0, 1, 4], True),
+                    ([-1, 2, -1], False), ([-1, -1, 0], False), ([1, -1, 3], False),
+                    ([1, -2, -1], False), ([-2, -1, -1], False), ([1, 1, -1], False),
+                    ([3, 2, -1], False), ([5, -1, -1], False), ([0, -1, -2 ** 31], False)):
+        case = Case(ss, [40], fmt=ko.FP8, dim=64, pt=16, kv_heads=1, seed=1)
+        want, book = Expected(case), case.c.book.clone()
+        case.c.keep(i32([0]), i32([5]), i32(row), i32([0, 3]))
+        if ok:
+            case.c.check()
+            want.keep(0, list(range(35)) + [35 + j for j in row if j >= 0])
+            want.check()
+            continue
+        with pytest.raises(ss.SemschedError) as e:
+            case.c.check()
+        assert e.value.code == ss.SEM_EINVAL, row
+        assert torch.equal(case.c.book, book), row
+
+
+def test_paths_that_the_gpu_alone_knows(ss):  # noqa: F811
+    """One graph, other paths in the same buffers for every replay."""
+    import torch
+    print("paths of a graph", flush=True)
+    steps = [[[0, 2, 3], [1]], [[], [0, 1, 2, 3, 5]], [[0, 1, 2, 3, 4], []], [[4], [2, 5]]]
+    case = Case(ss, [100, 70], fmt=ko.INT8, dim=64, pt=16, kv_heads=2, seed=4)
+    start = [t.clone() for t in (case.c.book, case.c.data, case.c.scale)]
+    seqs, last, cu, index = i32([0, 1]), i32([5, 6]), i32([0, 5, 10]), padded([[], []], 5)
+    case.c.keep(seqs, last, index, cu)
+    case.c.check()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        case.c.keep(seqs, last, index, cu)
+    for kept in steps:
+        for t, s in zip((case.c.book, case.c.data, case.c.scale), start):
+            t.copy_(s)
+        index.copy_(padded(kept, 5))
+        want = Expected(case)
+        graph.replay()
+        torch.cuda.synchronize()
+        for s, (n, m) in enumerate(((100, 5), (70, 6))):
+            want.keep(s, list(range(n - m)) + [n - m + j for j in kept[s]])
+        case.c.check()
+        want.check()
+        torch.ones(1000, device="cuda").sum()
