@@ -663,7 +663,8 @@ int sem_kv_attend_tree_async(const sem_kv_cache *cache, int32_t layer, const sem
  * whose tokens change gets as its scale the largest of those of the blocks that its
  * tokens come from, s', and a code of a block of another scale s becomes
  * round(c * s / s'), ties to even, in 32-bit arithmetic. Bytes behind the new length
- * stay what they are.
+ * stay what they are. sem_kv_weigh's mass is not moved: what leaves or moves is weighed
+ * afterwards.
  * seqs, last [n], index [total], cu [n + 1] from 0 to total: int32 DEVICE.
  * Device-detected SEM_EINVAL, which leaves the sequence as it was: a list that does
  * not ascend or leaves 0 .. last[i]-1, last[i] beyond the length, sequences, lengths,
@@ -689,6 +690,11 @@ int sem_kv_keep_async(const sem_kv_cache *cache, const int32_t *seqs, const int3
  * holds no numbers) adds nothing. Sums are of 32 bits, the same in every run.
  * Device-detected SEM_EINVAL: as for attend, and a list that names a sequence twice,
  * of which nothing is added.
+ * Rows of sem_kv_attend_tree are weighed once sem_kv_keep has run: those that stayed,
+ * in their order, as the last rows of their sequences and with the lse that they got.
+ * They see then what their masks showed them. (Before, they would add weights of keys
+ * that they did not see, which are not in their lse; and keep leaves mass alone.) Rows
+ * whose number only the GPU knows may have others before them, of lse -infinity.
  *   mass [slots][mass_stride] float DEVICE, mass_stride at least max_blocks *
  *   page_tokens. Entries of a sequence's keys from its length on are not changed:
  *   those of a token that is new, or of a slot that is taken again, have to be what

@@ -722,7 +722,7 @@ class KVCache:
     every layer ``append`` their keys and values (rotated by ``qk_rotate``) and
     ``attend``. A step of drafted tokens makes masks and positions of their ``tree``
     first and passes the masks to ``attend``; ``keep`` leaves the accepted path. Where
-    contexts are bounded, ``weigh`` adds up the attention that tokens get and
+    contexts are bounded, ``weigh`` then adds up the attention that tokens get and
     ``prune`` keeps the heaviest. Lists of sequences are int32 GPU tensors that name
     each at most once.
 
@@ -876,7 +876,8 @@ class KVCache:
         """Of the last last[i] tokens of seqs[i], those numbered index[cu[i]..cu[i+1]]
         (from 0, ascending) stay, in all layers: the accepted path of a drafted tree.
         The tokens before them stay, too; pages behind are given back. Lists may be
-        filled up with -1 at their ends, where only the GPU knows how many stay."""
+        filled up with -1 at their ends, where only the GPU knows how many stay. The
+        sums of ``weigh`` do not move: weigh the tokens that stay afterwards."""
         n, total = seqs.numel(), index.numel()
         self._needed("keep", n, total)
         rc = _enqueue(self._index, lib.sem_kv_keep_async, self._ref, self._list(seqs, "seqs"),
@@ -901,8 +902,10 @@ class KVCache:
         """Adds to ``mass`` (float32 [slots, max_blocks * page_tokens]) the softmax
         weights that the rows of q give to every cached token, over rows and heads.
         The arguments are those of ``attend`` of the same rows (or of the last ones of
-        each sequence), which returned ``lse`` (float32 [tokens, heads]). Entries of
-        tokens that were not weighed yet have to be zero."""
+        each sequence), which returned ``lse`` (float32 [tokens, heads]). Rows that were
+        attended with ``tree`` are weighed after ``keep``, those that stayed, as the
+        last ones of their sequences; rows of lse -inf add nothing and may stand before
+        them. Entries of tokens that were not weighed yet have to be zero."""
         dtype = self._rows(q, "q")
         tokens, heads, _ = q.shape
         if lse.dtype != torch.float32 or lse.get_device() != self._index \

@@ -160,3 +160,93 @@ def same_tokens(got, got_scale, want, want_scale, geom, table, n):
                 a = ko.read(got, got_scale, geom, table, n, layer, w, h)
                 b = ko.read(want, want_scale, geom, table, n, layer, w, h)
                 assert np.array_equal(a, b)
+
+
+class Drafts(Loop):
+    """Steps whose accepted paths the GPU alone knows: lists of one width, filled up, and the
+    accepted rows weighed with the sums of the tree's attention."""
+
+    PATHS = [[[0, 2, 5, 6], [0, 1]], [[], [0, 1, 2]], [[0, 1, 3], []], [[0, 2, 4], [0]],
+             [[0], [0, 1, 3]], [[0, 2, 5, 6], [0, 1, 2]]]
+
+    def __init__(self, ss, fmt):  # noqa: F811
+        import torch
+        super().__init__(ss, fmt)
+        self.paths = i32([[p + [-1] * (4 - len(p)) for p in step] for step in self.PATHS])
+        self.step, self.width = torch.zeros(1, dtype=torch.int64, device="cuda"), i32([0, 4, 8])
+        self.all_lse = torch.empty(LAYERS, 11, HEADS, device="cuda")
+        self.place = torch.arange(4, device="cuda")
+        self.state = (*self.state, self.step)
+
+    def turn(self):
+        import torch
+        c = self.c
+        c.reserve(self.seqs, self.new)
+        mask, positions = c.tree(self.parents, self.seqs, self.cu, self.starts, max_new=7)
+        asked = []
+        for layer in range(LAYERS):
+            x = self.x[layer]
+            q, k = self.ss.qk_rotate(x[:, :HEADS], x[:, HEADS:HEADS + KVH], positions, self.freq,
+                                     q_weight=self.weight, k_weight=self.weight)
+            c.append(layer, k, x[:, HEADS + KVH:], self.seqs, self.cu)
+            c.attend(layer, q, self.seqs, self.cu, max_new=7, max_len=64, tree=mask,
+                     lse=self.all_lse[layer])
+            asked.append(q)
+        index = self.paths.index_select(0, self.step)[0]  # (what verification would give)
+        self.step += 1
+        c.keep(self.seqs, self.new, index.view(-1), self.width)
+        there = index >= 0
+        count = there.to(torch.int32).sum(1, dtype=torch.int32)
+        self.starts += count
+        at = self.place - (4 - count)[:, None]  # the rows that stay come last
+        rows = self.cu[:-1, None] + index.gather(1, at.clamp(min=0)).clamp(min=0)
+        rows, real = rows.view(-1).long(), (at >= 0).view(-1, 1)
+        out = []
+        for layer in range(LAYERS):
+            q = asked[layer].index_select(0, rows)
+            lse = self.all_lse[layer].index_select(0, rows).where(real, -float("inf"))
+            c.weigh(layer, q, lse, self.mass, self.seqs, self.width, max_new=4, max_len=64)
+            out.append((q, lse))
+        return out
+
+
+@pytest.mark.parametrize("fmt", [ko.INT8, ko.FP8])
+def test_drafts_within_a_budget(ss, fmt):  # noqa: F811
+    import torch
+    print("drafts within a budget", fmt, flush=True)
+    loop = Drafts(ss, fmt)
+    geom, begin, want = (LAYERS, KVH, PT, DIM, fmt), [t.clone() for t in loop.state], []
+    for paths in Drafts.PATHS:
+        before, old = loop.mass.double().cpu().numpy(), loop.c.lens.tolist()
+        out = loop.turn()
+        loop.c.check()
+        data, scale, tables, lens, mass = loop.host()
+        add = np.zeros(mass.shape)
+        for i, s in enumerate((2, 0)):
+            assert lens[s] == old[s] + len(paths[i])
+            for layer in range(LAYERS):
+                q, lse = (x[4 * i:4 * i + 4].double().cpu().numpy() for x in out[layer])
+                assert np.isfinite(lse).all(1).tolist() == [False] * (4 - len(paths[i])) + [True] * len(
+                    paths[i])
+                for h in range(HEADS):
+                    k = ko.read(data, scale, geom, tables[s], lens[s], layer, 0, h // (HEADS // KVH))
+                    add[s, :lens[s]] += ko.weigh(q[:, h], k, DIM ** -0.5, True, 0, lse[:, h])
+        assert (np.abs(mass - before - add) <= 2.0 ** -14 * add + 2.0 ** -22 * (before + add)).all()
+        loop.bound()
+        loop.c.check()
+        assert [loop.c.lens.tolist()[s] for s in (2, 0)] == [min(lens[s], BUDGET) for s in (2, 0)]
+        want.append([t.clone() for t in loop.state])
+    for t, b in zip(loop.state, begin):
+        t.copy_(b)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        loop.turn()
+        loop.bound()
+    for w in want:
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, x in zip(loop.state, w):
+            assert torch.equal(got, x)
+        torch.ones(1000, device="cuda").sum()
+    loop.c.check()

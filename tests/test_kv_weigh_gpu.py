@@ -333,3 +333,46 @@ def test_a_sequence_twice_among_very_many(ss):  # noqa: F811
         with pytest.raises(ss.SemschedError) as e:
             c.check()
         assert e.value.code == ss.SEM_EINVAL and mass.sum() == 24
+
+
+def test_rows_of_a_tree_after_their_path_was_kept(ss):  # noqa: F811
+    """With the lse of the tree's attention the weights of a row that stays add up to 1:
+    it sees what its mask showed it. (One scale for all keys, so that they stay the same.)"""
+    import torch
+    print("rows of a tree", flush=True)
+    gen = torch.Generator("cuda").manual_seed(5)
+    parents, kept = [-1, 0, 0, 2, 3, 3, -1, 6], [0, 2, 3, 5]
+    for fmt, context in ((ko.INT8, 40), (ko.FP8, 75), (ko.INT8, 0)):
+        c = ss.KVCache(8, 2, 8, layers=1, kv_heads=2, head_dim=64, page_tokens=16, format=fmt)
+        c.data.zero_()
+        x = torch.randn(context + 8, 2, 2, 64, generator=gen, device="cuda").clamp(-2, 2).bfloat16()
+        x[:, :, :, 0] = 3.0
+        q = (2 * torch.randn(8, 4, 64, generator=gen, device="cuda")).bfloat16()
+        lse, seqs, cu = torch.empty(8, 4, device="cuda"), i32([1]), i32([0, 8])
+        if context:
+            c.reserve(seqs, i32([context]))
+            c.append(0, x[:context, 0], x[:context, 1], seqs, i32([0, context]))
+        c.reserve(seqs, i32([8]))
+        c.append(0, x[context:, 0], x[context:, 1], seqs, cu)
+        c.attend(0, q, seqs, cu, tree=c.tree(i32(parents), seqs, cu)[0], lse=lse)
+        c.keep(seqs, i32([8]), i32(kept + [-1] * 4), cu)
+        # rows that the host does not know of before those that stay
+        rows = [0] * 4 + kept
+        lse = lse[rows].contiguous()
+        lse[:4] = -float("inf")
+        mass = torch.zeros(2, 128, device="cuda")
+        c.weigh(0, q[rows], lse, mass, seqs, cu)
+        c.check()
+        got = mass.double().cpu().numpy()
+        data, scale = c.data.cpu().numpy(), c.scale.cpu().numpy()
+        want = np.zeros(context + 4)
+        for h in range(4):
+            k = ko.read(data, scale, (1, 2, 16, 64, fmt), c.tables[1].tolist(), context + 4, 0, 0,
+                        h // 2)
+            add = ko.weigh(q[kept, h].double().cpu().numpy(), k, 0.125, True, 0,
+                           lse[4:, h].double().cpu().numpy())
+            # (four rows' lse and weights, 2^-14 each)
+            assert abs(add.sum() - 4) <= 4 * 2.0 ** -13
+            want += add
+        assert (np.abs(got[1, :context + 4] - want) <= 2.0 ** -14 * want + 1e-12).all()
+        assert (got[1, context + 4:] == 0).all() and (got[0] == 0).all()
