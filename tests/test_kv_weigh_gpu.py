@@ -376,3 +376,34 @@ def test_rows_of_a_tree_after_their_path_was_kept(ss):  # noqa: F811
             want += add
         assert (np.abs(got[1, :context + 4] - want) <= 2.0 ** -14 * want + 1e-12).all()
         assert (got[1, context + 4:] == 0).all() and (got[0] == 0).all()
+
+
+@pytest.mark.parametrize("new", [1, 4, 40])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_a_query_that_is_no_number_stays_in_its_row(ss, new, dtype):  # noqa: F811
+    """Attention gives such a row a sum that is none; the rows beside it weigh as ever."""
+    import torch
+    print("no number", new, dtype, flush=True)
+    case = Case(ss, [50, 90], fmt=ko.FP8, dim=64, pt=16, kv_heads=2, seed=9)
+    q = case.queries([new, new], 4, dtype_of(dtype)).clone()
+    seqs, cu, lse = i32([0, 1]), offsets([new, new]), torch.empty(2 * new, 4, device="cuda")
+    spoiled = [(0, 1), (new, 2), (2 * new - 1, 0)]
+    for row, head in spoiled:
+        q[row, head, 5] = float("nan")
+    case.c.attend(1, q, seqs, cu, lse=lse)
+    finite = torch.ones(2 * new, 4, dtype=torch.bool)
+    for row, head in spoiled:
+        finite[row, head] = False
+    assert torch.equal(lse.isfinite().cpu(), finite)
+    mass = torch.zeros(2, case.c.max_blocks * 16, device="cuda")
+    case.c.weigh(1, q, lse, mass, seqs, cu)
+    case.c.check()
+    got, want = mass.double().cpu().numpy(), np.zeros(mass.shape)
+    qh, sums = q.double().cpu().numpy(), lse.double().cpu().numpy()
+    for i, n in enumerate((50, 90)):
+        rows = slice(i * new, (i + 1) * new)
+        for h in range(4):
+            k = ko.read(case.data, case.scale, case.geom, case.tables[i], n, 1, 0, h // 2)
+            want[i, :n] += ko.weigh(qh[rows, h], k, 0.125, True, 0, sums[rows, h])
+    assert np.isfinite(got).all()
+    assert (np.abs(got - want) <= 2.0 ** -14 * want + 1e-12).all()
