@@ -451,7 +451,8 @@ int sem_schedule_static(const uint8_t *priority, const int32_t *length, int64_t 
  * growth of appended sequences), but not what was written to data and scale: a
  * page that was given back and has since been taken holds its new owner's
  * tokens or copies, and a block that append put on a larger scale keeps it (and
- * its older codes, rounded again). A compact is not undone.
+ * its older codes, rounded again). A compact is not undone, nor are keep and prune,
+ * which move tokens.
  * All arrays are DEVICE memory of the caller, all zero (tables: -1) for an
  * empty cache; data need not be cleared. The structure itself is a HOST
  * pointer. page_tokens is a power of two from 16 to 1024, head_dim 64, 128 or

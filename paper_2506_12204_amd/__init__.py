@@ -713,8 +713,8 @@ class KVCache:
     ``tables``, each padded to 64 entries: copying it and putting it back
     undoes reserve, fork and free (and append's growth) of the steps between, as
     long as no page that they gave back has been taken and written since; what
-    append did to scales and older codes stays, and compact is not undone. The
-    three may be passed in; otherwise they are allocated, empty.
+    append did to scales and older codes stays, and compact, ``keep`` and ``prune``, which
+    move tokens, are not undone. The three may be passed in; otherwise they are allocated, empty.
 
     Every operation enqueues on the current stream without synchronising;
     ``check`` waits and raises on a device-detected error of any of them since

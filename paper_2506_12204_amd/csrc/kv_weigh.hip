@@ -20,6 +20,11 @@
 // for its queries with two waves on a SIMD: 32 rows each of four contexts of 8192 to 32768
 // keys, the same heads, take 70 us where the keys take 17 and the products 21. (Queries
 // that run two tiles ahead do not fit the registers and took 75.)
+//
+// A wave goes through all rows of its keys' sequence: tiles that see none of them are
+// multiplied, too, and their weights masked. So all 4096 rows of a prompt take 0.95 ms with
+// a window of 512 as without, and 2048 rows beside 250 single tokens take 7.5 ms, as work is
+// shared out by keys alone.
 #include <algorithm>
 
 #include "device_common.h"
@@ -222,7 +227,9 @@ __global__ __launch_bounds__(WW* kWave, 2) void kv_weigh(KvWeighArgs a) {
     if (blockIdx.x == 0 && threadIdx.x == 0) atomicOr(c.flags, kFlagInval);
     return;
   }
-  // The units of all sequences, 64 at a time; the first ones' are kept for the search.
+  // The units of all sequences, 64 at a time; the first ones' are kept for the search. (64,
+  // 256 or 512 of them: a context of 777 keys 8.0, 8.4, 8.7 us; 251 ragged requests 41 each,
+  // 4096 of 64 keys 119, 119, 113.)
   constexpr int kKept = 4;
   uint32_t units[kKept];
   bool bad = false;
